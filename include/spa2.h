@@ -270,6 +270,60 @@ int spa2_vd_loss_and_grad(const void* u_sparse, const void* u_full, int64_t n, d
                           void* workspace, size_t workspace_bytes, void* stream);
 int spa2_vd_rescale(void* grad, int64_t n, double weight, const double* upstream, void* stream);
 
+/* ---- norm of the heads of q and k, and rotation by position: what stands in front of the attention ----
+ * For every head of every token of q and of k, in one pass:
+ *   n_c = x_c * w_c * (mean_c x_c^2 + eps)^(-1/2)        y = R n
+ * where R turns the channel pairs of the first `rot` channels by their token's angles, (a, b) -> (a cos - b sin,
+ * b cos + a sin); pair i is (i, i + rot / 2), or (2 i, 2 i + 1) if `interleaved`.  Squares are summed in fp32 (inputs of
+ * 2^60 and more overflow them, as NaN and infinities do: the head is then lost); the result is rounded once, to bf16,
+ * which is what the attention takes.
+ *   q, k        bf16 or fp32 (shape->dtype); element (b, h, n, c) at b*sb + h*sh + n*sn + c with strides of their own
+ *               (q_*, k_*; 0 repeats an input), 16-byte aligned, strides multiples of 16 bytes.  Hq and Hk may differ.
+ *   q_out, k_out  bf16, strides qo_*, ko_*.
+ *   q_weight, k_weight  fp32 [d] or NULL (1).
+ *   cos, sin    fp32 [table_rows, rot / 2] (NULL if rot = 0).
+ *   positions   row of the tables of each token, [B, N] with batch stride pos_sb (0: all samples alike) and pos_bits 32 or
+ *               64; values outside the tables are taken as the nearest row.  NULL (pos_bits 0): token n uses row n.
+ * spa2_norm_rotate_bwd: gradients of q, k (dtype of q and k, in the strides of the outputs, as d_q_out and d_k_out are) and
+ * of the weights (fp32 [d]; NULL = not wanted).  The norms are computed again from q and k.  Sums over tokens are taken in
+ * a fixed order.  Workspace of spa2_norm_rotate_bwd_workspace_bytes(shape) bytes, only needed for the weights' gradients.
+ * Errors: SPA2_ERR_NULL, _SHAPE, _UNSUPPORTED (d not 64 or 128, dtype, rot not a multiple of 16 up to d, pos_bits), _ALIGN,
+ * _RANGE (eps not finite or <= 0), _WORKSPACE, _LAUNCH; checked before anything is launched. */
+typedef struct spa2_norm_shape {
+  int32_t B, Hq, Hk, N, d;
+  int32_t dtype;                       /* of q and k and of their gradients: SPA2_DTYPE_* */
+  int32_t rot, interleaved;
+  int32_t table_rows, pos_bits;
+  int64_t pos_sb;
+  int64_t q_sb, q_sh, q_sn, k_sb, k_sh, k_sn;             /* element strides of the inputs */
+  int64_t qo_sb, qo_sh, qo_sn, ko_sb, ko_sh, ko_sn;       /* of the results and of all gradients */
+} spa2_norm_shape;
+size_t spa2_norm_rotate_bwd_workspace_bytes(const spa2_norm_shape* shape);
+int spa2_norm_rotate(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* cos,
+                     const float* sin, const void* positions, const spa2_norm_shape* shape, float eps, void* q_out,
+                     void* k_out, void* stream);
+int spa2_norm_rotate_bwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* cos,
+                         const float* sin, const void* positions, const void* d_q_out, const void* d_k_out,
+                         const spa2_norm_shape* shape, float eps, void* dq, void* dk, float* d_q_weight,
+                         float* d_k_weight, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- dropout of a branch and the sum with the residual stream: what stands behind the attention ----
+ *   y = residual + x * keep / (1 - p')        p' = round(2^16 p) / 2^16, keep = 0 with probability p', else 1
+ * The mask is a function of (seed, offset, element number) alone and is never stored: the generator is Philox4x32-10 (Salmon
+ * et al., 2011) with the seed as key and the counter (element / 8, offset); element e has half e % 2 (low first) of word
+ * (e % 8) / 2 and is kept where these 16 bits are at least 2^16 p'.
+ *   x, y, residual  contiguous, n elements, 16-byte aligned; residual may be NULL and may be y, x may be y where their types
+ *                   agree.  x bf16 or fp32; residual of x's type, or fp32; y of the residual's type (x's without one).
+ *   seed_offset     device, two 64-bit numbers (seed, offset) read by the kernel instead of the two arguments, or NULL: for
+ *                   captured graphs whose replays draw other masks.
+ * spa2_dropout_bwd: dx = d_y * keep / (1 - p') with the mask of the forward call; d_y has y's type, dx that of x.  (The
+ * residual's gradient is d_y itself.)
+ * Errors: SPA2_ERR_NULL, _SHAPE (n <= 0), _UNSUPPORTED (types), _ALIGN, _RANGE (p outside [0, 1]), _LAUNCH. */
+int spa2_dropout_add(const void* x, const void* residual /* or NULL */, int64_t n, int32_t x_dtype, int32_t residual_dtype,
+                     double p, uint64_t seed, uint64_t offset, const int64_t* seed_offset /* or NULL */, void* y, void* stream);
+int spa2_dropout_bwd(const void* d_y, int64_t n, int32_t y_dtype, int32_t x_dtype, double p, uint64_t seed, uint64_t offset,
+                     const int64_t* seed_offset /* or NULL */, void* dx, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -41,6 +41,13 @@ class _Pattern(ctypes.Structure):
                 ("row_order", ctypes.c_void_p), ("col_order", ctypes.c_void_p)]
 
 
+class _NormShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "N", "d", "dtype", "rot", "interleaved", "table_rows",
+                                              "pos_bits")] \
+        + [(n, ctypes.c_int64) for n in ("pos_sb", "q_sb", "q_sh", "q_sn", "k_sb", "k_sh", "k_sn", "qo_sb", "qo_sh",
+                                         "qo_sn", "ko_sb", "ko_sh", "ko_sn")]
+
+
 _lib = None
 
 
@@ -113,6 +120,17 @@ def _load():
     lib.spa2_vd_loss_and_grad.argtypes = [vp, vp, ctypes.c_int64, ctypes.c_double, vp, vp, vp, sz, vp]
     lib.spa2_vd_rescale.restype = ctypes.c_int
     lib.spa2_vd_rescale.argtypes = [vp, ctypes.c_int64, ctypes.c_double, vp, vp]
+    i64, u64, f64, nrm = ctypes.c_int64, ctypes.c_uint64, ctypes.c_double, ctypes.POINTER(_NormShape)
+    lib.spa2_norm_rotate_bwd_workspace_bytes.restype = sz
+    lib.spa2_norm_rotate_bwd_workspace_bytes.argtypes = [nrm]
+    lib.spa2_norm_rotate.restype = ctypes.c_int
+    lib.spa2_norm_rotate.argtypes = [vp] * 7 + [nrm, f32, vp, vp, vp]
+    lib.spa2_norm_rotate_bwd.restype = ctypes.c_int
+    lib.spa2_norm_rotate_bwd.argtypes = [vp] * 9 + [nrm, f32, vp, vp, vp, vp, vp, sz, vp]
+    lib.spa2_dropout_add.restype = ctypes.c_int
+    lib.spa2_dropout_add.argtypes = [vp, vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
+    lib.spa2_dropout_bwd.restype = ctypes.c_int
+    lib.spa2_dropout_bwd.argtypes = [vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -123,7 +141,8 @@ EXPORTED_SYMBOLS = ("spa2_version", "spa2_strerror", "spa2_topk_blocks", "spa2_m
                     "spa2_bwd_dkdv", "spa2_bwd_dq", "spa2_error_workspace_bytes", "spa2_error_terms",
                     "spa2_vd_loss_workspace_bytes", "spa2_vd_loss", "spa2_vd_loss_grad", "spa2_vd_loss_and_grad",
                     "spa2_mask_fwd", "spa2_mask_fwd_workspace_bytes", "spa2_bwd_rows", "spa2_bwd_rows_workspace_bytes",
-                    "spa2_vd_rescale")
+                    "spa2_vd_rescale", "spa2_norm_rotate", "spa2_norm_rotate_bwd", "spa2_norm_rotate_bwd_workspace_bytes",
+                    "spa2_dropout_add", "spa2_dropout_bwd")
 
 
 # ------------------------------------------------------------------ plumbing (memory only)
@@ -458,3 +477,94 @@ def spa2_vd_rescale(grad: torch.Tensor, weight: float, upstream: torch.Tensor) -
         raise ValueError("upstream is a float64 CUDA tensor of one element")
     _check(_load().spa2_vd_rescale(grad.data_ptr(), grad.numel(), float(weight), upstream.data_ptr(), _stream(grad)),
            "spa2_vd_rescale")
+
+
+# ------------------------------------------------------------------ around the attention
+def _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, q_out, k_out):
+    """The shape of a norm-and-rotate call (q_out, k_out: results of the forward call, or anything of their strides)."""
+    for t in (q, k, q_out, k_out):
+        if t.dim() != 4 or t.stride(3) != 1:
+            raise ValueError("heads are 4-D views [B, H, N, d], d contiguous")
+    if q.dtype not in _VD_DTYPES or k.dtype != q.dtype:
+        raise ValueError("q and k are bfloat16 or float32, both of the same type")
+    if (k.shape[0], k.shape[2], k.shape[3]) != (q.shape[0], q.shape[2], q.shape[3]):
+        raise ValueError("q and k have the same batch, tokens and head dimension")
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("the results have the shapes of q and k")
+    for t in (q_weight, k_weight):
+        if t is not None and (t.dtype != torch.float32 or t.shape != q.shape[3:] or not t.is_contiguous()):
+            raise ValueError("weights are contiguous float32 tensors of d elements")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    if cos is not None:
+        for t in (cos, sin):
+            if t.dtype != torch.float32 or t.dim() != 2 or t.shape != cos.shape or not t.is_contiguous():
+                raise ValueError("cos and sin are contiguous float32 tables [rows, rotated channels / 2]")
+    B, Hq, N, d = q.shape
+    pos_bits, pos_sb = 0, 0
+    if positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous() \
+                or tuple(positions.shape) not in ((N,), (1, N), (B, N)):
+            raise ValueError("positions are contiguous int32 or int64 numbers [N] or [B, N]")
+        pos_bits, pos_sb = 8 * positions.element_size(), N if tuple(positions.shape) == (B, N) and B > 1 else 0
+    return _NormShape(B, Hq, k.shape[1], N, d, _VD_DTYPES[q.dtype], 0 if cos is None else 2 * cos.shape[1], int(interleaved),
+                      0 if cos is None else cos.shape[0], pos_bits, pos_sb, *q.stride()[:3], *k.stride()[:3],
+                      *q_out.stride()[:3], *k_out.stride()[:3])
+
+
+def spa2_norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps: float, interleaved: bool, q_out, k_out) -> None:
+    s = _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, q_out, k_out)
+    if q_out.dtype != torch.bfloat16 or k_out.dtype != torch.bfloat16:
+        raise ValueError("the results are bfloat16")
+    _check(_load().spa2_norm_rotate(q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin),
+                                    _ptr(positions), ctypes.byref(s), float(eps), q_out.data_ptr(), k_out.data_ptr(),
+                                    _stream(q)), "spa2_norm_rotate")
+
+
+def spa2_norm_rotate_bwd_workspace_bytes(q: torch.Tensor, k: torch.Tensor) -> int:
+    s = _norm_args(q, k, None, None, None, None, None, False, q, k)
+    return int(_load().spa2_norm_rotate_bwd_workspace_bytes(ctypes.byref(s)))
+
+
+def spa2_norm_rotate_bwd(q, k, q_weight, k_weight, cos, sin, positions, d_q_out, d_k_out, eps: float, interleaved: bool,
+                         dq, dk, d_q_weight=None, d_k_weight=None, workspace=None) -> None:
+    s = _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, d_q_out, d_k_out)
+    if d_q_out.dtype != torch.bfloat16 or d_k_out.dtype != torch.bfloat16:
+        raise ValueError("the upstream gradients are bfloat16")
+    for g, up, x in ((dq, d_q_out, q), (dk, d_k_out, k)):
+        if g.shape != up.shape or g.stride() != up.stride() or g.dtype != x.dtype:
+            raise ValueError("gradients have the strides of the upstream gradients and the type of q and k")
+    for t in (d_q_weight, d_k_weight):
+        if t is not None and (t.dtype != torch.float32 or t.shape != q.shape[3:] or not t.is_contiguous()):
+            raise ValueError("gradients of the weights are contiguous float32 tensors of d elements")
+    _check(_load().spa2_norm_rotate_bwd(q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin),
+                                        _ptr(positions), d_q_out.data_ptr(), d_k_out.data_ptr(), ctypes.byref(s), float(eps),
+                                        dq.data_ptr(), dk.data_ptr(), _ptr(d_q_weight), _ptr(d_k_weight), _ptr(workspace),
+                                        0 if workspace is None else _nbytes(workspace), _stream(q)), "spa2_norm_rotate_bwd")
+
+
+def _drop_args(x, like, seed_offset) -> None:
+    for t in (x, like):
+        if t.dtype not in _VD_DTYPES or not t.is_contiguous() or t.shape != x.shape:
+            raise ValueError("dropout takes contiguous bfloat16 or float32 tensors of one shape")
+    if seed_offset is not None and (seed_offset.dtype != torch.int64 or seed_offset.numel() != 2
+                                    or not seed_offset.is_contiguous() or seed_offset.device != x.device):
+        raise ValueError("seed and offset on the device are two int64 numbers")
+
+
+def spa2_dropout_add(x, residual, p: float, seed: int, offset: int, y, seed_offset=None) -> None:
+    _drop_args(x, y, seed_offset)
+    if residual is not None:
+        _drop_args(x, residual, None)
+    if y.dtype != (x if residual is None else residual).dtype:
+        raise ValueError("y has the type of the residual, or x's without one")
+    _check(_load().spa2_dropout_add(x.data_ptr(), _ptr(residual), x.numel(), _VD_DTYPES[x.dtype],
+                                    0 if residual is None else _VD_DTYPES[residual.dtype], float(p), seed % 2 ** 64,
+                                    offset % 2 ** 64, _ptr(seed_offset), y.data_ptr(), _stream(x)), "spa2_dropout_add")
+
+
+def spa2_dropout_bwd(d_y, p: float, seed: int, offset: int, dx, seed_offset=None) -> None:
+    _drop_args(d_y, dx, seed_offset)
+    _check(_load().spa2_dropout_bwd(d_y.data_ptr(), d_y.numel(), _VD_DTYPES[d_y.dtype], _VD_DTYPES[dx.dtype], float(p),
+                                    seed % 2 ** 64, offset % 2 ** 64, _ptr(seed_offset), dx.data_ptr(), _stream(d_y)),
+           "spa2_dropout_bwd")

@@ -9,7 +9,9 @@
 // mask and forward, and the backward pass runs in the engine's thread without the interpreter: 90 us (82 with the
 // kernels as they are now).  24 heads of 1,281 tokens 223 -> 133 us (116); sampling on 1,000 tokens, two heads 46 -> 28 us (17).
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
 
 #include "spa2.h"
@@ -231,9 +233,242 @@ Tensor velocity_loss(const Tensor& u_sparse, const Tensor& u_full, double weight
   return VelocityLoss::apply(u_sparse.contiguous(), u_full.detach().contiguous(), weight);
 }
 
+// ------------------------------------------------------------------ around the attention
+using OptTensor = std::optional<Tensor>;
+
+Tensor or_none(const OptTensor& t) { return t.value_or(Tensor()); }
+const void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+int32_t dtype_of(const Tensor& t) { return t.scalar_type() == at::kBFloat16 ? SPA2_DTYPE_BF16 : SPA2_DTYPE_F32; }
+bool float_kind(const Tensor& t) { return t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kFloat; }
+
+// A [B, H, N, d] tensor without gaps, tokens outside the heads where x has them so (what a projection leaves and takes).
+Tensor dense_like(const Tensor& x, at::ScalarType dtype) {
+  const auto o = x.options().dtype(dtype);
+  if (x.stride(2) > x.stride(1)) return at::empty({x.size(0), x.size(2), x.size(1), x.size(3)}, o).permute({0, 2, 1, 3});
+  return at::empty(x.sizes(), o);
+}
+// Strides as the kernels read them: a dimension of one element has none.
+std::array<int64_t, 3> strides_of(const Tensor& x) {
+  std::array<int64_t, 3> s;
+  for (int i = 0; i < 3; ++i) s[i] = x.size(i) > 1 ? x.stride(i) : 0;
+  return s;
+}
+
+// x in the memory order of ref (of another type maybe).
+Tensor in_order(const Tensor& x, const Tensor& ref) {
+  if (x.stride(3) == 1 && strides_of(x) == strides_of(ref)) return x;
+  const Tensor y = at::empty_strided(ref.sizes(), ref.strides(), x.options());
+  y.copy_(x);
+  return y;
+}
+
+// The results of a backward pass, which is no differentiable function itself: differentiating them is an error, not zero.
+variable_list once(variable_list grads, bool graph, const char* name) {
+  if (!graph) return grads;
+  variable_list there;
+  for (const auto& g : grads) if (g.defined()) there.push_back(g.detach().requires_grad_());
+  const int64_t n = (int64_t)there.size();
+  const auto error = std::make_shared<torch::autograd::DelayedError>(std::string(name) + " has no second derivative", n);
+  const at::AutoGradMode with_graph(true);
+  const variable_list out = (*error)(std::move(there));
+  size_t at = 0;
+  for (auto& g : grads) if (g.defined()) g = out[at++];
+  return grads;
+}
+
+// A backward pass that is captured while an eager graph of the same leaf lives would hand that leaf's gradient to the stream
+// the eager graph was made on, which breaks the capture and with it the process: refused here, before anything is captured.
+void capture_check(const Tensor& on, std::initializer_list<Tensor> leaves) {
+  if (!at::GradMode::is_enabled()) return;
+  const c10::DeviceGuard device(on.device());
+  if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
+  const c10::Stream now = c10::hip::getCurrentHIPStream().unwrap();
+  for (const Tensor& t : leaves) {
+    if (!t.defined() || !t.requires_grad() || !t.is_leaf()) continue;
+    const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
+    if (!node) continue;
+    const auto made_on = node->stream();
+    TORCH_CHECK(!made_on || *made_on == now, "an eager graph of one of the inputs is still alive: let go of its outputs "
+                "before capturing a backward pass (or capture without gradients)");
+  }
+}
+
+struct NormShape {
+  spa2_norm_shape s = {};
+  NormShape(const Tensor& q, const Tensor& k, const Tensor& cos, const Tensor& positions, bool interleaved, const Tensor& qo,
+            const Tensor& ko) {
+    s.B = (int32_t)q.size(0); s.Hq = (int32_t)q.size(1); s.Hk = (int32_t)k.size(1); s.N = (int32_t)q.size(2); s.d = (int32_t)q.size(3);
+    s.dtype = dtype_of(q);
+    if (cos.defined()) { s.rot = (int32_t)(2 * cos.size(1)); s.table_rows = (int32_t)cos.size(0); }
+    s.interleaved = interleaved;
+    if (positions.defined()) {
+      s.pos_bits = positions.scalar_type() == at::kInt ? 32 : 64;
+      s.pos_sb = positions.dim() == 2 && positions.size(0) > 1 ? q.size(2) : 0;
+    }
+    const auto a = strides_of(q), b = strides_of(k), c = strides_of(qo), d = strides_of(ko);
+    s.q_sb = a[0]; s.q_sh = a[1]; s.q_sn = a[2]; s.k_sb = b[0]; s.k_sh = b[1]; s.k_sn = b[2];
+    s.qo_sb = c[0]; s.qo_sh = c[1]; s.qo_sn = c[2]; s.ko_sb = d[0]; s.ko_sh = d[1]; s.ko_sn = d[2];
+  }
+};
+
+void norm_check(const Tensor& q, const Tensor& k, const Tensor& wq, const Tensor& wk, const Tensor& cos, const Tensor& sin,
+                const Tensor& positions) {
+  for (const Tensor* t : {&q, &k}) {
+    TORCH_CHECK_VALUE(t->is_cuda(), "q and k must live on the GPU: the operator has no CPU path");
+    TORCH_CHECK_VALUE(t->dim() == 4 && float_kind(*t), "q and k are bf16 or fp32 [B, H, N, d] views");
+    TORCH_CHECK_VALUE(t->stride(3) == 1, "the head dimension must be contiguous");
+  }
+  TORCH_CHECK_VALUE(k.scalar_type() == q.scalar_type() && k.device() == q.device() && k.size(0) == q.size(0) &&
+                    k.size(2) == q.size(2) && k.size(3) == q.size(3),
+                    "q and k share type, device, batch, tokens and head dimension");
+  for (const Tensor* t : {&wq, &wk})
+    TORCH_CHECK_VALUE(!t->defined() || (t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == q.size(3) &&
+                                        t->is_contiguous() && t->device() == q.device()),
+                      "weights are vectors of d elements, bf16 or fp32, on the device of q");
+  TORCH_CHECK_VALUE(cos.defined() == sin.defined(), "cos and sin come together");
+  for (const Tensor* t : {&cos, &sin})
+    TORCH_CHECK_VALUE(!t->defined() || (t->scalar_type() == at::kFloat && t->dim() == 2 && t->sizes() == cos.sizes() &&
+                                        t->is_contiguous() && t->device() == q.device()),
+                      "cos and sin are contiguous fp32 tables [rows, rotated channels / 2] on the device of q");
+  if (positions.defined()) {
+    TORCH_CHECK_VALUE(cos.defined(), "positions without tables");
+    TORCH_CHECK_VALUE((positions.scalar_type() == at::kInt || positions.scalar_type() == at::kLong) &&
+                      positions.device() == q.device() && positions.is_contiguous() &&
+                      ((positions.dim() == 1 && positions.size(0) == q.size(2)) ||
+                       (positions.dim() == 2 && positions.size(1) == q.size(2) &&
+                        (positions.size(0) == 1 || positions.size(0) == q.size(0)))),
+                      "positions are int32 or int64 numbers [N] or [B, N] on the device of q");
+  } else {
+    TORCH_CHECK_VALUE(!cos.defined() || cos.size(0) >= q.size(2), "the tables have fewer rows than there are tokens");
+  }
+}
+
+struct NormRotate : torch::autograd::Function<NormRotate> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const OptTensor& q_weight,
+                               const OptTensor& k_weight, const OptTensor& cos_, const OptTensor& sin_,
+                               const OptTensor& positions_, double eps, bool interleaved, bool weight_grads) {
+    const Tensor wq = or_none(q_weight), wk = or_none(k_weight), cos = or_none(cos_), sin = or_none(sin_), positions = or_none(positions_);
+    const c10::DeviceGuard device(q.device());
+    const Tensor qo = dense_like(q, at::kBFloat16), ko = dense_like(k, at::kBFloat16);
+    const NormShape n(q, k, cos, positions, interleaved, qo, ko);
+    check(spa2_norm_rotate(q.data_ptr(), k.data_ptr(), (const float*)ptr(wq), (const float*)ptr(wk), (const float*)ptr(cos),
+                           (const float*)ptr(sin), ptr(positions), &n.s, (float)eps, qo.data_ptr(), ko.data_ptr(),
+                           stream_of(q)), "spa2_norm_rotate");
+    ctx->save_for_backward({q, k, wq, wk, cos, sin, positions});
+    ctx->saved_data["eps"] = eps;
+    ctx->saved_data["interleaved"] = interleaved;
+    ctx->saved_data["weight_grads"] = weight_grads;
+    return {qo, ko};
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool graph = at::GradMode::is_enabled();
+    const at::NoGradGuard no_graph;
+    const variable_list s = ctx->get_saved_variables();
+    const Tensor &q = s[0], &k = s[1], &wq = s[2], &wk = s[3], &cos = s[4], &sin = s[5], &positions = s[6];
+    // (saved-tensor hooks may bring something else back)
+    norm_check(q, k, wq, wk, cos, sin, positions);
+    TORCH_CHECK_VALUE(grads[0].sizes() == q.sizes() && grads[1].sizes() == k.sizes() && grads[0].device() == q.device() &&
+                      grads[1].device() == q.device(), "saved q and k come back in their shapes on their GPU");
+    const c10::DeviceGuard device(q.device());
+    const Tensor dq = dense_like(q, q.scalar_type()), dk = dense_like(k, k.scalar_type());
+    const Tensor dqo = in_order(grads[0].to(at::kBFloat16), dq), dko = in_order(grads[1].to(at::kBFloat16), dk);
+    const bool weights = ctx->saved_data["weight_grads"].toBool();
+    const NormShape n(q, k, cos, positions, ctx->saved_data["interleaved"].toBool(), dq, dk);
+    Tensor dwq, dwk, ws;
+    if (weights) {
+      if (wq.defined()) dwq = at::empty_like(wq);
+      if (wk.defined()) dwk = at::empty_like(wk);
+      ws = bytes((int64_t)spa2_norm_rotate_bwd_workspace_bytes(&n.s), q);
+    }
+    check(spa2_norm_rotate_bwd(q.data_ptr(), k.data_ptr(), (const float*)ptr(wq), (const float*)ptr(wk), (const float*)ptr(cos),
+                               (const float*)ptr(sin), ptr(positions), dqo.data_ptr(), dko.data_ptr(), &n.s,
+                               (float)ctx->saved_data["eps"].toDouble(), dq.data_ptr(), dk.data_ptr(), (float*)ptr(dwq),
+                               (float*)ptr(dwk), (void*)ptr(ws), weights ? (size_t)ws.numel() : 0, stream_of(q)),
+          "spa2_norm_rotate_bwd");
+    return once({dq, dk, dwq, dwk, Variable(), Variable(), Variable(), Variable(), Variable(), Variable()}, graph,
+                "qk_norm_rotate");
+  }
+};
+
+// weights of any float type: the kernels read fp32 (the conversion is differentiated by PyTorch)
+OptTensor as_weight(const OptTensor& w) {
+  if (!w || !w->defined()) return std::nullopt;
+  return w->to(at::kFloat).contiguous();
+}
+
+std::tuple<Tensor, Tensor> norm_rotate(const Tensor& q, const Tensor& k, const OptTensor& q_weight, const OptTensor& k_weight,
+                                       const OptTensor& cos, const OptTensor& sin, const OptTensor& positions, double eps,
+                                       bool interleaved) {
+  const OptTensor wq = as_weight(q_weight), wk = as_weight(k_weight);
+  norm_check(q, k, or_none(wq), or_none(wk), or_none(cos), or_none(sin), or_none(positions));
+  capture_check(q, {q, k, or_none(q_weight), or_none(k_weight)});
+  const bool weight_grads = at::GradMode::is_enabled() && ((wq && wq->requires_grad()) || (wk && wk->requires_grad()));
+  const variable_list out = NormRotate::apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, weight_grads);
+  return {out[0], out[1]};
+}
+
+// x as the elementwise kernels take it: contiguous from a 16-byte boundary.
+Tensor packed(const Tensor& x) {
+  const Tensor y = x.contiguous();
+  return (reinterpret_cast<uintptr_t>(y.data_ptr()) & 15) == 0 ? y : y.clone();
+}
+
+void seed_check(const Tensor& s, const Tensor& x) {
+  TORCH_CHECK_VALUE(!s.defined() || (s.scalar_type() == at::kLong && s.numel() == 2 && s.is_contiguous() && s.device() == x.device()),
+                    "a seed on the device is two int64 numbers, seed and offset, on the device of x");
+}
+
+struct DropoutAdd : torch::autograd::Function<DropoutAdd> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& x_in, const OptTensor& residual_in, double p, int64_t seed,
+                        int64_t offset, const OptTensor& seed_offset) {
+    const c10::DeviceGuard device(x_in.device());
+    const Tensor x = packed(x_in), residual = residual_in ? packed(*residual_in) : Tensor(), so = or_none(seed_offset);
+    const Tensor y = at::empty_like(residual.defined() ? residual : x);
+    check(spa2_dropout_add(x.data_ptr(), ptr(residual), x.numel(), dtype_of(x), dtype_of(y), p, (uint64_t)seed,
+                           (uint64_t)offset, (const int64_t*)ptr(so), y.data_ptr(), stream_of(x)), "spa2_dropout_add");
+    ctx->save_for_backward({so});
+    ctx->saved_data["p"] = p;
+    ctx->saved_data["seed"] = seed;
+    ctx->saved_data["offset"] = offset;
+    ctx->saved_data["bf16"] = x.scalar_type() == at::kBFloat16;
+    ctx->saved_data["residual"] = residual.defined();
+    return y;
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool graph = at::GradMode::is_enabled();
+    const at::NoGradGuard no_graph;
+    const Tensor so = ctx->get_saved_variables()[0];
+    const Tensor dy = packed(grads[0]);
+    seed_check(so, dy);
+    const c10::DeviceGuard device(dy.device());
+    const Tensor dx = at::empty(dy.sizes(), dy.options().dtype(ctx->saved_data["bf16"].toBool() ? at::kBFloat16 : at::kFloat));
+    check(spa2_dropout_bwd(dy.data_ptr(), dy.numel(), dtype_of(dy), dtype_of(dx), ctx->saved_data["p"].toDouble(),
+                           (uint64_t)ctx->saved_data["seed"].toInt(), (uint64_t)ctx->saved_data["offset"].toInt(),
+                           (const int64_t*)ptr(so), dx.data_ptr(), stream_of(dy)), "spa2_dropout_bwd");
+    const variable_list first = once({dx}, graph, "dropout_add");
+    return {first[0], ctx->saved_data["residual"].toBool() ? grads[0] : Variable(), Variable(), Variable(), Variable(), Variable()};
+  }
+};
+
+Tensor dropout_add(const Tensor& x, const OptTensor& residual, double p, int64_t seed, int64_t offset, const OptTensor& seed_offset) {
+  TORCH_CHECK_VALUE(x.is_cuda(), "x must live on the GPU: the operator has no CPU path");
+  TORCH_CHECK_VALUE(float_kind(x), "x is bf16 or fp32");
+  if (residual)
+    TORCH_CHECK_VALUE(residual->sizes() == x.sizes() && residual->device() == x.device() &&
+                      (residual->scalar_type() == x.scalar_type() || residual->scalar_type() == at::kFloat),
+                      "the residual has the shape and device of x and its type, or fp32");
+  seed_check(or_none(seed_offset), x);
+  capture_check(x, {x, or_none(residual)});
+  return DropoutAdd::apply(x, residual, p, seed, offset, seed_offset);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("attention", &attention, py::call_guard<py::gil_scoped_release>());
+  m.def("norm_rotate", &norm_rotate, py::call_guard<py::gil_scoped_release>());
+  m.def("dropout_add", &dropout_add, py::call_guard<py::gil_scoped_release>());
   m.def("velocity_loss", &velocity_loss, py::call_guard<py::gil_scoped_release>());
 }
