@@ -307,6 +307,35 @@ int spa2_norm_rotate_bwd(const void* q, const void* k, const float* q_weight, co
                          const spa2_norm_shape* shape, float eps, void* dq, void* dk, float* d_q_weight,
                          float* d_k_weight, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- attention to another sequence (a prompt, a cache), forward and backward ----
+ *   O = softmax(scale Q K^T) V      over the keys 0 .. lengths[b] - 1 of sample b
+ * The kernels of spa2_fwd and spa2_bwd over whole rows and columns: dense, queries and keys of different number, Hq query
+ * heads that share Hk key heads (query head h reads key head h / (Hq / Hk)).  bf16, d in {64, 128}, any Nq, Nk >= 1.
+ *   q, o, o_res, d_o, dq   token tensors of Hq heads and Nq tokens that share strides q_*;
+ *   k, v                   of Hk heads and Nk tokens that share strides k_* (0 repeats a batch element or a head);
+ *   dk, dv                 the same with strides d_* (which the other calls do not look at).
+ *   lengths   device, int32 [B], clamped to [0, Nk]; NULL: Nk.  Keys and values behind a sample's length are not read.  A
+ *             sample without keys gets O = 0, LSE = -infinity and zero gradients.
+ *   lse       fp32 [B, Hq, Nq];  o_res as in spa2_fwd (NULL if no backward pass follows).
+ * spa2_cross_bwd recomputes the probabilities from LSE and writes dq, dk and dv everywhere, zeros behind the lengths; dk and
+ * dv are sums over the query heads of a key head, taken in fp32.  Lists of keys (queries) are cut over several workgroups where
+ * there are few rows (columns); the parts are joined in a fixed order, so results are deterministic.
+ * Workspaces: spa2_cross_fwd_workspace_bytes (may be 0), spa2_cross_bwd_workspace_bytes; 16-byte aligned, all of them needed.
+ * Errors: SPA2_ERR_NULL, _SHAPE (also: Hq no multiple of Hk, more than 2^23 blocks), _UNSUPPORTED (d), _ALIGN, _RANGE (scale),
+ * _WORKSPACE, _LAUNCH; checked before anything is launched. */
+typedef struct spa2_cross_shape {
+  int32_t B, Hq, Hk, Nq, Nk, d;
+  int64_t q_sb, q_sh, q_sn, k_sb, k_sh, k_sn, d_sb, d_sh, d_sn;      /* element strides of batch, head, token */
+} spa2_cross_shape;
+size_t spa2_cross_fwd_workspace_bytes(const spa2_cross_shape* shape);
+size_t spa2_cross_bwd_workspace_bytes(const spa2_cross_shape* shape);
+int spa2_cross_fwd(const void* q, const void* k, const void* v, const int32_t* lengths /* or NULL */,
+                   const spa2_cross_shape* shape, float scale, void* o, void* o_res /* or NULL */, float* lse,
+                   void* workspace, size_t workspace_bytes, void* stream);
+int spa2_cross_bwd(const void* q, const void* k, const void* v, const int32_t* lengths /* or NULL */, const void* o,
+                   const void* o_res /* or NULL */, const void* d_o, const float* lse, const spa2_cross_shape* shape,
+                   float scale, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- dropout of a branch and the sum with the residual stream: what stands behind the attention ----
  *   y = residual + x * keep / (1 - p')        p' = round(2^16 p) / 2^16, keep = 0 with probability p', else 1
  * The mask is a function of (seed, offset, element number) alone and is never stored: the generator is Philox4x32-10 (Salmon

@@ -48,6 +48,11 @@ class _NormShape(ctypes.Structure):
                                          "qo_sn", "ko_sb", "ko_sh", "ko_sn")]
 
 
+class _CrossShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hk", "Nq", "Nk", "d")] \
+        + [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_sn", "k_sb", "k_sh", "k_sn", "d_sb", "d_sh", "d_sn")]
+
+
 _lib = None
 
 
@@ -127,6 +132,15 @@ def _load():
     lib.spa2_norm_rotate.argtypes = [vp] * 7 + [nrm, f32, vp, vp, vp]
     lib.spa2_norm_rotate_bwd.restype = ctypes.c_int
     lib.spa2_norm_rotate_bwd.argtypes = [vp] * 9 + [nrm, f32, vp, vp, vp, vp, vp, sz, vp]
+    crs = ctypes.POINTER(_CrossShape)
+    lib.spa2_cross_fwd_workspace_bytes.restype = sz
+    lib.spa2_cross_fwd_workspace_bytes.argtypes = [crs]
+    lib.spa2_cross_bwd_workspace_bytes.restype = sz
+    lib.spa2_cross_bwd_workspace_bytes.argtypes = [crs]
+    lib.spa2_cross_fwd.restype = ctypes.c_int
+    lib.spa2_cross_fwd.argtypes = [vp, vp, vp, vp, crs, f32, vp, vp, vp, vp, sz, vp]
+    lib.spa2_cross_bwd.restype = ctypes.c_int
+    lib.spa2_cross_bwd.argtypes = [vp] * 8 + [crs, f32, vp, vp, vp, vp, sz, vp]
     lib.spa2_dropout_add.restype = ctypes.c_int
     lib.spa2_dropout_add.argtypes = [vp, vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
     lib.spa2_dropout_bwd.restype = ctypes.c_int
@@ -142,7 +156,8 @@ EXPORTED_SYMBOLS = ("spa2_version", "spa2_strerror", "spa2_topk_blocks", "spa2_m
                     "spa2_vd_loss_workspace_bytes", "spa2_vd_loss", "spa2_vd_loss_grad", "spa2_vd_loss_and_grad",
                     "spa2_mask_fwd", "spa2_mask_fwd_workspace_bytes", "spa2_bwd_rows", "spa2_bwd_rows_workspace_bytes",
                     "spa2_vd_rescale", "spa2_norm_rotate", "spa2_norm_rotate_bwd", "spa2_norm_rotate_bwd_workspace_bytes",
-                    "spa2_dropout_add", "spa2_dropout_bwd")
+                    "spa2_dropout_add", "spa2_dropout_bwd", "spa2_cross_fwd", "spa2_cross_bwd",
+                    "spa2_cross_fwd_workspace_bytes", "spa2_cross_bwd_workspace_bytes")
 
 
 # ------------------------------------------------------------------ plumbing (memory only)
@@ -541,6 +556,47 @@ def spa2_norm_rotate_bwd(q, k, q_weight, k_weight, cos, sin, positions, d_q_out,
                                         _ptr(positions), d_q_out.data_ptr(), d_k_out.data_ptr(), ctypes.byref(s), float(eps),
                                         dq.data_ptr(), dk.data_ptr(), _ptr(d_q_weight), _ptr(d_k_weight), _ptr(workspace),
                                         0 if workspace is None else _nbytes(workspace), _stream(q)), "spa2_norm_rotate_bwd")
+
+
+def _cross_args(q, k, v, lengths, dk=None) -> _CrossShape:
+    for t in (q, k, v):
+        if t.dim() != 4 or t.dtype != torch.bfloat16 or t.stride(3) != 1:
+            raise ValueError("q, k and v are bf16 [B, H, N, d] views, d contiguous")
+    if v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("k and v share shape and strides")
+    if (k.shape[0], k.shape[3]) != (q.shape[0], q.shape[3]):
+        raise ValueError("q and k share batch and head dimension")
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != q.shape[:1] or not lengths.is_contiguous()
+                                or lengths.device != q.device):
+        raise ValueError("lengths are int32 [B]")
+    B, Hq, Nq, d = q.shape
+    return _CrossShape(B, Hq, k.shape[1], Nq, k.shape[2], d, *q.stride()[:3], *k.stride()[:3], *(k if dk is None else dk).stride()[:3])
+
+
+def spa2_cross_fwd_workspace_bytes(q, k) -> int:
+    return int(_load().spa2_cross_fwd_workspace_bytes(ctypes.byref(_cross_args(q, k, k, None))))
+
+
+def spa2_cross_bwd_workspace_bytes(q, k) -> int:
+    return int(_load().spa2_cross_bwd_workspace_bytes(ctypes.byref(_cross_args(q, k, k, None))))
+
+
+def spa2_cross_fwd(q, k, v, lengths, scale: float, o, lse, o_res=None, workspace=None) -> None:
+    s = _cross_args(q, k, v, lengths)
+    _same_layout(q, o, *([o_res] if o_res is not None else []))
+    _check(_load().spa2_cross_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), ctypes.byref(s), float(scale),
+                                  o.data_ptr(), _ptr(o_res), lse.data_ptr(), _ptr(workspace),
+                                  0 if workspace is None else _nbytes(workspace), _stream(q)), "spa2_cross_fwd")
+
+
+def spa2_cross_bwd(q, k, v, lengths, o, d_o, lse, scale: float, dq, dk, dv, workspace, o_res=None) -> None:
+    s = _cross_args(q, k, v, lengths, dk)
+    _same_layout(q, o, d_o, dq, *([o_res] if o_res is not None else []))
+    if dk.shape != k.shape or dv.shape != k.shape or dk.stride() != dv.stride() or dk.dtype != k.dtype or dv.dtype != k.dtype:
+        raise ValueError("dk and dv have the shape and type of k and share strides")
+    _check(_load().spa2_cross_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), o.data_ptr(), _ptr(o_res),
+                                  d_o.data_ptr(), lse.data_ptr(), ctypes.byref(s), float(scale), dq.data_ptr(), dk.data_ptr(),
+                                  dv.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream(q)), "spa2_cross_bwd")
 
 
 def _drop_args(x, like, seed_offset) -> None:

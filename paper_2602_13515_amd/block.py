@@ -2,6 +2,8 @@
 
 * `qk_norm_rotate`   in front of it: the norm of every head of q and k and the rotation by position, in one pass
                      (`rotary_table` makes the tables of cosines and sines);
+* `cross_attention`  beside it: dense attention to another sequence, a prompt or a cache, whose samples have lengths of
+                     their own;
 * `dropout_add`      behind it: dropout of a branch and the sum with the residual stream, the mask drawn from a counter-based
                      generator and never stored.
 
@@ -10,6 +12,7 @@ refused.  The C entry points are in `binding` under their C names.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional, Sequence, Tuple, Union
 
 import torch
@@ -63,6 +66,22 @@ def qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Te
     `sparge_attn2` and `cross_attention` take.  Gradients: q, k (in their type) and the weights."""
     _refuse_others("qk_norm_rotate", q, k, q_weight, k_weight, cos, sin, positions)
     return _operator().norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, float(eps), bool(interleaved))
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None) -> torch.Tensor:
+    """softmax(scale q k^T) v over the first lengths[b] keys of sample b (None: all of them).
+
+    q [B, Hq, Nq, d], k, v [B, Hk, Nk, d]: bf16 views, d in {64, 128} contiguous; Hq is a multiple of Hk, and query head h
+    reads key head h // (Hq // Hk).  Any Nq, Nk >= 1: one query against a long cache as well as many against a short prompt.
+    lengths: int32 [B] on the GPU, clamped to [0, Nk]; what lies behind them in k and v is not read, and a sample without
+    keys gives zeros and zero gradients.  scale: 1 / sqrt(d) if None.  Returns bf16 with q's shape (and memory order).
+    Gradients: q, k, v; those of k and v are zero behind the lengths and summed over the query heads in fp32.  (A q with gaps
+    between its heads and v with other strides than k are copied first.)"""
+    _refuse_others("cross_attention", q, k, v, lengths)
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1]) if q.dim() and q.shape[-1] else 1.0      # (those are refused there)
+    return _operator().cross_attention(q, k, v, lengths, float(scale))
 
 
 def _signed(x: int) -> int:

@@ -1,5 +1,6 @@
 // Entry points of the operators around the block-sparse attention: argument checks, then the launches.
 #include "block_ops.h"
+#include "cross.h"
 #include "spa2_check.h"
 
 using namespace spa2;
@@ -42,9 +43,100 @@ bool dtype_ok(int32_t t) { return t == SPA2_DTYPE_BF16 || t == SPA2_DTYPE_F32; }
 
 uint32_t dropout_cut(double p) { return (uint32_t)floor(p * 65536.0 + 0.5); }
 
+constexpr int64_t CROSS_MAX_BLOCKS = 1 << 23;       // workgroups are numbered in 32 bits, also in threads
+
+// a stride triple of bf16 heads
+int check_strides(int64_t sb, int64_t sh, int64_t sn, int64_t least, int d) {
+  if (sb < least || sh < least || sn < d || sn > SPA2_MAX_TOKEN_STRIDE) return SPA2_ERR_SHAPE;
+  return sb % 8 || sh % 8 || sn % 8 ? SPA2_ERR_ALIGN : SPA2_OK;
+}
+
+int check_cross_shape(const spa2_cross_shape* s) {
+  if (!s) return SPA2_ERR_NULL;
+  if (s->B <= 0 || s->Hq <= 0 || s->Hk <= 0 || s->Nq <= 0 || s->Nk <= 0 || s->d <= 0 || s->Hq % s->Hk) return SPA2_ERR_SHAPE;
+  if (s->d != 64 && s->d != 128) return SPA2_ERR_UNSUPPORTED;
+  const int64_t tm = ((int64_t)s->Nq + SPA2_BQ - 1) / SPA2_BQ, tn = ((int64_t)s->Nk + SPA2_BKV - 1) / SPA2_BKV;
+  if ((int64_t)s->B * s->Hq > CROSS_MAX_BLOCKS || (int64_t)s->B * s->Hq * tm > CROSS_MAX_BLOCKS ||
+      (int64_t)s->B * s->Hk * tn > CROSS_MAX_BLOCKS)
+    return SPA2_ERR_SHAPE;
+  int rc = check_strides(s->q_sb, s->q_sh, s->q_sn, 1, s->d);
+  if (rc == SPA2_OK) rc = check_strides(s->k_sb, s->k_sh, s->k_sn, 0, s->d);
+  return rc;
+}
+
+CrossDims cross_dims(const spa2_cross_shape& s) {
+  CrossDims m;
+  m.q.B = s.B; m.q.H = s.Hq; m.q.N = s.Nq; m.q.d = s.d;
+  m.q.Tm = (s.Nq + SPA2_BQ - 1) / SPA2_BQ;
+  m.q.Tn = (s.Nk + SPA2_BKV - 1) / SPA2_BKV;
+  m.q.sb = s.q_sb; m.q.sh = s.q_sh; m.q.sn = s.q_sn;
+  m.Hk = s.Hk; m.Nk = s.Nk; m.group = s.Hq / s.Hk;
+  m.ksb = s.k_sb; m.ksh = s.k_sh; m.ksn = s.k_sn;
+  m.dsb = s.d_sb; m.dsh = s.d_sh; m.dsn = s.d_sn;
+  return m;
+}
+
+int check_cross(const void* q, const void* k, const void* v, const int32_t* lengths, const void* o, const void* o_res,
+                const float* lse, const spa2_cross_shape* shape, float scale) {
+  const int rc = check_cross_shape(shape);
+  if (rc != SPA2_OK) return rc;
+  if (!q || !k || !v || !o || !lse) return SPA2_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_res) || (uintptr_t)lengths % 4 ||
+      (uintptr_t)lse % 4)
+    return SPA2_ERR_ALIGN;
+  if (!(scale > 0.f) || !isfinite(scale)) return SPA2_ERR_RANGE;
+  return SPA2_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t spa2_cross_fwd_workspace_bytes(const spa2_cross_shape* shape) {
+  if (check_cross_shape(shape) != SPA2_OK) return 0;
+  return cross_fwd_ws(cross_dims(*shape)).total;
+}
+
+size_t spa2_cross_bwd_workspace_bytes(const spa2_cross_shape* shape) {
+  if (check_cross_shape(shape) != SPA2_OK) return 0;
+  return cross_bwd_ws(cross_dims(*shape)).total;
+}
+
+int spa2_cross_fwd(const void* q, const void* k, const void* v, const int32_t* lengths, const spa2_cross_shape* shape,
+                   float scale, void* o, void* o_res, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_cross(q, k, v, lengths, o, o_res, lse, shape, scale);
+  if (rc != SPA2_OK) return rc;
+  const CrossDims m = cross_dims(*shape);
+  const size_t need = cross_fwd_ws(m).total;
+  if (need && (!workspace || workspace_bytes < need)) return SPA2_ERR_WORKSPACE;
+  if (need && !aligned16(workspace)) return SPA2_ERR_ALIGN;
+  return launch_cross_fwd(q, k, v, m, lengths, scale, o, o_res, lse, workspace, (hipStream_t)stream) == hipSuccess
+             ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
+
+int spa2_cross_bwd(const void* q, const void* k, const void* v, const int32_t* lengths, const void* o, const void* o_res,
+                   const void* d_o, const float* lse, const spa2_cross_shape* shape, float scale, void* dq, void* dk, void* dv,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_cross(q, k, v, lengths, o, o_res, lse, shape, scale);
+  if (rc == SPA2_OK) rc = check_strides(shape->d_sb, shape->d_sh, shape->d_sn, 1, shape->d);
+  if (rc != SPA2_OK) return rc;
+  if (!d_o || !dq || !dk || !dv) return SPA2_ERR_NULL;
+  if (!aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv)) return SPA2_ERR_ALIGN;
+  const CrossDims m = cross_dims(*shape);
+  const CrossBwdWs w = cross_bwd_ws(m);
+  if (!workspace || workspace_bytes < w.total) return SPA2_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return SPA2_ERR_ALIGN;
+  char* ws = (char*)workspace;
+  float* delta = (float*)ws;
+  hipStream_t st = (hipStream_t)stream;
+  const SplitPlan cols = cross_plan(w.dkdv, ws + w.dkdv_counters, ws + w.dkdv_pool, dkdv_slot_bytes(m.q));
+  const SplitPlan rows = cross_plan(w.dq, ws + w.dq_counters, ws + w.dq_pool, dq_slot_bytes(m.q));
+  if (launch_cross_delta(o, o_res, d_o, m, delta, (int32_t*)(ws + w.dkdv_counters),
+                         (int)((w.dkdv_pool - w.dkdv_counters) / 4), st) != hipSuccess ||
+      launch_cross_dkdv(q, k, v, d_o, lse, delta, m, lengths, scale, dk, dv, cols, st) != hipSuccess)
+    return SPA2_ERR_LAUNCH;
+  return launch_cross_dq(q, k, v, d_o, lse, delta, m, lengths, scale, dq, rows, st) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
 
 size_t spa2_norm_rotate_bwd_workspace_bytes(const spa2_norm_shape* shape) {
   if (check_norm_shape(shape) != SPA2_OK) return 0;

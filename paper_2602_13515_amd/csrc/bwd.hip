@@ -12,6 +12,7 @@
 // dQ is produced by a second, row-oriented pass instead of atomics: results are
 // deterministic and there is no fp32 dQ scratch tensor.
 #include "columns.h"
+#include "cross.h"
 #include "row_delta.h"
 #include "row_map.h"
 #include "spa2_device.h"
@@ -35,6 +36,7 @@ hipError_t launch_bwd_delta(const void* o, const void* o_res, const void* d_o, c
 
 // ------------------------------------------------------------------ dQ
 struct DqArgs {
+  static constexpr bool CROSS = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v; const uint16_t* d_o;
   const float* lse; const float* delta; uint16_t* dq;
   const int32_t* row_cnt; const int32_t* row_idx; const int32_t* row_order;
@@ -48,6 +50,12 @@ struct DqArgs {
   OrderArgs col_order; ListArgs col_list;        // (one of them, by whether the launch is in stretches)
   int front, orders;
   bool stretches;
+};
+
+// Attention to another sequence (see fwd.hip).
+struct CrossDqArgs : DqArgs {
+  static constexpr bool CROSS = true;
+  CrossKeys kv;
 };
 
 // Partial result of one part of a split row: the fp32 accumulators as [pair of registers][thread] (see fwd.hip).
@@ -83,8 +91,9 @@ __device__ __forceinline__ void dq_store_rows(const DqArgs& a, int64_t base, int
 // tile, 128 of 336 vector instructions, the copies multiplied out their offsets, and all exponentials stood in one run).
 // Measured, us, before / after: 75,600 tokens, 40 heads 10877 / 9674; 32,760 tokens, 12 heads 662 / 574; 32,768 tokens,
 // 24 heads, half the rows long 6466 / 5435; 20,010 tokens, 6 heads, d = 64 89 / 78.
-template <int D>
-__global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
+  constexpr bool CROSS = Args::CROSS;
   constexpr int NK = D / 16, NMB = D / 32;           // contraction steps of S and dP, output blocks of dQ
   // K and V tiles, XOR-swizzled and unpadded (the layout a direct global -> LDS copy can write): K is read along rows
   // (S^T) and transposed (dQ^T), V along rows (dP^T).  (Aligned: compile-time parts are XORed into addresses.)
@@ -96,7 +105,21 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
   // Which row, and which part of its list (see fwd.hip: the first sp.pool_slots workgroups are the parts of split rows)
   int bh, i, part = 0, parts = 0, part_len = 0;
   bool whole = false;
-  const int slot = (int)blockIdx.x - a.front;
+  int slot = (int)blockIdx.x - (CROSS ? 0 : a.front);
+  int keys = a.N;             // keys that the row sees at most
+  if constexpr (CROSS) {
+    const int rows = stretch_wgs(a.BH * a.Tm);
+    const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
+    if (!hb.valid) return;
+    bh = hb.bh; i = hb.blk;
+    keys = cross_length(a.kv, bh / a.H);
+    const int all = (keys + BKV - 1) / BKV;
+    part = blockIdx.x / rows;
+    parts = all > a.sp.fixed_len ? (all + a.sp.fixed_len - 1) / a.sp.fixed_len : 0;
+    if (part >= max(parts, 1)) return;
+    if (parts) part_len = (all + parts - 1) / parts;
+    slot = (bh * a.Tm + i) * a.sp.fixed_parts + part;
+  } else {
   if (slot < 0) {
     if (blockIdx.x == 0) plan_block<256>(a.col_plan, *(PlanLds<256>*)smem);
     return;
@@ -121,20 +144,28 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
     i = a.row_order ? min(max(a.row_order[(int64_t)bh * a.Tm + hb.blk], 0), a.Tm - 1) : hb.blk;
     whole = a.sp.pool_slots != 0;
   }
+  }
   const int64_t base = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);     // wave-uniform, in a scalar register
   const int r32 = lane & 31, hf = lane >> 5;
   const int N = a.N;
   const int64_t unit = (int64_t)bh * a.Tm + i;
-  int cnt = min(max(a.row_cnt[unit], 0), a.Tn);   // clamped: see fwd.hip
-  const int split_at = *(whole ? a.sp.unit_slot + unit : a.row_cnt + unit);
   const int first = part * part_len;         // entries [first, first + part_len) of the list of a split row
-  const int32_t* idx = a.row_idx + unit * a.Tn + first;
+  int cnt, split_at = 0;
+  const int32_t* idx = nullptr;
+  if constexpr (CROSS) {
+    cnt = (keys + BKV - 1) / BKV;
+  } else {
+    cnt = min(max(a.row_cnt[unit], 0), a.Tn);   // clamped: see fwd.hip
+    split_at = *(whole ? a.sp.unit_slot + unit : a.row_cnt + unit);
+    idx = a.row_idx + unit * a.Tn + first;
+  }
   // the index list, 64 entries at a time in one register (lane l holds entry 64c + l): reading an entry is
   // a lane read, not a memory access whose result the loop would have to wait for.  (The first ones and the rows are
   // requested before the count is known: see fwd.hip.)
-  int idx_v = idx[min(lane, a.Tn - 1 - first)];
+  int idx_v = 0;
+  if constexpr (!CROSS) idx_v = idx[min(lane, a.Tn - 1 - first)];
   const int qrow = i * BQ + w * 32 + r32;
   const int qrow_ld = qrow < N ? qrow : N - 1;
   bf16x8 qf[D / 16], dof[D / 16];
@@ -161,6 +192,11 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
     return;
   }
 
+  int64_t key_base = base, key_sn = a.sn;
+  if constexpr (CROSS) {
+    key_base = (int64_t)(bh / a.H) * a.kv.sb + (int64_t)((bh % a.H) / a.kv.group) * a.kv.sh;
+    key_sn = a.kv.sn;
+  }
   // K/V tiles are copied global -> LDS directly (no staging registers).  The destination of a wave-wide
   // 16-byte-per-lane copy is linear (wave base + 16 * lane), so the swizzle is applied on the source side: the
   // lane that fills chunk position pc of a row fetches logical chunk pc ^ swz(row).  Thread t fills chunk
@@ -184,12 +220,12 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
     rows_set = last;
     const int t = fresh_tid(), ld_row = t / CPR, ld_c8 = ((t % CPR) ^ swz<D>(ld_row)) * 8;
 #pragma unroll
-    for (int r = 0; r < CH; ++r) voff[r] = (uint32_t)((min(ld_row + RSTEP * r, last) * a.sn + ld_c8) * 2);
+    for (int r = 0; r < CH; ++r) voff[r] = (uint32_t)((min(ld_row + RSTEP * r, last) * key_sn + ld_c8) * 2);
   };
   const uint32_t sm = lds_addr_of(smem);
-  const char* k_head = (const char*)(a.k + base);
-  const char* v_head = (const char*)(a.v + base);
-  const uint64_t tile_bytes = (uint64_t)a.sn * (2 * BKV);
+  const char* k_head = (const char*)(a.k + key_base);
+  const char* v_head = (const char*)(a.v + key_base);
+  const uint64_t tile_bytes = (uint64_t)key_sn * (2 * BKV);
   constexpr int NPIECE = 2 * CH;             // piece p of a tile's copies: rows p / 2 of K (p even) or V
   auto copy_piece = [&](auto P, const char* kp, const char* vp, uint32_t stage) {
     constexpr int p = decltype(P)::v, r = p >> 1;
@@ -215,22 +251,23 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
   const uint32_t kt_off1 = sm + 2 * swz_idx<D>(8 + 4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
 
   auto list_entry = [&](int t) -> int {      // t uniform, inside the chunk that idx_v holds
+    if constexpr (CROSS) return first + t;
     return min(max(__builtin_amdgcn_readlane(idx_v, t & 63), 0), a.Tn - 1);
   };
   int j_cur = list_entry(0);
-  set_rows(min(BKV - 1, N - 1 - j_cur * BKV));
+  set_rows(min(BKV - 1, keys - 1 - j_cur * BKV));
   static_for<0, NPIECE>([&](auto P) { copy_piece(P, k_head + j_cur * tile_bytes, v_head + j_cur * tile_bytes, sm); });
   raw_copies_done();
   __syncthreads();
 
   for (int t = 0; t < cnt; ++t) {
     const int j = j_cur;
-    if (((t + 1) & 63) == 0 && t + 1 < cnt) idx_v = list_load(idx, min(t + 1 + (fresh_tid() & 63), cnt - 1));     // next 64 entries
+    if (!CROSS && ((t + 1) & 63) == 0 && t + 1 < cnt) idx_v = list_load(idx, min(t + 1 + (fresh_tid() & 63), cnt - 1));     // next 64 entries
     // The copies of tile t+1 are handed out between the MFMAs of the S^T / dP^T products of iteration t: issued
     // back to back they keep the wave at the issue stage until the texture unit has taken the last one.  They are
     // unconditional (past the end of the list the last tile is requested again, into the buffer nobody reads).
     j_cur = list_entry(min(t + 1, cnt - 1));
-    set_rows(min(BKV - 1, N - 1 - j_cur * BKV));
+    set_rows(min(BKV - 1, keys - 1 - j_cur * BKV));
     const char* kpn = k_head + j_cur * tile_bytes;
     const char* vpn = v_head + j_cur * tile_bytes;
     const uint32_t nx_stage = sm + ((t + 1) & 1) * STAGE_B;
@@ -255,7 +292,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
       return join_tr(lds_tr4_at((kt0 ^ (mb << 6)) + o), lds_tr4_at((kt1 ^ (mb << 6)) + o));
     };
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const bool tail = (j + 1) * BKV > N;
+    const bool tail = (j + 1) * BKV > keys;
     f32x16 s[2], dp[2];
     uint32_t dsk[2][8];
     auto exp_unit = [&](auto KB, auto U) {   // P^T of two keys
@@ -266,7 +303,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(DqArgs a) {
     auto mask_tail = [&](auto KB) {          // keys past N (short last block): P = 0
       constexpr int kb = decltype(KB)::v;
       if (tail) {                            // (a branch: as selects it cost four instructions an element and tile)
-        const int valid = N - j * BKV - kb * 32 - 4 * ((fresh_tid() & 63) >> 5);
+        const int valid = keys - j * BKV - kb * 32 - 4 * ((fresh_tid() & 63) >> 5);
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (8 * (v >> 2) + (v & 3) >= valid) s[kb][v] = 0.f;
@@ -362,8 +399,8 @@ static hipError_t launch_dq(const void* q, const void* k, const void* v, const v
   }
   const int rows = launched_rows(a.BH, a.Tm, a.chunk);
   const dim3 grid((unsigned)(a.front + plan.pool_slots + rows + a.orders)), block(256);
-  if (m.d == 128) hipLaunchKernelGGL(dq_kernel<128>, grid, block, 0, stream, a);
-  else            hipLaunchKernelGGL(dq_kernel<64>, grid, block, 0, stream, a);
+  if (m.d == 128) hipLaunchKernelGGL((dq_kernel<128, DqArgs>), grid, block, 0, stream, a);
+  else            hipLaunchKernelGGL((dq_kernel<64, DqArgs>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -379,6 +416,43 @@ hipError_t launch_bwd_dq_columns(const void* q, const void* k, const void* v, co
                                  const int32_t* col_cnt, int32_t* col_order, const SplitPlan& col_plan, hipStream_t stream) {
   return launch_dq(q, k, v, d_o, lse, delta, m, row_cnt, row_idx, row_order, scale, dq, plan, &col_plan, col_cnt, col_order,
                    stream);
+}
+
+// ------------------------------------------------------------------ attention to another sequence
+CrossSection cross_dq_section(const CrossDims& m) {
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, 8, dq_slot_bytes(m.q));
+}
+
+// D of every query row, and zeros in the arrival counters of the two launches behind it.
+template <int D>
+__global__ __launch_bounds__(256) void cross_delta_kernel(DeltaArgs a, int32_t* zero, int zeros) {
+  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < zeros; x += (int64_t)gridDim.x * 256) zero[x] = 0;
+  delta_block<D>(a, blockIdx.x / a.chunks, blockIdx.x % a.chunks);
+}
+hipError_t launch_cross_delta(const void* o, const void* o_res, const void* d_o, const CrossDims& m, float* delta, int32_t* zero,
+                              int zeros, hipStream_t stream) {
+  const DeltaArgs a = delta_args(o, o_res, d_o, m.q, delta);
+  const dim3 grid((unsigned)(a.chunks * m.q.B * m.q.H)), block(256);
+  if (m.q.d == 128) hipLaunchKernelGGL(cross_delta_kernel<128>, grid, block, 0, stream, a, zero, zeros);
+  else              hipLaunchKernelGGL(cross_delta_kernel<64>, grid, block, 0, stream, a, zero, zeros);
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
+                           const CrossDims& m, const int32_t* lengths, float scale, void* dq, const SplitPlan& plan,
+                           hipStream_t stream) {
+  CrossDqArgs a = {};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
+  a.lse = lse; a.delta = delta; a.dq = (uint16_t*)dq;
+  a.BH = m.q.B * m.q.H; a.H = m.q.H; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
+  a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
+  a.scale = scale; a.scale_log2 = scale * LOG2E;
+  a.kv = cross_keys(m, lengths);
+  a.sp = plan;
+  const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tm))), block(256);
+  if (m.q.d == 128) hipLaunchKernelGGL((dq_kernel<128, CrossDqArgs>), grid, block, 0, stream, a);
+  else              hipLaunchKernelGGL((dq_kernel<64, CrossDqArgs>), grid, block, 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace spa2

@@ -2,6 +2,8 @@
 // kernels).  This file is compiled with -mllvm -amdgpu-mfma-vgpr-form: the S / dP products then leave their
 // results in ordinary vector registers, where the exp / dS arithmetic reads them directly, while the dK / dV
 // accumulators are pinned to the accumulation registers through mfma32_acc below.
+#include "cross.h"
+#include "row_map.h"
 #include "spa2_device.h"
 #include "spa2_internal.h"
 #include "work_queue.h"
@@ -20,6 +22,7 @@ __device__ __forceinline__ void mfma32_acc(bf16x8 a, bf16x8 b, f32x16& c) {
 
 // ------------------------------------------------------------------ dK, dV
 struct DkvArgs {
+  static constexpr bool CROSS = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v; const uint16_t* d_o;
   const float* lse; const float* delta; uint16_t* dk; uint16_t* dv;
   const int32_t* col_cnt; const int32_t* col_idx; const int32_t* col_order;
@@ -29,6 +32,44 @@ struct DkvArgs {
   SplitPlan sp;         // long columns cut into parts (split.hip); sp.pool_slots == 0: every column is walked whole
 };
 
+// Attention to another sequence: a column is a block of keys of one key head; its list is every query block of every query
+// head that reads this key head, one head after the other, so that the sums over the heads are taken in the accumulators.
+// (bh, H: key heads.  N, T_m, sb, sh, sn: of the queries.)
+struct CrossDkvArgs : DkvArgs {
+  static constexpr bool CROSS = true;
+  CrossKeys kv;
+  int64_t dsb, dsh, dsn;      // strides of dK and dV
+};
+// the walk of a workgroup that has one item
+struct OneItem {
+  int wave;
+  __device__ __forceinline__ void draw(const SplitPlan&) {}
+};
+
+// Where a column's keys lie and its results go.
+struct ColumnPlace { int64_t in, in_sn, out, out_sn; int keys, rows; };       // keys seen; rows of dK and dV
+template <class Args>
+__device__ __forceinline__ ColumnPlace column_place(const Args& a, int bh, int64_t base) {
+  if constexpr (Args::CROSS) {
+    const int b = bh / a.H, h = bh % a.H;
+    return {b * a.kv.sb + h * a.kv.sh, a.kv.sn, b * a.dsb + h * a.dsh, a.dsn, cross_length(a.kv, b), a.kv.Nk};
+  } else {
+    return {base, a.sn, base, a.sn, a.N, a.N};
+  }
+}
+template <class Args>
+__device__ __forceinline__ int cross_group(const Args& a) {
+  if constexpr (Args::CROSS) return a.kv.group;
+  else                       return 1;
+}
+// Query head and block of entry e of a column's list.
+struct CrossEntry { int g, i; };
+template <class Args>
+__device__ __forceinline__ CrossEntry cross_entry(const Args& a, int e) {
+  const int g = a.kv.group == 1 ? 0 : e / a.Tm;
+  return {g, e - g * a.Tm};
+}
+
 // Partial result of one part of a split column: the fp32 sums of the two waves, dK^T then dV^T, in the order
 // [tensor][finishing wave][output block][pair of registers][lane][register in the pair].
 template <int D> constexpr int dkdv_slot_floats() { return 2 * 2 * (D / 32) * 16 * 64; }
@@ -36,8 +77,8 @@ size_t dkdv_slot_bytes(const Dims& m) { return (size_t)(m.d == 128 ? dkdv_slot_f
 
 // The last part of a split column to arrive adds all of them in part order and stores the rows that wave w finishes, key0w ..
 // (area: 32 * D * 2 bytes of LDS of the wave's own).
-template <int D>
-__device__ __forceinline__ void dkdv_merge(const DkvArgs& a, const WorkItem& item, int64_t base, int key0w, int w, int lane,
+template <int D, class Args>
+__device__ __forceinline__ void dkdv_merge(const Args& a, const WorkItem& item, const ColumnPlace& at, int key0w, int w, int lane,
                                            uint32_t area) {
   constexpr int NMB = D / 32;
   const float* p0 = a.sp.pool + (int64_t)(item.slot - item.part) * a.sp.slot_floats + 2 * lane;
@@ -61,9 +102,10 @@ __device__ __forceinline__ void dkdv_merge(const DkvArgs& a, const WorkItem& ite
       for (int g = 0; g < 4; ++g) {
         const f32x2 lo = x[mb * 8 + 2 * g], hi = x[mb * 8 + 2 * g + 1];
         u32x2 pk2 = {pack_bf16(lo[0] * sc, lo[1] * sc), pack_bf16(hi[0] * sc, hi[1] * sc)};
+        if (Args::CROSS && key0w + (lane & 31) >= at.keys) pk2 = u32x2{0, 0};       // (see the end of dkdv_item)
         row_piece_put<D>(area, lane & 31, 4 * mb + g, lane >> 5, pk2);
       }
-    rows_store<D>(area, (round == 0 ? a.dk : a.dv) + base + (int64_t)key0w * a.sn, a.sn, a.N - key0w, lane);
+    rows_store<D>(area, (round == 0 ? a.dk : a.dv) + at.out + (int64_t)key0w * at.out_sn, at.out_sn, at.rows - key0w, lane);
   }
 }
 
@@ -93,9 +135,10 @@ __device__ __forceinline__ void dkdv_merge(const DkvArgs& a, const WorkItem& ite
 // copy stood behind a branch), 1.80 instead of 1.95 GHz.  Measured, us, before / after: 75,600 tokens, 40 heads
 // 14772 / 13440; 32,760 tokens, 12 heads 1026 / 921.
 // The two waves add their partial sums through LDS at the end of the column.
-template <int D>
-__device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item, Walk& walk, unsigned char* smem,
+template <int D, class Args, class Way>
+__device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, Way& walk, unsigned char* smem,
                                           unsigned char* stat_s) {
+  constexpr bool CROSS = Args::CROSS;
   constexpr int QW = 32;                             // query rows per wave and step
   constexpr int HQ = 64;                             // query rows per workgroup and step
   constexpr int NK = D / 16;                         // 16-wide contraction steps over the head dimension
@@ -107,23 +150,31 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
   constexpr int STAGE_B = 2 * TILE_B;                // Q rows, then dO rows
   constexpr int STAT_B = 512;                        // LSE of the 32 rows at +0, D at +256
   const int bh = item.bh, j = item.blk, part = item.part, parts = item.parts, part_len = item.part_len;
-  const int64_t base = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh;
+  const int64_t base = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh * (CROSS ? cross_group(a) : 1);
   const int lane = fresh_lane(), w = walk.wave;
   const int r32 = lane & 31, hf = lane >> 5;
   const int N = a.N;
-  int cnt = min(max(a.col_cnt[(int64_t)bh * a.Tn + j], 0), a.Tm);   // clamped: see fwd.hip
-  const int32_t* idx = a.col_idx + ((int64_t)bh * a.Tn + j) * a.Tm;
+  const ColumnPlace at = column_place(a, bh, base);
+  int cnt;
+  const int32_t* idx = nullptr;
+  if constexpr (CROSS) {
+    cnt = j * BKV < at.keys ? a.kv.group * a.Tm : 0;
+  } else {
+    cnt = min(max(a.col_cnt[(int64_t)bh * a.Tn + j], 0), a.Tm);   // clamped: see fwd.hip
+    idx = a.col_idx + ((int64_t)bh * a.Tn + j) * a.Tm;
+  }
+  const int first = part * part_len;
   if (parts) {                // entries [part * part_len, (part + 1) * part_len) of the list
-    idx += part * part_len;
-    cnt = min(cnt - part * part_len, part_len);
+    if constexpr (!CROSS) idx += first;
+    cnt = min(cnt - first, part_len);
   }
 
   const int key0 = j * BKV + r32;                    // this lane's key of half 0; half 1 is 32 further
 
   if (cnt == 0) {   // no query block selected this key block: zero gradients (wave w writes key half w)
     const int key = key0 + 32 * w;
-    if (key < N) {
-      const int64_t out_off = base + (int64_t)key * a.sn + 4 * hf;
+    if (key < at.rows) {
+      const int64_t out_off = at.out + (int64_t)key * at.out_sn + 4 * hf;
 #pragma unroll
       for (int c = 0; c < D / 8; ++c) {
         *(u32x2*)(a.dk + out_off + 8 * c) = u32x2{0, 0};
@@ -138,7 +189,7 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
   bf16x8 kf[2][NK], vf[2][NK];
 #pragma unroll
   for (int kh = 0; kh < 2; ++kh) {
-    const int64_t off = base + (int64_t)min(key0 + 32 * kh, N - 1) * a.sn + 8 * hf;
+    const int64_t off = at.in + (int64_t)min(key0 + 32 * kh, at.keys - 1) * at.in_sn + 8 * hf;
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       kf[kh][kk] = *(const bf16x8*)(a.k + off + 16 * kk);
@@ -175,14 +226,15 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
   };
   const char* q_head = (const char*)(a.q + base);
   const char* o_head = (const char*)(a.d_o + base);
-  const char* lse_head = (const char*)(a.lse + (int64_t)bh * N);
-  const char* dlt_head = (const char*)(a.delta + (int64_t)bh * N);
+  const int64_t stat_base = (int64_t)bh * N * (CROSS ? cross_group(a) : 1);
+  const char* lse_head = (const char*)(a.lse + stat_base);
+  const char* dlt_head = (const char*)(a.delta + stat_base);
   const uint64_t row_bytes = (uint64_t)a.sn * 2;
   const uint32_t wsm = lds_addr_of(smem) + 2 * w * STAGE_B;       // uniform LDS byte addresses
   const uint32_t wstat = lds_addr_of(stat_s) + 2 * w * STAT_B;
-  auto copy_stats = [&](int row, uint32_t stat_addr) {
-    raw_copy4_to_lds_at<0>(lse_head + (uint64_t)row * 4, soff, stat_addr);
-    raw_copy4_to_lds_at<256>(dlt_head + (uint64_t)row * 4, soff, stat_addr);
+  auto copy_stats = [&](uint64_t row, uint32_t stat_addr) {
+    raw_copy4_to_lds_at<0>(lse_head + row * 4, soff, stat_addr);
+    raw_copy4_to_lds_at<256>(dlt_head + row * 4, soff, stat_addr);
   };
   // Query rows past N get an LSE of +infinity once their copy has landed: their P is then exactly zero.
   auto mark_rows_past_end = [&](int row0, uint32_t stat_addr) {
@@ -193,11 +245,20 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
 
   // the index list, 64 entries at a time in one register (lane l holds entry 64c + l): reading entry t is a
   // lane read, not a memory access
-  int idx_v = idx[min(lane, cnt - 1)];
+  int idx_v = 0, g_at = 0;                   // (g_at: query head of the step asked for last)
+  if constexpr (!CROSS) idx_v = idx[min(lane, cnt - 1)];
   auto step_row = [&](int u) -> int {        // first row of step u (uniform, inside the chunk that idx_v holds)
+    if constexpr (CROSS) {
+      const CrossEntry e = cross_entry(a, first + (u >> 1));
+      g_at = e.g;
+      return e.i * BQ + (u & 1) * HQ + QW * w;
+    }
     const int i = min(max(__builtin_amdgcn_readlane(idx_v, (u >> 1) & 63), 0), a.Tm - 1);
     return i * BQ + (u & 1) * HQ + QW * w;
   };
+  // what is added to the first head's addresses for the step asked for last: bytes of Q and dO, rows of LSE and D
+  auto head_bytes = [&]() -> uint64_t { return CROSS ? (uint64_t)g_at * (uint64_t)a.sh * 2 : 0; };
+  auto head_rows = [&]() -> uint64_t { return CROSS ? (uint64_t)g_at * (uint64_t)N : 0; };
 
   // per-lane LDS byte offsets inside a 32-row tile.  Row reads: row r32, logical chunk 2kk + hf (the part that
   // depends on kk is XORed in as kk << 5).  Transposing reads: row 16c + 8*which + 4hf + (s16>>2), columns
@@ -211,11 +272,11 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
   {
     const int row0 = step_row(0), row_b = min(row0, N - 1);
     set_rows(min(QW - 1, N - 1 - row_b));
-    copy_stats(row_b, wstat);
+    copy_stats(head_rows() + row_b, wstat);
     static_for<0, NCP>([&](auto R) {
       constexpr int r = decltype(R)::v;
-      raw_copy16_to_lds_at<r * 1024>(q_head + (uint64_t)row_b * row_bytes, voff[r], wsm);
-      raw_copy16_to_lds_at<TILE_B + r * 1024>(o_head + (uint64_t)row_b * row_bytes, voff[r], wsm);
+      raw_copy16_to_lds_at<r * 1024>(q_head + head_bytes() + (uint64_t)row_b * row_bytes, voff[r], wsm);
+      raw_copy16_to_lds_at<TILE_B + r * 1024>(o_head + head_bytes() + (uint64_t)row_b * row_bytes, voff[r], wsm);
     });
     raw_copies_done();
     mark_rows_past_end(row0, wstat);
@@ -237,12 +298,13 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
   for (int u = 0; u < steps; ++u) {
     const int st = u & 1;
     const int un = min(u + 1, steps - 1);    // past the end the last step is requested again (nobody reads it)
-    if (((u + 1) & 127) == 0 && u + 1 < steps) idx_v = list_load(idx, min(((u + 1) >> 1) + fresh_lane(), cnt - 1));   // next 64 entries
+    if (!CROSS && ((u + 1) & 127) == 0 && u + 1 < steps) idx_v = list_load(idx, min(((u + 1) >> 1) + fresh_lane(), cnt - 1));   // next 64 entries
     const int row_nx = step_row(un), row_b = min(row_nx, N - 1);
     set_rows(min(QW - 1, N - 1 - row_b));
     const uint32_t nx_stage = wsm + (st ^ 1) * STAGE_B, nx_stat = wstat + (st ^ 1) * STAT_B;
-    const char* qn = q_head + (uint64_t)row_b * row_bytes;
-    const char* on = o_head + (uint64_t)row_b * row_bytes;
+    const char* qn = q_head + head_bytes() + (uint64_t)row_b * row_bytes;
+    const char* on = o_head + head_bytes() + (uint64_t)row_b * row_bytes;
+    const uint64_t stat_row = head_rows() + row_b;
     // this step's operand addresses (one add per step; the XOR of the compile-time part is one more op per read)
     const uint32_t q_rd = wsm + st * STAGE_B + a_off, q_t0 = wsm + st * STAGE_B + t_off0, q_t1 = wsm + st * STAGE_B + t_off1;
     const uint32_t lb = wstat + st * STAT_B + 16 * hf;
@@ -287,7 +349,7 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
       constexpr int y = decltype(Y)::v;
       s[0] = mfma32(fr[y % PD], kf[0][y], y == 0 ? zero : s[0]);
       s[1] = mfma32(fr[y % PD], kf[1][y], y == 0 ? zero : s[1]);
-      if constexpr (y == 0) copy_stats(row_b, nx_stat);
+      if constexpr (y == 0) copy_stats(stat_row, nx_stat);
       raw_copy16_to_lds_at<y * 1024>(qn, voff[y], nx_stage);
       if constexpr (y + PD == NK) raw_copies_left<2 + y + 1>();      // this step's dO rows have landed
       fr[y % PD] = row_frag(y + PD);
@@ -393,9 +455,13 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
     else        finish(Int<1>{}, put);
   } else {
     u32x2 done[8 * NMB];
+    // (a lane's sums are those of one key: keys behind the sample's length repeat its last key and get zeros)
+    const bool unseen = CROSS && key0w + (le & 31) >= at.keys;
     auto put = [&](int t, int mb, int g, f32x4 x) {
       const float sc = t == 0 ? -a.scale : 1.f;
-      done[(t * NMB + mb) * 4 + g] = u32x2{pack_bf16(x[0] * sc, x[1] * sc), pack_bf16(x[2] * sc, x[3] * sc)};
+      u32x2& d = done[(t * NMB + mb) * 4 + g];
+      d = u32x2{pack_bf16(x[0] * sc, x[1] * sc), pack_bf16(x[2] * sc, x[3] * sc)};
+      if (unseen) d = u32x2{0, 0};
     };
     if (w == 0) finish(Int<0>{}, put);
     else        finish(Int<1>{}, put);
@@ -405,12 +471,12 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
       constexpr int c = decltype(C)::v;
       row_piece_put<D>(area + (c / (4 * NMB)) * (32 * D * 2), le & 31, c % (4 * NMB), he, done[c]);
     });
-    rows_store<D>(area, a.dk + base + (int64_t)key0w * a.sn, a.sn, N - key0w, le);
-    rows_store<D>(area + 32 * D * 2, a.dv + base + (int64_t)key0w * a.sn, a.sn, N - key0w, le);
+    rows_store<D>(area, a.dk + at.out + (int64_t)key0w * at.out_sn, at.out_sn, at.rows - key0w, le);
+    rows_store<D>(area + 32 * D * 2, a.dv + at.out + (int64_t)key0w * at.out_sn, at.out_sn, at.rows - key0w, le);
     return;
   }
   if (!last_part(a.sp.arrive + item.slot - part, parts, (int*)stat_s)) return;
-  dkdv_merge<D>(a, item, base, key0w, w, le, lds_addr_of(scratch + w * REGION));
+  dkdv_merge<D>(a, item, at, key0w, w, le, lds_addr_of(scratch + w * REGION));
 }
 
 // Head dimension 64: one workgroup of two waves per key block, two waves per SIMD (256 registers), eight per CU.  Wave w owns
@@ -426,28 +492,38 @@ __device__ __forceinline__ void dkdv_item(const DkvArgs& a, const WorkItem& item
 // Bound: the copies out of the memory-side cache (9 TB/s over all compute units while every slot is busy).  Measured, us, a
 // training pass, one wave a SIMD with 64 keys a wave / this: 20,010 tokens, 6 heads 280 / 270; 40,296 tokens, 32 heads
 // 4202 / 3983.  256 columns of 4 entries, a workgroup a compute unit: 20.0 / 19.5 (the kernel).
-__device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& item, Walk& walk, unsigned char* smem,
+template <class Args, class Way>
+__device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item, Way& walk, unsigned char* smem,
                                             unsigned char* stat_s) {
+  constexpr bool CROSS = Args::CROSS;
   constexpr int D = 64, NK = D / 16, NMB = D / 32;
   constexpr int HQ = 64;                             // query rows per step
   constexpr int CPR = D / 8, RPI = 64 / CPR, NCP = 32 / RPI;         // (see dkdv_item)
   constexpr int TILE_B = HQ * D * 2, HALF_B = TILE_B / 2, STAGE_B = 2 * TILE_B;    // Q rows, then dO rows
   constexpr int STAT_B = 512;                        // a wave's 32 rows: LSE at +0, D at +256
   const int bh = item.bh, j = item.blk, part = item.part, parts = item.parts, part_len = item.part_len;
-  const int64_t base = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh;
+  const int64_t base = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh * (CROSS ? cross_group(a) : 1);
   const int lane = fresh_lane(), w = walk.wave;
   const int r32 = lane & 31, hf = lane >> 5;
   const int N = a.N;
-  int cnt = min(max(a.col_cnt[(int64_t)bh * a.Tn + j], 0), a.Tm);   // clamped: see fwd.hip
-  const int32_t* idx = a.col_idx + ((int64_t)bh * a.Tn + j) * a.Tm;
+  const ColumnPlace at = column_place(a, bh, base);
+  int cnt;
+  const int32_t* idx = nullptr;
+  if constexpr (CROSS) {
+    cnt = j * BKV < at.keys ? a.kv.group * a.Tm : 0;
+  } else {
+    cnt = min(max(a.col_cnt[(int64_t)bh * a.Tn + j], 0), a.Tm);   // clamped: see fwd.hip
+    idx = a.col_idx + ((int64_t)bh * a.Tn + j) * a.Tm;
+  }
+  const int first = part * part_len;
   if (parts) {                // entries [part * part_len, (part + 1) * part_len) of the list
-    idx += part * part_len;
-    cnt = min(cnt - part * part_len, part_len);
+    if constexpr (!CROSS) idx += first;
+    cnt = min(cnt - first, part_len);
   }
   const int key0w = j * BKV + 32 * w, key = key0w + r32;
   if (cnt == 0) {             // no query block selected this key block: zero gradients
-    if (key < N) {
-      const int64_t out_off = base + (int64_t)key * a.sn + 32 * hf;
+    if (key < at.rows) {
+      const int64_t out_off = at.out + (int64_t)key * at.out_sn + 32 * hf;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         *(u32x4*)(a.dk + out_off + 8 * c) = u32x4{0, 0, 0, 0};
@@ -460,7 +536,7 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
   // K^T / V^T fragments: lane = key, 8 consecutive channels per 16-wide k step (keys past N repeat the last token)
   bf16x8 kf[NK], vf[NK];
   {
-    const int64_t off = base + (int64_t)min(key, N - 1) * a.sn + 8 * hf;
+    const int64_t off = at.in + (int64_t)min(key, at.keys - 1) * at.in_sn + 8 * hf;
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
       kf[kk] = *(const bf16x8*)(a.k + off + 16 * kk);
@@ -489,14 +565,15 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
   };
   const char* q_head = (const char*)(a.q + base);
   const char* o_head = (const char*)(a.d_o + base);
-  const char* lse_head = (const char*)(a.lse + (int64_t)bh * N);
-  const char* dlt_head = (const char*)(a.delta + (int64_t)bh * N);
+  const int64_t stat_base = (int64_t)bh * N * (CROSS ? cross_group(a) : 1);
+  const char* lse_head = (const char*)(a.lse + stat_base);
+  const char* dlt_head = (const char*)(a.delta + stat_base);
   const uint64_t row_bytes = (uint64_t)a.sn * 2;
   const uint32_t sm = lds_addr_of(smem), stat = lds_addr_of(stat_s);
   const uint32_t sm_w = sm + w * HALF_B, stat_w = stat + w * STAT_B;         // this wave's rows of a stage
-  auto copy_stats = [&](int row, uint32_t stat_addr) {
-    raw_copy4_to_lds_at<0>(lse_head + (uint64_t)row * 4, soff, stat_addr);
-    raw_copy4_to_lds_at<256>(dlt_head + (uint64_t)row * 4, soff, stat_addr);
+  auto copy_stats = [&](uint64_t row, uint32_t stat_addr) {
+    raw_copy4_to_lds_at<0>(lse_head + row * 4, soff, stat_addr);
+    raw_copy4_to_lds_at<256>(dlt_head + row * 4, soff, stat_addr);
   };
   // Query rows past N get an LSE of +infinity once their copy has landed: their P is then exactly zero.
   auto mark_rows_past_end = [&](int row0, uint32_t stat_addr) {
@@ -505,11 +582,20 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
     if (row0 + row_l >= N) lds_stf(stat_addr + 4 * row_l, INFINITY);
   };
 
-  int idx_v = idx[min(lane, cnt - 1)];       // the index list, 64 entries at a time (see dkdv_item)
+  int idx_v = 0, g_at = 0;                   // the index list, 64 entries at a time (see dkdv_item)
+  if constexpr (!CROSS) idx_v = idx[min(lane, cnt - 1)];
   auto step_row = [&](int u) -> int {        // this wave's first row of step u (uniform, inside the chunk that idx_v holds)
+    if constexpr (CROSS) {
+      const CrossEntry e = cross_entry(a, first + (u >> 1));
+      g_at = e.g;
+      return e.i * BQ + (u & 1) * HQ + 32 * w;
+    }
     const int i = min(max(__builtin_amdgcn_readlane(idx_v, (u >> 1) & 63), 0), a.Tm - 1);
     return i * BQ + (u & 1) * HQ + 32 * w;
   };
+  // what is added to the first head's addresses for the step asked for last: bytes of Q and dO, rows of LSE and D
+  auto head_bytes = [&]() -> uint64_t { return CROSS ? (uint64_t)g_at * (uint64_t)a.sh * 2 : 0; };
+  auto head_rows = [&]() -> uint64_t { return CROSS ? (uint64_t)g_at * (uint64_t)N : 0; };
   const int s16 = lane & 15, hb16 = (lane >> 4) & 1;
   const uint32_t a_off = sm + 2 * swz_idx<D>(r32, 8 * hf);
   const uint32_t t_off0 = sm + 2 * swz_idx<D>(4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
@@ -519,11 +605,11 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
   {
     const int row0 = step_row(0), row_b = min(row0, N - 1);
     set_rows(min(31, N - 1 - row_b));
-    copy_stats(row_b, stat_w);
+    copy_stats(head_rows() + row_b, stat_w);
     static_for<0, NCP>([&](auto R) {
       constexpr int r = decltype(R)::v;
-      raw_copy16_to_lds_at<r * 1024>(q_head + (uint64_t)row_b * row_bytes, voff[r], sm_w);
-      raw_copy16_to_lds_at<TILE_B + r * 1024>(o_head + (uint64_t)row_b * row_bytes, voff[r], sm_w);
+      raw_copy16_to_lds_at<r * 1024>(q_head + head_bytes() + (uint64_t)row_b * row_bytes, voff[r], sm_w);
+      raw_copy16_to_lds_at<TILE_B + r * 1024>(o_head + head_bytes() + (uint64_t)row_b * row_bytes, voff[r], sm_w);
     });
     raw_copies_done();
     mark_rows_past_end(row0, stat_w);
@@ -544,12 +630,13 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
   for (int u = 0; u < steps; ++u) {
     const int st = u & 1;
     const int un = min(u + 1, steps - 1);    // past the end the last step is requested again (nobody reads it)
-    if (((u + 1) & 127) == 0 && u + 1 < steps) idx_v = list_load(idx, min(((u + 1) >> 1) + fresh_lane(), cnt - 1));   // next 64 entries
+    if (!CROSS && ((u + 1) & 127) == 0 && u + 1 < steps) idx_v = list_load(idx, min(((u + 1) >> 1) + fresh_lane(), cnt - 1));   // next 64 entries
     const int row_nx = step_row(un), row_b = min(row_nx, N - 1);
     set_rows(min(31, N - 1 - row_b));
     const uint32_t nx_stage = sm_w + (st ^ 1) * STAGE_B, nx_stat = stat_w + (st ^ 1) * 2 * STAT_B;
-    const char* qn = q_head + (uint64_t)row_b * row_bytes;
-    const char* on = o_head + (uint64_t)row_b * row_bytes;
+    const char* qn = q_head + head_bytes() + (uint64_t)row_b * row_bytes;
+    const char* on = o_head + head_bytes() + (uint64_t)row_b * row_bytes;
+    const uint64_t stat_row = head_rows() + row_b;
     uint32_t q_rd = a_off + st * STAGE_B, q_t0 = t_off0 + st * STAGE_B, q_t1 = t_off1 + st * STAGE_B;
     const uint32_t lb = stat + st * 2 * STAT_B + 16 * hf;
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -595,7 +682,7 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
       constexpr int y = decltype(Y)::v, rh = y / NK, kk = y % NK;
       s[rh] = mfma32(fr[y % PD], kf[kk], kk == 0 ? zero : s[rh]);
       fr[y % PD] = row_frag(q_rd, y + PD);
-      if constexpr (y == 0) copy_stats(row_b, nx_stat);
+      if constexpr (y == 0) copy_stats(stat_row, nx_stat);
       if constexpr (y < NCP) raw_copy16_to_lds_at<y * 1024>(qn, voff[y], nx_stage);
       else                   raw_copy16_to_lds_at<TILE_B + (y - NCP) * 1024>(on, voff[y - NCP], nx_stage);
       if constexpr (y == NK) load_d(0);
@@ -649,20 +736,22 @@ __device__ __forceinline__ void dkdv_item64(const DkvArgs& a, const WorkItem& it
       part_store2(ps + ((t * 2 + w) * NMB * 8 + c % (8 * NMB)) * 128, x[v], x[v + 1]);
     });
     if (!last_part(a.sp.arrive + item.slot - part, parts, (int*)stat_s)) return;
-    dkdv_merge<D>(a, item, base, key0w, w, le, sm + w * TILE_B);
+    dkdv_merge<D>(a, item, at, key0w, w, le, sm + w * TILE_B);
     return;
   }
   __syncthreads();
   const uint32_t area = sm + w * TILE_B;             // dK, then dV rows of this wave
+  const bool unseen = CROSS && key0w + (le & 31) >= at.keys;         // (see dkdv_item)
   static_for<0, 2 * NMB * 4>([&](auto C) {
     constexpr int c = decltype(C)::v, t = c / (4 * NMB), mb = (c / 4) % NMB, v = 4 * (c % 4);
     const f32x16& x = t == 0 ? dk_acc[mb] : dv_acc[mb];
     const float sc = t == 0 ? -a.scale : 1.f;
-    row_piece_put<D>(area + t * (32 * D * 2), le & 31, c % (4 * NMB), le >> 5,
-                     u32x2{pack_bf16(x[v] * sc, x[v + 1] * sc), pack_bf16(x[v + 2] * sc, x[v + 3] * sc)});
+    u32x2 d = {pack_bf16(x[v] * sc, x[v + 1] * sc), pack_bf16(x[v + 2] * sc, x[v + 3] * sc)};
+    if (unseen) d = u32x2{0, 0};
+    row_piece_put<D>(area + t * (32 * D * 2), le & 31, c % (4 * NMB), le >> 5, d);
   });
-  rows_store<D>(area, a.dk + base + (int64_t)key0w * a.sn, a.sn, N - key0w, le);
-  rows_store<D>(area + 32 * D * 2, a.dv + base + (int64_t)key0w * a.sn, a.sn, N - key0w, le);
+  rows_store<D>(area, a.dk + at.out + (int64_t)key0w * at.out_sn, at.out_sn, at.rows - key0w, le);
+  rows_store<D>(area + 32 * D * 2, a.dv + at.out + (int64_t)key0w * at.out_sn, at.out_sn, at.rows - key0w, le);
 }
 
 template <int D>
@@ -704,6 +793,54 @@ hipError_t launch_bwd_dkdv(const void* q, const void* k, const void* v, const vo
   const dim3 grid((unsigned)(plan.queue && !plan.queue_if_full ? plan.resident : plan.pool_slots + columns)), block(128);
   if (m.d == 128) hipLaunchKernelGGL(dkdv_kernel<128>, grid, block, 0, stream, a);
   else            hipLaunchKernelGGL(dkdv_kernel<64>, grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ attention to another sequence
+template <int D>
+__global__ __attribute__((amdgpu_flat_work_group_size(128, 128), amdgpu_waves_per_eu(D == 128 ? 1 : 2, D == 128 ? 1 : 2)))
+void cross_dkdv_kernel(CrossDkvArgs) {
+  __shared__ __align__(1024) unsigned char smem[2 * 2 * 64 * D * 2];
+  __shared__ __align__(1024) unsigned char stat_s[2 * 2 * 512];
+  const CrossDkvArgs& a = fresh_args<CrossDkvArgs>();
+  const int columns = stretch_wgs(a.BH * a.Tn);
+  const HeadBlock hb = stretch_row(blockIdx.x % columns, a.BH, a.Tn);
+  if (!hb.valid) return;
+  WorkItem item;
+  item.bh = hb.bh; item.blk = hb.blk;
+  item.part = blockIdx.x / columns; item.parts = 0; item.part_len = 0; item.slot = 0;
+  const int all = a.kv.group * a.Tm;
+  const bool seen = hb.blk * BKV < cross_length(a.kv, hb.bh / a.H);         // (else: one workgroup writes zeros)
+  if (seen && all > a.sp.fixed_len) {
+    item.parts = (all + a.sp.fixed_len - 1) / a.sp.fixed_len;
+    item.part_len = a.sp.fixed_len;
+    item.slot = (hb.bh * a.Tn + hb.blk) * a.sp.fixed_parts + item.part;
+  }
+  if (item.part >= max(item.parts, 1)) return;
+  OneItem walk{__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)};
+  if constexpr (D == 128) dkdv_item<D>(a, item, walk, smem, stat_s);
+  else                    dkdv_item64(a, item, walk, smem, stat_s);
+}
+
+CrossSection cross_dkdv_section(const CrossDims& m) {
+  return cross_section((int64_t)m.q.B * m.Hk * m.q.Tn, m.group * m.q.Tm, dkdv_resident(m.q), 4, dkdv_slot_bytes(m.q));
+}
+
+hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
+                             const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
+                             hipStream_t stream) {
+  CrossDkvArgs a = {};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
+  a.lse = lse; a.delta = delta; a.dk = (uint16_t*)dk; a.dv = (uint16_t*)dv;
+  a.BH = m.q.B * m.Hk; a.H = m.Hk; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
+  a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
+  a.scale = scale; a.scale_log2 = scale * LOG2E;
+  a.kv = cross_keys(m, lengths);
+  a.dsb = m.dsb; a.dsh = m.dsh; a.dsn = m.dsn;
+  a.sp = plan;
+  const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tn))), block(128);
+  if (m.q.d == 128) hipLaunchKernelGGL(cross_dkdv_kernel<128>, grid, block, 0, stream, a);
+  else              hipLaunchKernelGGL(cross_dkdv_kernel<64>, grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

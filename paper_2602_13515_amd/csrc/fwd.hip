@@ -12,6 +12,7 @@
 // B-operand layout the second product wants, so P never leaves registers, and
 // the running maximum / sum of Alg. 1 (m_ij, l_ij) are per-lane scalars that
 // need one exchange between the two halves of the wave per tile.
+#include "cross.h"
 #include "row_map.h"
 #include "spa2_device.h"
 #include "spa2_internal.h"
@@ -19,6 +20,7 @@
 namespace spa2 {
 
 struct FwdArgs {
+  static constexpr bool CROSS = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v;
   uint16_t* o; uint16_t* o_res; float* lse;
   const int32_t* row_cnt; const int32_t* row_idx; const int32_t* row_order;
@@ -26,6 +28,13 @@ struct FwdArgs {
   int64_t sb, sh, sn;
   float scale_log2;     // scale * log2(e): softmax is evaluated with exp2
   SplitPlan sp;         // long rows cut into parts (split.hip); sp.pool_slots == 0: every row is walked whole
+};
+
+// Attention to another sequence: row i of a head takes every key block of its key head up to the sample's length.  There are
+// no lists (entry t of a row is key block t) and no plan (parts by size alone).
+struct CrossFwdArgs : FwdArgs {
+  static constexpr bool CROSS = true;
+  CrossKeys kv;
 };
 
 // Partial result of one part of a split row: the unnormalised accumulator as [pair of accumulator registers][thread],
@@ -67,8 +76,9 @@ __device__ __forceinline__ void fwd_store_rows(const FwdArgs& a, int bh, int64_t
   if (hf == 0 && r32 < valid) a.lse[(int64_t)bh * a.N + q0 + r32] = m_run * LN2 + __logf(l_tot);
 }
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
+  constexpr bool CROSS = Args::CROSS;
   constexpr int NK = D / 16, NMB = D / 32;           // contraction steps of S, output blocks of O
   // Three K and two V tiles, XOR-swizzled and unpadded (the layout a direct global -> LDS copy can write); two
   // workgroups of 80 KB share a compute unit.  (Aligned: compile-time parts are XORed into addresses.)
@@ -80,7 +90,20 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
   int bh, i, part = 0, parts = 0, part_len = 0;
   bool whole = false;         // a row of the plan that may be split: its parts are the first workgroups
   int slot = blockIdx.x;
-  if (a.sp.fixed_len) {       // a small launch: the sizes say which part of which row (with_fixed_parts)
+  int keys = a.N;             // keys that the row sees at most
+  if constexpr (CROSS) {
+    const int rows = stretch_wgs(a.BH * a.Tm);
+    const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
+    if (!hb.valid) return;
+    bh = hb.bh; i = hb.blk;
+    keys = cross_length(a.kv, bh / a.H);
+    const int all = (keys + BKV - 1) / BKV;
+    part = blockIdx.x / rows;
+    parts = all > a.sp.fixed_len ? (all + a.sp.fixed_len - 1) / a.sp.fixed_len : 0;
+    if (part >= max(parts, 1)) return;
+    if (parts) part_len = (all + parts - 1) / parts;
+    slot = (bh * a.Tm + i) * a.sp.fixed_parts + part;
+  } else if (a.sp.fixed_len) {       // a small launch: the sizes say which part of which row (with_fixed_parts)
     const int rows = stretch_wgs(a.BH * a.Tm);
     const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
     if (!hb.valid) return;
@@ -114,15 +137,22 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
   // counts and indices come from the caller's pattern: clamp them so that a corrupt list cannot
   // address memory outside the tensors
   const int64_t unit = (int64_t)bh * a.Tm + i;
-  int cnt = min(max(a.row_cnt[unit], 0), a.Tn);
-  const int split_at = *(whole ? a.sp.unit_slot + unit : a.row_cnt + unit);
   const int first = part * part_len;         // entries [first, first + part_len) of the list of a split row (never empty)
-  const int32_t* idx = a.row_idx + unit * a.Tn + first;
+  int cnt, split_at = 0;
+  const int32_t* idx = nullptr;
+  if constexpr (CROSS) {
+    cnt = (keys + BKV - 1) / BKV;
+  } else {
+    cnt = min(max(a.row_cnt[unit], 0), a.Tn);
+    split_at = *(whole ? a.sp.unit_slot + unit : a.row_cnt + unit);
+    idx = a.row_idx + unit * a.Tn + first;
+  }
   // The list's first 64 entries and the queries are requested before the count (or whether the row is split) is known:
   // one wait for all of these instead of three, each a round trip to memory.  (Measured, us, before / after: 1000 tokens,
   // 2 heads 14.8 / 14.3, 4 samples of 1281 tokens 32.5 / 31.9, 20,010 tokens, 6 heads, d = 64 64.0 / 63.6; the same in dQ 31.0 /
   // 30.4 and 72.1 / 71.4.  In dK/dV it gave 0.3 us on the short ones and cost 2.6 of 126 on the last, so it is not there.)
-  int idx_v = idx[min(lane, a.Tn - 1 - first)];
+  int idx_v = 0;
+  if constexpr (!CROSS) idx_v = idx[min(lane, a.Tn - 1 - first)];
   const int qrow = i * BQ + w * 32 + r32;
   // Q^T fragments (B operand): lane = query row, 8 consecutive channels per 16-wide k step.
   const int qrow_ld = qrow < N ? qrow : N - 1;
@@ -151,6 +181,11 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
     return;
   }
 
+  int64_t key_base = base, key_sn = a.sn;
+  if constexpr (CROSS) {
+    key_base = (int64_t)(bh / a.H) * a.kv.sb + (int64_t)((bh % a.H) / a.kv.group) * a.kv.sh;
+    key_sn = a.kv.sn;
+  }
   // K/V tiles are copied global -> LDS directly.  The destination of a wave-wide 16-byte-per-lane copy is linear (wave
   // base + 16 * lane), so the swizzle is applied on the source side: the lane that fills chunk position pc of a row
   // fetches logical chunk pc ^ swz(row).  Thread t fills chunk position t % CPR of rows t / CPR + r * RSTEP; RSTEP is a
@@ -170,17 +205,17 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
   uint32_t voff[CH];
   int rows_set = -1;
   auto set_rows = [&](int j) {               // for the tile of key block j (uniform)
-    const int last = min(BKV - 1, N - 1 - j * BKV);
+    const int last = min(BKV - 1, keys - 1 - j * BKV);
     if (last == rows_set) return;
     rows_set = last;
     const int t = fresh_tid(), ld_row = t / CPR, ld_c8 = ((t % CPR) ^ swz<D>(ld_row)) * 8;
 #pragma unroll
-    for (int r = 0; r < CH; ++r) voff[r] = (uint32_t)((min(ld_row + RSTEP * r, last) * a.sn + ld_c8) * 2);
+    for (int r = 0; r < CH; ++r) voff[r] = (uint32_t)((min(ld_row + RSTEP * r, last) * key_sn + ld_c8) * 2);
   };
   const uint32_t sm = lds_addr_of(smem), sm_w = sm + w * 1024;
-  const char* k_head = (const char*)(a.k + base);
-  const char* v_head = (const char*)(a.v + base);
-  const uint64_t tile_bytes = (uint64_t)a.sn * (2 * BKV);
+  const char* k_head = (const char*)(a.k + key_base);
+  const char* v_head = (const char*)(a.v + key_base);
+  const uint64_t tile_bytes = (uint64_t)key_sn * (2 * BKV);
   auto copy_tile = [&](const char* src, uint32_t slot) {
     static_for<0, CH>([&](auto R) { raw_copy16_to_lds_at<decltype(R)::v * 4096>(src, voff[decltype(R)::v], sm_w + slot); });
   };
@@ -210,8 +245,9 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
   // free up, one row-duration spread over its 64 slots; so a row that starts 1/64 of a row-duration later
   // also starts 1/64 of the key range further on: all of them sweep the keys together and share K/V tiles
   // through the XCD's L2.  The start depends on the row alone, so results do not depend on the launch order.
+  // (Whole rows are all taken from their first block on: they are in step by themselves.)
   int pos = 0;                               // place in the list of the next entry (idx_v: the 64 entries around it)
-  {
+  if constexpr (!CROSS) {
     const int start_blk = (int)(((int64_t)(i & 63) * a.Tn) >> 6);
     pos = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < cnt && idx_v < start_blk));
     for (int c = 64; c < cnt; c += 64) {
@@ -224,6 +260,11 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
   }
   int left = cnt - 1;                        // entries behind the one at pos (past the end the last one is taken again)
   auto next_entry = [&]() -> int {
+    if constexpr (CROSS) {
+      const int j = first + pos;
+      if (left > 0) { --left; ++pos; }
+      return j;
+    }
     const int j = min(max(__builtin_amdgcn_readlane(idx_v, pos & 63), 0), a.Tn - 1);
     if (left > 0) {
       --left;
@@ -247,8 +288,8 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(FwdArgs a) {
   };
   // keys past N (short last block) do not take part in the softmax
   auto mask_tail = [&](f32x16 (&s)[2], int j) {
-    if ((j + 1) * BKV > N) {
-      const int valid = N - j * BKV - 4 * ((fresh_tid() & 63) >> 5);
+    if ((j + 1) * BKV > keys) {
+      const int valid = keys - j * BKV - 4 * ((fresh_tid() & 63) >> 5);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -472,8 +513,40 @@ hipError_t launch_fwd(const void* q, const void* k, const void* v, const Dims& m
   }
   const dim3 grid((unsigned)(plan.fixed_len ? plan.fixed_parts * stretch_wgs(a.BH * a.Tm)
                                             : plan.pool_slots + launched_rows(a.BH, a.Tm, a.chunk))), block(256);
-  if (m.d == 128) hipLaunchKernelGGL(fwd_kernel<128>, grid, block, 0, stream, a);
-  else            hipLaunchKernelGGL(fwd_kernel<64>, grid, block, 0, stream, a);
+  if (m.d == 128) hipLaunchKernelGGL((fwd_kernel<128, FwdArgs>), grid, block, 0, stream, a);
+  else            hipLaunchKernelGGL((fwd_kernel<64, FwdArgs>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ attention to another sequence
+CrossSection cross_fwd_section(const CrossDims& m) {
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, 8, fwd_slot_bytes(m.q));
+}
+
+__global__ __launch_bounds__(256) void zero_ints_kernel(int32_t* p, int n) {
+  const int x = blockIdx.x * 256 + threadIdx.x;
+  if (x < n) p[x] = 0;
+}
+
+hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
+                            void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
+  CrossFwdArgs a = {};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.o = (uint16_t*)o; a.o_res = (uint16_t*)o_res; a.lse = lse;
+  a.BH = m.q.B * m.q.H; a.H = m.q.H; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
+  a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
+  a.scale_log2 = scale * LOG2E;
+  a.kv = cross_keys(m, lengths);
+  const CrossFwdWs w = cross_fwd_ws(m);
+  a.sp = cross_plan(w.s, ws, (char*)ws + w.pool, fwd_slot_bytes(m.q));
+  if (w.s.slots) {
+    hipLaunchKernelGGL(zero_ints_kernel, dim3((unsigned)((w.s.slots + 255) / 256)), dim3(256), 0, stream, a.sp.arrive, w.s.slots);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid((unsigned)(w.s.cut.parts * stretch_wgs(a.BH * a.Tm))), block(256);
+  if (m.q.d == 128) hipLaunchKernelGGL((fwd_kernel<128, CrossFwdArgs>), grid, block, 0, stream, a);
+  else              hipLaunchKernelGGL((fwd_kernel<64, CrossFwdArgs>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -408,6 +408,106 @@ std::tuple<Tensor, Tensor> norm_rotate(const Tensor& q, const Tensor& k, const O
   return {out[0], out[1]};
 }
 
+// ---- attention to another sequence
+struct CrossShape {
+  spa2_cross_shape s = {};
+  // strides of a dimension of one element are never used: any that pass the checks
+  static void set(const Tensor& x, int64_t& sb, int64_t& sh, int64_t& sn) {
+    const int64_t any = (x.size(3) + 7) & ~(int64_t)7;
+    sb = x.size(0) > 1 ? x.stride(0) : any; sh = x.size(1) > 1 ? x.stride(1) : any; sn = x.size(2) > 1 ? x.stride(2) : any;
+  }
+  CrossShape(const Tensor& q, const Tensor& k, const Tensor& dk) {
+    s.B = (int32_t)q.size(0); s.Hq = (int32_t)q.size(1); s.Hk = (int32_t)k.size(1); s.Nq = (int32_t)q.size(2);
+    s.Nk = (int32_t)k.size(2); s.d = (int32_t)q.size(3);
+    set(q, s.q_sb, s.q_sh, s.q_sn);
+    set(k, s.k_sb, s.k_sh, s.k_sn);
+    set(dk, s.d_sb, s.d_sh, s.d_sn);
+  }
+};
+
+void cross_check(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& lengths) {
+  const std::pair<const char*, const Tensor*> named[] = {{"q", &q}, {"k", &k}, {"v", &v}};
+  for (const auto& [name, t] : named) {
+    TORCH_CHECK_VALUE(t->is_cuda(), name, " must live on the GPU: the operator has no CPU path");
+    TORCH_CHECK_VALUE(t->scalar_type() == at::kBFloat16 && t->dim() == 4, name, " must be a bf16 [B, H, N, d] view");
+    TORCH_CHECK_VALUE(t->stride(3) == 1, "the head dimension must be contiguous");
+  }
+  TORCH_CHECK_VALUE(v.sizes() == k.sizes(), "k and v share one shape");
+  TORCH_CHECK_VALUE(k.size(0) == q.size(0) && k.size(3) == q.size(3), "q and k share batch and head dimension");
+  TORCH_CHECK_VALUE(k.size(1) > 0 && q.size(1) % k.size(1) == 0, "the number of query heads is a multiple of that of key heads");
+  TORCH_CHECK_VALUE(k.device() == q.device() && v.device() == q.device(), "q, k and v live on one GPU");
+  TORCH_CHECK_VALUE(!lengths.defined() || (lengths.scalar_type() == at::kInt && lengths.dim() == 1 && lengths.size(0) == q.size(0) &&
+                                           lengths.is_contiguous() && lengths.device() == q.device()),
+                    "lengths are int32 [B] on the device of q");
+}
+
+Tensor copy_of(const Tensor& x) {
+  const Tensor y = dense_like(x, x.scalar_type());
+  y.copy_(x);
+  return y;
+}
+// One layout for a query tensor and all that is shaped like it: q itself where it has no gaps, else a copy without them.
+Tensor without_gaps(const Tensor& q) { return q.is_non_overlapping_and_dense() ? q : copy_of(q); }
+
+struct CrossAttention : torch::autograd::Function<CrossAttention> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in,
+                        const OptTensor& lengths_, double scale, bool training) {
+    const c10::DeviceGuard device(q_in.device());
+    const bool one_layout = strides_of(k_in) == strides_of(v_in);
+    const Tensor q = without_gaps(q_in), k = one_layout ? k_in : copy_of(k_in), v = one_layout ? v_in : in_order(v_in, k),
+                 lengths = or_none(lengths_);
+    const CrossShape c(q, k, k);
+    const Tensor o = like(q);
+    Tensor o_res, lse;
+    if (training) o_res = like(q);
+    lse = at::empty({q.size(0), q.size(1), q.size(2)}, q.options().dtype(at::kFloat));
+    const int64_t need = (int64_t)spa2_cross_fwd_workspace_bytes(&c.s);
+    const Tensor ws = need ? bytes(need, q) : Tensor();
+    check(spa2_cross_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), (const int32_t*)ptr(lengths), &c.s, (float)scale,
+                         o.data_ptr(), (void*)ptr(o_res), (float*)lse.data_ptr(), (void*)ptr(ws), (size_t)need, stream_of(q)),
+          "spa2_cross_fwd");
+    if (training) {
+      ctx->save_for_backward({q, k, v, o, o_res, lse, lengths});
+      ctx->saved_data["keys"] = k.sizes().vec();
+      ctx->saved_data["scale"] = scale;
+    }
+    return o;
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool graph = at::GradMode::is_enabled();
+    const at::NoGradGuard no_graph;
+    const variable_list s = ctx->get_saved_variables();
+    const Tensor &q = s[0], &k = s[1], &v = s[2], &o = s[3], &o_res = s[4], &lse = s[5], &lengths = s[6];
+    // (saved-tensor hooks may bring something else back)
+    cross_check(q, k, v, lengths);
+    TORCH_CHECK_VALUE(k.sizes().vec() == ctx->saved_data["keys"].toIntVector() && strides_of(k) == strides_of(v),
+                      "saved k and v come back in their shape and one layout");
+    TORCH_CHECK_VALUE(grads[0].sizes() == q.sizes() && grads[0].device() == q.device(), "saved q comes back in its shape on its GPU");
+    same_layout(q, {&o, &o_res});
+    TORCH_CHECK_VALUE(lse.device() == q.device() && lse.scalar_type() == at::kFloat && lse.is_contiguous() &&
+                      lse.numel() == q.size(0) * q.size(1) * q.size(2), "the log-sum-exp comes back as B * H * N contiguous fp32 numbers");
+    const c10::DeviceGuard device(q.device());
+    const Tensor d_o = in_order(grads[0].to(at::kBFloat16), q);
+    const Tensor dq = like(q), dk = dense_like(k, k.scalar_type()), dv = dense_like(k, k.scalar_type());
+    const CrossShape c(q, k, dk);
+    const int64_t need = (int64_t)spa2_cross_bwd_workspace_bytes(&c.s);
+    const Tensor ws = bytes(need, q);
+    check(spa2_cross_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), (const int32_t*)ptr(lengths), o.data_ptr(), o_res.data_ptr(),
+                         d_o.data_ptr(), (const float*)lse.data_ptr(), &c.s, (float)ctx->saved_data["scale"].toDouble(),
+                         dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), (size_t)need, stream_of(q)),
+          "spa2_cross_bwd");
+    return once({dq, dk, dv, Variable(), Variable(), Variable()}, graph, "cross_attention");
+  }
+};
+
+Tensor cross_attention(const Tensor& q, const Tensor& k, const Tensor& v, const OptTensor& lengths, double scale) {
+  cross_check(q, k, v, or_none(lengths));
+  capture_check(q, {q, k, v});
+  const bool training = at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad());
+  return CrossAttention::apply(q, k, v, lengths, scale, training);
+}
+
 // x as the elementwise kernels take it: contiguous from a 16-byte boundary.
 Tensor packed(const Tensor& x) {
   const Tensor y = x.contiguous();
@@ -469,6 +569,7 @@ Tensor dropout_add(const Tensor& x, const OptTensor& residual, double p, int64_t
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("attention", &attention, py::call_guard<py::gil_scoped_release>());
   m.def("norm_rotate", &norm_rotate, py::call_guard<py::gil_scoped_release>());
+  m.def("cross_attention", &cross_attention, py::call_guard<py::gil_scoped_release>());
   m.def("dropout_add", &dropout_add, py::call_guard<py::gil_scoped_release>());
   m.def("velocity_loss", &velocity_loss, py::call_guard<py::gil_scoped_release>());
 }

@@ -16,4 +16,10 @@ __device__ __forceinline__ HeadBlock launched_row(const SplitPlan& sp, int wg, i
   r.valid = r.valid && wg < xcd_map_wgs(heads, rows_per_head, chunk, SHORT_ROWS);
   return r;
 }
+
+// Keys that a sample's queries see (caller data: clamped).
+template <class Keys>
+__device__ __forceinline__ int cross_length(const Keys& kv, int b) {
+  return kv.lengths ? min(max(scalar_ld(kv.lengths + b), 0), kv.Nk) : kv.Nk;
+}
 }  // namespace spa2

@@ -65,3 +65,53 @@ def keep_mask(n, p, seed, offset):
     bits = np.stack([h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], -1).reshape(-1)[:n]
     cut = int(np.floor(p * 65536 + 0.5))
     return bits >= np.uint64(cut), 65536.0 / (65536 - cut) if cut < 65536 else 0.0
+
+
+# ------------------------------------------------------------------ attention to another sequence
+U = 2.0 ** -8           # half a step of bf16, relative
+
+
+def cross(q, k, v, lengths, scale, do=None):
+    """One batch of fp64 arrays [B, H, N, d].  Returns {name: (value, bound)}; the bounds count what the kernels round.
+
+    Forward: probabilities are rounded to bf16 and divided by the sum of the rounded ones, so that the weights are off by U
+    of each against their mean: U sum p |v - o| <= U (sum p |v| + |o|); the result is rounded, U |o|.  Scores, exponentials
+    and sums in fp32: 2^-13 of sum p |v| is far more than they lose.
+    Backward: p from a log-sum-exp that holds the mean rounding of a row, and rounded itself, 2 U; dS = p (dP - D) with a D that
+    holds the weights' error of o (o is there to 16 bits), and rounded, U; every result is rounded, U."""
+    B, Hq, Nq, d = q.shape
+    Hk, Nk = k.shape[1:3]
+    out = {n: (np.zeros(s), np.zeros(s)) for n, s in (("o", q.shape), ("dq", q.shape), ("dk", k.shape), ("dv", k.shape))}
+    lse = np.full((B, Hq, Nq), -np.inf)
+    small = 2.0 ** -13
+    for b in range(B):
+        n = Nk if lengths is None else int(min(max(lengths[b], 0), Nk))
+        if n == 0:
+            continue
+        for h in range(Hq):
+            g = h // (Hq // Hk)
+            kk, vv = k[b, g, :n], v[b, g, :n]
+            s = scale * q[b, h] @ kk.T
+            top = s.max(-1, keepdims=True)
+            e = np.exp(s - top)
+            p = e / e.sum(-1, keepdims=True)
+            lse[b, h] = top[:, 0] + np.log(e.sum(-1))
+            o, pv = p @ vv, p @ np.abs(vv)
+            weights = U * (pv + np.abs(o)) + small * pv
+            out["o"][0][b, h], out["o"][1][b, h] = o, weights + U * np.abs(o)
+            if do is None:
+                continue
+            up = do[b, h]
+            dp = up @ vv.T
+            D = (up * o).sum(-1, keepdims=True)
+            ds = p * (dp - D)
+            ds_bound = p * (np.abs(up) * (weights + 2.0 ** -15 * np.abs(o))).sum(-1, keepdims=True) + 3 * U * np.abs(ds) \
+                + small * p * (np.abs(up) @ np.abs(vv).T + np.abs(D))
+            out["dq"][0][b, h], out["dq"][1][b, h] = scale * ds @ kk, scale * ds_bound @ np.abs(kk)
+            out["dk"][0][b, g, :n] += scale * ds.T @ q[b, h]
+            out["dk"][1][b, g, :n] += scale * ds_bound.T @ np.abs(q[b, h])
+            out["dv"][0][b, g, :n] += p.T @ up
+            out["dv"][1][b, g, :n] += (2 * U + small) * p.T @ np.abs(up)
+    for n in ("dq", "dk", "dv"):
+        out[n] = (out[n][0], out[n][1] + U * np.abs(out[n][0]))
+    return out, lse

@@ -76,8 +76,56 @@ def test_dropout_refuses():
     assert b(ODD, 8, 0, 0, 0.5, 1, 2, None, FAKE, None) == -4
 
 
+CROSS = dict(B=2, Hq=4, Hk=2, Nq=10, Nk=20, d=128, q_sb=5120, q_sh=128, q_sn=512, k_sb=5120, k_sh=128, k_sn=256,
+             d_sb=5120, d_sh=128, d_sn=256)
+
+
+def _cross_call(null=None, odd=None, scale=0.1, backward=False, ws_bytes=1 << 60, **change):
+    s = binding._CrossShape(**{**CROSS, **change})
+    at = lambda n: None if n == null else (ODD if n == odd else FAKE)
+    if backward:
+        args = [at(n) for n in ("q", "k", "v", "lengths", "o", "o_res", "d_o", "lse")]
+        return binding._load().spa2_cross_bwd(*args, ctypes.byref(s), scale, at("dq"), at("dk"), at("dv"), at("workspace"), ws_bytes, None)
+    args = [at(n) for n in ("q", "k", "v", "lengths")]
+    return binding._load().spa2_cross_fwd(*args, ctypes.byref(s), scale, at("o"), at("o_res"), at("lse"), at("workspace"), ws_bytes, None)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("code,change", [
+    (-1, dict(null="q")), (-1, dict(null="k")), (-1, dict(null="v")), (-1, dict(null="o")), (-1, dict(null="lse")),
+    (-2, dict(B=0)), (-2, dict(Nq=0)), (-2, dict(Nk=-1)), (-2, dict(Hk=3)), (-2, dict(Hk=0)), (-2, dict(Hq=0)),
+    (-2, dict(q_sn=64)), (-2, dict(q_sh=0)), (-2, dict(k_sn=(1 << 23) + 8)), (-2, dict(k_sb=-8)),
+    (-2, dict(B=1 << 13, Hq=1 << 11, Hk=1)), (-2, dict(Nq=1 << 30)), (-2, dict(Nk=1 << 29)),
+    (-3, dict(d=96)), (-3, dict(d=32)),
+    (-4, dict(odd="q")), (-4, dict(odd="k")), (-4, dict(odd="v")), (-4, dict(odd="o")), (-4, dict(odd="o_res")),
+    (-4, dict(q_sn=516)), (-4, dict(k_sh=132)),
+    (-5, dict(scale=0.0)), (-5, dict(scale=-1.0)), (-5, dict(scale=float("nan"))), (-5, dict(scale=float("inf"))),
+])
+def test_cross_attention_refuses(code, change, backward):
+    assert _cross_call(backward=backward, **change) == code
+
+
+def test_cross_attention_refuses_its_own():
+    for name in ("d_o", "dq", "dk", "dv"):
+        assert _cross_call(null=name, backward=True) == -1 and _cross_call(odd=name, backward=True) == -4
+    assert _cross_call(d_sb=0, backward=True) == -2 and _cross_call(d_sn=260, backward=True) == -4
+    assert _cross_call(null="workspace", backward=True) == -6 and _cross_call(ws_bytes=79, backward=True) == -6
+    assert _cross_call(odd="workspace", backward=True) == -4
+    # one query against a long cache is cut into parts: those need a workspace in the forward pass too
+    long = dict(Nk=50000, k_sb=50000 * 256)
+    assert _cross_call(null="workspace", **long) == -6 and _cross_call(ws_bytes=1000, **long) == -6
+    assert _cross_call(odd="workspace", **long) == -4
+    lib = binding._load()
+    for f in (lib.spa2_cross_fwd_workspace_bytes, lib.spa2_cross_bwd_workspace_bytes):
+        assert f(None) == 0 and f(ctypes.byref(binding._CrossShape(**{**CROSS, "d": 80}))) == 0
+    assert lib.spa2_cross_bwd_workspace_bytes(ctypes.byref(binding._CrossShape(**CROSS))) >= 2 * 4 * 10 * 4
+    assert lib.spa2_cross_fwd(FAKE, FAKE, FAKE, None, None, 0.1, FAKE, None, FAKE, None, 0, None) == -1
+
+
 def test_operators_have_no_cpu_path():
     x = torch.zeros((1, 2, 16, 64))
+    with pytest.raises(ValueError):
+        spa2.cross_attention(x.bfloat16(), x.bfloat16(), x.bfloat16())
     with pytest.raises(ValueError):
         spa2.qk_norm_rotate(x, x)
     with pytest.raises(ValueError):
@@ -126,3 +174,16 @@ def test_rotary_table():
     for sizes, d in (((), 64), ((0,), 64), ((2, 2, 2), 4), (4, 63)):
         with pytest.raises(ValueError):
             spa2.rotary_table(sizes, d)
+
+
+def test_attention_gradient_formula_against_differences():
+    rng = np.random.default_rng(1)
+    q, k, v = rng.standard_normal((2, 4, 5, 8)), rng.standard_normal((2, 2, 7, 8)), rng.standard_normal((2, 2, 7, 8))
+    do, lengths, h = rng.standard_normal(q.shape), np.array([7, 3]), 1e-5
+    g, _ = ref.cross(q, k, v, lengths, 0.4, do)
+    f = lambda q, k, v: (ref.cross(q, k, v, lengths, 0.4)[0]["o"][0] * do).sum()
+    for _ in range(8):
+        w = [rng.standard_normal(x.shape) for x in (q, k, v)]
+        diff = (f(*(x + h * y for x, y in zip((q, k, v), w))) - f(*(x - h * y for x, y in zip((q, k, v), w)))) / (2 * h)
+        terms = [(g[n][0] * y) for n, y in zip(("dq", "dk", "dv"), w)]
+        assert abs(diff - sum(t.sum() for t in terms)) <= 1e-7 * sum(np.abs(t).sum() for t in terms)

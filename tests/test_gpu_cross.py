@@ -1,0 +1,281 @@
+"""Attention to another sequence, forward and backward, against the fp64 formulas (bounds: block_ref.cross), and as a whole:
+2-norm within the framework's bar for attention in bf16."""
+import numpy as np
+import pytest
+import torch
+
+import block_ref as ref
+import paper_2602_13515_amd as spa2
+from gpu_util import REL_L2, Guarded, dev
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _heads(g, B, H, N, d, layout="bnhd"):
+    x = torch.randn((B, N, H, d), generator=g).to(BF).to(dev())
+    if layout == "bnhd":
+        return x.permute(0, 2, 1, 3)
+    if layout == "bhnd":
+        return x.permute(0, 2, 1, 3).contiguous()
+    if layout == "gaps":
+        wide = torch.full((B, N, 2 * H + 1, d), float("nan"), dtype=BF, device=dev())
+        wide[:, :, 1:H + 1] = x
+        return wide[:, :, 1:H + 1].permute(0, 2, 1, 3)
+    assert layout == "shared"
+    return x[:, :, :1].permute(0, 2, 1, 3).expand(B, H, N, d)
+
+
+def _inputs(B, Hq, Hk, Nq, Nk, d, lengths, layouts=("bnhd", "bnhd", "bnhd"), seed=0):
+    g = torch.Generator().manual_seed(seed + Nq + 7 * Nk + d)
+    q, k, v = _heads(g, B, Hq, Nq, d, layouts[0]), _heads(g, B, Hk, Nk, d, layouts[1]), _heads(g, B, Hk, Nk, d, layouts[2])
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=dev())
+    do = torch.randn((B, Nq, Hq, d), generator=g).to(BF).to(dev()).permute(0, 2, 1, 3)
+    return q, k, v, lens, do
+
+
+def _compare(got, want, name, keys=32):
+    """keys: the fewest of any sample.  With few keys dS = p (dP - D) is a difference of nearly equal numbers, and with one it is
+    zero (dP = D): a bar relative to the result cannot hold for dQ and dK there, the bound by magnitudes does."""
+    value, bound = want
+    x = f64(got)
+    assert np.isfinite(x).all(), name
+    err = np.abs(x - value)
+    assert (err <= bound + 1e-30).all(), (name, (err - bound).max(), err.max())
+    if keys >= 32 or name in ("o", "dv"):
+        norm = np.linalg.norm(value)
+        assert np.linalg.norm(x - value) <= REL_L2 * norm + 1e-30, (name, np.linalg.norm(x - value), norm)
+
+
+def _check(q, k, v, lens, do, scale=None):
+    s = q.shape[-1] ** -0.5 if scale is None else scale
+    want, _ = ref.cross(f64(q), f64(k), f64(v), None if lens is None else lens.cpu().numpy(), s, f64(do))
+    with torch.no_grad():
+        plain = spa2.cross_attention(q, k, v, lens, scale)
+    leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+    o = spa2.cross_attention(*leaves, lens, scale)
+    assert torch.equal(o, plain) and o.shape == q.shape
+    grads = torch.autograd.grad(o, leaves, do)
+    seen = [k.shape[2]] if lens is None else [min(n, k.shape[2]) for n in lens.tolist() if n > 0]
+    for name, t in zip(("o", "dq", "dk", "dv"), (o, *grads)):
+        _compare(t, want[name], name, min(seen, default=0))
+    again = torch.autograd.grad(spa2.cross_attention(*leaves, lens, scale), leaves, do)
+    for a, b in zip(grads, again):
+        assert torch.equal(a, b)
+    if lens is not None:
+        for b, n in enumerate(lens.tolist()):
+            n = min(max(n, 0), k.shape[2])
+            assert not grads[1][b, :, n:].any() and not grads[2][b, :, n:].any()
+            if n == 0:
+                assert not o[b].any() and not grads[0][b].any()
+    return o, grads
+
+
+CASES = [
+    # B, Hq, Hk, Nq, Nk, d, lengths
+    (1, 1, 1, 1, 1, 64, None),
+    (1, 1, 1, 1, 1, 128, None),
+    (2, 2, 1, 1, 64, 128, [64, 63]),
+    (1, 2, 2, 3, 65, 64, None),
+    (4, 4, 2, 33, 77, 64, [77, 1, 0, 64]),
+    (3, 6, 2, 129, 77, 128, [0, 65, 900]),
+    (2, 5, 1, 127, 130, 64, [-3, 129]),
+    (1, 3, 3, 128, 64, 128, None),
+    (2, 3, 3, 1281, 512, 128, None),
+    (1, 2, 1, 2000, 333, 64, [300]),
+    (4, 6, 2, 1281, 77, 64, [77, 57, 19, 0]),
+    (1, 8, 8, 5, 4099, 64, None),                  # few rows, long lists: parts
+    (3, 10, 2, 1, 8191, 128, [8191, 100, 4097]),
+    (2, 4, 1, 300, 6000, 128, [6000, 5]),
+    (1, 2, 2, 9000, 60, 128, None),                # few columns, long lists: parts
+    (1, 2, 1, 9000, 60, 64, [31]),
+    (2, 40, 40, 257, 200, 64, None),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(map(str, c[:6])) + ("r" if c[6] else ""))
+def test_results_and_gradients(case):
+    print("case", case, flush=True)
+    _check(*_inputs(*case))
+
+
+@pytest.mark.parametrize("layouts", [("bhnd",) * 3, ("gaps",) * 3, ("bnhd", "shared", "shared"), ("gaps", "bhnd", "bnhd"),
+                                     ("shared", "gaps", "shared")], ids="-".join)
+@pytest.mark.parametrize("d", [64, 128])
+def test_layouts(layouts, d):
+    _check(*_inputs(2, 4, 2, 150, 90, d, [90, 13], layouts))
+
+
+@pytest.mark.parametrize("scale", [1e-3, 0.7, 30.0])
+def test_scales(scale):
+    q, k, v, lens, do = _inputs(2, 2, 2, 200, 150, 64, [150, 1])
+    # (scores up to scale * 8 * 64: at 30 a row is one key; the fp32 error of such a score, 2^-24 * 6000 * log2(e), is 5e-4)
+    if scale < 1:
+        _check(q, k, v, lens, do, scale)
+    else:
+        o = spa2.cross_attention(q, k, v, lens, scale)
+        want, _ = ref.cross(f64(q), f64(k), f64(v), lens.cpu().numpy(), scale)
+        assert np.linalg.norm(f64(o) - want["o"][0]) <= REL_L2 * np.linalg.norm(want["o"][0])
+
+
+def test_what_lies_behind_the_lengths_is_not_read():
+    q, k, v, lens, do = _inputs(3, 4, 2, 70, 200, 128, [200, 131, 0])
+    clean = [t.clone() for t in (k, v)]
+    for b, n in enumerate(lens.tolist()):
+        for t, fill in ((k, float("nan")), (v, float("inf"))):
+            t[b, :, n:] = fill
+        for t in clean:
+            t[b, :, n:] = 0
+    results = []
+    for kk, vv in ((k, v), clean):
+        leaves = [t.detach().requires_grad_(True) for t in (q, kk, vv)]
+        o = spa2.cross_attention(*leaves, lens)
+        results.append([o.detach(), *torch.autograd.grad(o, leaves, do)])
+    for a, b in zip(*results):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+def test_infinite_scores():
+    """A key whose score is minus infinity takes no part; an infinity in one head or sample stays there."""
+    q, k, v, _, _ = _inputs(2, 2, 2, 40, 70, 64, None)
+    k[0, 0, 5, 0] = float("-inf")
+    q[0, 0, :, 0] = q[0, 0, :, 0].abs() + 0.1
+    o = spa2.cross_attention(q, k, v)
+    kept = [n for n in range(70) if n != 5]
+    want, _ = ref.cross(f64(q[:1, :1]), f64(k[:1, :1, kept]), f64(v[:1, :1, kept]), None, 0.125)
+    _compare(o[:1, :1], want["o"], "o")
+    assert torch.isfinite(o).all()
+
+
+def test_caches_past_32_bits():
+    """Keys and values whose rows lie more than 4 GiB behind the first, and samples and heads too."""
+    B, Hk, N, d, step = 1, 2, 6000, 64, 2 * 200_000
+    free, _ = torch.cuda.mem_get_info()
+    if free < 12 << 30:
+        pytest.skip("needs 10 GB")
+    store = torch.empty(N * step, dtype=BF, device=dev())
+    k = store.as_strided((B, Hk, N, d), (N * step, 128, step, 1))
+    v = store.as_strided((B, Hk, N, d), (N * step, 128, step, 1), storage_offset=64)
+    g = torch.Generator().manual_seed(3)
+    for t in (k, v):
+        t.copy_(torch.randn((B, Hk, N, d), generator=g))
+    q = torch.randn((B, 4, 9, d), generator=g).to(BF).to(dev())
+    do = torch.randn((B, 4, 9, d), generator=g).to(BF).to(dev())
+    results = []
+    for kk, vv in ((k, v), (k.contiguous(), v.contiguous())):
+        leaves = [t.detach().requires_grad_(True) for t in (q, kk, vv)]
+        o = spa2.cross_attention(*leaves)
+        results.append([o.detach(), *torch.autograd.grad(o, leaves, do)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_buffers_next_to_the_results_stay_untouched(d):
+    g = Guarded()
+    for Nq, Nk, lengths in ((130, 70, [70, 9]), (3, 3000, [3000, 700]), (5000, 40, [40, 0])):
+        q, k, v, lens, do = _inputs(2, 4, 2, Nq, Nk, d, lengths, ("bhnd",) * 3)
+        scale = d ** -0.5
+        o, o_res, dq = (g.alloc(q.shape, BF, dev(), float("nan")) for _ in range(3))
+        dk, dv = (g.alloc(k.shape, BF, dev(), float("nan")) for _ in range(2))
+        lse = g.alloc(q.shape[:3], torch.float32, dev(), float("nan"))
+        ws = g.alloc((max(spa2.spa2_cross_fwd_workspace_bytes(q, k), 16),), torch.uint8, dev(), 0xA5)
+        spa2.spa2_cross_fwd(q, k, v, lens, scale, o, lse, o_res, ws)
+        wb = g.alloc((spa2.spa2_cross_bwd_workspace_bytes(q, k),), torch.uint8, dev(), 0xA5)
+        do = do.contiguous()
+        spa2.spa2_cross_bwd(q, k, v, lens, o, do, lse, scale, dq, dk, dv, wb, o_res)
+        torch.cuda.synchronize()
+        g.check(f"cross attention {Nq} {Nk}")
+        want, want_lse = ref.cross(f64(q), f64(k), f64(v), lens.cpu().numpy(), scale, f64(do))
+        for name, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+            _compare(t, want[name], name, min(n for n in lengths if n))
+        # the log-sum-exp is that of the rounded probabilities: their mean rounding at most, and fp32
+        got = f64(lse)
+        empty = np.isinf(want_lse)
+        assert np.array_equal(np.isneginf(got), empty)
+        assert (np.abs(got[~empty] - want_lse[~empty]) <= ref.U + 2.0 ** -13).all()
+
+
+def test_refusals():
+    q, k, v, lens, _ = _inputs(2, 4, 2, 16, 20, 64, [20, 3])
+    f = spa2.cross_attention
+    for bad in (lambda: f(q.float(), k, v), lambda: f(q, k.half(), v), lambda: f(q[0], k[0], v[0]), lambda: f(q, k, v[:, :, :19]),
+                lambda: f(q[:1], k, v), lambda: f(q[:, :3], k, v), lambda: f(q[..., :32], k, v), lambda: f(q, k, v, lens[:1]),
+                lambda: f(q, k, v, lens.long()), lambda: f(q, k, v, lens.cpu()), lambda: f(q.cpu(), k, v),
+                lambda: f(q.transpose(2, 3), k, v), lambda: f(q, k[:, :0], v[:, :0])):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: f(q[..., :32], k[..., :32], v[..., :32]), lambda: f(q, k, v, scale=0.0), lambda: f(q, k, v, scale=float("nan")),
+                lambda: f(q[:, :, :0], k, v), lambda: f(q, k[:, :, :0], v[:, :, :0]),
+                lambda: f(q, *(torch.empty(2 * 2 * 20 * 68, dtype=BF, device=dev()).as_strided((2, 2, 20, 64), (2720, 1360, 68, 1)) for _ in range(2)))):
+        with pytest.raises(spa2.Spa2Error):
+            bad()
+
+
+def test_second_derivative_is_refused():
+    q, k, v, _, do = _inputs(1, 1, 1, 8, 8, 64, None)
+    q.requires_grad_(True)
+    (dq,) = torch.autograd.grad(spa2.cross_attention(q, k, v), q, do, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivative"):
+        dq.float().sum().backward()
+
+
+@pytest.mark.parametrize("case", [(2, 4, 2, 200, 300, 64, [300, 9]), (2, 4, 2, 3, 5000, 128, [5000, 333]), (1, 2, 2, 9000, 60, 64, None)],
+                         ids=["rows", "long-keys", "long-columns"])
+def test_another_stream_and_a_captured_graph(case):
+    q, k, v, lens, do = _inputs(*case)
+    leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+
+    def step():
+        o = spa2.cross_attention(*leaves, lens)
+        return [o.detach(), *torch.autograd.grad(o, leaves, do)]
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = step()
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    graphs, held = [], []
+    for _ in range(2):                       # two captured steps, whose replays alternate
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held.append(step())
+        graphs.append(graph)
+    for change in range(3):
+        with torch.no_grad():
+            leaves[0].mul_(1.25)
+            if lens is not None:
+                lens.sub_(3)
+        want = [t.clone() for t in step()]
+        for graph, out in zip(graphs, held):
+            for t in out:
+                t.zero_()
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for out in held:
+            for a, b in zip(out, want):
+                assert torch.equal(a, b), change
+
+
+def test_saved_tensors_that_come_back_changed_are_refused():
+    q, k, v, lens, do = _inputs(1, 2, 1, 40, 50, 64, [50])
+    for change in (lambda x: x.float() if x.dtype == BF else x, lambda x: x[:, :, :-1] if x.dim() == 4 and x.shape[1] == 1 else x,
+                   lambda x: x.double() if x.dtype == torch.float32 else x, lambda x: x.long() if x.dtype == torch.int32 else x,
+                   lambda x: x.cpu()):
+        leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+        with torch.autograd.graph.saved_tensors_hooks(lambda x: x.detach(), change):
+            o = spa2.cross_attention(*leaves, lens)
+        try:
+            torch.autograd.grad(o, leaves, do)
+            raised = False
+        except ValueError:
+            raised = True
+        assert raised
