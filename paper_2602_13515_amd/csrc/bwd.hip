@@ -52,10 +52,14 @@ struct DqArgs {
   bool stretches;
 };
 
-// Attention to another sequence (see fwd.hip).
+// Attention to another sequence (see fwd.hip).  D is made here, for this kernel and for dK/dV behind it: as a launch of its own
+// it read dO once more.  32,760 queries, 12 heads, 512 keys, d = 128, backward pass: DELTA.
 struct CrossDqArgs : DqArgs {
   static constexpr bool CROSS = true;
   CrossKeys kv;
+  const uint16_t* o; const uint16_t* o_res;
+  float* delta_out;
+  int32_t* zero; int zeros;   // arrival counters of the dK/dV launch
 };
 
 // Partial result of one part of a split row: the fp32 accumulators as [pair of registers][thread] (see fwd.hip).
@@ -108,6 +112,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   int slot = (int)blockIdx.x - (CROSS ? 0 : a.front);
   int keys = a.N;             // keys that the row sees at most
   if constexpr (CROSS) {
+    for (int x = (int)(blockIdx.x * 256 + threadIdx.x); x < a.zeros; x += (int)(gridDim.x * 256)) a.zero[x] = 0;
     const int rows = stretch_wgs(a.BH * a.Tm);
     const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
     if (!hb.valid) return;
@@ -178,7 +183,30 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     }
   }
   const float lse2 = a.lse[(int64_t)bh * N + qrow_ld] * LOG2E;
-  const float dlt = a.delta[(int64_t)bh * N + qrow_ld];
+  float dlt;
+  if constexpr (CROSS) {
+    const int64_t off = base + (int64_t)qrow_ld * a.sn + 8 * hf;
+    u32x4 of[D / 16], rf[D / 16];
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) of[kk] = *(const u32x4*)(a.o + off + 16 * kk);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) rf[kk] = a.o_res ? *(const u32x4*)(a.o_res + off + 16 * kk) : u32x4{0, 0, 0, 0};
+    dlt = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const u32x4 up = __builtin_bit_cast(u32x4, dof[kk]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t u = up[c], x = of[kk][c], r = rf[kk][c];
+        dlt = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u), __builtin_bit_cast(bf16x2, x), dlt, false);
+        dlt = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u), __builtin_bit_cast(bf16x2, r), dlt, false);
+      }
+    }
+    dlt = sum_halves(dlt);
+    if (hf == 0 && qrow < N && part == 0) a.delta_out[(int64_t)bh * N + qrow] = dlt;
+  } else {
+    dlt = a.delta[(int64_t)bh * N + qrow_ld];
+  }
   requested();
   if (whole && split_at >= 0) return;
   if (parts) cnt = min(cnt - first, part_len);
@@ -420,30 +448,17 @@ hipError_t launch_bwd_dq_columns(const void* q, const void* k, const void* v, co
 
 // ------------------------------------------------------------------ attention to another sequence
 CrossSection cross_dq_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, 8, dq_slot_bytes(m.q));
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, dq_slot_bytes(m.q));
 }
 
-// D of every query row, and zeros in the arrival counters of the two launches behind it.
-template <int D>
-__global__ __launch_bounds__(256) void cross_delta_kernel(DeltaArgs a, int32_t* zero, int zeros) {
-  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < zeros; x += (int64_t)gridDim.x * 256) zero[x] = 0;
-  delta_block<D>(a, blockIdx.x / a.chunks, blockIdx.x % a.chunks);
-}
-hipError_t launch_cross_delta(const void* o, const void* o_res, const void* d_o, const CrossDims& m, float* delta, int32_t* zero,
-                              int zeros, hipStream_t stream) {
-  const DeltaArgs a = delta_args(o, o_res, d_o, m.q, delta);
-  const dim3 grid((unsigned)(a.chunks * m.q.B * m.q.H)), block(256);
-  if (m.q.d == 128) hipLaunchKernelGGL(cross_delta_kernel<128>, grid, block, 0, stream, a, zero, zeros);
-  else              hipLaunchKernelGGL(cross_delta_kernel<64>, grid, block, 0, stream, a, zero, zeros);
-  return hipGetLastError();
-}
-
-hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
-                           const CrossDims& m, const int32_t* lengths, float scale, void* dq, const SplitPlan& plan,
-                           hipStream_t stream) {
+hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
+                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, void* dq,
+                           int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
   CrossDqArgs a = {};
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
-  a.lse = lse; a.delta = delta; a.dq = (uint16_t*)dq;
+  a.lse = lse; a.delta_out = delta; a.dq = (uint16_t*)dq;
+  a.o = (const uint16_t*)o; a.o_res = (const uint16_t*)o_res;
+  a.zero = zero; a.zeros = zeros;
   a.BH = m.q.B * m.q.H; a.H = m.q.H; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
   a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
   a.scale = scale; a.scale_log2 = scale * LOG2E;

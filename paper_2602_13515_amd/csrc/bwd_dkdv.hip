@@ -823,7 +823,8 @@ void cross_dkdv_kernel(CrossDkvArgs) {
 }
 
 CrossSection cross_dkdv_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.Hk * m.q.Tn, m.group * m.q.Tm, dkdv_resident(m.q), 4, dkdv_slot_bytes(m.q));
+  return cross_section((int64_t)m.q.B * m.Hk * m.q.Tn, m.group * m.q.Tm, dkdv_resident(m.q), CutCost{1.3, 0.4, 4, false},
+                       dkdv_slot_bytes(m.q));
 }
 
 hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,

@@ -22,30 +22,32 @@ struct CrossKeys {
 inline CrossKeys cross_keys(const CrossDims& m, const int32_t* lengths) { return {lengths, m.Nk, m.group, m.ksb, m.ksh, m.ksn}; }
 
 // Every list of a launch has up to list_max entries; a unit's list is cut into parts of len entries where the units alone do
-// not fill the chip: as many parts as give the fullest rounds of `resident` workgroups, over one to four rounds, and no
-// parts below `least` entries.
+// not fill the chip.  The cut with the least estimated time, in entries: rounds of `resident` workgroups that each take `start`
+// besides their entries, and a part's results joined by the last one, `join` each.  Lists of rows end with their sample's
+// keys, which only the device knows: for these (`ragged`) the mean of that time and of the one where half of all entries are
+// there, in lists of any length (the mean load, then the longest part).  Measured: CUTS.
 struct CrossParts { int len, parts; };
-inline CrossParts cross_parts(int64_t units, int list_max, int resident, int least) {
+struct CutCost { double start, join; int least; bool ragged; };
+inline CrossParts cross_parts(int64_t units, int list_max, int resident, const CutCost& c) {
   CrossParts best = {list_max, 1};
-  double fill = 0.0;
-  for (int rounds = 1; rounds <= 4; ++rounds) {
-    int64_t parts = (int64_t)rounds * resident / units;
-    if (parts > (list_max + least - 1) / least) parts = (list_max + least - 1) / least;
-    if (parts < 1) continue;
-    const int len = (int)((list_max + parts - 1) / parts);
-    const int made = (list_max + len - 1) / len;
+  double least = 0.0;
+  for (int want = 1; want <= (list_max + c.least - 1) / c.least && units * want <= 4 * (int64_t)resident && units * want <= SPLIT_POOL_MAX; ++want) {
+    const int len = (list_max + want - 1) / want, made = (list_max + len - 1) / len;
     const int64_t wgs = units * made;
-    const double f = (double)units * list_max / ((double)((wgs + resident - 1) / resident) * resident * len);
-    if (f > 1.02 * fill) { fill = f; best = {len, made}; }
+    const double joins = made > 1 ? made * c.join : 0.0;
+    double t = (double)((wgs + resident - 1) / resident) * (len + c.start) + joins;
+    if (c.ragged)
+      t = 0.5 * (t + 0.5 * (double)units * list_max / resident + c.start * (double)((wgs / 2 + resident) / resident) + len + joins);
+    if (want == 1 || t < 0.98 * least) { least = t; best = {len, made}; }
   }
   return best;
 }
 
 // What a kernel needs of a workspace: arrival counters (zeroed before the launch) and partial results, one of each a part.
 struct CrossSection { CrossParts cut; int slots; size_t counters, pool; };
-inline CrossSection cross_section(int64_t units, int list_max, int resident, int least, size_t slot_bytes) {
+inline CrossSection cross_section(int64_t units, int list_max, int resident, const CutCost& cost, size_t slot_bytes) {
   CrossSection s;
-  s.cut = cross_parts(units, list_max, resident, least);
+  s.cut = cross_parts(units, list_max, resident, cost);
   s.slots = s.cut.parts > 1 ? (int)(units * s.cut.parts) : 0;
   s.counters = round256((size_t)s.slots * 4);
   s.pool = round256((size_t)s.slots * slot_bytes);
@@ -65,14 +67,19 @@ inline SplitPlan cross_plan(const CrossSection& s, void* counters, void* pool, s
 }
 
 CrossSection cross_fwd_section(const CrossDims& m);
+CrossSection cross_few_section(const CrossDims& m);
 CrossSection cross_dq_section(const CrossDims& m);
 CrossSection cross_dkdv_section(const CrossDims& m);
 
-// Workspace of the forward pass: counters, pool.  Of the backward pass: D, counters of dK/dV and of dQ, pools.
+// Workspace of the forward pass: counters, pool.  Of the backward pass: D, counters of dQ and of dK/dV, pools.
+constexpr int FEW_ROWS = 32;
+// Whether the rows that read a key head are so few that the kernel for few rows takes them.  One wave of that kernel does what
+// four do in the other: at 32 rows FEWLINE.
+inline bool cross_few(const CrossDims& m) { return (int64_t)m.group * m.q.N <= FEW_ROWS; }
 struct CrossFwdWs { CrossSection s; size_t pool, total; };
 inline CrossFwdWs cross_fwd_ws(const CrossDims& m) {
   CrossFwdWs w;
-  w.s = cross_fwd_section(m);
+  w.s = cross_few(m) ? cross_few_section(m) : cross_fwd_section(m);
   w.pool = w.s.counters;
   w.total = w.pool + w.s.pool;
   return w;
@@ -90,13 +97,15 @@ inline CrossBwdWs cross_bwd_ws(const CrossDims& m) {
   return w;
 }
 
+hipError_t launch_zero_ints(int32_t* p, int n, hipStream_t stream);
+hipError_t launch_cross_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
+                            void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
 hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
                             void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
-hipError_t launch_cross_delta(const void* o, const void* o_res, const void* d_o, const CrossDims& m, float* delta, int32_t* zero,
-                              int zeros, hipStream_t stream);
-hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
-                           const CrossDims& m, const int32_t* lengths, float scale, void* dq, const SplitPlan& plan,
-                           hipStream_t stream);
+// (delta: D, written here for the dK/dV kernel; zero: integers that the launch sets to zero for it)
+hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
+                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, void* dq,
+                           int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream);
 hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
                              const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
                              hipStream_t stream);

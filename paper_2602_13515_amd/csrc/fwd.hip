@@ -338,8 +338,11 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   f32x16 sA[2], sB[2];
   {
 #if defined(__HIP_DEVICE_COMPILE__)
+    // (Q is waited for before the copies, not with them.  Where no list has to come first, the copies do not wait either.)
+    if constexpr (!CROSS) {
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) asm volatile("" : "+v"(qf[kk]));   // (Q is waited for before the copies, not with them)
+      for (int kk = 0; kk < NK; ++kk) asm volatile("" : "+v"(qf[kk]));
+    }
 #endif
     const int j0 = next_entry();
     j1 = next_entry(); j2 = next_entry();
@@ -520,12 +523,16 @@ hipError_t launch_fwd(const void* q, const void* k, const void* v, const Dims& m
 
 // ------------------------------------------------------------------ attention to another sequence
 CrossSection cross_fwd_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, 8, fwd_slot_bytes(m.q));
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, fwd_slot_bytes(m.q));
 }
 
 __global__ __launch_bounds__(256) void zero_ints_kernel(int32_t* p, int n) {
   const int x = blockIdx.x * 256 + threadIdx.x;
   if (x < n) p[x] = 0;
+}
+hipError_t launch_zero_ints(int32_t* p, int n, hipStream_t stream) {
+  hipLaunchKernelGGL(zero_ints_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, p, n);
+  return hipGetLastError();
 }
 
 hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
@@ -540,8 +547,7 @@ hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const C
   const CrossFwdWs w = cross_fwd_ws(m);
   a.sp = cross_plan(w.s, ws, (char*)ws + w.pool, fwd_slot_bytes(m.q));
   if (w.s.slots) {
-    hipLaunchKernelGGL(zero_ints_kernel, dim3((unsigned)((w.s.slots + 255) / 256)), dim3(256), 0, stream, a.sp.arrive, w.s.slots);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_zero_ints(a.sp.arrive, w.s.slots, stream);
     if (e != hipSuccess) return e;
   }
   const dim3 grid((unsigned)(w.s.cut.parts * stretch_wgs(a.BH * a.Tm))), block(256);

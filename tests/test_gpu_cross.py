@@ -94,6 +94,12 @@ CASES = [
     (1, 2, 2, 9000, 60, 128, None),                # few columns, long lists: parts
     (1, 2, 1, 9000, 60, 64, [31]),
     (2, 40, 40, 257, 200, 64, None),
+    (2, 10, 2, 6, 1000, 128, [1000, 31]),          # 30 rows of five heads, whose queries do not follow each other in memory
+    (1, 4, 1, 8, 2500, 64, None),                  # 32 rows: the last that the kernel for few rows takes
+    (1, 3, 1, 11, 2500, 64, [2470]),               # 33
+    (5, 8, 8, 2, 33, 128, [33, 32, 0, 1, 31]),
+    (1, 1, 1, 7, 128, 128, [97]),                  # one tile of 32 keys for each wave, the last of one key
+    (300, 1, 1, 1, 70, 64, None),
 ]
 
 
