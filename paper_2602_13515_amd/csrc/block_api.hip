@@ -85,6 +85,8 @@ CrossDims cross_dims(const spa2_cross_shape& s) {
   return m;
 }
 
+size_t cross_fwd_bytes(const CrossDims& m) { return cross_few(m) ? cross_few_ws(m).total : cross_fwd_ws(m).total; }
+
 int check_cross(const void* q, const void* k, const void* v, const int32_t* lengths, const void* o, const void* o_res,
                 const float* lse, const spa2_cross_shape* shape, float scale) {
   const int rc = check_cross_shape(shape);
@@ -103,7 +105,7 @@ extern "C" {
 
 size_t spa2_cross_fwd_workspace_bytes(const spa2_cross_shape* shape) {
   if (check_cross_shape(shape) != SPA2_OK) return 0;
-  return cross_fwd_ws(cross_dims(*shape)).total;
+  return cross_fwd_bytes(cross_dims(*shape));
 }
 
 size_t spa2_cross_bwd_workspace_bytes(const spa2_cross_shape* shape) {
@@ -116,7 +118,7 @@ int spa2_cross_fwd(const void* q, const void* k, const void* v, const int32_t* l
   const int rc = check_cross(q, k, v, lengths, o, o_res, lse, shape, scale);
   if (rc != SPA2_OK) return rc;
   const CrossDims m = cross_dims(*shape);
-  const size_t need = cross_fwd_ws(m).total;
+  const size_t need = cross_fwd_bytes(m);
   if (need && (!workspace || workspace_bytes < need)) return SPA2_ERR_WORKSPACE;
   if (need && !aligned16(workspace)) return SPA2_ERR_ALIGN;
   return (cross_few(m) ? launch_cross_few : launch_cross_fwd)(q, k, v, m, lengths, scale, o, o_res, lse, workspace,

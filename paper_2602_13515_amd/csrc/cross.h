@@ -67,7 +67,6 @@ inline SplitPlan cross_plan(const CrossSection& s, void* counters, void* pool, s
 }
 
 CrossSection cross_fwd_section(const CrossDims& m);
-CrossSection cross_few_section(const CrossDims& m);
 CrossSection cross_dq_section(const CrossDims& m);
 CrossSection cross_dkdv_section(const CrossDims& m);
 
@@ -76,10 +75,12 @@ constexpr int FEW_ROWS = 32;
 // Whether the rows that read a key head are so few that the kernel for few rows takes them.  One wave of that kernel does what
 // four do in the other: at 32 rows FEWLINE.
 inline bool cross_few(const CrossDims& m) { return (int64_t)m.group * m.q.N <= FEW_ROWS; }
+struct CrossFewWs { int workers; size_t counters, pool, total; };
+CrossFewWs cross_few_ws(const CrossDims& m);
 struct CrossFwdWs { CrossSection s; size_t pool, total; };
 inline CrossFwdWs cross_fwd_ws(const CrossDims& m) {
   CrossFwdWs w;
-  w.s = cross_few(m) ? cross_few_section(m) : cross_fwd_section(m);
+  w.s = cross_fwd_section(m);
   w.pool = w.s.counters;
   w.total = w.pool + w.s.pool;
   return w;

@@ -101,11 +101,23 @@ CASES = [
     (1, 1, 1, 7, 128, 128, [97]),                  # one tile of 32 keys for each wave, the last of one key
     (300, 1, 1, 1, 70, 64, None),
 ]
+_lengths = np.random.default_rng(6).integers
+CASES += [
+    # a line of key blocks that workgroups share evenly: many samples of any length, some empty; more than one chunk of 64 samples;
+    # stretches that begin and end inside of samples, with them, and hold several
+    (7, 4, 2, 1, 3000, 128, [0, 3000, 1, 64, 65, 2999, 0]),
+    (70, 3, 1, 2, 700, 64, list(_lengths(0, 701, 70))),
+    (200, 1, 1, 1, 400, 128, [0] * 100 + list(_lengths(0, 401, 100))),
+    (1000, 1, 1, 1, 100, 64, list(_lengths(-5, 130, 1000))),
+    (64, 2, 2, 3, 256, 128, [256] * 63 + [0]),
+    (1030, 1, 1, 1, 70, 64, list(_lengths(0, 71, 1030))),          # more samples than a line has
+    (600, 2, 2, 1, 70, 128, list(_lengths(0, 71, 600))),           # more pairs than are worth sharing
+]
 
 
-@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(map(str, c[:6])) + ("r" if c[6] else ""))
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "x".join(map(str, c[:6])) + ("r" if c[6] is not None else ""))
 def test_results_and_gradients(case):
-    print("case", case, flush=True)
+    print("case", case[:6], flush=True)
     _check(*_inputs(*case))
 
 
