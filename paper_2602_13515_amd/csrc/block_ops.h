@@ -9,6 +9,8 @@
 
 namespace spa2 {
 
+constexpr int64_t CACHE_BYTES = 256ll << 20;         // memory-side cache of the card
+
 struct NormTables { const float* cos; const float* sin; const void* positions; };
 
 size_t norm_rotate_partials_bytes(const spa2_norm_shape& s);

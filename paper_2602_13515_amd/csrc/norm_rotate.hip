@@ -6,12 +6,13 @@
 // Backward, with dn = R^T dy:
 //   dw_c = sum over rows of dn_c x_c r      dx = r (g - x r^2 mean_c(g x)),  g = dn w
 //
-// D / 16 lanes own a row, 16 channels each, in vectors of 16 bytes of the input that lie next to those of the neighbouring lanes
-// (8 channels of bf16, 4 of fp32) and hold both halves of the lane's 8 pairs: a rotation needs no exchange between lanes.  Lanes
-// behind the rotated channels turn theirs by an angle of zero.  A lane stays with its token and walks over heads: the cosines and
+// A lane owns two vectors of V channels of a row, which lie next to those of the neighbouring lanes and hold both halves of the
+// lane's V pairs: a rotation needs no exchange between lanes.  V is 8 in the forward pass of bf16 (16 bytes), else 4.  Lanes behind
+// the rotated channels turn theirs by an angle of zero.  A lane stays with its token and walks over heads: the cosines and
 // sines (4 bytes for each 2-byte channel of a head) are read once for its heads and held in registers.  A workgroup takes few
 // tokens and many of their heads, which lie next to each other in what a projection leaves.
-// Bound: HBM.  Measured: NORM
+// Bound: HBM.  75,600 tokens, 40 heads, d = 128, bf16 561 us (5.6 TB/s); 32,760 tokens, 12 heads, fp32, forward 104, backward 178 us
+// (5.8, 5.7 TB/s) and 6 for the weights (with vectors of 8 channels of fp32, 32 bytes apart, 123 and 239).
 #include "block_ops.h"
 #include "spa2_device.h"
 
@@ -32,6 +33,9 @@ struct NormArgs {
   float eps;
   float* part;                                         // backward: [workgroup][D] sums of dn x r, or null
 };
+
+constexpr int norm_vector(size_t size, bool backward) { return size == 2 && !backward ? 8 : 4; }
+constexpr int norm_lanes(int d, size_t size, bool backward) { return d / (2 * norm_vector(size, backward)); }
 
 // V channels as fp32
 template <int V> __device__ __forceinline__ void norm_load(const uint16_t* p, float* x) {
@@ -66,13 +70,19 @@ template <int V> __device__ __forceinline__ void norm_load(const float* p, float
     }
   }
 }
-template <int V> __device__ __forceinline__ void norm_store(uint16_t* p, const float* x) {
-  if constexpr (V == 8) *(u32x4*)p = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
-  else                  *(u32x2*)p = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+template <bool PAST, typename P>
+__device__ __forceinline__ void norm_put(P* p, P x) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, p);
+  else                *p = x;
 }
-template <int V> __device__ __forceinline__ void norm_store(float* p, const float* x) {
-#pragma unroll
-  for (int q = 0; q < V; q += 4) *(f32x4*)(p + q) = f32x4{x[q], x[q + 1], x[q + 2], x[q + 3]};
+// PAST: past the memory-side cache
+template <int V, bool PAST> __device__ __forceinline__ void norm_store(uint16_t* p, const float* x) {
+  if constexpr (V == 8) norm_put<PAST>((u32x4*)p, u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])});
+  else                  norm_put<PAST>((u32x2*)p, u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
+}
+template <int V, bool PAST> __device__ __forceinline__ void norm_store(float* p, const float* x) {
+  static_assert(V == 4, "16 bytes");
+  norm_put<PAST>((f32x4*)p, f32x4{x[0], x[1], x[2], x[3]});
 }
 
 // sum over the LANES lanes that own a row
@@ -83,24 +93,23 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// A lane's 16 channels turned by its angles (BACK: by minus the angles).  Pair i: channels 2 i and 2 i + 1 of the lane's where
-// pairs are interleaved, else i and 8 + i (its first vectors lie in the first half of the rotated channels, the others behind).
-template <bool INTERLEAVED, bool BACK>
-__device__ __forceinline__ void rotate(float (&x)[16], const float (&cs)[8], const float (&sn)[8]) {
+// A lane's 2 V channels turned by its angles (BACK: by minus the angles).  Pair i: channels 2 i and 2 i + 1 of the lane's where
+// pairs are interleaved, else i and V + i (its first vector lies in the first half of the rotated channels, the second behind).
+template <bool INTERLEAVED, bool BACK, int V>
+__device__ __forceinline__ void rotate(float (&x)[2 * V], const float (&cs)[V], const float (&sn)[V]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < V; ++i) {
     float& p = x[INTERLEAVED ? 2 * i : i];
-    float& q = x[INTERLEAVED ? 2 * i + 1 : 8 + i];
+    float& q = x[INTERLEAVED ? 2 * i + 1 : V + i];
     const float s = BACK ? -sn[i] : sn[i], u = p, v = q;
     p = fmaf(u, cs[i], -(v * s));
     q = fmaf(v, cs[i], u * s);
   }
 }
 
-// (backward: four waves a SIMD instead of three, 371 -> 361 us on the training case above)
-template <int D, typename T, bool INTERLEAVED, bool BACKWARD>
-__global__ __launch_bounds__(256, BACKWARD ? 4 : 5) void norm_rotate_kernel(NormArgs a) {
-  constexpr int LANES = D / 16, GROUPS = 256 / LANES, V = 16 / sizeof(T), NV = 16 / V;
+template <int D, typename T, bool INTERLEAVED, bool BACKWARD, bool PAST>
+__global__ __launch_bounds__(256) void norm_rotate_kernel(NormArgs a) {
+  constexpr int V = norm_vector(sizeof(T), BACKWARD), LANES = norm_lanes(D, sizeof(T), BACKWARD), GROUPS = 256 / LANES;
   const int tid = threadIdx.x, u = tid % LANES, group = tid / LANES;
   const int wgs_q = a.side[0].slices * a.side[0].walkers;
   const bool is_k = (int)blockIdx.x >= wgs_q;
@@ -109,18 +118,13 @@ __global__ __launch_bounds__(256, BACKWARD ? 4 : 5) void norm_rotate_kernel(Norm
   const int head0 = slice * z.per_slice + group / z.tokens, head1 = min((slice + 1) * z.per_slice, z.heads);
   const int head_step = GROUPS / z.tokens;
   // channels of this lane's vectors
-  const int turning = a.rot / 16;                      // lanes of a row that turn theirs
+  const int turning = a.rot / (2 * V);                 // lanes of a row that turn theirs: the first
   const bool turned = u < turning;
-  int at[NV];
+  const int first = turned ? V * u : a.rot + V * (u - turning), second = first + V * (turned ? turning : LANES - turning);
+  const int at[2] = {first, second};                   // (the turning lanes' first vectors are the first half of the rotated channels)
+  float w[2 * V], sums[2 * V];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    if (!turned)          at[k] = a.rot + V * (u - turning + k * (LANES - turning));
-    else if (INTERLEAVED) at[k] = V * (u + k * turning);
-    else                  at[k] = V * (u + (k % (NV / 2)) * turning) + (k >= NV / 2 ? a.rot / 2 : 0);
-  }
-  float w[16], sums[16];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
+  for (int k = 0; k < 2; ++k) {
     if (z.w) norm_load<V>(z.w + at[k], w + V * k);
     else
 #pragma unroll
@@ -128,71 +132,69 @@ __global__ __launch_bounds__(256, BACKWARD ? 4 : 5) void norm_rotate_kernel(Norm
   }
   if (BACKWARD) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sums[i] = 0.f;
+    for (int i = 0; i < 2 * V; ++i) sums[i] = 0.f;
   }
   const int64_t all = (int64_t)a.B * a.N;
   for (int tile = wg % z.walkers; tile < z.tiles; tile += z.walkers) {
     const int64_t token = (int64_t)tile * z.tokens + group % z.tokens;
     if (token >= all) break;                           // (later tiles are further on still)
     const int b = (int)(token / a.N), n = (int)(token - (int64_t)b * a.N);
-    float cs[8], sn[8];
+    float cs[V], sn[V];
     if (turned) {
       int64_t row = n;
       if (a.pos_bits == 32) row = ((const int32_t*)a.positions)[b * a.pos_sb + n];
       if (a.pos_bits == 64) row = ((const int64_t*)a.positions)[b * a.pos_sb + n];
       row = min(max(row, (int64_t)0), (int64_t)a.table_rows - 1);        // (caller data)
-      const int64_t first = row * (a.rot / 2);
+      const int64_t angles = row * (a.rot / 2);
       if constexpr (INTERLEAVED) {                     // half of a vector's channels are pairs
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          norm_load<V / 2>(a.cos + first + at[k] / 2, cs + V / 2 * k);
-          norm_load<V / 2>(a.sin + first + at[k] / 2, sn + V / 2 * k);
+        for (int k = 0; k < 2; ++k) {
+          norm_load<V / 2>(a.cos + angles + at[k] / 2, cs + V / 2 * k);
+          norm_load<V / 2>(a.sin + angles + at[k] / 2, sn + V / 2 * k);
         }
       } else {
-#pragma unroll
-        for (int k = 0; k < NV / 2; ++k) {
-          norm_load<V>(a.cos + first + at[k], cs + V * k);
-          norm_load<V>(a.sin + first + at[k], sn + V * k);
-        }
+        norm_load<V>(a.cos + angles + first, cs);
+        norm_load<V>(a.sin + angles + first, sn);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+      for (int i = 0; i < V; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
     }
     const T* x0 = (const T*)z.x + b * z.sb + n * z.sn;
     const int64_t out0 = b * z.osb + n * z.osn;
+#pragma unroll 1
     for (int h = head0; h < head1; h += head_step) {
-      float x[16];
+      float x[2 * V];
 #pragma unroll
-      for (int k = 0; k < NV; ++k) norm_load<V>(x0 + h * z.sh + at[k], x + V * k);
+      for (int k = 0; k < 2; ++k) norm_load<V>(x0 + h * z.sh + at[k], x + V * k);
       const int64_t out = out0 + h * z.osh;
       float square = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) square = fmaf(x[i], x[i], square);
+      for (int i = 0; i < 2 * V; ++i) square = fmaf(x[i], x[i], square);
       if constexpr (!BACKWARD) {
         const float r = 1.f / sqrtf(row_sum<LANES>(square) * (1.f / D) + a.eps);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
-        rotate<INTERLEAVED, false>(x, cs, sn);
+        for (int i = 0; i < 2 * V; ++i) x[i] = x[i] * r * w[i];
+        rotate<INTERLEAVED, false, V>(x, cs, sn);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) norm_store<V>((uint16_t*)z.y + out + at[k], x + V * k);
+        for (int k = 0; k < 2; ++k) norm_store<V, PAST>((uint16_t*)z.y + out + at[k], x + V * k);
       } else {
-        float g[16], inner = 0.f;
+        float g[2 * V], inner = 0.f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) norm_load<V>((const uint16_t*)z.dy + out + at[k], g + V * k);
-        rotate<INTERLEAVED, true>(g, cs, sn);
+        for (int k = 0; k < 2; ++k) norm_load<V>((const uint16_t*)z.dy + out + at[k], g + V * k);
+        rotate<INTERLEAVED, true, V>(g, cs, sn);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) inner = fmaf(g[i] * w[i], x[i], inner);
+        for (int i = 0; i < 2 * V; ++i) inner = fmaf(g[i] * w[i], x[i], inner);
         const float r = 1.f / sqrtf(row_sum<LANES>(square) * (1.f / D) + a.eps);
         inner = row_sum<LANES>(inner) * r * (1.f / D);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 2 * V; ++i) {
           const float hat = x[i] * r;
           sums[i] = fmaf(g[i], hat, sums[i]);
           x[i] = r * fmaf(-hat, inner, g[i] * w[i]);
         }
 #pragma unroll
-        for (int k = 0; k < NV; ++k) norm_store<V>((T*)z.y + out + at[k], x + V * k);
+        for (int k = 0; k < 2; ++k) norm_store<V, PAST>((T*)z.y + out + at[k], x + V * k);
       }
     }
   }
@@ -201,13 +203,13 @@ __global__ __launch_bounds__(256, BACKWARD ? 4 : 5) void norm_rotate_kernel(Norm
     // sums of the lanes that hold the same channels: over a wave by exchange, over the waves through LDS
     __shared__ float lds[4][D];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 2 * V; ++i) {
 #pragma unroll
       for (int s = LANES; s < 64; s <<= 1) sums[i] += __shfl_xor(sums[i], s, 64);
     }
     if ((tid & 63) < LANES) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k) norm_store<V>(&lds[tid >> 6][at[k]], sums + V * k);
+      for (int k = 0; k < 2; ++k) norm_store<V, false>(&lds[tid >> 6][at[k]], sums + V * k);
     }
     __syncthreads();
     if (tid < D) a.part[(int64_t)blockIdx.x * D + tid] = (lds[0][tid] + lds[1][tid]) + (lds[2][tid] + lds[3][tid]);
@@ -245,10 +247,11 @@ namespace {
 // lie next to each other.  (75,600 tokens, 40 heads, heads at a time 1 / 2 / 4 / 8 / 16 / 32: 671 / 661 / 656 / 642 / 628 / 642 us.)
 // Heads of a token go to several workgroups where whole tokens would leave compute units idle.
 void norm_side(NormSide& z, const spa2_norm_shape& s, int heads, bool backward) {
-  const int groups = 256 / (s.d / 16);
+  const int groups = 256 / norm_lanes(s.d, s.dtype == SPA2_DTYPE_BF16 ? 2 : 4, backward);
   const int64_t all = (int64_t)s.B * s.N;
   int at_once = 1;
-  while (2 * at_once <= heads && 2 * at_once <= groups / 2) at_once *= 2;
+  for (int x = 2; x <= heads && x <= groups / 2; x *= 2)
+    if (4 * ((heads + x - 1) / x * x) <= 5 * heads) at_once = x;          // (an idle group in five at most)
   z.heads = heads;
   z.tokens = groups / at_once;
   z.tiles = (int)((all + z.tokens - 1) / z.tokens);
@@ -279,17 +282,22 @@ NormArgs norm_args(const NormTables& t, const spa2_norm_shape& s, const float* q
 }
 
 template <int D, typename T, bool BACKWARD>
-void launch_typed(const NormArgs& a, bool interleaved, hipStream_t stream) {
+void launch_typed(const NormArgs& a, bool interleaved, bool past, hipStream_t stream) {
   const dim3 grid((unsigned)(norm_wgs(a.side[0]) + norm_wgs(a.side[1]))), block(256);
-  if (interleaved) hipLaunchKernelGGL((norm_rotate_kernel<D, T, true, BACKWARD>), grid, block, 0, stream, a);
-  else             hipLaunchKernelGGL((norm_rotate_kernel<D, T, false, BACKWARD>), grid, block, 0, stream, a);
+  const auto kernel = interleaved ? (past ? norm_rotate_kernel<D, T, true, BACKWARD, true> : norm_rotate_kernel<D, T, true, BACKWARD, false>)
+                                  : (past ? norm_rotate_kernel<D, T, false, BACKWARD, true> : norm_rotate_kernel<D, T, false, BACKWARD, false>);
+  hipLaunchKernelGGL(kernel, grid, block, 0, stream, a);
 }
 
 template <bool BACKWARD>
 hipError_t launch_any(const NormArgs& a, const spa2_norm_shape& s, hipStream_t stream) {
   const bool bf16 = s.dtype == SPA2_DTYPE_BF16, il = s.interleaved != 0;
-  if (s.d == 128) bf16 ? launch_typed<128, uint16_t, BACKWARD>(a, il, stream) : launch_typed<128, float, BACKWARD>(a, il, stream);
-  else            bf16 ? launch_typed<64, uint16_t, BACKWARD>(a, il, stream) : launch_typed<64, float, BACKWARD>(a, il, stream);
+  // Stored past the memory-side cache where what is read and written does not fit in it.  75,600 tokens, 40 heads 588 / 562 us,
+  // 32,760 tokens, 12 heads, fp32, both passes 361 / 351.
+  const int64_t size = bf16 ? 2 : 4;
+  const bool past = (int64_t)s.B * s.N * (s.Hq + s.Hk) * s.d * (BACKWARD ? 2 * size + 2 : size + 2) > CACHE_BYTES;
+  if (s.d == 128) bf16 ? launch_typed<128, uint16_t, BACKWARD>(a, il, past, stream) : launch_typed<128, float, BACKWARD>(a, il, past, stream);
+  else            bf16 ? launch_typed<64, uint16_t, BACKWARD>(a, il, past, stream) : launch_typed<64, float, BACKWARD>(a, il, past, stream);
   return hipGetLastError();
 }
 
