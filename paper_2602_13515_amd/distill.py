@@ -4,30 +4,47 @@ The paper fine-tunes video diffusion models whose weights are not available here
 without them is the training step itself: a frozen teacher with full attention, a student that shares its
 initialisation and differs only in the attention operator, identical noisy inputs x_t = t x_1 + (1 - t) x_0
 for both, and the loss ||u_sparse - u_full||^2 back-propagated through the block-sparse backward kernels.
-`ToyBlock` is one pre-norm attention block that stands in for the velocity network.
+`ToyBlock` is one pre-norm attention block that stands in for the velocity network; on request with what such a network has
+around its attention: the norm of q and k with the rotation by position, attention to a prompt, dropout of its branches.
 """
 from __future__ import annotations
 
 import copy
-from typing import Callable, Dict, Iterable, Optional, Tuple
+from typing import Callable, Dict, Iterable, Optional, Sequence, Tuple
 
 import torch
 
 from . import binding as _b
 from .autograd import _operator, _plain, sparge_attn2
+from .block import cross_attention, dropout_add, qk_norm_rotate, rotary_table
 
 
 class ToyBlock(torch.nn.Module):
     """x -> x + proj(attention(norm(x))): fp32 parameters, bf16 attention on [B, N, H, d] activations that reach
-    the kernels as permuted views (no copy).  `k_frac`, `top_p` None means full attention (the teacher)."""
+    the kernels as permuted views (no copy).  `k_frac`, `top_p` None means full attention (the teacher).
 
-    def __init__(self, dim: int, heads: int, k_frac: Optional[float] = None, top_p: Optional[float] = None):
+    grid: extents of the tokens' grid (frames, height, width): the heads of q and k are normed and rotated by position.
+    context_dim: a second branch attends to `context` [B, M, context_dim], of which sample b has `lengths[b]` rows (a batch of
+    prompts, padded).  dropout: of both branches, in training mode; the masks' seed comes from PyTorch's default generator."""
+
+    def __init__(self, dim: int, heads: int, k_frac: Optional[float] = None, top_p: Optional[float] = None,
+                 grid: Optional[Sequence[int]] = None, context_dim: Optional[int] = None, dropout: float = 0.0):
         super().__init__()
         assert dim % heads == 0 and dim // heads in (64, 128)
-        self.heads, self.k_frac, self.top_p = heads, k_frac, top_p
+        self.heads, self.k_frac, self.top_p, self.dropout = heads, k_frac, top_p, float(dropout)
         self.norm = torch.nn.LayerNorm(dim)
         self.qkv = torch.nn.Linear(dim, 3 * dim)
         self.proj = torch.nn.Linear(dim, dim)
+        self.grid, self.context_dim = grid, context_dim
+        if grid is not None:
+            self.q_weight, self.k_weight = (torch.nn.Parameter(torch.ones(dim // heads)) for _ in range(2))
+            for name, table in zip(("cos", "sin"), rotary_table(grid, dim // heads)):
+                self.register_buffer(name, table, persistent=False)
+        if context_dim is not None:
+            self.context_norm = torch.nn.LayerNorm(dim)
+            self.context_q = torch.nn.Linear(dim, dim)
+            self.context_kv = torch.nn.Linear(context_dim, 2 * dim)
+            self.context_proj = torch.nn.Linear(dim, dim)
         self._full = None                     # the all-ones pattern, built once per input shape
 
     def _attention(self, q, k, v):
@@ -39,18 +56,39 @@ class ToyBlock(torch.nn.Module):
             _b.spa2_pattern_full(q.detach(), self._full)
         return sparge_attn2(q, k, v, 0.0, 0.0, pattern=self._full)
 
-    def forward(self, x: torch.Tensor) -> torch.Tensor:
+    def _add(self, x: torch.Tensor, branch: torch.Tensor, seed: Optional[int], number: int) -> torch.Tensor:
+        """x plus a branch, dropped in places (each branch draws with an offset of its own)."""
+        return x + branch if seed is None else dropout_add(branch, x, self.dropout, seed, number)
+
+    def forward(self, x: torch.Tensor, context: Optional[torch.Tensor] = None,
+                lengths: Optional[torch.Tensor] = None) -> torch.Tensor:
         B, N, C = x.shape
-        qkv = self.qkv(self.norm(x)).to(torch.bfloat16).view(B, N, 3, self.heads, C // self.heads)
-        q, k, v = (qkv[:, :, i].permute(0, 2, 1, 3) for i in range(3))         # [B, H, N, d] views
+        d = C // self.heads
+        seed = int(torch.randint(2 ** 63 - 1, ()).item()) if self.training and self.dropout > 0.0 else None
+        qkv = self.qkv(self.norm(x))
+        if self.grid is None:
+            qkv = qkv.to(torch.bfloat16).view(B, N, 3, self.heads, d)
+            q, k, v = (qkv[:, :, i].permute(0, 2, 1, 3) for i in range(3))         # [B, H, N, d] views
+        else:                                 # (the norm reads the projection in fp32 and writes what the attention takes)
+            q, k, v = (t.permute(0, 2, 1, 3) for t in qkv.view(B, N, 3, self.heads, d).unbind(2))
+            q, k = qk_norm_rotate(q, k, self.q_weight, self.k_weight, self.cos, self.sin, interleaved=True)
+            v = v.to(torch.bfloat16)
         o = self._attention(q, k, v)                                            # strides of q
-        return x + self.proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float())
+        x = self._add(x, self.proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float()), seed, 0)
+        if self.context_dim is None:
+            return x
+        q = self.context_q(self.context_norm(x)).to(torch.bfloat16).view(B, N, self.heads, d).permute(0, 2, 1, 3)
+        k, v = (t.permute(0, 2, 1, 3) for t in
+                self.context_kv(context).to(torch.bfloat16).view(B, -1, 2, self.heads, d).unbind(2))
+        o = cross_attention(q, k, v, lengths)
+        return self._add(x, self.context_proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float()), seed, 1)
 
 
-def make_student(teacher: ToyBlock, k_frac: float, top_p: float) -> ToyBlock:
-    """Alg. 2 steps 3-4: same weights, attention replaced by SpargeAttn2(., ., ., k%, p%); the teacher is frozen."""
+def make_student(teacher: ToyBlock, k_frac: float, top_p: float, dropout: float = 0.0) -> ToyBlock:
+    """Alg. 2 steps 3-4: same weights, attention replaced by SpargeAttn2(., ., ., k%, p%); the teacher is frozen.  `dropout` is
+    the student's (the teacher keeps its own)."""
     student = copy.deepcopy(teacher)
-    student.k_frac, student.top_p, student._full = float(k_frac), float(top_p), None
+    student.k_frac, student.top_p, student._full, student.dropout = float(k_frac), float(top_p), None, float(dropout)
     for p in teacher.parameters():
         p.requires_grad_(False)
     return student
@@ -101,17 +139,17 @@ def velocity_distillation_loss(u_sparse: torch.Tensor, u_full: torch.Tensor, red
     return _VelocityDistillationLoss.apply(u_sparse.contiguous(), u_full.contiguous(), weight)
 
 
-def distill(student: torch.nn.Module, teacher: torch.nn.Module, batches: Iterable[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]],
+def distill(student: torch.nn.Module, teacher: torch.nn.Module, batches: Iterable[Tuple[torch.Tensor, ...]],
             lr: float = 1e-3, on_step: Optional[Callable[[int, float], None]] = None) -> Dict[str, list]:
     """The loop of Alg. 2 over `batches` of (x_1, x_0, t): teacher and student see the same x_t, only the student
-    is updated.  Returns the loss per step."""
+    is updated.  What a batch holds behind these three (a context and its lengths) both get too.  Returns the loss per step."""
     opt = torch.optim.Adam([p for p in student.parameters() if p.requires_grad], lr=lr)
     losses = []
-    for step, (x1, x0, t) in enumerate(batches):
+    for step, (x1, x0, t, *more) in enumerate(batches):
         xt = noisy_latent(x1, x0, t)
         with torch.no_grad():
-            u_full = teacher(xt)
-        loss = velocity_distillation_loss(student(xt), u_full)
+            u_full = teacher(xt, *more)
+        loss = velocity_distillation_loss(student(xt, *more), u_full)
         opt.zero_grad(set_to_none=True)
         loss.backward()
         opt.step()
