@@ -22,12 +22,13 @@ from .autograd import _operator, _plain
 
 def _refuse_others(name: str, *tensors: Optional[torch.Tensor]) -> None:
     given = [t for t in tensors if t is not None]
+    if _plain(*given):
+        return
     if not all(isinstance(t, torch.Tensor) for t in given):
         raise TypeError(f"{name} takes tensors")
     if not all(t.is_cuda for t in given):
         raise ValueError(f"{name} runs on the GPU only: it has no CPU path")
-    if not _plain(*given):
-        raise RuntimeError(f"{name} takes plain CUDA tensors, outside tracing, compilation and function transforms")
+    raise RuntimeError(f"{name} takes plain CUDA tensors, outside tracing, compilation and function transforms")
 
 
 def rotary_table(sizes: Union[int, Sequence[int]], d: int, theta: float = 10000.0,

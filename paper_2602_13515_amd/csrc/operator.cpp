@@ -243,9 +243,16 @@ bool float_kind(const Tensor& t) { return t.scalar_type() == at::kBFloat16 || t.
 
 // A [B, H, N, d] tensor without gaps, tokens outside the heads where x has them so (what a projection leaves and takes).
 Tensor dense_like(const Tensor& x, at::ScalarType dtype) {
-  const auto o = x.options().dtype(dtype);
-  if (x.stride(2) > x.stride(1)) return at::empty({x.size(0), x.size(2), x.size(1), x.size(3)}, o).permute({0, 2, 1, 3});
-  return at::empty(x.sizes(), o);
+  const int64_t h = x.size(1), n = x.size(2), d = x.size(3);
+  const bool tokens_outside = x.stride(2) > x.stride(1);
+  return at::empty_strided(x.sizes(), {h * n * d, tokens_outside ? d : n * d, tokens_outside ? h * d : d, 1}, x.options().dtype(dtype));
+}
+// Whether a call is one that autograd has to see: with a gradient to come, or a tangent (which it refuses).
+bool differentiated(std::initializer_list<const Tensor*> inputs) {
+  const bool grad = at::GradMode::is_enabled();
+  for (const Tensor* t : inputs)
+    if (t->defined() && ((grad && t->requires_grad()) || t->_fw_grad(0).defined())) return true;
+  return false;
 }
 // Strides as the kernels read them: a dimension of one element has none.
 std::array<int64_t, 3> strides_of(const Tensor& x) {
@@ -343,17 +350,23 @@ void norm_check(const Tensor& q, const Tensor& k, const Tensor& wq, const Tensor
   }
 }
 
+std::pair<Tensor, Tensor> norm_rotate_call(const Tensor& q, const Tensor& k, const Tensor& wq, const Tensor& wk, const Tensor& cos,
+                                           const Tensor& sin, const Tensor& positions, double eps, bool interleaved) {
+  const c10::DeviceGuard device(q.device());
+  const Tensor qo = dense_like(q, at::kBFloat16), ko = dense_like(k, at::kBFloat16);
+  const NormShape n(q, k, cos, positions, interleaved, qo, ko);
+  check(spa2_norm_rotate(q.data_ptr(), k.data_ptr(), (const float*)ptr(wq), (const float*)ptr(wk), (const float*)ptr(cos),
+                         (const float*)ptr(sin), ptr(positions), &n.s, (float)eps, qo.data_ptr(), ko.data_ptr(),
+                         stream_of(q)), "spa2_norm_rotate");
+  return {qo, ko};
+}
+
 struct NormRotate : torch::autograd::Function<NormRotate> {
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const OptTensor& q_weight,
                                const OptTensor& k_weight, const OptTensor& cos_, const OptTensor& sin_,
                                const OptTensor& positions_, double eps, bool interleaved, bool weight_grads) {
     const Tensor wq = or_none(q_weight), wk = or_none(k_weight), cos = or_none(cos_), sin = or_none(sin_), positions = or_none(positions_);
-    const c10::DeviceGuard device(q.device());
-    const Tensor qo = dense_like(q, at::kBFloat16), ko = dense_like(k, at::kBFloat16);
-    const NormShape n(q, k, cos, positions, interleaved, qo, ko);
-    check(spa2_norm_rotate(q.data_ptr(), k.data_ptr(), (const float*)ptr(wq), (const float*)ptr(wk), (const float*)ptr(cos),
-                           (const float*)ptr(sin), ptr(positions), &n.s, (float)eps, qo.data_ptr(), ko.data_ptr(),
-                           stream_of(q)), "spa2_norm_rotate");
+    const auto [qo, ko] = norm_rotate_call(q, k, wq, wk, cos, sin, positions, eps, interleaved);
     ctx->save_for_backward({q, k, wq, wk, cos, sin, positions});
     ctx->saved_data["eps"] = eps;
     ctx->saved_data["interleaved"] = interleaved;
@@ -394,6 +407,7 @@ struct NormRotate : torch::autograd::Function<NormRotate> {
 // weights of any float type: the kernels read fp32 (the conversion is differentiated by PyTorch)
 OptTensor as_weight(const OptTensor& w) {
   if (!w || !w->defined()) return std::nullopt;
+  if (w->scalar_type() == at::kFloat && w->is_contiguous()) return *w;
   return w->to(at::kFloat).contiguous();
 }
 
@@ -402,6 +416,9 @@ std::tuple<Tensor, Tensor> norm_rotate(const Tensor& q, const Tensor& k, const O
                                        bool interleaved) {
   const OptTensor wq = as_weight(q_weight), wk = as_weight(k_weight);
   norm_check(q, k, or_none(wq), or_none(wk), or_none(cos), or_none(sin), or_none(positions));
+  const Tensor w0 = or_none(wq), w1 = or_none(wk);
+  if (!differentiated({&q, &k, &w0, &w1}))
+    return norm_rotate_call(q, k, w0, w1, or_none(cos), or_none(sin), or_none(positions), eps, interleaved);
   capture_check(q, {q, k, or_none(q_weight), or_none(k_weight)});
   const bool weight_grads = at::GradMode::is_enabled() && ((wq && wq->requires_grad()) || (wk && wk->requires_grad()));
   const variable_list out = NormRotate::apply(q, k, wq, wk, cos, sin, positions, eps, interleaved, weight_grads);
@@ -449,29 +466,37 @@ Tensor copy_of(const Tensor& x) {
 // One layout for a query tensor and all that is shaped like it: q itself where it has no gaps, else a copy without them.
 Tensor without_gaps(const Tensor& q) { return q.is_non_overlapping_and_dense() ? q : copy_of(q); }
 
+struct CrossResult { Tensor q, k, v, o, o_res, lse; };       // (q, k and v in the layouts that the kernels took)
+CrossResult cross_call(const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Tensor& lengths, double scale, bool training) {
+  const c10::DeviceGuard device(q_in.device());
+  const bool one_layout = strides_of(k_in) == strides_of(v_in);
+  CrossResult r;
+  r.q = without_gaps(q_in);
+  r.k = one_layout ? k_in : copy_of(k_in);
+  r.v = one_layout ? v_in : in_order(v_in, r.k);
+  const CrossShape c(r.q, r.k, r.k);
+  r.o = like(r.q);
+  if (training) r.o_res = like(r.q);
+  // one scratch buffer; a log-sum-exp that nobody reads lies behind the workspace
+  const int64_t need = (int64_t)spa2_cross_fwd_workspace_bytes(&c.s), at = (need + 255) & ~(int64_t)255;
+  const int64_t rows = r.q.size(0) * r.q.size(1) * r.q.size(2);
+  if (training) r.lse = at::empty({r.q.size(0), r.q.size(1), r.q.size(2)}, r.q.options().dtype(at::kFloat));
+  const Tensor ws = !training || need ? bytes(training ? need : at + 4 * rows, r.q) : Tensor();
+  float* lse = training ? (float*)r.lse.data_ptr() : (float*)((char*)ws.data_ptr() + at);
+  check(spa2_cross_fwd(r.q.data_ptr(), r.k.data_ptr(), r.v.data_ptr(), (const int32_t*)ptr(lengths), &c.s, (float)scale,
+                       r.o.data_ptr(), (void*)ptr(r.o_res), lse, (void*)ptr(ws), (size_t)need, stream_of(r.q)), "spa2_cross_fwd");
+  return r;
+}
+
 struct CrossAttention : torch::autograd::Function<CrossAttention> {
-  static Tensor forward(AutogradContext* ctx, const Tensor& q_in, const Tensor& k_in, const Tensor& v_in,
-                        const OptTensor& lengths_, double scale, bool training) {
-    const c10::DeviceGuard device(q_in.device());
-    const bool one_layout = strides_of(k_in) == strides_of(v_in);
-    const Tensor q = without_gaps(q_in), k = one_layout ? k_in : copy_of(k_in), v = one_layout ? v_in : in_order(v_in, k),
-                 lengths = or_none(lengths_);
-    const CrossShape c(q, k, k);
-    const Tensor o = like(q);
-    Tensor o_res, lse;
-    if (training) o_res = like(q);
-    lse = at::empty({q.size(0), q.size(1), q.size(2)}, q.options().dtype(at::kFloat));
-    const int64_t need = (int64_t)spa2_cross_fwd_workspace_bytes(&c.s);
-    const Tensor ws = need ? bytes(need, q) : Tensor();
-    check(spa2_cross_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), (const int32_t*)ptr(lengths), &c.s, (float)scale,
-                         o.data_ptr(), (void*)ptr(o_res), (float*)lse.data_ptr(), (void*)ptr(ws), (size_t)need, stream_of(q)),
-          "spa2_cross_fwd");
-    if (training) {
-      ctx->save_for_backward({q, k, v, o, o_res, lse, lengths});
-      ctx->saved_data["keys"] = k.sizes().vec();
-      ctx->saved_data["scale"] = scale;
-    }
-    return o;
+  static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const OptTensor& lengths_,
+                        double scale) {
+    const Tensor lengths = or_none(lengths_);
+    const CrossResult r = cross_call(q, k, v, lengths, scale, true);
+    ctx->save_for_backward({r.q, r.k, r.v, r.o, r.o_res, r.lse, lengths});
+    ctx->saved_data["keys"] = r.k.sizes().vec();
+    ctx->saved_data["scale"] = scale;
+    return r.o;
   }
 
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
@@ -497,15 +522,15 @@ struct CrossAttention : torch::autograd::Function<CrossAttention> {
                          d_o.data_ptr(), (const float*)lse.data_ptr(), &c.s, (float)ctx->saved_data["scale"].toDouble(),
                          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), (size_t)need, stream_of(q)),
           "spa2_cross_bwd");
-    return once({dq, dk, dv, Variable(), Variable(), Variable()}, graph, "cross_attention");
+    return once({dq, dk, dv, Variable(), Variable()}, graph, "cross_attention");
   }
 };
 
 Tensor cross_attention(const Tensor& q, const Tensor& k, const Tensor& v, const OptTensor& lengths, double scale) {
   cross_check(q, k, v, or_none(lengths));
+  if (!differentiated({&q, &k, &v})) return cross_call(q, k, v, or_none(lengths), scale, false).o;
   capture_check(q, {q, k, v});
-  const bool training = at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad());
-  return CrossAttention::apply(q, k, v, lengths, scale, training);
+  return CrossAttention::apply(q, k, v, lengths, scale);
 }
 
 // x as the elementwise kernels take it: contiguous from a 16-byte boundary.
@@ -519,14 +544,20 @@ void seed_check(const Tensor& s, const Tensor& x) {
                     "a seed on the device is two int64 numbers, seed and offset, on the device of x");
 }
 
+Tensor dropout_call(const Tensor& x_in, const Tensor& residual_in, double p, int64_t seed, int64_t offset, const Tensor& so) {
+  const c10::DeviceGuard device(x_in.device());
+  const Tensor x = packed(x_in), residual = residual_in.defined() ? packed(residual_in) : Tensor();
+  const Tensor y = at::empty_like(residual.defined() ? residual : x);
+  check(spa2_dropout_add(x.data_ptr(), ptr(residual), x.numel(), dtype_of(x), dtype_of(y), p, (uint64_t)seed,
+                         (uint64_t)offset, (const int64_t*)ptr(so), y.data_ptr(), stream_of(x)), "spa2_dropout_add");
+  return y;
+}
+
 struct DropoutAdd : torch::autograd::Function<DropoutAdd> {
-  static Tensor forward(AutogradContext* ctx, const Tensor& x_in, const OptTensor& residual_in, double p, int64_t seed,
+  static Tensor forward(AutogradContext* ctx, const Tensor& x, const OptTensor& residual_in, double p, int64_t seed,
                         int64_t offset, const OptTensor& seed_offset) {
-    const c10::DeviceGuard device(x_in.device());
-    const Tensor x = packed(x_in), residual = residual_in ? packed(*residual_in) : Tensor(), so = or_none(seed_offset);
-    const Tensor y = at::empty_like(residual.defined() ? residual : x);
-    check(spa2_dropout_add(x.data_ptr(), ptr(residual), x.numel(), dtype_of(x), dtype_of(y), p, (uint64_t)seed,
-                           (uint64_t)offset, (const int64_t*)ptr(so), y.data_ptr(), stream_of(x)), "spa2_dropout_add");
+    const Tensor residual = or_none(residual_in), so = or_none(seed_offset);
+    const Tensor y = dropout_call(x, residual, p, seed, offset, so);
     ctx->save_for_backward({so});
     ctx->saved_data["p"] = p;
     ctx->saved_data["seed"] = seed;
@@ -560,7 +591,9 @@ Tensor dropout_add(const Tensor& x, const OptTensor& residual, double p, int64_t
                       (residual->scalar_type() == x.scalar_type() || residual->scalar_type() == at::kFloat),
                       "the residual has the shape and device of x and its type, or fp32");
   seed_check(or_none(seed_offset), x);
-  capture_check(x, {x, or_none(residual)});
+  const Tensor r = or_none(residual);
+  if (!differentiated({&x, &r})) return dropout_call(x, r, p, seed, offset, or_none(seed_offset));
+  capture_check(x, {x, r});
   return DropoutAdd::apply(x, residual, p, seed, offset, seed_offset);
 }
 

@@ -101,6 +101,14 @@ CASES = [
     (1, 1, 1, 7, 128, 128, [97]),                  # one tile of 32 keys for each wave, the last of one key
     (300, 1, 1, 1, 70, 64, None),
 ]
+CASES += [
+    # more rows than the chip holds at a time: a workgroup takes several, one after the other; lists of one block and more, odd and
+    # even, samples without keys, the last row of a head short, the last workgroup of a head with fewer rows
+    (2, 8, 8, 9999, 50, 64, [50, 0]),
+    (1, 6, 3, 15000, 130, 64, None),
+    (3, 8, 4, 6401, 200, 128, [200, 64, 1]),
+    (1, 20, 20, 4000, 321, 128, None),
+]
 _lengths = np.random.default_rng(6).integers
 CASES += [
     # a line of key blocks that workgroups share evenly: many samples of any length, some empty; more than one chunk of 64 samples;
@@ -297,3 +305,15 @@ def test_saved_tensors_that_come_back_changed_are_refused():
         except ValueError:
             raised = True
         assert raised
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_inputs_with_tangents_are_refused(grad):
+    import torch.autograd.forward_ad as fwad
+    x = torch.randn(1, 2, 8, 64, device=dev()).bfloat16()
+    f = lambda t: spa2.cross_attention(t, x, x)
+    with torch.set_grad_enabled(grad), fwad.dual_level():
+        want = f(x)
+        with pytest.raises(RuntimeError):
+            f(fwad.make_dual(x, torch.ones_like(x)))
+    assert torch.equal(f(x), want)

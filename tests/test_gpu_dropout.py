@@ -172,3 +172,15 @@ def test_capture_beside_an_eager_graph_of_the_same_leaf_is_refused():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(held, y.detach())
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_inputs_with_tangents_are_refused(grad):
+    import torch.autograd.forward_ad as fwad
+    x = torch.randn(1, 2, 8, 64, device=dev())
+    f = lambda t: spa2.dropout_add(t, x, 0.5, 1)
+    with torch.set_grad_enabled(grad), fwad.dual_level():
+        want = f(x)
+        with pytest.raises(RuntimeError):
+            f(fwad.make_dual(x, torch.ones_like(x)))
+    assert torch.equal(f(x), want)

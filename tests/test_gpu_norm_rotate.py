@@ -230,3 +230,15 @@ def test_another_stream_and_a_captured_graph():
         torch.cuda.synchronize()
         for a, b in zip(held, want):
             assert torch.equal(a, b), change
+
+
+@pytest.mark.parametrize("grad", [False, True])
+def test_inputs_with_tangents_are_refused(grad):
+    import torch.autograd.forward_ad as fwad
+    x = torch.randn(1, 2, 8, 64, device=dev())
+    f = lambda t: spa2.qk_norm_rotate(t, x)[0]
+    with torch.set_grad_enabled(grad), fwad.dual_level():
+        want = f(x)
+        with pytest.raises(RuntimeError):
+            f(fwad.make_dual(x, torch.ones_like(x)))
+    assert torch.equal(f(x), want)
