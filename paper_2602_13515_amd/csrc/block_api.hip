@@ -66,7 +66,7 @@ int check_cross_shape(const spa2_cross_shape* s) {
 
 // The query heads of a key head are taken as one head of more rows where a stride says so (one query a head, or heads whose
 // queries follow each other in memory): their keys and values are then read once, not once a head.  One query, 8 samples of up
-// to 32,760 keys, 40 heads sharing 8, d = 128: 523 us head by head, GROUPED.
+// to 32,760 keys, 40 heads sharing 8, d = 128, by the kernel for many rows: 523 us head by head, 175 together.
 CrossDims cross_dims(const spa2_cross_shape& s) {
   CrossDims m;
   m.q.B = s.B; m.q.H = s.Hq; m.q.N = s.Nq; m.q.d = s.d;

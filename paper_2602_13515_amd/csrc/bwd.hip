@@ -53,7 +53,7 @@ struct DqArgs {
 };
 
 // Attention to another sequence (see fwd.hip).  D is made here, for this kernel and for dK/dV behind it: as a launch of its own
-// it read dO once more.  32,760 queries, 12 heads, 512 keys, d = 128, backward pass: DELTA.
+// it read dO once more: 32,760 queries, 12 heads, 512 keys, d = 128, D 55 and dQ 164 us; dQ with D 199.
 struct CrossDqArgs : DqArgs {
   static constexpr bool CROSS = true;
   CrossKeys kv;

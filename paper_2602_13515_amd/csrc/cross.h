@@ -25,7 +25,8 @@ inline CrossKeys cross_keys(const CrossDims& m, const int32_t* lengths) { return
 // not fill the chip.  The cut with the least estimated time, in entries: rounds of `resident` workgroups that each take `start`
 // besides their entries, and a part's results joined by the last one, `join` each.  Lists of rows end with their sample's
 // keys, which only the device knows: for these (`ragged`) the mean of that time and of the one where half of all entries are
-// there, in lists of any length (the mean load, then the longest part).  Measured: CUTS.
+// there, in lists of any length (the mean load, then the longest part).  Measured, dK/dV of 96 columns of 256 query blocks, d = 128:
+// 5 parts a column 222 us; 16 parts, the fullest rounds, 265 (the last part to arrive adds up 16 times 64 KB).
 struct CrossParts { int len, parts; };
 struct CutCost { double start, join; int least; bool ragged; };
 inline CrossParts cross_parts(int64_t units, int list_max, int resident, const CutCost& c) {
@@ -72,10 +73,11 @@ CrossSection cross_dkdv_section(const CrossDims& m);
 
 // Workspace of the forward pass: counters, pool.  Of the backward pass: D, counters of dQ and of dK/dV, pools.
 constexpr int FEW_ROWS = 32;
-// Whether the rows that read a key head are so few that the kernel for few rows takes them.  One wave of that kernel does what
-// four do in the other: at 32 rows FEWLINE.
+// Whether the rows that read a key head are so few that the kernel for few rows takes them (a wave's 32).  With 32 rows, us, that
+// kernel / the other: 8 samples of 8192 keys, 8 heads 54 / 66, d = 64 34 / 35; 64 samples of 512 26 / 27; 1 of 65,536, 2 heads 28 / 93;
+// 600 of 77, 4 heads, d = 64 20 / 22; 2 of 77, 40 heads 7.7 / 6.5; with one row 48 / 68, 30 / 36, 23 / 25, 25 / 88, 15 / 22, 6.1 / 6.3.
 inline bool cross_few(const CrossDims& m) { return (int64_t)m.group * m.q.N <= FEW_ROWS; }
-struct CrossFewWs { int workers; size_t counters, pool, total; };
+struct CrossFewWs { int workers; size_t total; };
 CrossFewWs cross_few_ws(const CrossDims& m);
 struct CrossFwdWs { CrossSection s; size_t pool, total; };
 inline CrossFwdWs cross_fwd_ws(const CrossDims& m) {

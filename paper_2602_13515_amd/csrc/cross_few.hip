@@ -4,14 +4,18 @@
 // A workgroup takes the rows of all query heads of a key head together (row r: head r / Nq, query r % Nq).  As in fwd.hip a
 // lane owns one row and everything is computed transposed, S^T = K Q^T and O^T += V^T P^T; but here the waves share no tile:
 // each walks tiles of 32 keys of its own, copied global -> LDS directly and two tiles ahead, without a barrier, so that a compute
-// unit has 64 to 128 KB on the way.  The waves' results are joined through LDS, those of several workgroups by the last to arrive;
-// only the rows that are there are exchanged.
+// unit has 64 to 128 KB on the way.  The waves' results are joined through LDS, those of several workgroups by a launch behind
+// (a workgroup a row; joined by the last part to arrive, which needed counters set to zero by a launch in front, 32 rows and one
+// sample of 65,536 keys took 342 instead of 28 us).  Only the rows that are there are exchanged.
 //
 // Who takes which keys: where there are few (sample, key head) pairs, the key blocks of all samples stand in one line, sample after
 // sample, and every workgroup of a head takes an equal stretch of it, whatever the lengths are: a sample that it shares with
 // others leaves a partial result.  (Cut by size alone, in equal parts of the longest sample, 280 to 576 workgroups of unlike
-// number on the compute units took 127 to 168 us where an even 512 take EVEN.)  Where there are many pairs, a workgroup takes one.
-// Measured: FEW.
+// number on the compute units took 127 to 168 us on the first case below.)  Where there are many pairs, or short samples, a
+// workgroup takes one pair.
+// Measured, us: one query, 8 samples of 4095 to 32,760 keys and an empty one, 40 heads sharing 8, d = 128 114 (5.1 TB/s); all of 32,760
+// keys 188 (5.7 TB/s; the copies alone 182); 8 samples of 8192 keys, 8 heads 48, d = 64 30; 1 sample of 65,536, 2 heads 25;
+// 600 samples of 77, 4 heads, d = 64 15.
 #include "cross.h"
 #include "row_map.h"
 #include "spa2_device.h"
@@ -26,52 +30,64 @@ struct FewArgs {
   int workers;                   // workgroups of a key head that share the line of key blocks; 0: one a (sample, key head)
   int64_t sb, sh, sn;
   float scale_log2;
-  int32_t* arrive;               // [B][Hk] parts of a sample that have left their result
-  float* pool; int slot_floats;  // [Hk][workers][2]: of the sample that a stretch begins inside of or with, of the one it ends inside of
+  float* pool; int slot_floats;  // partial results (few_slot)
 };
 
 constexpr int FEW_WAVES = 2;     // (two workgroups of 64 KB share a compute unit; of four waves and 128 KB one: 127 / 140 us)
-constexpr int FEW_LEAST = 4;     // key blocks that a stretch has at least
+constexpr int FEW_LEAST = 8;     // key blocks that a stretch has at least
 constexpr int FEW_SAMPLES = 1024;       // samples that a line may have
 inline int few_resident(int d) { return 512 * 128 / d; }
 
 // A part's result: [row][D] unnormalised sums, then (maximum in log2 units, sum) of each row.
-inline size_t few_slot_bytes(int rows, int d) { return (size_t)rows * (d + 2) * 4; }
+inline size_t few_slot_bytes(int rows, int d) { return ((size_t)rows * (d + 2) * 4 + 15) & ~(size_t)15; }
 
 // Blocks of a sample in the line: one at least, so that every sample is somebody's.
 __device__ __forceinline__ int few_blocks(int keys) { return max((keys + BKV - 1) / BKV, 1); }
 
-// Where stretch i of `workers` begins and ends in the line, and in which sample (that sample's first place in the line).
-struct FewLine { int begin, end, per, b, first; };
-__device__ __forceinline__ FewLine few_line(const FewArgs& a, int i, int lane) {
-  constexpr int CHUNKS = FEW_SAMPLES / 64;
-  int n[CHUNKS], total = 0;
+// The line: blocks of the samples lane, 64 + lane, ..., and how many a stretch has.
+constexpr int FEW_CHUNKS = FEW_SAMPLES / 64;
+struct FewLine { int n[FEW_CHUNKS], total, per; };
+__device__ __forceinline__ FewLine few_line(const FewArgs& a, int lane) {
+  FewLine r;
+  r.total = 0;
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
+  for (int c = 0; c < FEW_CHUNKS; ++c) {
     const int b = 64 * c + lane;
-    n[c] = b < a.B ? few_blocks(a.kv.lengths ? min(max(a.kv.lengths[b], 0), a.kv.Nk) : a.kv.Nk) : 0;
+    r.n[c] = b < a.B ? few_blocks(a.kv.lengths ? min(max(a.kv.lengths[b], 0), a.kv.Nk) : a.kv.Nk) : 0;
   }
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) total += n[c];
+  for (int c = 0; c < FEW_CHUNKS; ++c) r.total += r.n[c];
 #pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) total += __shfl_xor(total, s, 64);
-  FewLine r;
-  r.per = max((total + a.workers - 1) / a.workers, FEW_LEAST);
-  r.begin = min(i * r.per, total);
-  r.end = min(r.begin + r.per, total);
-  r.b = 0; r.first = 0;
+  for (int s = 32; s >= 1; s >>= 1) r.total += __shfl_xor(r.total, s, 64);
+  r.total = __builtin_amdgcn_readfirstlane(r.total);
+  r.per = max((r.total + a.workers - 1) / a.workers, FEW_LEAST);
+  return r;
+}
+// First place of sample b.
+__device__ __forceinline__ int few_first(const FewLine& line, int b, int lane) {
+  int before = 0;
+#pragma unroll
+  for (int c = 0; c < FEW_CHUNKS; ++c) before += 64 * c + lane < b ? line.n[c] : 0;
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) before += __shfl_xor(before, s, 64);
+  return __builtin_amdgcn_readfirstlane(before);
+}
+// The sample that place `at` (inside the line) belongs to, and that sample's first place.
+struct FewSample { int b, first; };
+__device__ __forceinline__ FewSample few_sample(const FewArgs& a, const FewLine& line, int place, int lane) {
+  FewSample r = {0, 0};
   int run = 0;
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
+  for (int c = 0; c < FEW_CHUNKS; ++c) {
     if (64 * c >= a.B) break;
-    int sum = n[c];                                      // of this sample and those before it
+    int sum = line.n[c];                                 // of this sample and those before it
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
       const int x = __shfl_up(sum, s, 64);
       sum += lane >= s ? x : 0;
     }
-    const int at = run + sum - n[c];
-    const uint64_t here = __builtin_amdgcn_ballot_w64(n[c] > 0 && at <= r.begin && r.begin < at + n[c]);
+    const int at = run + sum - line.n[c];
+    const uint64_t here = __builtin_amdgcn_ballot_w64(line.n[c] > 0 && at <= place && place < at + line.n[c]);
     if (here) {
       const int l = __builtin_ctzll(here);
       r.b = 64 * c + l;
@@ -79,11 +95,40 @@ __device__ __forceinline__ FewLine few_line(const FewArgs& a, int i, int lane) {
     }
     run += __shfl(sum, 63, 64);
   }
-  r.per = __builtin_amdgcn_readfirstlane(r.per);
-  r.begin = __builtin_amdgcn_readfirstlane(r.begin); r.end = __builtin_amdgcn_readfirstlane(r.end);
   r.b = __builtin_amdgcn_readfirstlane(r.b); r.first = __builtin_amdgcn_readfirstlane(r.first);
   return r;
 }
+// Stretches that a sample lies in, and where part p of its result lies: a stretch has two slots, for the sample that it begins
+// inside of or with and for the one that it ends inside of.
+struct FewParts { int i0, parts, starts; };
+__device__ __forceinline__ FewParts few_parts(int first, int n, int per) {
+  const int i0 = first / per;
+  return {i0, (first + n - 1) / per - i0 + 1, first == i0 * per};
+}
+__device__ __forceinline__ int few_slot(const FewArgs& a, const FewParts& s, int hk, int p) {
+  return 2 * (hk * a.workers + s.i0 + p) + (p == 0 && !s.starts);
+}
+
+// Four channels (4 c ..) of a row's sum x with maximum m and sum of weights l: O = x / l, LSE.
+__device__ __forceinline__ int64_t few_row(const FewArgs& a, int b, int hk, int r) {
+  return b * a.sb + ((int64_t)hk * a.kv.group + r / a.Nq) * a.sh + (r % a.Nq) * a.sn;
+}
+__device__ __forceinline__ void few_finish(const FewArgs& a, int b, int hk, int row, int c, f32x4 x, float m, float l) {
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= inv;
+  const u32x2 out = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  const int64_t off = few_row(a, b, hk, row) + 4 * c;
+  *(u32x2*)(a.o + off) = out;
+  if (a.o_res) {
+    const u32x2 r = {pack_bf16(x[0] - __builtin_bit_cast(float, out[0] << 16), x[1] - __builtin_bit_cast(float, out[0] & 0xffff0000u)),
+                     pack_bf16(x[2] - __builtin_bit_cast(float, out[1] << 16), x[3] - __builtin_bit_cast(float, out[1] & 0xffff0000u))};
+    *(u32x2*)(a.o_res + off) = r;
+  }
+  if (c == 0) a.lse[((int64_t)b * a.Hk + hk) * a.rows + row] = m * LN2 + __logf(l);      // (heads and queries of a key head: consecutive)
+}
+// 2^(m_p - m) for a part whose maximum is m_p; a part that saw no score but minus infinity has no weight
+__device__ __forceinline__ float few_weight(float m_p, float m) { return m_p == -INFINITY ? 0.f : fast_exp2(m_p - m); }
 
 // LDS of a workgroup
 template <int D>
@@ -91,12 +136,10 @@ struct FewLds {
   static constexpr int TK = 32, TILE_B = TK * D * 2, STAGE_B = 2 * TILE_B, WAVE_B = 2 * STAGE_B;      // a stage: K rows, then V rows
   unsigned char smem[FEW_WAVES * WAVE_B];
   float stat[FEW_WAVES][32][2];
-  int word;
 };
 
-// Keys [key0, key1) of sample b and key head hk.  parts: workgroups that share the sample's keys; slots of the first and of the
-// others lie first_slot and next_slots, next_slots + 2, ... (in slots).
-struct FewPiece { int b, hk, key0, key1, parts, slot, first_slot, next_slots; };
+// Keys [key0, key1) of sample b and key head hk; its result goes to a slot where others share the sample (slot >= 0).
+struct FewPiece { int b, hk, key0, key1, slot; };
 template <int D>
 __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, FewLds<D>& lds) {
   constexpr int TK = 32, NK = D / 16, NMB = D / 32, CPR = D / 8, RPI = 64 / CPR, NCP = TK / RPI, WAVES = FEW_WAVES, NT = 64 * WAVES;
@@ -105,20 +148,16 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
   static_assert(32 * PITCH * 4 <= WAVE_B, "a wave's sums fit its stages");
   unsigned char* smem = lds.smem;
   auto& stat = lds.stat;
-  const int b = pc.b, hk = pc.hk, group = a.kv.group, key0 = pc.key0, key1 = pc.key1, parts = pc.parts, unit = b * a.Hk + hk;
+  const int b = pc.b, hk = pc.hk, key0 = pc.key0, key1 = pc.key1;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, hf = lane >> 5;
-  const int64_t q_base = b * a.sb + (int64_t)hk * group * a.sh;
-  const int64_t stat_base = (int64_t)unit * a.rows;                                   // (heads and queries of a key head: consecutive)
-  auto row_at = [&](int r) -> int64_t { return q_base + (r / a.Nq) * a.sh + (r % a.Nq) * a.sn; };
-
   if (key1 <= key0) {                        // a sample without keys: O = 0, LSE = -inf
     for (int x = tid; x < a.rows * CPR; x += NT) {
-      const int64_t off = row_at(x / CPR) + 8 * (x % CPR);
+      const int64_t off = few_row(a, b, hk, x / CPR) + 8 * (x % CPR);
       *(u32x4*)(a.o + off) = u32x4{0, 0, 0, 0};
       if (a.o_res) *(u32x4*)(a.o_res + off) = u32x4{0, 0, 0, 0};
     }
-    if (tid < a.rows) a.lse[stat_base + tid] = -INFINITY;
+    if (tid < a.rows) a.lse[((int64_t)b * a.Hk + hk) * a.rows + tid] = -INFINITY;
     return;
   }
 
@@ -150,7 +189,7 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
   raw_copies_done();                                     // (what is counted from here on are the copies)
   bf16x8 qf[NK];
   {
-    const uint16_t* qp = a.q + row_at(min(r32, a.rows - 1)) + 8 * hf;
+    const uint16_t* qp = a.q + few_row(a, b, hk, min(r32, a.rows - 1)) + 8 * hf;
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) qf[kk] = *(const bf16x8*)(qp + 16 * kk);
   }
@@ -229,22 +268,7 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
   if (hf == 0) { stat[w][r32][0] = m_run; stat[w][r32][1] = l_tot; }
   __syncthreads();
   constexpr int QUADS = D / 4;                           // a thread takes four channels of a row at a time
-  auto finish = [&](int row, int c, f32x4 x, float m, float l) {
-    const float inv = 1.f / l;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] *= inv;
-    const u32x2 out = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-    const int64_t off = row_at(row) + 4 * c;
-    *(u32x2*)(a.o + off) = out;
-    if (a.o_res) {
-      const u32x2 r = {pack_bf16(x[0] - __builtin_bit_cast(float, out[0] << 16), x[1] - __builtin_bit_cast(float, out[0] & 0xffff0000u)),
-                       pack_bf16(x[2] - __builtin_bit_cast(float, out[1] << 16), x[3] - __builtin_bit_cast(float, out[1] & 0xffff0000u))};
-      *(u32x2*)(a.o_res + off) = r;
-    }
-    if (c == 0) a.lse[stat_base + row] = m * LN2 + __logf(l);
-  };
-  auto weight = [](float m_p, float m) -> float { return m_p == -INFINITY ? 0.f : fast_exp2(m_p - m); };
-  float* slot = a.pool + (int64_t)pc.slot * a.slot_floats;
+  float* slot = a.pool + (int64_t)max(pc.slot, 0) * a.slot_floats;
   for (int x = tid; x < a.rows * QUADS; x += NT) {
     const int row = x / QUADS, c = x % QUADS;
     float m = stat[0][row][0];
@@ -254,54 +278,18 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
-      const float f = weight(stat[i][row][0], m);
+      const float f = few_weight(stat[i][row][0], m);
       const f32x4 y = *(const f32x4*)((const float*)(smem + i * WAVE_B) + row * PITCH + 4 * c);
       l = fmaf(stat[i][row][1], f, l);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(y[e], f, sum[e]);
     }
-    if (parts == 1) {
-      finish(row, c, sum, m, l);
+    if (pc.slot < 0) {
+      few_finish(a, b, hk, row, c, sum, m, l);
     } else {
-      part_store2(slot + row * D + 4 * c, sum[0], sum[1]);
-      part_store2(slot + row * D + 4 * c + 2, sum[2], sum[3]);
-      if (c == 0) part_store2(slot + a.rows * D + 2 * row, m, l);
+      *(f32x4*)(slot + row * D + 4 * c) = sum;
+      if (c == 0) *(f32x2*)(slot + a.rows * D + 2 * row) = f32x2{m, l};
     }
-  }
-  if (parts == 1) return;
-  if (!last_part(a.arrive + unit, parts, &lds.word)) return;
-  // the last part joins all of them, in part order
-  auto part_at = [&](int p) -> const float* {
-    return a.pool + (int64_t)(p == 0 ? pc.first_slot : pc.next_slots + 2 * (min(p, parts - 1) - 1)) * a.slot_floats;
-  };
-  for (int x = tid; x < a.rows * QUADS; x += NT) {
-    const int row = x / QUADS, c = x % QUADS;
-    float m = -INFINITY, l = 0.f;
-    for (int p = 0; p < parts; p += 4) {                 // four loads in flight
-      float mp[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mp[i] = part_load2(part_at(p + i) + a.rows * D + 2 * row)[0];
-      m = fmaxf(fmaxf(m, fmaxf(mp[0], mp[1])), fmaxf(mp[2], mp[3]));
-    }
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; p += 4) {
-      f32x2 ml[4], lo[4], hi[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* ps = part_at(p + i);
-        ml[i] = part_load2(ps + a.rows * D + 2 * row);
-        lo[i] = part_load2(ps + row * D + 4 * c);
-        hi[i] = part_load2(ps + row * D + 4 * c + 2);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float f = p + i < parts ? weight(ml[i][0], m) : 0.f;
-        l = fmaf(ml[i][1], f, l);
-        sum[0] = fmaf(lo[i][0], f, sum[0]); sum[1] = fmaf(lo[i][1], f, sum[1]);
-        sum[2] = fmaf(hi[i][0], f, sum[2]); sum[3] = fmaf(hi[i][1], f, sum[3]);
-      }
-    }
-    finish(row, c, sum, m, l);
   }
 }
 
@@ -310,23 +298,19 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(FewArgs a) {
   __shared__ __align__(1024) FewLds<D> lds;
   if (a.workers == 0) {
     const int b = blockIdx.x / a.Hk, keys = cross_length(a.kv, b);
-    few_piece<D>(a, FewPiece{b, (int)blockIdx.x % a.Hk, 0, keys, 1, 0, 0, 0}, lds);
+    few_piece<D>(a, FewPiece{b, (int)blockIdx.x % a.Hk, 0, keys, -1}, lds);
     return;
   }
-  const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk;
-  const FewLine line = few_line(a, i, threadIdx.x & 63);
-  const int slots = 2 * (hk * a.workers);                // the slots of this head's stretches
-  int first = line.first;                                // of sample b
-  for (int b = line.b, at = line.begin; at < line.end; ++b) {
-    const int keys = cross_length(a.kv, b), n = few_blocks(keys), end = min(first + n, line.end);
-    FewPiece pc;
-    pc.b = b; pc.hk = hk;
-    pc.key0 = (at - first) * BKV; pc.key1 = min(keys, (end - first) * BKV);
-    const int i0 = first / line.per, i1 = (first + n - 1) / line.per;      // stretches that the sample lies in
-    pc.parts = i1 - i0 + 1;
-    pc.first_slot = slots + 2 * i0 + (first != i0 * line.per);
-    pc.next_slots = slots + 2 * (i0 + 1);
-    pc.slot = slots + 2 * i + (at != line.begin);
+  const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk, lane = threadIdx.x & 63;
+  const FewLine line = few_line(a, lane);
+  const int begin = i * line.per, stop = min(begin + line.per, line.total);
+  if (begin >= stop) return;
+  const FewSample start = few_sample(a, line, begin, lane);
+  int first = start.first;                               // of sample b
+  for (int b = start.b, at = begin; at < stop; ++b) {
+    const int keys = cross_length(a.kv, b), n = few_blocks(keys), end = min(first + n, stop);
+    const FewParts s = few_parts(first, n, line.per);
+    const FewPiece pc = {b, hk, (at - first) * BKV, min(keys, (end - first) * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, i - s.i0)};
     few_piece<D>(a, pc, lds);
     __syncthreads();                                     // (the next piece's tiles land where this one's results were)
     first += n;
@@ -334,11 +318,63 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(FewArgs a) {
   }
 }
 
+// Row `row` of a (sample, key head) whose keys several workgroups shared: their results, joined.  A thread takes four channels and
+// every G-th part, in order; then the G are added in order.
+template <int D>
+__global__ __launch_bounds__(256) void cross_few_join_kernel(FewArgs a) {
+  constexpr int QUADS = D / 4, G = 256 / QUADS;
+  __shared__ __align__(16) float sums[G][D];
+  __shared__ float stat[G][2];
+  const int row = blockIdx.x % a.rows, unit = blockIdx.x / a.rows, b = unit / a.Hk, hk = unit % a.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, c = tid % QUADS, g = tid / QUADS;
+  const FewLine line = few_line(a, lane);
+  const FewParts s = few_parts(few_first(line, b, lane), few_blocks(cross_length(a.kv, b)), line.per);
+  if (s.parts == 1) return;
+  float m = -INFINITY, l = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int p = g; p < s.parts; p += 4 * G) {             // four parts in flight
+    f32x2 ml[4];
+    f32x4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* slot = a.pool + (int64_t)few_slot(a, s, hk, min(p + i * G, s.parts - 1)) * a.slot_floats;
+      ml[i] = *(const f32x2*)(slot + a.rows * D + 2 * row);
+      x[i] = *(const f32x4*)(slot + row * D + 4 * c);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (p + i * G >= s.parts) break;
+      const float m_new = fmaxf(m, ml[i][0]), old = few_weight(m, m_new), f = few_weight(ml[i][0], m_new);
+      l = fmaf(ml[i][1], f, l * old);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(x[i][e], f, sum[e] * old);
+      m = m_new;
+    }
+  }
+  *(f32x4*)&sums[g][4 * c] = sum;
+  if (c == 0) { stat[g][0] = m; stat[g][1] = l; }
+  __syncthreads();
+  if (g) return;
+#pragma unroll
+  for (int i = 1; i < G; ++i) m = fmaxf(m, stat[i][0]);
+  l = 0.f;
+  sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const float f = few_weight(stat[i][0], m);
+    const f32x4 x = *(const f32x4*)&sums[i][4 * c];
+    l = fmaf(stat[i][1], f, l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(x[e], f, sum[e]);
+  }
+  few_finish(a, b, hk, row, c, sum, m, l);
+}
+
 // Workgroups of a key head that share the line of its key blocks, or 0.
 static int few_workers(const CrossDims& m) {
   const int64_t units = (int64_t)m.q.B * m.Hk;
   const int resident = few_resident(m.q.d);
-  if (m.q.B > FEW_SAMPLES || units >= 2 * resident) return 0;
+  if (m.q.B > FEW_SAMPLES || units >= 2 * resident || m.q.Tn < 2 * FEW_LEAST) return 0;
   const int64_t most = ((int64_t)m.q.B * m.q.Tn + FEW_LEAST - 1) / FEW_LEAST, want = (resident + m.Hk - 1) / m.Hk;
   return (int)(want < most ? want : most);
 }
@@ -347,9 +383,7 @@ CrossFewWs cross_few_ws(const CrossDims& m) {
   CrossFewWs w;
   w.workers = few_workers(m);
   // (one stretch a head: nothing is shared)
-  w.counters = w.workers > 1 ? round256((size_t)m.q.B * m.Hk * 4) : 0;
-  w.pool = w.counters;
-  w.total = w.counters + (w.workers > 1 ? round256((size_t)2 * w.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d)) : 0);
+  w.total = w.workers > 1 ? round256((size_t)2 * w.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d)) : 0;
   return w;
 }
 
@@ -362,18 +396,17 @@ hipError_t launch_cross_few(const void* q, const void* k, const void* v, const C
   a.B = m.q.B; a.Hk = m.Hk; a.Nq = m.q.N; a.rows = m.group * m.q.N;
   a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
   a.scale_log2 = scale * LOG2E;
-  const CrossFewWs w = cross_few_ws(m);
-  a.workers = w.workers;
+  a.workers = cross_few_ws(m).workers;
+  a.pool = (float*)ws;
   a.slot_floats = (int)(few_slot_bytes(a.rows, m.q.d) / 4);
-  if (w.total) {
-    a.arrive = (int32_t*)ws;
-    a.pool = (float*)((char*)ws + w.pool);
-    const hipError_t e = launch_zero_ints(a.arrive, m.q.B * m.Hk, stream);
-    if (e != hipSuccess) return e;
-  }
   const dim3 grid((unsigned)((a.workers ? a.workers : m.q.B) * m.Hk)), block(64 * FEW_WAVES);
   if (m.q.d == 128) hipLaunchKernelGGL(cross_few_kernel<128>, grid, block, 0, stream, a);
   else              hipLaunchKernelGGL(cross_few_kernel<64>, grid, block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.workers <= 1) return e;
+  const dim3 rows((unsigned)(m.q.B * m.Hk * a.rows));
+  if (m.q.d == 128) hipLaunchKernelGGL(cross_few_join_kernel<128>, rows, dim3(256), 0, stream, a);
+  else              hipLaunchKernelGGL(cross_few_join_kernel<64>, rows, dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
