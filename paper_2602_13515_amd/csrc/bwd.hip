@@ -447,10 +447,6 @@ hipError_t launch_bwd_dq_columns(const void* q, const void* k, const void* v, co
 }
 
 // ------------------------------------------------------------------ attention to another sequence
-CrossSection cross_dq_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, dq_slot_bytes(m.q));
-}
-
 hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
                            const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, void* dq,
                            int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {

@@ -822,11 +822,6 @@ void cross_dkdv_kernel(CrossDkvArgs) {
   else                    dkdv_item64(a, item, walk, smem, stat_s);
 }
 
-CrossSection cross_dkdv_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.Hk * m.q.Tn, m.group * m.q.Tm, dkdv_resident(m.q), CutCost{1.3, 0.4, 4, false},
-                       dkdv_slot_bytes(m.q));
-}
-
 hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
                              const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
                              hipStream_t stream) {

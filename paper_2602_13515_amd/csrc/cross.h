@@ -67,9 +67,17 @@ inline SplitPlan cross_plan(const CrossSection& s, void* counters, void* pool, s
   return p;
 }
 
-CrossSection cross_fwd_section(const CrossDims& m);
-CrossSection cross_dq_section(const CrossDims& m);
-CrossSection cross_dkdv_section(const CrossDims& m);
+// (start and join in key blocks of 128 rows, or query blocks of 64 keys)
+inline CrossSection cross_fwd_section(const CrossDims& m) {
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, fwd_slot_bytes(m.q));
+}
+inline CrossSection cross_dq_section(const CrossDims& m) {
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, dq_slot_bytes(m.q));
+}
+inline CrossSection cross_dkdv_section(const CrossDims& m) {
+  return cross_section((int64_t)m.q.B * m.Hk * m.q.Tn, m.group * m.q.Tm, dkdv_resident(m.q), CutCost{1.3, 0.4, 4, false},
+                       dkdv_slot_bytes(m.q));
+}
 
 // Workspace of the forward pass: counters, pool.  Of the backward pass: D, counters of dQ and of dK/dV, pools.
 constexpr int FEW_ROWS = 32;
@@ -77,8 +85,22 @@ constexpr int FEW_ROWS = 32;
 // kernel / the other: 8 samples of 8192 keys, 8 heads 54 / 66, d = 64 34 / 35; 64 samples of 512 26 / 27; 1 of 65,536, 2 heads 28 / 93;
 // 600 of 77, 4 heads, d = 64 20 / 22; 2 of 77, 40 heads 7.7 / 6.5; with one row 48 / 68, 30 / 36, 23 / 25, 25 / 88, 15 / 22, 6.1 / 6.3.
 inline bool cross_few(const CrossDims& m) { return (int64_t)m.group * m.q.N <= FEW_ROWS; }
+// The kernel for few rows: workgroups of a key head that share the line of its key blocks (cross_few.hip), or 0; a part's result:
+// [row][D] unnormalised sums, then (maximum in log2 units, sum) of each row.
+constexpr int FEW_LEAST = 8;            // key blocks that a stretch of the line has at least
+constexpr int FEW_SAMPLES = 1024;       // samples that a line may have
+inline size_t few_slot_bytes(int rows, int d) { return ((size_t)rows * (d + 2) * 4 + 15) & ~(size_t)15; }
 struct CrossFewWs { int workers; size_t total; };
-CrossFewWs cross_few_ws(const CrossDims& m);
+inline CrossFewWs cross_few_ws(const CrossDims& m) {
+  CrossFewWs w = {0, 0};
+  const int64_t units = (int64_t)m.q.B * m.Hk, resident = 512 * 128 / m.q.d;        // (workgroups that run at a time)
+  if (m.q.B > FEW_SAMPLES || units >= 2 * resident || m.q.Tn < 2 * FEW_LEAST) return w;
+  const int64_t most = ((int64_t)m.q.B * m.q.Tn + FEW_LEAST - 1) / FEW_LEAST, want = (resident + m.Hk - 1) / m.Hk;
+  w.workers = (int)(want < most ? want : most);
+  // (one stretch a head: nothing is shared)
+  if (w.workers > 1) w.total = round256((size_t)2 * w.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d));
+  return w;
+}
 struct CrossFwdWs { CrossSection s; size_t pool, total; };
 inline CrossFwdWs cross_fwd_ws(const CrossDims& m) {
   CrossFwdWs w;

@@ -34,13 +34,6 @@ struct FewArgs {
 };
 
 constexpr int FEW_WAVES = 2;     // (two workgroups of 64 KB share a compute unit; of four waves and 128 KB one: 127 / 140 us)
-constexpr int FEW_LEAST = 8;     // key blocks that a stretch has at least
-constexpr int FEW_SAMPLES = 1024;       // samples that a line may have
-inline int few_resident(int d) { return 512 * 128 / d; }
-
-// A part's result: [row][D] unnormalised sums, then (maximum in log2 units, sum) of each row.
-inline size_t few_slot_bytes(int rows, int d) { return ((size_t)rows * (d + 2) * 4 + 15) & ~(size_t)15; }
-
 // Blocks of a sample in the line: one at least, so that every sample is somebody's.
 __device__ __forceinline__ int few_blocks(int keys) { return max((keys + BKV - 1) / BKV, 1); }
 
@@ -368,23 +361,6 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(FewArgs a) {
     for (int e = 0; e < 4; ++e) sum[e] = fmaf(x[e], f, sum[e]);
   }
   few_finish(a, b, hk, row, c, sum, m, l);
-}
-
-// Workgroups of a key head that share the line of its key blocks, or 0.
-static int few_workers(const CrossDims& m) {
-  const int64_t units = (int64_t)m.q.B * m.Hk;
-  const int resident = few_resident(m.q.d);
-  if (m.q.B > FEW_SAMPLES || units >= 2 * resident || m.q.Tn < 2 * FEW_LEAST) return 0;
-  const int64_t most = ((int64_t)m.q.B * m.q.Tn + FEW_LEAST - 1) / FEW_LEAST, want = (resident + m.Hk - 1) / m.Hk;
-  return (int)(want < most ? want : most);
-}
-
-CrossFewWs cross_few_ws(const CrossDims& m) {
-  CrossFewWs w;
-  w.workers = few_workers(m);
-  // (one stretch a head: nothing is shared)
-  w.total = w.workers > 1 ? round256((size_t)2 * w.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d)) : 0;
-  return w;
 }
 
 hipError_t launch_cross_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,

@@ -522,10 +522,6 @@ hipError_t launch_fwd(const void* q, const void* k, const void* v, const Dims& m
 }
 
 // ------------------------------------------------------------------ attention to another sequence
-CrossSection cross_fwd_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, fwd_slot_bytes(m.q));
-}
-
 __global__ __launch_bounds__(256) void zero_ints_kernel(int32_t* p, int n) {
   const int x = blockIdx.x * 256 + threadIdx.x;
   if (x < n) p[x] = 0;

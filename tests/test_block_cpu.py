@@ -187,3 +187,47 @@ def test_attention_gradient_formula_against_differences():
         diff = (f(*(x + h * y for x, y in zip((q, k, v), w))) - f(*(x - h * y for x, y in zip((q, k, v), w)))) / (2 * h)
         terms = [(g[n][0] * y) for n, y in zip(("dq", "dk", "dv"), w)]
         assert abs(diff - sum(t.sum() for t in terms)) <= 1e-7 * sum(np.abs(t).sum() for t in terms)
+
+
+def test_argument_checks_under_host_sanitizers():
+    """csrc/block_api.hip with AddressSanitizer and UndefinedBehaviorSanitizer on the host side, launchers that abort, driven by
+    tests/abi_sanitize/block_driver.c."""
+    import os
+    import shutil
+    import subprocess
+    import tempfile
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    hipcc, clang = shutil.which("hipcc") or "/opt/rocm/bin/hipcc", "/opt/rocm/lib/llvm/bin/clang"
+    if not (os.path.exists(hipcc) and os.path.exists(clang)):
+        pytest.skip("no ROCm toolchain")
+    csrc, here = os.path.join(root, "paper_2602_13515_amd", "csrc"), os.path.join(root, "tests", "abi_sanitize")
+    inc = ["-I", os.path.join(root, "include"), "-I", csrc]
+    san = ["-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined"]
+    host = ["--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-Wno-unused-command-line-argument",
+            *(x for s in san for x in ("-Xarch_host", s))]
+    with tempfile.TemporaryDirectory() as td:
+        o = lambda n: os.path.join(td, n)
+        for cmd in ([clang, "-std=c99", "-g", "-c", *san, *inc, os.path.join(here, "block_driver.c"), "-o", o("driver.o")],
+                    [hipcc, *host, *inc, "-c", os.path.join(csrc, "block_api.hip"), "-o", o("api.o")],
+                    [hipcc, *host, *inc, "-x", "hip", "-c", os.path.join(here, "block_stubs.cpp"), "-o", o("stubs.o")],
+                    [hipcc, "--offload-arch=gfx950", "-fsanitize=address", "-fsanitize=undefined", "-fno-gpu-sanitize",
+                     o("api.o"), o("stubs.o"), o("driver.o"), "-o", o("check")]):
+            r = subprocess.run(cmd, capture_output=True, text=True)
+            assert r.returncode == 0, r.stderr[-3000:]
+        r = subprocess.run([o("check")], capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0 and "all rejected before launch" in r.stdout, (r.stdout[-2000:], r.stderr[-3000:])
+        assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr, r.stderr[-3000:]
+
+
+@pytest.mark.parametrize("units,list_max", [(1, 1), (1, 4096), (2, 1024), (64, 512), (300, 7), (512, 40), (513, 100), (2049, 100)])
+def test_workspaces_hold_what_the_kernels_use(units, list_max):
+    """Sizes grow with the parts and never exceed what 2048 parts need; small ones are no larger than D and counters."""
+    lib, d = binding._load(), 128
+    s = binding._CrossShape(units, 1, 1, 128, 64 * list_max, d, 128 * d, 128 * d, d, 64 * list_max * d, 64 * list_max * d, d,
+                            64 * list_max * d, 64 * list_max * d, d)
+    slot = (256 * d // 2 + 512) * 4
+    fwd, bwd = lib.spa2_cross_fwd_workspace_bytes(ctypes.byref(s)), lib.spa2_cross_bwd_workspace_bytes(ctypes.byref(s))
+    assert fwd <= 2048 * (slot + 4) + 512 and bwd >= units * 128 * 4
+    assert bwd <= units * 128 * 4 + 2 * (2048 * (slot + 4) + 512) + 512
+    if units > 2048:
+        assert fwd == 0
