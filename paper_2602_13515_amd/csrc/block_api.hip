@@ -141,8 +141,7 @@ int spa2_cross_bwd(const void* q, const void* k, const void* v, const int32_t* l
   float* delta = (float*)ws;
   hipStream_t st = (hipStream_t)stream;
   const SplitPlan cols = cross_plan(w.dkdv, ws + w.dkdv_counters, ws + w.dkdv_pool, dkdv_slot_bytes(m.q));
-  const SplitPlan rows = cross_plan(w.dq, ws + w.dq_counters, ws + w.dq_pool, dq_slot_bytes(m.q));
-  if (w.dq.slots && launch_zero_ints(rows.arrive, w.dq.slots, st) != hipSuccess) return SPA2_ERR_LAUNCH;
+  const SplitPlan rows = cross_plan(w.dq, nullptr, ws + w.dq_pool, dq_slot_bytes(m.q));
   if (launch_cross_dq(q, k, v, o, o_res, d_o, lse, m, lengths, scale, delta, dq, cols.arrive, w.dkdv.slots, rows, st) != hipSuccess)
     return SPA2_ERR_LAUNCH;
   return launch_cross_dkdv(q, k, v, d_o, lse, delta, m, lengths, scale, dk, dv, cols, st) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     keys = cross_length(a.kv, bh / a.H);
     const int all = (keys + BKV - 1) / BKV;
     part = blockIdx.x / rows;
-    parts = all > a.sp.fixed_len ? (all + a.sp.fixed_len - 1) / a.sp.fixed_len : 0;
+    parts = cross_parts_of(a, bh);
     if (part >= max(parts, 1)) return;
     if (parts) part_len = (all + parts - 1) / parts;
     slot = (bh * a.Tm + i) * a.sp.fixed_parts + part;
@@ -156,14 +156,15 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   const int r32 = lane & 31, hf = lane >> 5;
   const int N = a.N;
   const int64_t unit = (int64_t)bh * a.Tm + i;
-  const int first = part * part_len;         // entries [first, first + part_len) of the list of a split row
-  int cnt, split_at = 0;
+  int cnt, split_at = 0, first;              // entries [first, first + part_len) of the list of a split row
   const int32_t* idx = nullptr;
   if constexpr (CROSS) {
     cnt = (keys + BKV - 1) / BKV;
+    first = part * part_len;
   } else {
     cnt = min(max(a.row_cnt[unit], 0), a.Tn);   // clamped: see fwd.hip
     split_at = *(whole ? a.sp.unit_slot + unit : a.row_cnt + unit);
+    first = part * part_len;
     idx = a.row_idx + unit * a.Tn + first;
   }
   // the index list, 64 entries at a time in one register (lane l holds entry 64c + l): reading an entry is
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     }
   }
   const float lse2 = a.lse[(int64_t)bh * N + qrow_ld] * LOG2E;
-  float dlt;
+  float dlt = CROSS ? 0.f : a.delta[(int64_t)bh * N + qrow_ld];
   if constexpr (CROSS) {
     const int64_t off = base + (int64_t)qrow_ld * a.sn + 8 * hf;
     u32x4 of[D / 16], rf[D / 16];
@@ -191,7 +192,6 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     for (int kk = 0; kk < D / 16; ++kk) of[kk] = *(const u32x4*)(a.o + off + 16 * kk);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) rf[kk] = a.o_res ? *(const u32x4*)(a.o_res + off + 16 * kk) : u32x4{0, 0, 0, 0};
-    dlt = 0.f;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const u32x4 up = __builtin_bit_cast(u32x4, dof[kk]);
@@ -204,8 +204,6 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     }
     dlt = sum_halves(dlt);
     if (hf == 0 && qrow < N && part == 0) a.delta_out[(int64_t)bh * N + qrow] = dlt;
-  } else {
-    dlt = a.delta[(int64_t)bh * N + qrow_ld];
   }
   requested();
   if (whole && split_at >= 0) return;
@@ -377,6 +375,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     for (int mb = 0; mb < D / 32; ++mb)
 #pragma unroll
       for (int g = 0; g < 8; ++g) part_store2(ps + ((mb * 8 + g) * 256 + tid) * 2, acc[mb][2 * g], acc[mb][2 * g + 1]);
+    if constexpr (CROSS) return;             // (joined by a launch behind)
     if (!last_part(a.sp.arrive + first, parts, (int*)smem)) return;
 #pragma unroll
     for (int mb = 0; mb < D / 32; ++mb)
@@ -447,6 +446,44 @@ hipError_t launch_bwd_dq_columns(const void* q, const void* k, const void* v, co
 }
 
 // ------------------------------------------------------------------ attention to another sequence
+// The sums of a row's parts, added in part order (see cross_fwd_join_kernel).
+template <int D>
+__global__ __launch_bounds__(256) void cross_dq_join_kernel(CrossDqArgs a) {
+  constexpr int NMB = D / 32;
+  __shared__ float sums[4][16][64];
+  const int mb = blockIdx.x % NMB, w = blockIdx.x / NMB % 4, unit = blockIdx.x / (4 * NMB), bh = unit / a.Tm, i = unit % a.Tm;
+  const int parts = cross_parts_of(a, bh), lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  const int row = i * BQ + 32 * w + (lane & 31), hf = lane >> 5;
+  if (parts == 0 || i * BQ + 32 * w >= a.N) return;
+  const float* p0 = a.sp.pool + (int64_t)unit * a.sp.fixed_parts * a.sp.slot_floats + (mb * 8 * 256 + 64 * w + lane) * 2;
+  float x[16];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) x[v] = 0.f;
+  for (int p = g; p < parts; p += 16) {                  // four parts in flight
+    f32x2 y[4][8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) y[u][c] = *(const f32x2*)(p0 + (int64_t)min(p + 4 * u, parts - 1) * a.sp.slot_floats + c * 512);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (p + 4 * u >= parts) break;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] += y[u][v / 2][v % 2];
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v) sums[g][v][lane] = x[v];
+  __syncthreads();
+  if (g || row >= a.N) return;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) x[v] = ((sums[0][v][lane] + sums[1][v][lane]) + (sums[2][v][lane] + sums[3][v][lane])) * a.scale;
+  uint16_t* out = a.dq + (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh + (int64_t)row * a.sn + 32 * mb + 4 * hf;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)                            // channels 32 mb + 8 q + 4 hf ..
+    *(u32x2*)(out + 8 * q) = u32x2{pack_bf16(x[4 * q], x[4 * q + 1]), pack_bf16(x[4 * q + 2], x[4 * q + 3])};
+}
+
 hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
                            const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, void* dq,
                            int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
@@ -463,6 +500,11 @@ hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const vo
   const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tm))), block(256);
   if (m.q.d == 128) hipLaunchKernelGGL((dq_kernel<128, CrossDqArgs>), grid, block, 0, stream, a);
   else              hipLaunchKernelGGL((dq_kernel<64, CrossDqArgs>), grid, block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !plan.pool_slots) return e;
+  const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));
+  if (m.q.d == 128) hipLaunchKernelGGL(cross_dq_join_kernel<128>, joins, block, 0, stream, a);
+  else              hipLaunchKernelGGL(cross_dq_join_kernel<64>, joins, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -23,7 +23,7 @@ inline CrossKeys cross_keys(const CrossDims& m, const int32_t* lengths) { return
 
 // Every list of a launch has up to list_max entries; a unit's list is cut into parts of len entries where the units alone do
 // not fill the chip.  The cut with the least estimated time, in entries: rounds of `resident` workgroups that each take `start`
-// besides their entries, and a part's results joined by the last one, `join` each.  Lists of rows end with their sample's
+// besides their entries, and a part's results joined, `join` each.  Lists of rows end with their sample's
 // keys, which only the device knows: for these (`ragged`) the mean of that time and of the one where half of all entries are
 // there, in lists of any length (the mean load, then the longest part).  Measured, dK/dV of 96 columns of 256 query blocks, d = 128:
 // 5 parts a column 222 us; 16 parts, the fullest rounds, 265 (the last part to arrive adds up 16 times 64 KB).
@@ -44,7 +44,8 @@ inline CrossParts cross_parts(int64_t units, int list_max, int resident, const C
   return best;
 }
 
-// What a kernel needs of a workspace: arrival counters (zeroed before the launch) and partial results, one of each a part.
+// What a kernel needs of a workspace: a partial result for each part, and arrival counters (dK/dV: the last part of a column to
+// arrive adds up all of them; the counters are set to zero by the launch in front).
 struct CrossSection { CrossParts cut; int slots; size_t counters, pool; };
 inline CrossSection cross_section(int64_t units, int list_max, int resident, const CutCost& cost, size_t slot_bytes) {
   CrossSection s;
@@ -69,17 +70,17 @@ inline SplitPlan cross_plan(const CrossSection& s, void* counters, void* pool, s
 
 // (start and join in key blocks of 128 rows, or query blocks of 64 keys)
 inline CrossSection cross_fwd_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, fwd_slot_bytes(m.q));
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.03, 8, true}, fwd_slot_bytes(m.q));
 }
 inline CrossSection cross_dq_section(const CrossDims& m) {
-  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.5, 8, true}, dq_slot_bytes(m.q));
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, m.q.Tn, RESIDENT_WGS, CutCost{3.5, 0.03, 8, true}, dq_slot_bytes(m.q));
 }
 inline CrossSection cross_dkdv_section(const CrossDims& m) {
   return cross_section((int64_t)m.q.B * m.Hk * m.q.Tn, m.group * m.q.Tm, dkdv_resident(m.q), CutCost{1.3, 0.4, 4, false},
                        dkdv_slot_bytes(m.q));
 }
 
-// Workspace of the forward pass: counters, pool.  Of the backward pass: D, counters of dQ and of dK/dV, pools.
+// Workspace of the forward pass: the pool.  Of the backward pass: D, counters of dK/dV, pools.
 constexpr int FEW_ROWS = 32;
 // Whether the rows that read a key head are so few that the kernel for few rows takes them (a wave's 32).  With 32 rows, us, that
 // kernel / the other: 8 samples of 8192 keys, 8 heads 54 / 66, d = 64 34 / 35; 64 samples of 512 26 / 27; 1 of 65,536, 2 heads 28 / 93;
@@ -101,28 +102,25 @@ inline CrossFewWs cross_few_ws(const CrossDims& m) {
   if (w.workers > 1) w.total = round256((size_t)2 * w.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d));
   return w;
 }
-struct CrossFwdWs { CrossSection s; size_t pool, total; };
+struct CrossFwdWs { CrossSection s; size_t total; };
 inline CrossFwdWs cross_fwd_ws(const CrossDims& m) {
   CrossFwdWs w;
   w.s = cross_fwd_section(m);
-  w.pool = w.s.counters;
-  w.total = w.pool + w.s.pool;
+  w.total = w.s.pool;
   return w;
 }
-struct CrossBwdWs { CrossSection dkdv, dq; size_t dkdv_counters, dq_counters, dkdv_pool, dq_pool, total; };
+struct CrossBwdWs { CrossSection dkdv, dq; size_t dkdv_counters, dkdv_pool, dq_pool, total; };
 inline CrossBwdWs cross_bwd_ws(const CrossDims& m) {
   CrossBwdWs w;
   w.dkdv = cross_dkdv_section(m);
   w.dq = cross_dq_section(m);
   w.dkdv_counters = round256((size_t)m.q.B * m.q.H * m.q.N * sizeof(float));
-  w.dq_counters = w.dkdv_counters + w.dkdv.counters;
-  w.dkdv_pool = w.dq_counters + w.dq.counters;
+  w.dkdv_pool = w.dkdv_counters + w.dkdv.counters;
   w.dq_pool = w.dkdv_pool + w.dkdv.pool;
   w.total = w.dq_pool + w.dq.pool;
   return w;
 }
 
-hipError_t launch_zero_ints(int32_t* p, int n, hipStream_t stream);
 hipError_t launch_cross_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
                             void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
 hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
     keys = cross_length(a.kv, bh / a.H);
     const int all = (keys + BKV - 1) / BKV;
     part = blockIdx.x / rows;
-    parts = all > a.sp.fixed_len ? (all + a.sp.fixed_len - 1) / a.sp.fixed_len : 0;
+    parts = cross_parts_of(a, bh);
     if (part >= max(parts, 1)) return;
     if (parts) part_len = (all + parts - 1) / parts;
     slot = (bh * a.Tm + i) * a.sp.fixed_parts + part;
@@ -137,14 +137,15 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   // counts and indices come from the caller's pattern: clamp them so that a corrupt list cannot
   // address memory outside the tensors
   const int64_t unit = (int64_t)bh * a.Tm + i;
-  const int first = part * part_len;         // entries [first, first + part_len) of the list of a split row (never empty)
-  int cnt, split_at = 0;
+  int cnt, split_at = 0, first;              // entries [first, first + part_len) of the list of a split row (never empty)
   const int32_t* idx = nullptr;
   if constexpr (CROSS) {
     cnt = (keys + BKV - 1) / BKV;
+    first = part * part_len;
   } else {
     cnt = min(max(a.row_cnt[unit], 0), a.Tn);
     split_at = *(whole ? a.sp.unit_slot + unit : a.row_cnt + unit);
+    first = part * part_len;
     idx = a.row_idx + unit * a.Tn + first;
   }
   // The list's first 64 entries and the queries are requested before the count (or whether the row is split) is known:
@@ -462,6 +463,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
 #pragma unroll
       for (int g = 0; g < 8; ++g) part_store2(ps + ((mb * 8 + g) * 256 + tid) * 2, oacc[mb][2 * g], oacc[mb][2 * g + 1]);
     part_store2(ps + 256 * (D / 2) + 2 * tid, m_run, l_tot);
+    if constexpr (CROSS) return;             // (joined by a launch behind)
     if (!last_part(a.sp.arrive + first, parts, (int*)smem)) return;
     // The last part to arrive combines all of them, in part order (so the result does not depend on which one that
     // is): m = max m_p, l = sum l_p 2^(m_p - m), O = sum O_p 2^(m_p - m) / l.
@@ -522,13 +524,73 @@ hipError_t launch_fwd(const void* q, const void* k, const void* v, const Dims& m
 }
 
 // ------------------------------------------------------------------ attention to another sequence
-__global__ __launch_bounds__(256) void zero_ints_kernel(int32_t* p, int n) {
-  const int x = blockIdx.x * 256 + threadIdx.x;
-  if (x < n) p[x] = 0;
-}
-hipError_t launch_zero_ints(int32_t* p, int n, hipStream_t stream) {
-  hipLaunchKernelGGL(zero_ints_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, p, n);
-  return hipGetLastError();
+// The results of a row's parts, joined in part order: a workgroup takes 32 rows and 32 channels, each of its waves every fourth
+// part, and then adds up the four.  (Joined by the last part to arrive,
+// 128 queries, 2 heads, 65,536 keys, d = 128 took 96 us, forward and backward 263; now 62 and 192.)
+template <int D>
+__global__ __launch_bounds__(256) void cross_fwd_join_kernel(CrossFwdArgs a) {
+  constexpr int NMB = D / 32;
+  __shared__ float sums[4][16][64], stat[4][2][64];
+  const int mb = blockIdx.x % NMB, w = blockIdx.x / NMB % 4, unit = blockIdx.x / (4 * NMB), bh = unit / a.Tm, i = unit % a.Tm;
+  const int parts = cross_parts_of(a, bh), lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  const int row = i * BQ + 32 * w + (lane & 31), hf = lane >> 5;
+  if (parts == 0 || i * BQ + 32 * w >= a.N) return;
+  const float* p0 = a.sp.pool + (int64_t)unit * a.sp.fixed_parts * a.sp.slot_floats;
+  float m = -INFINITY, l = 0.f, x[16];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) x[v] = 0.f;
+  auto weight = [](float m_p, float m) -> float { return m_p == -INFINITY ? 0.f : fast_exp2(m_p - m); };
+  for (int p = g; p < parts; p += 16) {                  // four parts in flight
+    f32x2 y[4][8], ml[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float* ps = p0 + (int64_t)min(p + 4 * u, parts - 1) * a.sp.slot_floats;
+      ml[u] = *(const f32x2*)(ps + 256 * (D / 2) + 2 * (64 * w + lane));
+#pragma unroll
+      for (int c = 0; c < 8; ++c) y[u][c] = *(const f32x2*)(ps + ((mb * 8 + c) * 256 + 64 * w + lane) * 2);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (p + 4 * u >= parts) break;
+      const float m_new = fmaxf(m, ml[u][0]), old = weight(m, m_new), f = weight(ml[u][0], m_new);
+      l = fmaf(ml[u][1], f, l * old);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = fmaf(y[u][v / 2][v % 2], f, x[v] * old);
+      m = m_new;
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v) sums[g][v][lane] = x[v];
+  stat[g][0][lane] = m; stat[g][1][lane] = l;
+  __syncthreads();
+  if (g || row >= a.N) return;
+  m = fmaxf(fmaxf(stat[0][0][lane], stat[1][0][lane]), fmaxf(stat[2][0][lane], stat[3][0][lane]));
+  l = 0.f;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) x[v] = 0.f;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float f = weight(stat[u][0][lane], m);
+    l = fmaf(stat[u][1][lane], f, l);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = fmaf(sums[u][v][lane], f, x[v]);
+  }
+  const float inv = 1.f / l;
+  const int64_t off = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh + (int64_t)row * a.sn + 32 * mb + 4 * hf;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {                          // channels 32 mb + 8 q + 4 hf ..
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[4 * q + e] * inv;
+    const u32x2 o = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    *(u32x2*)(a.o + off + 8 * q) = o;
+    if (a.o_res) {
+      const u32x2 r = {pack_bf16(y[0] - __builtin_bit_cast(float, o[0] << 16), y[1] - __builtin_bit_cast(float, o[0] & 0xffff0000u)),
+                       pack_bf16(y[2] - __builtin_bit_cast(float, o[1] << 16), y[3] - __builtin_bit_cast(float, o[1] & 0xffff0000u))};
+      *(u32x2*)(a.o_res + off + 8 * q) = r;
+    }
+  }
+  if (mb == 0 && hf == 0) a.lse[(int64_t)bh * a.N + row] = m * LN2 + __logf(l);
 }
 
 hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
@@ -541,14 +603,15 @@ hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const C
   a.scale_log2 = scale * LOG2E;
   a.kv = cross_keys(m, lengths);
   const CrossFwdWs w = cross_fwd_ws(m);
-  a.sp = cross_plan(w.s, ws, (char*)ws + w.pool, fwd_slot_bytes(m.q));
-  if (w.s.slots) {
-    const hipError_t e = launch_zero_ints(a.sp.arrive, w.s.slots, stream);
-    if (e != hipSuccess) return e;
-  }
+  a.sp = cross_plan(w.s, nullptr, ws, fwd_slot_bytes(m.q));
   const dim3 grid((unsigned)(w.s.cut.parts * stretch_wgs(a.BH * a.Tm))), block(256);
   if (m.q.d == 128) hipLaunchKernelGGL((fwd_kernel<128, CrossFwdArgs>), grid, block, 0, stream, a);
   else              hipLaunchKernelGGL((fwd_kernel<64, CrossFwdArgs>), grid, block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !w.s.slots) return e;
+  const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));
+  if (m.q.d == 128) hipLaunchKernelGGL(cross_fwd_join_kernel<128>, joins, block, 0, stream, a);
+  else              hipLaunchKernelGGL(cross_fwd_join_kernel<64>, joins, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -22,4 +22,10 @@ template <class Keys>
 __device__ __forceinline__ int cross_length(const Keys& kv, int b) {
   return kv.lengths ? min(max(scalar_ld(kv.lengths + b), 0), kv.Nk) : kv.Nk;
 }
+// Parts that the rows of head bh are cut into; 0: walked whole.
+template <class Args>
+__device__ __forceinline__ int cross_parts_of(const Args& a, int bh) {
+  const int all = (cross_length(a.kv, bh / a.H) + BKV - 1) / BKV;
+  return all > a.sp.fixed_len ? (all + a.sp.fixed_len - 1) / a.sp.fixed_len : 0;
+}
 }  // namespace spa2

@@ -19,7 +19,6 @@ hipError_t launch_norm_rotate_bwd(const void*, const void*, const float*, const 
 }
 hipError_t launch_dropout(const void*, int, const void*, int, int64_t, uint32_t, uint64_t, uint64_t, const int64_t*, void*, int,
                           hipStream_t) { reached("launch_dropout"); }
-hipError_t launch_zero_ints(int32_t*, int, hipStream_t) { reached("launch_zero_ints"); }
 hipError_t launch_cross_few(const void*, const void*, const void*, const CrossDims&, const int32_t*, float, void*, void*, float*, void*,
                             hipStream_t) { reached("launch_cross_few"); }
 hipError_t launch_cross_fwd(const void*, const void*, const void*, const CrossDims&, const int32_t*, float, void*, void*, float*, void*,
