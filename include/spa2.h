@@ -316,7 +316,8 @@ int spa2_norm_rotate_bwd(const void* q, const void* k, const float* q_weight, co
  *   dk, dv                 the same with strides d_* (which the other calls do not look at).
  *   lengths   device, int32 [B], clamped to [0, Nk]; NULL: Nk.  Keys and values behind a sample's length are not read.  A
  *             sample without keys gets O = 0, LSE = -infinity and zero gradients.
- *   lse       fp32 [B, Hq, Nq];  o_res as in spa2_fwd (NULL if no backward pass follows).
+ *   lse       fp32 [B, Hq, Nq];  o_res as in spa2_fwd (NULL if no backward pass follows, or with Nk <= 64: D of a sample
+ *             of up to 64 keys is taken from its P and dP, and neither o nor o_res is read).
  * spa2_cross_bwd recomputes the probabilities from LSE and writes dq, dk and dv everywhere, zeros behind the lengths; dk and
  * dv are sums over the query heads of a key head, taken in fp32.  Lists of keys (queries) are cut over several workgroups where
  * there are few rows (columns); the parts are joined in a fixed order, so results are deterministic.

@@ -66,7 +66,7 @@ int check_cross_shape(const spa2_cross_shape* s) {
 
 // The query heads of a key head are taken as one head of more rows where a stride says so (one query a head, or heads whose
 // queries follow each other in memory): their keys and values are then read once, not once a head.  One query, 8 samples of up
-// to 32,760 keys, 40 heads sharing 8, d = 128, by the kernel for many rows: 523 us head by head, 175 together.
+// to 32,760 keys, 40 heads sharing 8, d = 128, by the kernel for many rows: 554 us head by head, 168 together (by the one for few rows 113).
 CrossDims cross_dims(const spa2_cross_shape& s) {
   CrossDims m;
   m.q.B = s.B; m.q.H = s.Hq; m.q.N = s.Nq; m.q.d = s.d;
@@ -138,13 +138,14 @@ int spa2_cross_bwd(const void* q, const void* k, const void* v, const int32_t* l
   if (!workspace || workspace_bytes < w.total) return SPA2_ERR_WORKSPACE;
   if (!aligned16(workspace)) return SPA2_ERR_ALIGN;
   char* ws = (char*)workspace;
-  float* delta = (float*)ws;
+  float *delta = (float*)ws, *lse_again = (float*)(ws + w.lse);
   hipStream_t st = (hipStream_t)stream;
   const SplitPlan cols = cross_plan(w.dkdv, ws + w.dkdv_counters, ws + w.dkdv_pool, dkdv_slot_bytes(m.q));
   const SplitPlan rows = cross_plan(w.dq, nullptr, ws + w.dq_pool, dq_slot_bytes(m.q));
-  if (launch_cross_dq(q, k, v, o, o_res, d_o, lse, m, lengths, scale, delta, dq, cols.arrive, w.dkdv.slots, rows, st) != hipSuccess)
+  if (launch_cross_dq(q, k, v, o, o_res, d_o, lse, m, lengths, scale, delta, lse_again, dq, cols.arrive, w.dkdv.slots, rows,
+                      st) != hipSuccess)
     return SPA2_ERR_LAUNCH;
-  return launch_cross_dkdv(q, k, v, d_o, lse, delta, m, lengths, scale, dk, dv, cols, st) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
+  return launch_cross_dkdv(q, k, v, d_o, lse_again, delta, m, lengths, scale, dk, dv, cols, st) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
 }
 
 size_t spa2_norm_rotate_bwd_workspace_bytes(const spa2_norm_shape* shape) {

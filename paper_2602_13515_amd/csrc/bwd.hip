@@ -36,7 +36,7 @@ hipError_t launch_bwd_delta(const void* o, const void* o_res, const void* d_o, c
 
 // ------------------------------------------------------------------ dQ
 struct DqArgs {
-  static constexpr bool CROSS = false;
+  static constexpr bool CROSS = false, FINE = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v; const uint16_t* d_o;
   const float* lse; const float* delta; uint16_t* dq;
   const int32_t* row_cnt; const int32_t* row_idx; const int32_t* row_order;
@@ -58,8 +58,12 @@ struct CrossDqArgs : DqArgs {
   static constexpr bool CROSS = true;
   CrossKeys kv;
   const uint16_t* o; const uint16_t* o_res;
-  float* delta_out;
+  float* delta_out; float* lse_out;      // D and LSE for the dK/dV kernel
   int32_t* zero; int zeros;   // arrival counters of the dK/dV launch
+};
+// The same with dS in two bf16 parts (cross_few).
+struct CrossDqFineArgs : CrossDqArgs {
+  static constexpr bool FINE = true;
 };
 
 // Partial result of one part of a split row: the fp32 accumulators as [pair of registers][thread] (see fwd.hip).
@@ -97,7 +101,7 @@ __device__ __forceinline__ void dq_store_rows(const DqArgs& a, int64_t base, int
 // 24 heads, half the rows long 6466 / 5435; 20,010 tokens, 6 heads, d = 64 89 / 78.
 template <int D, class Args>
 __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
-  constexpr bool CROSS = Args::CROSS;
+  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE;
   constexpr int NK = D / 16, NMB = D / 32;           // contraction steps of S and dP, output blocks of dQ
   // K and V tiles, XOR-swizzled and unpadded (the layout a direct global -> LDS copy can write): K is read along rows
   // (S^T) and transposed (dQ^T), V along rows (dP^T).  (Aligned: compile-time parts are XORed into addresses.)
@@ -183,9 +187,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       dof[kk] = *(const bf16x8*)(a.d_o + off + 16 * kk);
     }
   }
-  const float lse2 = a.lse[(int64_t)bh * N + qrow_ld] * LOG2E;
+  float lse2 = a.lse[(int64_t)bh * N + qrow_ld] * LOG2E;
   float dlt = CROSS ? 0.f : a.delta[(int64_t)bh * N + qrow_ld];
-  if constexpr (CROSS) {
+  if constexpr (CROSS) if (keys > BKV) {
     const int64_t off = base + (int64_t)qrow_ld * a.sn + 8 * hf;
     u32x4 of[D / 16], rf[D / 16];
 #pragma unroll
@@ -203,7 +207,6 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       }
     }
     dlt = sum_halves(dlt);
-    if (hf == 0 && qrow < N && part == 0) a.delta_out[(int64_t)bh * N + qrow] = dlt;
   }
   requested();
   if (whole && split_at >= 0) return;
@@ -286,6 +289,41 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   raw_copies_done();
   __syncthreads();
 
+  if constexpr (CROSS) {
+    // All keys in one tile: LSE and D are taken again, D = sum P dP, from the very values that dS is made of.  The forward
+    // pass's LSE and O are of P rounded to bf16, which few keys do not average out: with 3 keys the error of dQ and dK was
+    // 1.5 times that of their own rounding to bf16, so 1.4, which is that and the rounding of dS.  (It is faster, too: 32,760
+    // queries, 12 heads, 60 keys, the backward pass 204 -> 157 us, as O and what its rounding dropped are not read.)
+    if (keys <= BKV) {
+      float sum = 0.f, total = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+          s = mfma32(lds_ld16((ka_off ^ (kk << 5)) + kb * 32 * D * 2), qf[kk], s);
+          dp = mfma32(lds_ld16((ka_off ^ (kk << 5)) + TILE_B + kb * 32 * D * 2), dof[kk], dp);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (32 * kb + 8 * (v >> 2) + (v & 3) + 4 * hf < keys) {
+            const float p = fast_exp2(fmaf(s[v], a.scale_log2, -lse2));
+            total += p;
+            sum = fmaf(p, dp[v], sum);
+          }
+      }
+      total = sum_halves(total);
+      dlt = sum_halves(sum) / total;
+      lse2 += __builtin_amdgcn_logf(total);        // (log2)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) neg_d[v] = -dlt;
+    }
+    if (hf == 0 && qrow < N && part == 0) {
+      a.delta_out[(int64_t)bh * N + qrow] = dlt;
+      a.lse_out[(int64_t)bh * N + qrow] = lse2 * (1.f / LOG2E);
+    }
+  }
+
   for (int t = 0; t < cnt; ++t) {
     const int j = j_cur;
     if (!CROSS && ((t + 1) & 63) == 0 && t + 1 < cnt) idx_v = list_load(idx, min(t + 1 + (fresh_tid() & 63), cnt - 1));     // next 64 entries
@@ -320,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const bool tail = (j + 1) * BKV > keys;
     f32x16 s[2], dp[2];
-    uint32_t dsk[2][8];
+    uint32_t dsk[2][8], ds_rest[2][8];       // (ds_rest: FINE)
     auto exp_unit = [&](auto KB, auto U) {   // P^T of two keys
       constexpr int kb = decltype(KB)::v, v = 2 * decltype(U)::v;
       s[kb][v] = fast_exp2(fmaf(s[kb][v], a.scale_log2, -lse2));
@@ -338,6 +376,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     auto ds_unit = [&](auto KB, auto U) {    // dS^T of two keys
       constexpr int kb = decltype(KB)::v, u = decltype(U)::v;
       dsk[kb][u] = pack_bf16(s[kb][2 * u] * dp[kb][2 * u], s[kb][2 * u + 1] * dp[kb][2 * u + 1]);
+      if constexpr (FINE) ds_rest[kb][u] = pack_rest(s[kb][2 * u] * dp[kb][2 * u], s[kb][2 * u + 1] * dp[kb][2 * u + 1], dsk[kb][u]);
     };
     bf16x8 fr[PDQ], f2[PDT];
 #pragma unroll
@@ -359,6 +398,10 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       constexpr int y = decltype(Y)::v, kb = y / (2 * NMB), cc = (y / NMB) % 2, mb = y % NMB;
       const u32x4 du = {dsk[kb][4 * cc], dsk[kb][4 * cc + 1], dsk[kb][4 * cc + 2], dsk[kb][4 * cc + 3]};
       acc[mb] = mfma32(f2[y % PDT], __builtin_bit_cast(bf16x8, du), acc[mb]);
+      if constexpr (FINE) {
+        const u32x4 dr = {ds_rest[kb][4 * cc], ds_rest[kb][4 * cc + 1], ds_rest[kb][4 * cc + 2], ds_rest[kb][4 * cc + 3]};
+        acc[mb] = mfma32(f2[y % PDT], __builtin_bit_cast(bf16x8, dr), acc[mb]);
+      }
       if constexpr (y + PDT < NM2) f2[y % PDT] = frag2(y + PDT);
       if constexpr (kb == 0) static_for<(y * 8) / (2 * NMB), ((y + 1) * 8) / (2 * NMB)>([&](auto U) { ds_unit(Int<1>{}, U); });
       __builtin_amdgcn_sched_barrier(0);
@@ -485,11 +528,11 @@ __global__ __launch_bounds__(256) void cross_dq_join_kernel(CrossDqArgs a) {
 }
 
 hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
-                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, void* dq,
-                           int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
-  CrossDqArgs a = {};
+                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, float* lse_out,
+                           void* dq, int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
+  CrossDqFineArgs a = {};
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
-  a.lse = lse; a.delta_out = delta; a.dq = (uint16_t*)dq;
+  a.lse = lse; a.delta_out = delta; a.lse_out = lse_out; a.dq = (uint16_t*)dq;
   a.o = (const uint16_t*)o; a.o_res = (const uint16_t*)o_res;
   a.zero = zero; a.zeros = zeros;
   a.BH = m.q.B * m.q.H; a.H = m.q.H; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
@@ -498,8 +541,11 @@ hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const vo
   a.kv = cross_keys(m, lengths);
   a.sp = plan;
   const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tm))), block(256);
-  if (m.q.d == 128) hipLaunchKernelGGL((dq_kernel<128, CrossDqArgs>), grid, block, 0, stream, a);
-  else              hipLaunchKernelGGL((dq_kernel<64, CrossDqArgs>), grid, block, 0, stream, a);
+  const bool fine = cross_few(m);
+  if (m.q.d == 128 && fine) hipLaunchKernelGGL((dq_kernel<128, CrossDqFineArgs>), grid, block, 0, stream, a);
+  else if (m.q.d == 128)    hipLaunchKernelGGL((dq_kernel<128, CrossDqArgs>), grid, block, 0, stream, a);
+  else if (fine)            hipLaunchKernelGGL((dq_kernel<64, CrossDqFineArgs>), grid, block, 0, stream, a);
+  else                      hipLaunchKernelGGL((dq_kernel<64, CrossDqArgs>), grid, block, 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !plan.pool_slots) return e;
   const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));

@@ -22,7 +22,7 @@ __device__ __forceinline__ void mfma32_acc(bf16x8 a, bf16x8 b, f32x16& c) {
 
 // ------------------------------------------------------------------ dK, dV
 struct DkvArgs {
-  static constexpr bool CROSS = false;
+  static constexpr bool CROSS = false, FINE = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v; const uint16_t* d_o;
   const float* lse; const float* delta; uint16_t* dk; uint16_t* dv;
   const int32_t* col_cnt; const int32_t* col_idx; const int32_t* col_order;
@@ -39,6 +39,10 @@ struct CrossDkvArgs : DkvArgs {
   static constexpr bool CROSS = true;
   CrossKeys kv;
   int64_t dsb, dsh, dsn;      // strides of dK and dV
+};
+// The same with P and dS in two bf16 parts (cross_few).
+struct CrossDkvFineArgs : CrossDkvArgs {
+  static constexpr bool FINE = true;
 };
 // the walk of a workgroup that has one item
 struct OneItem {
@@ -68,6 +72,15 @@ template <class Args>
 __device__ __forceinline__ CrossEntry cross_entry(const Args& a, int e) {
   const int g = a.kv.group == 1 ? 0 : e / a.Tm;
   return {g, e - g * a.Tm};
+}
+
+// What the rounding of value(8 c) .. value(8 c + 7) to the packed pairs p[4 c] .. p[4 c + 3] dropped.
+template <class F>
+__device__ __forceinline__ bf16x8 rest_of(F&& value, const uint32_t (&p)[8], int c) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = pack_rest(value(8 * c + 2 * i), value(8 * c + 2 * i + 1), p[4 * c + i]);
+  return __builtin_bit_cast(bf16x8, r);
 }
 
 // Partial result of one part of a split column: the fp32 sums of the two waves, dK^T then dV^T, in the order
@@ -138,7 +151,7 @@ __device__ __forceinline__ void dkdv_merge(const Args& a, const WorkItem& item, 
 template <int D, class Args, class Way>
 __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, Way& walk, unsigned char* smem,
                                           unsigned char* stat_s) {
-  constexpr bool CROSS = Args::CROSS;
+  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE;
   constexpr int QW = 32;                             // query rows per wave and step
   constexpr int HQ = 64;                             // query rows per workgroup and step
   constexpr int NK = D / 16;                         // 16-wide contraction steps over the head dimension
@@ -247,11 +260,14 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
   // lane read, not a memory access
   int idx_v = 0, g_at = 0;                   // (g_at: query head of the step asked for last)
   if constexpr (!CROSS) idx_v = idx[min(lane, cnt - 1)];
+  // (attention to another sequence with no more queries than a half has: one half an entry.  32 rows of 8 heads, 8 samples of
+  // 8192 keys, the backward pass, d = 128: 297 -> 270 us; d = 64 112 -> 97)
+  const int halves = CROSS && N <= HQ ? 0 : 1;
   auto step_row = [&](int u) -> int {        // first row of step u (uniform, inside the chunk that idx_v holds)
     if constexpr (CROSS) {
-      const CrossEntry e = cross_entry(a, first + (u >> 1));
+      const CrossEntry e = cross_entry(a, first + (u >> halves));
       g_at = e.g;
-      return e.i * BQ + (u & 1) * HQ + QW * w;
+      return e.i * BQ + (u & halves) * HQ + QW * w;
     }
     const int i = min(max(__builtin_amdgcn_readlane(idx_v, (u >> 1) & 63), 0), a.Tm - 1);
     return i * BQ + (u & 1) * HQ + QW * w;
@@ -268,7 +284,7 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
   const uint32_t t_off0 = 2 * swz_idx<D>(4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
   const uint32_t t_off1 = 2 * swz_idx<D>(8 + 4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
 
-  const int steps = 2 * cnt;                 // step u: half u & 1 of list entry u >> 1
+  const int steps = CROSS ? cnt << halves : 2 * cnt;    // step u: half u & 1 of list entry u >> 1
   {
     const int row0 = step_row(0), row_b = min(row0, N - 1);
     set_rows(min(QW - 1, N - 1 - row_b));
@@ -342,6 +358,10 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
     auto quad = [](const uint32_t (&p)[8], int c) -> bf16x8 {
       return __builtin_bit_cast(bf16x8, u32x4{p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]});
     };
+    auto p_rest = [&](int x, int c) -> bf16x8 {         // (FINE) what quad(pk[x], c) dropped, quad(dsk[x], c)
+      return rest_of([&](int v) { return s[x][v]; }, pk[x], c);
+    };
+    auto ds_rest = [&](int x, int c) -> bf16x8 { return rest_of([&](int v) { return s[x][v] * dp[x][v]; }, dsk[x], c); };
 
     // ---- S = Q K^T; the next step's LSE, D and Q rows are requested
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -381,6 +401,10 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
       constexpr int x = decltype(X)::v, c = x / NMB, mb = x % NMB;
       mfma32_acc(ft[x % PDT], quad(pk[0], c), dv_acc[0][mb]);
       mfma32_acc(ft[x % PDT], quad(pk[1], c), dv_acc[1][mb]);
+      if constexpr (FINE) {
+        mfma32_acc(ft[x % PDT], p_rest(0, c), dv_acc[0][mb]);
+        mfma32_acc(ft[x % PDT], p_rest(1, c), dv_acc[1][mb]);
+      }
       ft[x % PDT] = x + PDT < NX ? tr_frag(1, x + PDT) : tr_frag(0, x + PDT - NX);
       if constexpr (c == 0) static_for<EB + mb * (16 - EB) / NMB, EB + (mb + 1) * (16 - EB) / NMB>(exp_unit);
       else                  static_for<mb * 8 / NMB, (mb + 1) * 8 / NMB>(ds_unit);
@@ -393,6 +417,10 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
       constexpr int x = decltype(X)::v, c = x / NMB, mb = x % NMB;
       mfma32_acc(ft[x % PDT], quad(dsk[0], c), dk_acc[0][mb]);
       mfma32_acc(ft[x % PDT], quad(dsk[1], c), dk_acc[1][mb]);
+      if constexpr (FINE) {
+        mfma32_acc(ft[x % PDT], ds_rest(0, c), dk_acc[0][mb]);
+        mfma32_acc(ft[x % PDT], ds_rest(1, c), dk_acc[1][mb]);
+      }
       if constexpr (x + PDT < NX) ft[x % PDT] = tr_frag(0, x + PDT);
       if constexpr (c == 0) static_for<8 + mb * 8 / NMB, 8 + (mb + 1) * 8 / NMB>(ds_unit);
       if constexpr (x == NMB) {
@@ -495,7 +523,7 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
 template <class Args, class Way>
 __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item, Way& walk, unsigned char* smem,
                                             unsigned char* stat_s) {
-  constexpr bool CROSS = Args::CROSS;
+  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE;
   constexpr int D = 64, NK = D / 16, NMB = D / 32;
   constexpr int HQ = 64;                             // query rows per step
   constexpr int CPR = D / 8, RPI = 64 / CPR, NCP = 32 / RPI;         // (see dkdv_item)
@@ -584,11 +612,12 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
 
   int idx_v = 0, g_at = 0;                   // the index list, 64 entries at a time (see dkdv_item)
   if constexpr (!CROSS) idx_v = idx[min(lane, cnt - 1)];
+  const int halves = CROSS && N <= HQ ? 0 : 1;         // (see dkdv_item)
   auto step_row = [&](int u) -> int {        // this wave's first row of step u (uniform, inside the chunk that idx_v holds)
     if constexpr (CROSS) {
-      const CrossEntry e = cross_entry(a, first + (u >> 1));
+      const CrossEntry e = cross_entry(a, first + (u >> halves));
       g_at = e.g;
-      return e.i * BQ + (u & 1) * HQ + 32 * w;
+      return e.i * BQ + (u & halves) * HQ + 32 * w;
     }
     const int i = min(max(__builtin_amdgcn_readlane(idx_v, (u >> 1) & 63), 0), a.Tm - 1);
     return i * BQ + (u & 1) * HQ + 32 * w;
@@ -601,7 +630,7 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
   const uint32_t t_off0 = sm + 2 * swz_idx<D>(4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
   const uint32_t t_off1 = sm + 2 * swz_idx<D>(8 + 4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
 
-  const int steps = 2 * cnt;                 // step u: half u & 1 of list entry u >> 1
+  const int steps = CROSS ? cnt << halves : 2 * cnt;    // step u: half u & 1 of list entry u >> 1
   {
     const int row0 = step_row(0), row_b = min(row0, N - 1);
     set_rows(min(31, N - 1 - row_b));
@@ -676,6 +705,10 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
     auto quad = [](const uint32_t (&p)[8], int c) -> bf16x8 {
       return __builtin_bit_cast(bf16x8, u32x4{p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]});
     };
+    auto p_rest = [&](int x, int c) -> bf16x8 {         // (FINE) what quad(pk[x], c) dropped, quad(dsk[x], c)
+      return rest_of([&](int v) { return s[x][v]; }, pk[x], c);
+    };
+    auto ds_rest = [&](int x, int c) -> bf16x8 { return rest_of([&](int v) { return s[x][v] * dp[x][v]; }, dsk[x], c); };
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     // ---- S = Q K^T of both halves; the next step's LSE, D, Q and dO rows are requested
     static_for<0, NR>([&](auto Y) {
@@ -704,6 +737,7 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
     static_for<0, NX>([&](auto X) {
       constexpr int x = decltype(X)::v, mb = x % NMB, c = (x / NMB) % 2, rh = x / (2 * NMB);
       dv_acc[mb] = mfma32(ft[x % PDT], quad(pk[rh], c), dv_acc[mb]);
+      if constexpr (FINE) dv_acc[mb] = mfma32(ft[x % PDT], p_rest(rh, c), dv_acc[mb]);
       ft[x % PDT] = x + PDT < NX ? tr_frag(1, x + PDT) : tr_frag(0, x + PDT - NX);
       static_for<x * 2, x * 2 + 2>(ds_unit);
       __builtin_amdgcn_sched_barrier(0);
@@ -713,6 +747,7 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
     static_for<0, NX>([&](auto X) {
       constexpr int x = decltype(X)::v, mb = x % NMB, c = (x / NMB) % 2, rh = x / (2 * NMB);
       dk_acc[mb] = mfma32(ft[x % PDT], quad(dsk[rh], c), dk_acc[mb]);
+      if constexpr (FINE) dk_acc[mb] = mfma32(ft[x % PDT], ds_rest(rh, c), dk_acc[mb]);
       if constexpr (x + PDT < NX) ft[x % PDT] = tr_frag(0, x + PDT);
       if constexpr (x == NX - PDT) {
         raw_copies_done();
@@ -797,12 +832,12 @@ hipError_t launch_bwd_dkdv(const void* q, const void* k, const void* v, const vo
 }
 
 // ------------------------------------------------------------------ attention to another sequence
-template <int D>
+template <int D, class Args>
 __global__ __attribute__((amdgpu_flat_work_group_size(128, 128), amdgpu_waves_per_eu(D == 128 ? 1 : 2, D == 128 ? 1 : 2)))
-void cross_dkdv_kernel(CrossDkvArgs) {
+void cross_dkdv_kernel(Args) {
   __shared__ __align__(1024) unsigned char smem[2 * 2 * 64 * D * 2];
   __shared__ __align__(1024) unsigned char stat_s[2 * 2 * 512];
-  const CrossDkvArgs& a = fresh_args<CrossDkvArgs>();
+  const Args& a = fresh_args<Args>();
   const int columns = stretch_wgs(a.BH * a.Tn);
   const HeadBlock hb = stretch_row(blockIdx.x % columns, a.BH, a.Tn);
   if (!hb.valid) return;
@@ -825,7 +860,7 @@ void cross_dkdv_kernel(CrossDkvArgs) {
 hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
                              const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
                              hipStream_t stream) {
-  CrossDkvArgs a = {};
+  CrossDkvFineArgs a = {};
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
   a.lse = lse; a.delta = delta; a.dk = (uint16_t*)dk; a.dv = (uint16_t*)dv;
   a.BH = m.q.B * m.Hk; a.H = m.Hk; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
@@ -835,8 +870,11 @@ hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const 
   a.dsb = m.dsb; a.dsh = m.dsh; a.dsn = m.dsn;
   a.sp = plan;
   const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tn))), block(128);
-  if (m.q.d == 128) hipLaunchKernelGGL(cross_dkdv_kernel<128>, grid, block, 0, stream, a);
-  else              hipLaunchKernelGGL(cross_dkdv_kernel<64>, grid, block, 0, stream, a);
+  const bool fine = cross_few(m);
+  if (m.q.d == 128 && fine) hipLaunchKernelGGL((cross_dkdv_kernel<128, CrossDkvFineArgs>), grid, block, 0, stream, a);
+  else if (m.q.d == 128)    hipLaunchKernelGGL((cross_dkdv_kernel<128, CrossDkvArgs>), grid, block, 0, stream, a);
+  else if (fine)            hipLaunchKernelGGL((cross_dkdv_kernel<64, CrossDkvFineArgs>), grid, block, 0, stream, a);
+  else                      hipLaunchKernelGGL((cross_dkdv_kernel<64, CrossDkvArgs>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -80,11 +80,15 @@ inline CrossSection cross_dkdv_section(const CrossDims& m) {
                        dkdv_slot_bytes(m.q));
 }
 
-// Workspace of the forward pass: the pool.  Of the backward pass: D, counters of dK/dV, pools.
+// Workspace of the forward pass: the pool.  Of the backward pass: D, LSE, counters of dK/dV, pools.
 constexpr int FEW_ROWS = 32;
 // Whether the rows that read a key head are so few that the kernel for few rows takes them (a wave's 32).  With 32 rows, us, that
-// kernel / the other: 8 samples of 8192 keys, 8 heads 54 / 66, d = 64 34 / 35; 64 samples of 512 26 / 27; 1 of 65,536, 2 heads 28 / 93;
-// 600 of 77, 4 heads, d = 64 20 / 22; 2 of 77, 40 heads 7.7 / 6.5; with one row 48 / 68, 30 / 36, 23 / 25, 25 / 88, 15 / 22, 6.1 / 6.3.
+// kernel / the other: 8 samples of 8192 keys, 8 heads 54 / 74, d = 64 34 / 36; 64 samples of 512 26 / 27; 1 of 65,536, 2 heads 28 / 61;
+// 600 of 77, 4 heads, d = 64 20 / 22; 2 of 77, 40 heads 7.6 / 6.6; with one row 49 / 76, 30 / 36, 23 / 25, 25 / 59, 15 / 22, 6.1 / 6.2.
+// The backward pass of such rows takes P and dS into their products in two bf16 parts: nothing averages over so few rows, and one
+// part leaves an error of dQ, dK and dV of sqrt(2), for single rows and keys up to 2.2, times that of their own rounding to bf16; two
+// leave that alone.  Two parts / one, us: 8 samples of 8192 keys, 8 heads of 32 rows 285 / 270, d = 64 109 / 97; 64 samples of 512, one
+// row 128 / 118; 1 of 65,536, 2 heads, one row 124 / 114; 600 of 77, 4 heads of 32 rows, d = 64 69 / 64; 2 of 77, 40 heads 19.4 / 18.2.
 inline bool cross_few(const CrossDims& m) { return (int64_t)m.group * m.q.N <= FEW_ROWS; }
 // The kernel for few rows: workgroups of a key head that share the line of its key blocks (cross_few.hip), or 0; a part's result:
 // [row][D] unnormalised sums, then (maximum in log2 units, sum) of each row.
@@ -109,12 +113,13 @@ inline CrossFwdWs cross_fwd_ws(const CrossDims& m) {
   w.total = w.s.pool;
   return w;
 }
-struct CrossBwdWs { CrossSection dkdv, dq; size_t dkdv_counters, dkdv_pool, dq_pool, total; };
+struct CrossBwdWs { CrossSection dkdv, dq; size_t lse, dkdv_counters, dkdv_pool, dq_pool, total; };
 inline CrossBwdWs cross_bwd_ws(const CrossDims& m) {
   CrossBwdWs w;
   w.dkdv = cross_dkdv_section(m);
   w.dq = cross_dq_section(m);
-  w.dkdv_counters = round256((size_t)m.q.B * m.q.H * m.q.N * sizeof(float));
+  w.lse = round256((size_t)m.q.B * m.q.H * m.q.N * sizeof(float));
+  w.dkdv_counters = 2 * w.lse;
   w.dkdv_pool = w.dkdv_counters + w.dkdv.counters;
   w.dq_pool = w.dkdv_pool + w.dkdv.pool;
   w.total = w.dq_pool + w.dq.pool;
@@ -125,10 +130,10 @@ hipError_t launch_cross_few(const void* q, const void* k, const void* v, const C
                             void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
 hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
                             void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
-// (delta: D, written here for the dK/dV kernel; zero: integers that the launch sets to zero for it)
+// (delta, lse_out: D and LSE, written here for the dK/dV kernel; zero: integers that the launch sets to zero for it)
 hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
-                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, void* dq,
-                           int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream);
+                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, float* lse_out,
+                           void* dq, int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream);
 hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
                              const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
                              hipStream_t stream);

@@ -476,7 +476,7 @@ CrossResult cross_call(const Tensor& q_in, const Tensor& k_in, const Tensor& v_i
   r.v = one_layout ? v_in : in_order(v_in, r.k);
   const CrossShape c(r.q, r.k, r.k);
   r.o = like(r.q);
-  if (training) r.o_res = like(r.q);
+  if (training && r.k.size(2) > 64) r.o_res = like(r.q);       // (up to 64 keys the backward pass takes D without O)
   // one scratch buffer; a log-sum-exp that nobody reads lies behind the workspace
   const int64_t need = (int64_t)spa2_cross_fwd_workspace_bytes(&c.s), at = (need + 255) & ~(int64_t)255;
   const int64_t rows = r.q.size(0) * r.q.size(1) * r.q.size(2);
@@ -509,7 +509,8 @@ struct CrossAttention : torch::autograd::Function<CrossAttention> {
     TORCH_CHECK_VALUE(k.sizes().vec() == ctx->saved_data["keys"].toIntVector() && strides_of(k) == strides_of(v),
                       "saved k and v come back in their shape and one layout");
     TORCH_CHECK_VALUE(grads[0].sizes() == q.sizes() && grads[0].device() == q.device(), "saved q comes back in its shape on its GPU");
-    same_layout(q, {&o, &o_res});
+    same_layout(q, {&o});
+    if (o_res.defined()) same_layout(q, {&o_res});
     TORCH_CHECK_VALUE(lse.device() == q.device() && lse.scalar_type() == at::kFloat && lse.is_contiguous() &&
                       lse.numel() == q.size(0) * q.size(1) * q.size(2), "the log-sum-exp comes back as B * H * N contiguous fp32 numbers");
     const c10::DeviceGuard device(q.device());
@@ -518,7 +519,7 @@ struct CrossAttention : torch::autograd::Function<CrossAttention> {
     const CrossShape c(q, k, dk);
     const int64_t need = (int64_t)spa2_cross_bwd_workspace_bytes(&c.s);
     const Tensor ws = bytes(need, q);
-    check(spa2_cross_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), (const int32_t*)ptr(lengths), o.data_ptr(), o_res.data_ptr(),
+    check(spa2_cross_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), (const int32_t*)ptr(lengths), o.data_ptr(), (void*)ptr(o_res),
                          d_o.data_ptr(), (const float*)lse.data_ptr(), &c.s, (float)ctx->saved_data["scale"].toDouble(),
                          dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), (size_t)need, stream_of(q)),
           "spa2_cross_bwd");

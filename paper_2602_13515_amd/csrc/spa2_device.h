@@ -43,6 +43,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   bf16x2 r = __builtin_convertvector(v, bf16x2);
   return __builtin_bit_cast(uint32_t, r);
 }
+// what the rounding of (a, b) to the packed pair p dropped, as a packed pair: the two together have 16 bits of the values
+__device__ __forceinline__ uint32_t pack_rest(float a, float b, uint32_t p) {
+  return pack_bf16(a - __builtin_bit_cast(float, p << 16), b - __builtin_bit_cast(float, p & 0xffff0000u));
+}
 
 // Transposing LDS read (ds_read_b64_tr_b16).  Within each group of 16 lanes,
 // lane s supplies the address of four consecutive 16-bit elements; lane i of

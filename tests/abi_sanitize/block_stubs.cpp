@@ -24,7 +24,7 @@ hipError_t launch_cross_few(const void*, const void*, const void*, const CrossDi
 hipError_t launch_cross_fwd(const void*, const void*, const void*, const CrossDims&, const int32_t*, float, void*, void*, float*, void*,
                             hipStream_t) { reached("launch_cross_fwd"); }
 hipError_t launch_cross_dq(const void*, const void*, const void*, const void*, const void*, const void*, const float*, const CrossDims&,
-                           const int32_t*, float, float*, void*, int32_t*, int, const SplitPlan&, hipStream_t) {
+                           const int32_t*, float, float*, float*, void*, int32_t*, int, const SplitPlan&, hipStream_t) {
   reached("launch_cross_dq");
 }
 hipError_t launch_cross_dkdv(const void*, const void*, const void*, const void*, const float*, const float*, const CrossDims&,

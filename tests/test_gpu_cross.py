@@ -317,3 +317,67 @@ def test_inputs_with_tangents_are_refused(grad):
         with pytest.raises(RuntimeError):
             f(fwad.make_dual(x, torch.ones_like(x)))
     assert torch.equal(f(x), want)
+
+
+def _rounded(x):
+    return f64(torch.from_numpy(np.ascontiguousarray(x)).float().to(BF))
+
+
+def _errors(case, parts):
+    """{gradient: (error of the kernels, error of the formula in 64 bits where P and dS before their products (parts = 1) and the
+    results are rounded to bf16)}, in the 2-norm."""
+    q, k, v, lens, do = _inputs(*case)
+    s = q.shape[-1] ** -0.5
+    seen = None if lens is None else lens.cpu().numpy()
+    exact = {n: x[0] for n, x in ref.cross(f64(q), f64(k), f64(v), seen, s, f64(do))[0].items()}
+    leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+    got = torch.autograd.grad(spa2.cross_attention(*leaves, lens, s), leaves, do)
+    model = _model(f64(q), f64(k), f64(v), seen, s, f64(do), _rounded if parts == 1 else lambda x: x)
+    return {n: (np.linalg.norm(f64(t) - exact[n]), np.linalg.norm(_rounded(model[n]) - exact[n])) for n, t in zip(("dq", "dk", "dv"), got)}
+
+
+def _model(q, k, v, lengths, scale, do, rounded):
+    out = {"dq": np.zeros_like(q), "dk": np.zeros_like(k), "dv": np.zeros_like(v)}
+    for b in range(q.shape[0]):
+        n = k.shape[2] if lengths is None else min(max(int(lengths[b]), 0), k.shape[2])
+        for h in range(q.shape[1] if n else 0):
+            g = h // (q.shape[1] // k.shape[1])
+            S = scale * q[b, h] @ k[b, g, :n].T
+            P = np.exp(S - S.max(-1, keepdims=True))
+            P /= P.sum(-1, keepdims=True)
+            dP = do[b, h] @ v[b, g, :n].T
+            dS = rounded(P * (dP - (P * dP).sum(-1, keepdims=True)))
+            out["dq"][b, h] = scale * dS @ k[b, g, :n]
+            out["dk"][b, g, :n] += scale * dS.T @ q[b, h]
+            out["dv"][b, g, :n] += rounded(P).T @ do[b, h]
+    return out
+
+
+@pytest.mark.parametrize("case", [(2, 2, 2, 1, 5, 128, None), (1, 6, 6, 8, 4, 128, None), (2, 5, 1, 3, 20, 64, [20, 3]), (1, 2, 2, 1, 300, 64, None),
+                                  (3, 8, 2, 8, 1000, 128, [1000, 65, 0]), (4, 4, 4, 32, 90, 64, [90, 64, 2, 33])], ids=str)
+def test_gradients_of_few_rows_keep_two_parts(case):
+    # P and dS in two parts have 16 bits, a relative error of 2^-17: what is left is the rounding of the result, whose 2-norm is about
+    # 2^-9.2 of it.  1.1 allows an error of 0.46 of that besides, 2^-10.3.
+    for name, (err, own) in _errors(case, 2).items():
+        assert err <= 1.1 * own, (name, err, own)
+
+
+@pytest.mark.parametrize("case", [(1, 12, 12, 200, 3, 64, None), (2, 4, 2, 300, 8, 128, [8, 3]), (2, 3, 3, 150, 64, 64, [64, 2])], ids=str)
+def test_gradients_of_few_keys(case):
+    # The kernels' P and dS before their rounding are off by some 2^-17, a hundredth of a bf16 step, so that nearly all of them round
+    # as the model's do; the few that do not are off by at most that much more than half a step.  With LSE and D from the forward
+    # pass, whose P is rounded, few keys show that (1.07 and more of the model).
+    for name, (err, model) in _errors(case, 1).items():
+        assert err <= 1.03 * model, (name, err, model)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq", [1, 200])
+def test_one_key_has_no_gradient_of_scores(Nq, d):
+    # P = 1 up to the fp32 error e of exp(S - LSE), about 2^-24 * (2 |LSE| log2(e) + 2) < 2^-19 for |LSE| < 10, and D = P dP, so that
+    # dS = P (dP - D) = dP e; |dP| < 8 sqrt(d), and |k|, |q| < 6.
+    q, k, v, lens, do = _inputs(2, 3, 3, Nq, 1, d, None)
+    leaves = [t.detach().requires_grad_(True) for t in (q, k, v)]
+    dq, dk, _ = torch.autograd.grad(spa2.cross_attention(*leaves), leaves, do)
+    bar = 2.0 ** -19 * 8 * d ** 0.5 * 6 * d ** -0.5
+    assert dq.abs().max().item() <= bar and dk.abs().max().item() <= bar * Nq
