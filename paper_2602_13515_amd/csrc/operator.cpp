@@ -1,7 +1,8 @@
-// The two differentiable operators in native code: block-sparse attention (pattern from q and k, forward, backward) and
-// the velocity distillation loss, as autograd functions over the C ABI.  Same results, checks and errors as the Python
-// functions in autograd.py and distill.py, which stay for the calls that this module does not take (a pattern asked for,
-// overlapping backward kernels, tracing, function transforms, tensors that are not plain CUDA tensors).
+// The differentiable operators in native code, as autograd functions over the C ABI: block-sparse attention (pattern from q
+// and k, forward, backward) and the velocity distillation loss, with the results, checks and errors of the Python functions in
+// autograd.py and distill.py, which stay for the calls that this module does not take (a pattern asked for, overlapping
+// backward kernels, tracing, function transforms, tensors that are not plain CUDA tensors); and the operators around the
+// attention (block.py), which have no other route.
 //
 // Why: the Python route cost more host time than the kernels take on small layers.  Two heads of 2,048 tokens, forward and
 // backward: 82 us of kernels and the gaps between them, 226 us a pass, in which the backward pass waited for the
