@@ -262,9 +262,13 @@ std::array<int64_t, 3> strides_of(const Tensor& x) {
   return s;
 }
 
-// x in the memory order of ref (of another type maybe).
+// Whether x starts where the kernels read 16 bytes at a time.  (Upstream gradients need not: the backward of a concatenation
+// hands out views of its buffer at any element.)
+bool aligned(const Tensor& x) { return (reinterpret_cast<uintptr_t>(x.data_ptr()) & 15) == 0; }
+
+// x in the memory order of ref (of another type maybe), from a 16-byte boundary.
 Tensor in_order(const Tensor& x, const Tensor& ref) {
-  if (x.stride(3) == 1 && strides_of(x) == strides_of(ref)) return x;
+  if (x.stride(3) == 1 && strides_of(x) == strides_of(ref) && aligned(x)) return x;
   const Tensor y = at::empty_strided(ref.sizes(), ref.strides(), x.options());
   y.copy_(x);
   return y;
@@ -405,11 +409,11 @@ struct NormRotate : torch::autograd::Function<NormRotate> {
   }
 };
 
-// weights of any float type: the kernels read fp32 (the conversion is differentiated by PyTorch)
+// weights of any float type, anywhere in memory: the kernels read fp32 from a 16-byte boundary (PyTorch differentiates this)
 OptTensor as_weight(const OptTensor& w) {
   if (!w || !w->defined()) return std::nullopt;
-  if (w->scalar_type() == at::kFloat && w->is_contiguous()) return *w;
-  return w->to(at::kFloat).contiguous();
+  const Tensor x = w->to(at::kFloat).contiguous();
+  return aligned(x) ? x : x.clone();
 }
 
 std::tuple<Tensor, Tensor> norm_rotate(const Tensor& q, const Tensor& k, const OptTensor& q_weight, const OptTensor& k_weight,
@@ -538,7 +542,7 @@ Tensor cross_attention(const Tensor& q, const Tensor& k, const Tensor& v, const 
 // x as the elementwise kernels take it: contiguous from a 16-byte boundary.
 Tensor packed(const Tensor& x) {
   const Tensor y = x.contiguous();
-  return (reinterpret_cast<uintptr_t>(y.data_ptr()) & 15) == 0 ? y : y.clone();
+  return aligned(y) ? y : y.clone();
 }
 
 void seed_check(const Tensor& s, const Tensor& x) {
