@@ -150,7 +150,9 @@ class _SpargeAttn2(torch.autograd.Function):
             raise ValueError("saved token tensors come back on their GPU")
         if lse.device != q.device or lse.dtype != torch.float32 or lse.numel() != q.shape[:3].numel() or not lse.is_contiguous():
             raise ValueError("the log-sum-exp comes back as B * H * N contiguous fp32 numbers")
-        d_o = _match(d_o.to(torch.bfloat16), q)
+        d_o = d_o.to(torch.bfloat16)
+        # (the backward of a concatenation hands out views of its buffer at any element; the kernels read 16 bytes at a time)
+        d_o = _match(d_o if d_o.data_ptr() % 16 == 0 else d_o.clone(), q)
         _b._same_layout(q, k, v, o, o_res, d_o)
         dq, dk, dv = _like(q), _like(q), _like(q)
         ws = torch.empty(lay.bwd_ws, dtype=torch.uint8, device=q.device)

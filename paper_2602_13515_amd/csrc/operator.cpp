@@ -47,6 +47,10 @@ Tensor match(const Tensor& x, const Tensor& ref) {
   return y;
 }
 
+// Whether x starts where the kernels read 16 bytes at a time.  (Upstream gradients need not: the backward of a concatenation
+// hands out views of its buffer at any element.)
+bool aligned(const Tensor& x) { return (reinterpret_cast<uintptr_t>(x.data_ptr()) & 15) == 0; }
+
 constexpr const char* ONE_LAYOUT = "all token tensors of one call share shape, strides, dtype and device";
 
 void same_layout(const Tensor& ref, std::initializer_list<const Tensor*> others) {
@@ -157,7 +161,7 @@ struct Attention : torch::autograd::Function<Attention> {
     const Tensor &q = saved[0], &k = saved[1], &v = saved[2], &o = saved[3], &o_res = saved[4], &lse = saved[5];
     check_saved(q, lse, ctx->saved_data["gpu"].toInt());
     const c10::DeviceGuard device(q.device());
-    const Tensor d_o = match(grads[0].to(at::kBFloat16), q);
+    const Tensor up = grads[0].to(at::kBFloat16), d_o = match(aligned(up) ? up : up.clone(), q);
     // (all of them, not d_o alone: saved-tensor hooks may bring a tensor back in another layout)
     same_layout(q, {&k, &v, &o, &o_res, &d_o});
     const spa2_shape s = shape_of(q);
@@ -261,10 +265,6 @@ std::array<int64_t, 3> strides_of(const Tensor& x) {
   for (int i = 0; i < 3; ++i) s[i] = x.size(i) > 1 ? x.stride(i) : 0;
   return s;
 }
-
-// Whether x starts where the kernels read 16 bytes at a time.  (Upstream gradients need not: the backward of a concatenation
-// hands out views of its buffer at any element.)
-bool aligned(const Tensor& x) { return (reinterpret_cast<uintptr_t>(x.data_ptr()) & 15) == 0; }
 
 // x in the memory order of ref (of another type maybe), from a 16-byte boundary.
 Tensor in_order(const Tensor& x, const Tensor& ref) {

@@ -74,3 +74,17 @@ def test_weights_of_the_norm(by):
         results.append([*(y.detach() for y in out), *torch.autograd.grad(out, weights, ups)])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("overlap", [False, True])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("by", [1, 4])
+def test_block_sparse_attention(by, given, overlap):
+    torch.manual_seed(by)
+    leaves = [_heads(1, 2, 300, 64).requires_grad_(True) for _ in range(3)]
+    pattern = spa2.build_pattern(leaves[0].detach(), leaves[1].detach(), 0.5, 0.5) if given else None
+    up = _heads(1, 2, 300, 64)
+    want, got = (torch.autograd.grad(spa2.sparge_attn2(*leaves, 0.5, 0.5, pattern=pattern, overlap_backward=overlap), leaves, g)
+                 for g in (up, _shifted(up, by)))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
