@@ -12,6 +12,8 @@
 // B-operand layout the second product wants, so P never leaves registers, and
 // the running maximum / sum of Alg. 1 (m_ij, l_ij) are per-lane scalars that
 // need one exchange between the two halves of the wave per tile.
+#include <float.h>
+
 #include "cross.h"
 #include "row_map.h"
 #include "spa2_device.h"
@@ -370,7 +372,9 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
     float mx = sA[0][0];
 #pragma unroll
     for (int v = 1; v < 32; ++v) mx = fmaxf(mx, sA[v / 16][v % 16]);
-    m_run = max_halves(mx) * a.scale_log2;
+    // (never minus infinity: where all scores are that so far, as products that overflow can be, their weights are
+    // 2^(-inf + FLT_MAX) = 0 and not 2^(-inf + inf); the first finite score rescales zeros)
+    m_run = fmaxf(max_halves(mx) * a.scale_log2, -FLT_MAX);
     raw_copies_left<CH>();
     __syncthreads();
   }
