@@ -65,7 +65,8 @@ def qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Te
     a multiple of 16 (None: no rotation); pair i is (i, i + r / 2), or (2 i, 2 i + 1) if `interleaved`.  positions: int32 or
     int64 [N] or [B, N], the row of the tables that a token uses (clamped to them); None: token n uses row n.
     Returns bf16 tensors of the shapes of q and k without gaps, tokens outside the heads where the inputs have them so: what
-    `sparge_attn2` and `cross_attention` take.  Gradients: q, k (in their type) and the weights."""
+    `sparge_attn2` and `cross_attention` take.  Gradients: q, k (in their type) and the weights; tables that require one, or
+    carry a tangent, are refused."""
     _refuse_others("qk_norm_rotate", q, k, q_weight, k_weight, cos, sin, positions)
     return _operator().norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, float(eps), bool(interleaved))
 

@@ -342,6 +342,8 @@ void norm_check(const Tensor& q, const Tensor& k, const Tensor& wq, const Tensor
     TORCH_CHECK_VALUE(!t->defined() || (t->scalar_type() == at::kFloat && t->dim() == 2 && t->sizes() == cos.sizes() &&
                                         t->is_contiguous() && t->device() == q.device()),
                       "cos and sin are contiguous fp32 tables [rows, rotated channels / 2] on the device of q");
+  for (const Tensor* t : {&cos, &sin})
+    TORCH_CHECK_VALUE(!t->defined() || !differentiated({t}), "cos and sin get no gradient: detach them");
   if (positions.defined()) {
     TORCH_CHECK_VALUE(cos.defined(), "positions without tables");
     TORCH_CHECK_VALUE((positions.scalar_type() == at::kInt || positions.scalar_type() == at::kLong) &&
