@@ -495,6 +495,14 @@ def spa2_vd_rescale(grad: torch.Tensor, weight: float, upstream: torch.Tensor) -
 
 
 # ------------------------------------------------------------------ around the attention
+def _one_gpu(x: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """Before a call: the kernels read and write every tensor at its address."""
+    if any(t is not None and t.device != x.device for t in others):
+        raise ValueError("all tensors of one call live on one GPU")
+    if not x.is_cuda:
+        raise ValueError("spa2 runs on the GPU only: tensors must be CUDA tensors")
+
+
 def _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, q_out, k_out):
     """The shape of a norm-and-rotate call (q_out, k_out: results of the forward call, or anything of their strides)."""
     for t in (q, k, q_out, k_out):
@@ -529,6 +537,7 @@ def _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, q_out
 
 def spa2_norm_rotate(q, k, q_weight, k_weight, cos, sin, positions, eps: float, interleaved: bool, q_out, k_out) -> None:
     s = _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, q_out, k_out)
+    _one_gpu(q, k, q_weight, k_weight, cos, sin, positions, q_out, k_out)
     if q_out.dtype != torch.bfloat16 or k_out.dtype != torch.bfloat16:
         raise ValueError("the results are bfloat16")
     _check(_load().spa2_norm_rotate(q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(cos), _ptr(sin),
@@ -544,6 +553,7 @@ def spa2_norm_rotate_bwd_workspace_bytes(q: torch.Tensor, k: torch.Tensor) -> in
 def spa2_norm_rotate_bwd(q, k, q_weight, k_weight, cos, sin, positions, d_q_out, d_k_out, eps: float, interleaved: bool,
                          dq, dk, d_q_weight=None, d_k_weight=None, workspace=None) -> None:
     s = _norm_args(q, k, q_weight, k_weight, cos, sin, positions, interleaved, d_q_out, d_k_out)
+    _one_gpu(q, k, q_weight, k_weight, cos, sin, positions, d_q_out, d_k_out, dq, dk, d_q_weight, d_k_weight, workspace)
     if d_q_out.dtype != torch.bfloat16 or d_k_out.dtype != torch.bfloat16:
         raise ValueError("the upstream gradients are bfloat16")
     for g, up, x in ((dq, d_q_out, q), (dk, d_k_out, k)):
@@ -566,8 +576,7 @@ def _cross_args(q, k, v, lengths, dk=None) -> _CrossShape:
         raise ValueError("k and v share shape and strides")
     if (k.shape[0], k.shape[3]) != (q.shape[0], q.shape[3]):
         raise ValueError("q and k share batch and head dimension")
-    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != q.shape[:1] or not lengths.is_contiguous()
-                                or lengths.device != q.device):
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != q.shape[:1] or not lengths.is_contiguous()):
         raise ValueError("lengths are int32 [B]")
     B, Hq, Nq, d = q.shape
     return _CrossShape(B, Hq, k.shape[1], Nq, k.shape[2], d, *q.stride()[:3], *k.stride()[:3], *(k if dk is None else dk).stride()[:3])
@@ -581,8 +590,15 @@ def spa2_cross_bwd_workspace_bytes(q, k) -> int:
     return int(_load().spa2_cross_bwd_workspace_bytes(ctypes.byref(_cross_args(q, k, k, None))))
 
 
+def _check_lse(q, lse) -> None:
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:3] or not lse.is_contiguous():
+        raise ValueError("the log-sum-exp is a contiguous float32 tensor [B, Hq, Nq]")
+
+
 def spa2_cross_fwd(q, k, v, lengths, scale: float, o, lse, o_res=None, workspace=None) -> None:
     s = _cross_args(q, k, v, lengths)
+    _one_gpu(q, k, v, lengths, o, o_res, lse, workspace)
+    _check_lse(q, lse)
     _same_layout(q, o, *([o_res] if o_res is not None else []))
     _check(_load().spa2_cross_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), ctypes.byref(s), float(scale),
                                   o.data_ptr(), _ptr(o_res), lse.data_ptr(), _ptr(workspace),
@@ -591,9 +607,12 @@ def spa2_cross_fwd(q, k, v, lengths, scale: float, o, lse, o_res=None, workspace
 
 def spa2_cross_bwd(q, k, v, lengths, o, d_o, lse, scale: float, dq, dk, dv, workspace, o_res=None) -> None:
     s = _cross_args(q, k, v, lengths, dk)
+    _one_gpu(q, k, v, lengths, o, o_res, d_o, lse, dq, dk, dv, workspace)
+    _check_lse(q, lse)
     _same_layout(q, o, d_o, dq, *([o_res] if o_res is not None else []))
-    if dk.shape != k.shape or dv.shape != k.shape or dk.stride() != dv.stride() or dk.dtype != k.dtype or dv.dtype != k.dtype:
-        raise ValueError("dk and dv have the shape and type of k and share strides")
+    if dk.shape != k.shape or dv.shape != k.shape or dk.stride() != dv.stride() or dk.dtype != k.dtype or dv.dtype != k.dtype \
+            or dk.stride(3) != 1:
+        raise ValueError("dk and dv have the shape and type of k and share strides, d contiguous")
     _check(_load().spa2_cross_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), o.data_ptr(), _ptr(o_res),
                                   d_o.data_ptr(), lse.data_ptr(), ctypes.byref(s), float(scale), dq.data_ptr(), dk.data_ptr(),
                                   dv.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream(q)), "spa2_cross_bwd")
@@ -604,7 +623,7 @@ def _drop_args(x, like, seed_offset) -> None:
         if t.dtype not in _VD_DTYPES or not t.is_contiguous() or t.shape != x.shape:
             raise ValueError("dropout takes contiguous bfloat16 or float32 tensors of one shape")
     if seed_offset is not None and (seed_offset.dtype != torch.int64 or seed_offset.numel() != 2
-                                    or not seed_offset.is_contiguous() or seed_offset.device != x.device):
+                                    or not seed_offset.is_contiguous()):
         raise ValueError("seed and offset on the device are two int64 numbers")
 
 
@@ -612,6 +631,7 @@ def spa2_dropout_add(x, residual, p: float, seed: int, offset: int, y, seed_offs
     _drop_args(x, y, seed_offset)
     if residual is not None:
         _drop_args(x, residual, None)
+    _one_gpu(x, residual, y, seed_offset)
     if y.dtype != (x if residual is None else residual).dtype:
         raise ValueError("y has the type of the residual, or x's without one")
     _check(_load().spa2_dropout_add(x.data_ptr(), _ptr(residual), x.numel(), _VD_DTYPES[x.dtype],
@@ -621,6 +641,7 @@ def spa2_dropout_add(x, residual, p: float, seed: int, offset: int, y, seed_offs
 
 def spa2_dropout_bwd(d_y, p: float, seed: int, offset: int, dx, seed_offset=None) -> None:
     _drop_args(d_y, dx, seed_offset)
+    _one_gpu(d_y, dx, seed_offset)
     _check(_load().spa2_dropout_bwd(d_y.data_ptr(), d_y.numel(), _VD_DTYPES[d_y.dtype], _VD_DTYPES[dx.dtype], float(p),
                                     seed % 2 ** 64, offset % 2 ** 64, _ptr(seed_offset), dx.data_ptr(), _stream(d_y)),
            "spa2_dropout_bwd")
