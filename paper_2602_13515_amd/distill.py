@@ -10,7 +10,7 @@ around its attention: the norm of q and k with the rotation by position, attenti
 from __future__ import annotations
 
 import copy
-from typing import Callable, Dict, Iterable, Optional, Sequence, Tuple
+from typing import Callable, Dict, Iterable, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -25,7 +25,8 @@ class ToyBlock(torch.nn.Module):
 
     grid: extents of the tokens' grid (frames, height, width): the heads of q and k are normed and rotated by position.
     context_dim: a second branch attends to `context` [B, M, context_dim], of which sample b has `lengths[b]` rows (a batch of
-    prompts, padded).  dropout: of both branches, in training mode; the masks' seed comes from PyTorch's default generator."""
+    prompts, padded).  dropout: of both branches, in training mode; the masks' seed comes from PyTorch's default generator, in
+    a captured step from the GPU's, so that every replay draws other masks."""
 
     def __init__(self, dim: int, heads: int, k_frac: Optional[float] = None, top_p: Optional[float] = None,
                  grid: Optional[Sequence[int]] = None, context_dim: Optional[int] = None, dropout: float = 0.0):
@@ -56,15 +57,26 @@ class ToyBlock(torch.nn.Module):
             _b.spa2_pattern_full(q.detach(), self._full)
         return sparge_attn2(q, k, v, 0.0, 0.0, pattern=self._full)
 
-    def _add(self, x: torch.Tensor, branch: torch.Tensor, seed: Optional[int], number: int) -> torch.Tensor:
+    def _seed(self, x: torch.Tensor) -> Union[None, int, torch.Tensor]:
+        """Of this call's masks: a number, or under capture, where that would be the same on every replay, a (seed, offset) on
+        the GPU for each of the two branches."""
+        if not self.training or self.dropout <= 0.0:
+            return None
+        if x.is_cuda and torch.cuda.is_current_stream_capturing():
+            return torch.randint(2 ** 63 - 1, (2, 2), device=x.device)
+        return int(torch.randint(2 ** 63 - 1, ()).item())
+
+    def _add(self, x: torch.Tensor, branch: torch.Tensor, seed: Union[None, int, torch.Tensor], number: int) -> torch.Tensor:
         """x plus a branch, dropped in places (each branch draws with an offset of its own)."""
-        return x + branch if seed is None else dropout_add(branch, x, self.dropout, seed, number)
+        if seed is None:
+            return x + branch
+        return dropout_add(branch, x, self.dropout, *((seed, number) if isinstance(seed, int) else (seed[number],)))
 
     def forward(self, x: torch.Tensor, context: Optional[torch.Tensor] = None,
                 lengths: Optional[torch.Tensor] = None) -> torch.Tensor:
         B, N, C = x.shape
         d = C // self.heads
-        seed = int(torch.randint(2 ** 63 - 1, ()).item()) if self.training and self.dropout > 0.0 else None
+        seed = self._seed(x)
         qkv = self.qkv(self.norm(x))
         if self.grid is None:
             qkv = qkv.to(torch.bfloat16).view(B, N, 3, self.heads, d)
