@@ -8,7 +8,8 @@
                      generator and never stored.
 
 They take plain CUDA tensors, in eager mode and under HIP graph capture; tracing, compilation and function transforms are
-refused.  The C entry points are in `binding` under their C names.
+refused, and so is a captured call with gradients while an eager graph of its inputs, made on the default stream, is alive
+(PyTorch would end the process in the captured backward pass).  The C entry points are in `binding` under their C names.
 """
 from __future__ import annotations
 

@@ -15,6 +15,8 @@
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
 
+#include <unordered_set>
+
 #include "spa2.h"
 
 namespace {
@@ -289,19 +291,29 @@ variable_list once(variable_list grads, bool graph, const char* name) {
 }
 
 // A backward pass that is captured while an eager graph of the same leaf lives would hand that leaf's gradient to the stream
-// the eager graph was made on, which breaks the capture and with it the process: refused here, before anything is captured.
-void capture_check(const Tensor& on, std::initializer_list<Tensor> leaves) {
+// the eager graph was made on.  If that is the default stream, which cannot take part in a capture, this breaks the capture and
+// with it the process: refused here, before anything is captured, for the inputs and all that they were computed from.
+// (Other streams are joined to the capture, as that of a warm-up whose loss is still held.)
+void capture_check(const Tensor& on, std::initializer_list<Tensor> inputs) {
   if (!at::GradMode::is_enabled()) return;
   const c10::DeviceGuard device(on.device());
   if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) return;
-  const c10::Stream now = c10::hip::getCurrentHIPStream().unwrap();
-  for (const Tensor& t : leaves) {
-    if (!t.defined() || !t.requires_grad() || !t.is_leaf()) continue;
-    const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
-    if (!node) continue;
+  const auto eager = c10::hip::getDefaultHIPStream();
+  std::vector<std::shared_ptr<torch::autograd::Node>> open;
+  std::unordered_set<const torch::autograd::Node*> seen;
+  auto visit = [&](const std::shared_ptr<torch::autograd::Node>& node) {
+    if (node && seen.insert(node.get()).second) open.push_back(node);
+  };
+  for (const Tensor& t : inputs)
+    if (t.defined() && t.requires_grad()) visit(t.is_leaf() ? torch::autograd::impl::try_get_grad_accumulator(t) : t.grad_fn());
+  while (!open.empty()) {
+    const std::shared_ptr<torch::autograd::Node> node = std::move(open.back());
+    open.pop_back();
     const auto made_on = node->stream();
-    TORCH_CHECK(!made_on || *made_on == now, "an eager graph of one of the inputs is still alive: let go of its outputs "
+    TORCH_CHECK(!made_on || made_on->id() != eager.id() || made_on->device_index() != eager.device_index(),
+                "an eager graph of one of the inputs, or of what they were computed from, is still alive: let go of its outputs "
                 "before capturing a backward pass (or capture without gradients)");
+    for (const auto& edge : node->next_edges()) visit(edge.function);
   }
 }
 
