@@ -83,8 +83,8 @@ inline CrossSection cross_dkdv_section(const CrossDims& m) {
 // Workspace of the forward pass: the pool.  Of the backward pass: D, LSE, counters of dK/dV, pools.
 constexpr int FEW_ROWS = 32;
 // Whether the rows that read a key head are so few that the kernel for few rows takes them (a wave's 32).  With 32 rows, us, that
-// kernel / the other: 8 samples of 8192 keys, 8 heads 54 / 74, d = 64 34 / 36; 64 samples of 512 26 / 27; 1 of 65,536, 2 heads 28 / 61;
-// 600 of 77, 4 heads, d = 64 20 / 22; 2 of 77, 40 heads 7.6 / 6.6; with one row 49 / 76, 30 / 36, 23 / 25, 25 / 59, 15 / 22, 6.1 / 6.2.
+// kernel / the other: 8 samples of 8192 keys, 8 heads 56 / 74, d = 64 34 / 36; 64 samples of 512 27 / 27; 1 of 65,536, 2 heads 29 / 61;
+// 600 of 77, 4 heads, d = 64 21 / 22; 2 of 77, 40 heads 8.1 / 6.6; with one row 50 / 76, 30 / 36, 24 / 25, 26 / 59, 16 / 22, 6.2 / 6.2.
 // The backward pass of such rows takes P and dS into their products in two bf16 parts: nothing averages over so few rows, and one
 // part leaves an error of dQ, dK and dV of sqrt(2), for single rows and keys up to 2.2, times that of their own rounding to bf16; two
 // leave that alone.  Two parts / one, us: 8 samples of 8192 keys, 8 heads of 32 rows 285 / 270, d = 64 109 / 97; 64 samples of 512, one

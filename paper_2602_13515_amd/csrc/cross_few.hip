@@ -13,9 +13,12 @@
 // others leaves a partial result.  (Cut by size alone, in equal parts of the longest sample, 280 to 576 workgroups of unlike
 // number on the compute units took 127 to 168 us on the first case below.)  Where there are many pairs, or short samples, a
 // workgroup takes one pair.
-// Measured, us: one query, 8 samples of 4095 to 32,760 keys and an empty one, 40 heads sharing 8, d = 128 114 (5.1 TB/s); all of 32,760
-// keys 188 (5.7 TB/s; the copies alone 182); 8 samples of 8192 keys, 8 heads 48, d = 64 30; 1 sample of 65,536, 2 heads 25;
-// 600 samples of 77, 4 heads, d = 64 15.
+// Measured, us: one query, seven samples of 8190 to 32,760 keys and an empty one, 40 heads sharing 8, d = 128 115 (5.1 TB/s); 8
+// samples of 32,760 keys 188 (5.7 TB/s; the copies alone 182); 8 samples of 8192 keys, 8 heads 50, d = 64 30; 1 sample of 65,536, 2
+// heads 26; 600 samples of 77, 4 heads, d = 64 16.
+// P goes into its product in two bf16 parts, as in the backward pass of such rows (cross.h): few sums average its rounding.  The
+// error of O is then that of its own rounding, where one part left 1.07 to 1.29 times that; the price is 0 to 1 us of the above, and
+// with 32 rows 55.3 / 55.7, d = 64 33.9 / 34.2, 28.0 / 28.9 and 20.1 / 20.6.
 #include "cross.h"
 #include "row_map.h"
 #include "spa2_device.h"
@@ -229,21 +232,26 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
         for (int v = 0; v < 16; ++v) oacc[mb][v] *= alpha;
       m_run = m_new;
     }
-    uint32_t pk[8];
+    uint32_t pk[8], rest[8];                             // P in two bf16 parts
     const float shift = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {                        // (the sum is taken over the rounded values: see fwd.hip)
-      pk[u] = pack_bf16(fast_exp2(fmaf(s[2 * u], a.scale_log2, -shift)), fast_exp2(fmaf(s[2 * u + 1], a.scale_log2, -shift)));
-      l_run = dot2_ones(pk[u], l_run);
+    for (int u = 0; u < 8; ++u) {
+      const float p0 = fast_exp2(fmaf(s[2 * u], a.scale_log2, -shift)), p1 = fast_exp2(fmaf(s[2 * u + 1], a.scale_log2, -shift));
+      pk[u] = pack_bf16(p0, p1);
+      rest[u] = pack_rest(p0, p1, pk[u]);
+      l_run += p0 + p1;
     }
     raw_copies_left<2 * NCP>();                          // and V
 #pragma unroll
     for (int cc = 0; cc < 2; ++cc) {
       const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pk[4 * cc], pk[4 * cc + 1], pk[4 * cc + 2], pk[4 * cc + 3]});
+      const bf16x8 p_rest = __builtin_bit_cast(bf16x8, u32x4{rest[4 * cc], rest[4 * cc + 1], rest[4 * cc + 2], rest[4 * cc + 3]});
 #pragma unroll
       for (int mb = 0; mb < NMB; ++mb) {
         const int o = cc * 16 * D * 2;
-        oacc[mb] = mfma32(join_tr(lds_tr4_at((v0 ^ (mb << 6)) + o), lds_tr4_at((v1 ^ (mb << 6)) + o)), p, oacc[mb]);
+        const bf16x8 x = join_tr(lds_tr4_at((v0 ^ (mb << 6)) + o), lds_tr4_at((v1 ^ (mb << 6)) + o));
+        oacc[mb] = mfma32(x, p, oacc[mb]);
+        oacc[mb] = mfma32(x, p_rest, oacc[mb]);
       }
     }
     copy_tile(min(t + 2, tiles - 1), stage);             // (the products above have read this stage)
