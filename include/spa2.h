@@ -280,8 +280,8 @@ int spa2_vd_rescale(void* grad, int64_t n, double weight, const double* upstream
  *   q, k        bf16 or fp32 (shape->dtype); element (b, h, n, c) at b*sb + h*sh + n*sn + c with strides of their own
  *               (q_*, k_*; 0 repeats an input), 16-byte aligned, strides multiples of 16 bytes.  Hq and Hk may differ.
  *   q_out, k_out  bf16, strides qo_*, ko_*.
- *   q_weight, k_weight  fp32 [d] or NULL (1).
- *   cos, sin    fp32 [table_rows, rot / 2] (NULL if rot = 0).
+ *   q_weight, k_weight  fp32 [d], 16-byte aligned, or NULL (1).
+ *   cos, sin    fp32 [table_rows, rot / 2], 16-byte aligned (NULL if rot = 0).
  *   positions   row of the tables of each token, [B, N] with batch stride pos_sb (0: all samples alike) and pos_bits 32 or
  *               64; values outside the tables are taken as the nearest row.  NULL (pos_bits 0): token n uses row n.
  * spa2_norm_rotate_bwd: gradients of q, k (dtype of q and k, in the strides of the outputs, as d_q_out and d_k_out are) and
@@ -315,7 +315,8 @@ int spa2_norm_rotate_bwd(const void* q, const void* k, const float* q_weight, co
  *   k, v                   of Hk heads and Nk tokens that share strides k_* (0 repeats a batch element or a head);
  *   dk, dv                 the same with strides d_* (which the other calls do not look at).
  *   lengths   device, int32 [B], clamped to [0, Nk]; NULL: Nk.  Keys and values behind a sample's length are not read.  A
- *             sample without keys gets O = 0, LSE = -infinity and zero gradients.
+ *             sample without keys gets O = 0, LSE = -infinity and zero gradients.  (Keys whose score is minus infinity take no
+ *             part; a row with no other gets NaN.)
  *   lse       fp32 [B, Hq, Nq];  o_res as in spa2_fwd (NULL if no backward pass follows, or with Nk <= 64: D of a sample
  *             of up to 64 keys is taken from its P and dP, and neither o nor o_res is read).
  * spa2_cross_bwd recomputes the probabilities from LSE and writes dq, dk and dv everywhere, zeros behind the lengths; dk and

@@ -62,9 +62,10 @@ def qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Te
 
     q [B, Hq, N, d], k [B, Hk, N, d]: bf16 or fp32 views with rows on 16-byte boundaries, d in {64, 128} contiguous; Hk may differ
     from Hq.
-    q_weight, k_weight [d]: bf16 or fp32, or None.  cos, sin: fp32 [rows, r / 2] for the rotation of the first r channels, r
-    a multiple of 16 (None: no rotation); pair i is (i, i + r / 2), or (2 i, 2 i + 1) if `interleaved`.  positions: int32 or
-    int64 [N] or [B, N], the row of the tables that a token uses (clamped to them); None: token n uses row n.
+    q_weight, k_weight [d]: bf16 or fp32, or None.  cos, sin: fp32 [rows, r / 2], contiguous from a 16-byte boundary, for the
+    rotation of the first r channels, r a multiple of 16 (None: no rotation); pair i is (i, i + r / 2), or (2 i, 2 i + 1) if
+    `interleaved`.  positions: contiguous int32 or int64 [N] or [B, N], the row of the tables that a token uses (clamped to them);
+    None: token n uses row n.
     Returns bf16 tensors of the shapes of q and k without gaps, tokens outside the heads where the inputs have them so: what
     `sparge_attn2` and `cross_attention` take.  Gradients: q, k (in their type) and the weights; tables that require one, or
     carry a tangent, are refused."""
@@ -78,8 +79,9 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: 
 
     q [B, Hq, Nq, d], k, v [B, Hk, Nk, d]: bf16 views with rows on 16-byte boundaries, d in {64, 128} contiguous; Hq is a multiple
     of Hk, and query head h reads key head h // (Hq // Hk).  Any Nq, Nk >= 1: one query against a long cache as well as many against a short prompt.
-    lengths: int32 [B] on the GPU, clamped to [0, Nk]; what lies behind them in k and v is not read, and a sample without
-    keys gives zeros and zero gradients.  scale: 1 / sqrt(d) if None.  Returns bf16 with q's shape (and memory order).
+    lengths: contiguous int32 [B] on the GPU, clamped to [0, Nk]; what lies behind them in k and v is not read, and a sample
+    without keys gives zeros and zero gradients.  (Keys whose score is minus infinity take no part; a row with no other is NaN, as
+    softmax has it.)  scale: 1 / sqrt(d) if None.  Returns bf16 with q's shape (and memory order).
     Gradients: q, k, v; those of k and v are zero behind the lengths and summed over the query heads in fp32.  (A q with gaps
     between its heads and v with other strides than k are copied first.)"""
     _refuse_others("cross_attention", q, k, v, lengths)

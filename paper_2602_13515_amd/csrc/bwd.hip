@@ -61,7 +61,7 @@ struct CrossDqArgs : DqArgs {
   float* delta_out; float* lse_out;      // D and LSE for the dK/dV kernel
   int32_t* zero; int zeros;   // arrival counters of the dK/dV launch
 };
-// The same with dS in two bf16 parts (cross_few).
+// The same with dS in two bf16 parts (cross_few).  (Many rows take one: the price of two is at CrossFwdArgs in fwd.hip.)
 struct CrossDqFineArgs : CrossDqArgs {
   static constexpr bool FINE = true;
 };

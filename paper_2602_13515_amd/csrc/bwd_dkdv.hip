@@ -40,7 +40,7 @@ struct CrossDkvArgs : DkvArgs {
   CrossKeys kv;
   int64_t dsb, dsh, dsn;      // strides of dK and dV
 };
-// The same with P and dS in two bf16 parts (cross_few).
+// The same with P and dS in two bf16 parts (cross_few).  (Many rows take one: the price of two is at CrossFwdArgs in fwd.hip.)
 struct CrossDkvFineArgs : CrossDkvArgs {
   static constexpr bool FINE = true;
 };

@@ -16,9 +16,9 @@
 // Measured, us: one query, seven samples of 8190 to 32,760 keys and an empty one, 40 heads sharing 8, d = 128 115 (5.1 TB/s); 8
 // samples of 32,760 keys 188 (5.7 TB/s; the copies alone 182); 8 samples of 8192 keys, 8 heads 50, d = 64 30; 1 sample of 65,536, 2
 // heads 26; 600 samples of 77, 4 heads, d = 64 16.
-// P goes into its product in two bf16 parts, as in the backward pass of such rows (cross.h): few sums average its rounding.  The
-// error of O is then that of its own rounding, where one part left 1.07 to 1.29 times that; the price is 0 to 1 us of the above, and
-// with 32 rows 55.3 / 55.7, d = 64 33.9 / 34.2, 28.0 / 28.9 and 20.1 / 20.6.
+// P goes into its product in two bf16 parts, as in the backward pass of such rows (cross.h): the matrix cores wait for the copies
+// anyway.  The error of O is then that of its own rounding, where one part left 1.07 to 1.29 times that; the price is 0 to 1 us of
+// the above, and with 32 rows, one part / two, 55.3 / 55.7, d = 64 33.9 / 34.2, 28.0 / 28.9 and 20.1 / 20.6.  (Many rows: fwd.hip.)
 #include "cross.h"
 #include "row_map.h"
 #include "spa2_device.h"

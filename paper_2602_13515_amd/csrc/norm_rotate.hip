@@ -11,8 +11,8 @@
 // the rotated channels turn theirs by an angle of zero.  A lane stays with its token and walks over heads: the cosines and
 // sines (4 bytes for each 2-byte channel of a head) are read once for its heads and held in registers.  A workgroup takes few
 // tokens and many of their heads, which lie next to each other in what a projection leaves.
-// Bound: HBM.  75,600 tokens, 40 heads, d = 128, bf16 561 us (5.6 TB/s); 32,760 tokens, 12 heads, fp32, forward 104, backward 178 us
-// (5.8, 5.7 TB/s) and 6 for the weights (with vectors of 8 channels of fp32, 32 bytes apart, 123 and 239).
+// Bound: HBM.  75,600 tokens, 40 heads, d = 128, bf16 567 us (5.5 TB/s); 32,760 tokens, 12 heads, fp32, forward 108, backward 183 us
+// (5.6, 5.5 TB/s) and 8 for the weights (with vectors of 8 channels of fp32, 32 bytes apart, 123 and 239).
 #include "block_ops.h"
 #include "spa2_device.h"
 
