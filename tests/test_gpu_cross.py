@@ -102,8 +102,8 @@ CASES = [
     (300, 1, 1, 1, 70, 64, None),
 ]
 CASES += [
-    # more rows than the chip holds at a time: a workgroup takes several, one after the other; lists of one block and more, odd and
-    # even, samples without keys, the last row of a head short, the last workgroup of a head with fewer rows
+    # more blocks of rows than the chip holds at a time; lists of one key block and more, odd and even, samples without keys, the
+    # last block of a head short
     (2, 8, 8, 9999, 50, 64, [50, 0]),
     (1, 6, 3, 15000, 130, 64, None),
     (3, 8, 4, 6401, 200, 128, [200, 64, 1]),
