@@ -355,6 +355,72 @@ int spa2_dropout_add(const void* x, const void* residual /* or NULL */, int64_t 
 int spa2_dropout_bwd(const void* d_y, int64_t n, int32_t y_dtype, int32_t x_dtype, double p, uint64_t seed, uint64_t offset,
                      const int64_t* seed_offset /* or NULL */, void* dx, void* stream);
 
+/* ---- a branch, normed and gated, added to the residual stream, and the norm of the sum, modulated ----
+ * What stands between two branches of a transformer block, for every token's row of `width` channels:
+ *   u = b * (mean b^2 + eps)^(-1/2) * w_b  (post; else u = b)       y = x + gate * u, rounded to x's type
+ *   h = (y - mean y) * (var y + eps)^(-1/2)  (SPA2_NORM_LAYER),  y * (mean y^2 + eps)^(-1/2)  (SPA2_NORM_RMS)
+ *   n = (h * weight + bias) * (1 + scale) + shift, rounded once
+ * The norm is that of y as it is stored.  Squares are summed in fp32 (rows whose squares overflow it, as NaN and infinities do,
+ * are lost); the deviation is taken about means, not as a difference of sums.
+ *   x, y        [samples, tokens, width] without gaps, bf16 or fp32 (x_dtype).
+ *   branch      the same shape, bf16 or x's type (branch_dtype), or NULL: y = x, and y is not written (may be NULL).
+ *   n           the same shape, bf16 or x's type (out_dtype); not written with SPA2_NORM_NONE (may be NULL).
+ *   params      vectors of `width` elements of one type (param_dtype), each or NULL (gate 1, weights 1, bias, scale and shift 0);
+ *               gate, scale, shift with an element stride between samples (gate_sb, ..., 0: one for all of them).
+ *   stats       fp32 [3][samples * tokens] (written), what the backward pass needs besides y; or NULL.
+ * All addresses are multiples of their elements' size; rows may start anywhere (width is any number up to SPA2_GATE_MAX_WIDTH).
+ * spa2_gate_norm_bwd: dy (x_dtype) and dn (out_dtype) are the upstream gradients of y and n (dy may be NULL: zero; dn is only
+ * read with a norm), y and stats those of the forward call (without a branch y is x).  dx and dbranch have x's and the branch's type
+ * and may be NULL (not wanted); so may the members of grads, which have the parameters' shapes and type.  Sums over tokens are
+ * taken in fp32 a workgroup and joined in fp64, in a fixed order.  Workspace of spa2_gate_norm_bwd_workspace_bytes(shape) bytes,
+ * 16-byte aligned, only needed for the parameters' gradients.
+ * Errors: SPA2_ERR_NULL, _SHAPE, _UNSUPPORTED (types, kind), _ALIGN, _RANGE (eps not finite or <= 0), _WORKSPACE, _LAUNCH; checked
+ * before anything is launched. */
+#define SPA2_NORM_NONE  0
+#define SPA2_NORM_LAYER 1
+#define SPA2_NORM_RMS   2
+#define SPA2_GATE_MAX_WIDTH 16384
+typedef struct spa2_gate_shape {
+  int64_t samples, tokens;
+  int64_t gate_sb, scale_sb, shift_sb;
+  int32_t width, kind, post;
+  int32_t x_dtype, branch_dtype, out_dtype, param_dtype;    /* SPA2_DTYPE_* */
+} spa2_gate_shape;
+typedef struct spa2_gate_params {
+  const void *gate, *branch_weight, *weight, *bias, *scale, *shift;      /* (branch_weight: only with post) */
+} spa2_gate_params;
+typedef struct spa2_gate_grads {
+  void *gate, *branch_weight, *weight, *bias, *scale, *shift;
+} spa2_gate_grads;
+size_t spa2_gate_norm_bwd_workspace_bytes(const spa2_gate_shape* shape);
+int spa2_gate_norm(const void* x, const void* branch, const spa2_gate_params* params, const spa2_gate_shape* shape, float eps,
+                   void* y, void* n, float* stats, void* stream);
+int spa2_gate_norm_bwd(const void* branch, const spa2_gate_params* params, const spa2_gate_shape* shape, float eps, const void* y,
+                       const void* dy, const void* dn, const float* stats, void* dx, void* dbranch,
+                       const spa2_gate_grads* grads /* or NULL */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- the norm over all gradients of a step, and the gradients scaled to a largest norm ----
+ *   norm = (sum over all gradients of x^2)^(1/2)        out = x * min(1, max_norm / (norm + eps))
+ *   gradients  HOST array of `count` entries, read during the call alone: device tensors without gaps of n >= 0 elements of
+ *              `dtype` (bf16 or fp32), at any element's address, and their results of `out_dtype`.  out may be x (with its type), or
+ *              NULL: the gradient counts towards the norm alone.  Nothing that is written may overlap anything else of the call.
+ *   max_norm   at least 0, or infinity: no limit.   eps: at least 0.
+ *   norm       device, one fp32 (written).
+ * Squares are taken and summed in fp64, in a fixed order; the product is taken in fp64 and rounded to out's type.  Where the
+ * factor is 1, gradients whose result lies in their own place are not touched.  An infinity or NaN among the gradients makes the
+ * norm one, and the formula is applied as it stands.  Workspace of spa2_clip_workspace_bytes() bytes, 16-byte aligned.
+ * Errors: SPA2_ERR_NULL, _SHAPE (count < 1, n < 0, more than 2^42 elements), _UNSUPPORTED (types), _ALIGN (an address that is no
+ * multiple of its elements' size), _RANGE (max_norm, eps), _WORKSPACE, _LAUNCH; checked before anything is launched. */
+typedef struct spa2_gradient {
+  const void* x;
+  void* out;
+  int64_t n;
+  int32_t dtype, out_dtype;            /* SPA2_DTYPE_* */
+} spa2_gradient;
+size_t spa2_clip_workspace_bytes(void);
+int spa2_clip_gradients(const spa2_gradient* gradients, int32_t count, double max_norm, double eps, float* norm,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

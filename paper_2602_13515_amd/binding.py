@@ -53,6 +53,20 @@ class _CrossShape(ctypes.Structure):
         + [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_sn", "k_sb", "k_sh", "k_sn", "d_sb", "d_sh", "d_sn")]
 
 
+class _GateShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("samples", "tokens", "gate_sb", "scale_sb", "shift_sb")] \
+        + [(n, ctypes.c_int32) for n in ("width", "kind", "post", "x_dtype", "branch_dtype", "out_dtype", "param_dtype")]
+
+
+class _GateParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "branch_weight", "weight", "bias", "scale", "shift")]
+
+
+class _Gradient(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -145,6 +159,17 @@ def _load():
     lib.spa2_dropout_add.argtypes = [vp, vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
     lib.spa2_dropout_bwd.restype = ctypes.c_int
     lib.spa2_dropout_bwd.argtypes = [vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
+    gsh, gpr = ctypes.POINTER(_GateShape), ctypes.POINTER(_GateParams)
+    lib.spa2_gate_norm_bwd_workspace_bytes.restype = sz
+    lib.spa2_gate_norm_bwd_workspace_bytes.argtypes = [gsh]
+    lib.spa2_gate_norm.restype = ctypes.c_int
+    lib.spa2_gate_norm.argtypes = [vp, vp, gpr, gsh, f32, vp, vp, vp, vp]
+    lib.spa2_gate_norm_bwd.restype = ctypes.c_int
+    lib.spa2_gate_norm_bwd.argtypes = [vp, gpr, gsh, f32, vp, vp, vp, vp, vp, vp, gpr, vp, sz, vp]
+    lib.spa2_clip_workspace_bytes.restype = sz
+    lib.spa2_clip_workspace_bytes.argtypes = []
+    lib.spa2_clip_gradients.restype = ctypes.c_int
+    lib.spa2_clip_gradients.argtypes = [ctypes.POINTER(_Gradient), i32, f64, f64, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -157,7 +182,9 @@ EXPORTED_SYMBOLS = ("spa2_version", "spa2_strerror", "spa2_topk_blocks", "spa2_m
                     "spa2_mask_fwd", "spa2_mask_fwd_workspace_bytes", "spa2_bwd_rows", "spa2_bwd_rows_workspace_bytes",
                     "spa2_vd_rescale", "spa2_norm_rotate", "spa2_norm_rotate_bwd", "spa2_norm_rotate_bwd_workspace_bytes",
                     "spa2_dropout_add", "spa2_dropout_bwd", "spa2_cross_fwd", "spa2_cross_bwd",
-                    "spa2_cross_fwd_workspace_bytes", "spa2_cross_bwd_workspace_bytes")
+                    "spa2_cross_fwd_workspace_bytes", "spa2_cross_bwd_workspace_bytes",
+                    "spa2_gate_norm", "spa2_gate_norm_bwd", "spa2_gate_norm_bwd_workspace_bytes",
+                    "spa2_clip_gradients", "spa2_clip_workspace_bytes")
 
 
 # ------------------------------------------------------------------ plumbing (memory only)
@@ -645,3 +672,98 @@ def spa2_dropout_bwd(d_y, p: float, seed: int, offset: int, dx, seed_offset=None
     _check(_load().spa2_dropout_bwd(d_y.data_ptr(), d_y.numel(), _VD_DTYPES[d_y.dtype], _VD_DTYPES[dx.dtype], float(p),
                                     seed % 2 ** 64, offset % 2 ** 64, _ptr(seed_offset), dx.data_ptr(), _stream(d_y)),
            "spa2_dropout_bwd")
+
+
+# ------------------------------------------------------------------ a training step around the attention
+NORM_KINDS = {None: 0, "layer": 1, "rms": 2}
+_GATE_PARAMS = tuple(n for n, _ in _GateParams._fields_)
+
+
+def _gate_args(x, branch, params, kind, out_dtype):
+    """x: any tensor of the shape and type of the residual stream.  params: gate, branch_weight, weight, bias, scale, shift."""
+    C = x.shape[-1] if x.dim() else 0
+    for t in (x, branch):
+        if t is not None and (t.dtype not in _VD_DTYPES or not t.is_contiguous() or t.shape != x.shape):
+            raise ValueError("the residual stream and the branch are contiguous bfloat16 or float32 tensors of one shape")
+    given = {n: t for n, t in zip(_GATE_PARAMS, params) if t is not None}
+    own = any(t.dim() == 2 for t in given.values())
+    for n, t in given.items():
+        if t.dtype not in _VD_DTYPES or not t.is_contiguous() or t.dtype != next(iter(given.values())).dtype:
+            raise ValueError("parameters are contiguous bfloat16 or float32 tensors of one type")
+        if t.shape != (C,) and not (n in ("gate", "scale", "shift") and x.dim() >= 2 and t.shape == (x.shape[0], C)):
+            raise ValueError("parameters are vectors [width]; gate, scale and shift also [samples, width]")
+    samples = x.shape[0] if own else 1
+    stride = lambda n: C if n in given and given[n].dim() == 2 else 0
+    pdt = _VD_DTYPES[next(iter(given.values())).dtype] if given else 1
+    s = _GateShape(samples, x.numel() // max(C * samples, 1), stride("gate"), stride("scale"), stride("shift"), C, NORM_KINDS[kind],
+                   int("branch_weight" in given), _VD_DTYPES[x.dtype], _VD_DTYPES[(x if branch is None else branch).dtype],
+                   _VD_DTYPES[out_dtype], pdt)
+    return s, _GateParams(*(_ptr(given.get(n)) for n in _GATE_PARAMS))
+
+
+def _gate_like(x, name, *others) -> None:
+    for t in others:
+        if t is not None and (t.shape != x.shape or not t.is_contiguous() or t.dtype not in _VD_DTYPES):
+            raise ValueError(f"{name} are contiguous and have the shape of x")
+
+
+def _gate_stats(s: _GateShape, stats) -> None:
+    if stats is not None and (stats.dtype != torch.float32 or stats.numel() != 3 * s.samples * s.tokens or not stats.is_contiguous()):
+        raise ValueError("stats are 3 * tokens contiguous float32 numbers")
+
+
+def spa2_gate_norm(x, branch, params, kind: Optional[str], eps: float, y, n, stats=None) -> None:
+    s, p = _gate_args(x, branch, params, kind, x.dtype if n is None else n.dtype)
+    _one_gpu(x, branch, *params, y, n, stats)
+    _gate_like(x, "results", y, n)
+    if y is not None and y.dtype != x.dtype:
+        raise ValueError("y has the type of x")
+    _gate_stats(s, stats)
+    _check(_load().spa2_gate_norm(x.data_ptr(), _ptr(branch), ctypes.byref(p), ctypes.byref(s), float(eps), _ptr(y), _ptr(n),
+                                  _ptr(stats), _stream(x)), "spa2_gate_norm")
+
+
+def spa2_gate_norm_bwd_workspace_bytes(x, branch, params, kind: Optional[str]) -> int:
+    s, _ = _gate_args(x, branch, params, kind, x.dtype)
+    return int(_load().spa2_gate_norm_bwd_workspace_bytes(ctypes.byref(s)))
+
+
+def spa2_gate_norm_bwd(branch, params, kind: Optional[str], eps: float, y, dy, dn, stats, dx=None, dbranch=None,
+                       grads=(None,) * 6, workspace=None) -> None:
+    """params, grads: gate, branch_weight, weight, bias, scale, shift and their gradients (None: not wanted)."""
+    s, p = _gate_args(y, branch, params, kind, y.dtype if dn is None else dn.dtype)
+    _one_gpu(y, branch, *params, dy, dn, stats, dx, dbranch, *grads, workspace)
+    _gate_like(y, "gradients", dy, dn, dx, dbranch)
+    if any(t is not None and t.dtype != y.dtype for t in (dy, dx)) or (dbranch is not None and dbranch.dtype != branch.dtype):
+        raise ValueError("gradients have the types of what they belong to")
+    for t, g in zip(params, grads):
+        if g is not None and (t is None or g.shape != t.shape or g.dtype != t.dtype or not g.is_contiguous()):
+            raise ValueError("gradients of the parameters have their shapes and type")
+    _gate_stats(s, stats)
+    d = _GateParams(*(_ptr(g) for g in grads))
+    _check(_load().spa2_gate_norm_bwd(_ptr(branch), ctypes.byref(p), ctypes.byref(s), float(eps), y.data_ptr(), _ptr(dy), _ptr(dn),
+                                      _ptr(stats), _ptr(dx), _ptr(dbranch), ctypes.byref(d), _ptr(workspace),
+                                      0 if workspace is None else _nbytes(workspace), _stream(y)), "spa2_gate_norm_bwd")
+
+
+def spa2_clip_workspace_bytes() -> int:
+    return int(_load().spa2_clip_workspace_bytes())
+
+
+def spa2_clip_gradients(gradients, outs, max_norm: float, eps: float, norm, workspace) -> None:
+    """outs: a result for each gradient (the gradient itself, or None: it counts towards the norm alone)."""
+    if not gradients or len(outs) != len(gradients):
+        raise ValueError("a result, or None, for each of at least one gradient")
+    for g, o in zip(gradients, outs):
+        if g.dtype not in _VD_DTYPES or not g.is_contiguous():
+            raise ValueError("gradients are contiguous bfloat16 or float32 tensors")
+        if o is not None and (o.dtype not in _VD_DTYPES or o.shape != g.shape or not o.is_contiguous()):
+            raise ValueError("results are contiguous bfloat16 or float32 tensors with the shapes of the gradients")
+    if norm.dtype != torch.float32 or norm.numel() != 1:
+        raise ValueError("norm is a float32 tensor of one element")
+    _one_gpu(gradients[0], *gradients, *outs, norm, workspace)
+    table = (_Gradient * len(gradients))(*(
+        _Gradient(g.data_ptr(), _ptr(o), g.numel(), _VD_DTYPES[g.dtype], _VD_DTYPES[(g if o is None else o).dtype])
+        for g, o in zip(gradients, outs)))
+    _check(_load().spa2_clip_gradients(table, len(gradients), float(max_norm), float(eps), norm.data_ptr(), workspace.data_ptr(),
+                                       _nbytes(workspace), _stream(gradients[0])), "spa2_clip_gradients")

@@ -5,7 +5,9 @@
 * `cross_attention`  beside it: dense attention to another sequence, a prompt or a cache, whose samples have lengths of
                      their own;
 * `dropout_add`      behind it: dropout of a branch and the sum with the residual stream, the mask drawn from a counter-based
-                     generator and never stored.
+                     generator and never stored;
+* `gate_add_norm`    between two branches: a branch, normed and gated, added to the residual stream, and the norm of the sum,
+                     modulated.
 
 They take plain CUDA tensors, in eager mode and under HIP graph capture; tracing, compilation and function transforms are
 refused, and so is a captured call with gradients while an eager graph of its inputs, made on the default stream, is alive
@@ -19,6 +21,7 @@ from typing import Optional, Sequence, Tuple, Union
 import torch
 
 from .autograd import _operator, _plain
+from .binding import NORM_KINDS
 
 
 def _refuse_others(name: str, *tensors: Optional[torch.Tensor]) -> None:
@@ -112,3 +115,25 @@ def dropout_add(x: torch.Tensor, residual: Optional[torch.Tensor], p: float, see
         raise ValueError("a seed on the device brings its offset along")
     return _operator().dropout_add(x, residual, float(p), 0 if on_device is not None else _signed(seed), _signed(offset),
                                    on_device)
+
+
+def gate_add_norm(x: torch.Tensor, branch: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                  branch_weight: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                  bias: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                  kind: Optional[str] = "layer", eps: float = 1e-6,
+                  dtype: Optional[torch.dtype] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """What stands between two branches of a block, in one pass: (y, n) with
+
+        u = branch * rsqrt(mean(branch^2) + eps) * branch_weight        (without branch_weight: the branch itself)
+        y = x + gate * u                                                 in x's type
+        n = norm(y) * weight + bias, times (1 + scale), plus shift       in `dtype`: x's (None) or bf16
+
+    norm: over the last dimension, "layer" (mean and deviation), "rms" (root mean square), or None: y alone, n is None.  It is that
+    of y as it is returned.  Without a branch y is x.
+    x [..., width], bf16 or fp32, width up to 16384; the branch has its shape, and its type or bf16 (tensors with gaps are copied
+    first).  Parameters: vectors [width], bf16 or fp32, each or None; gate, scale and shift also [samples, width] for x
+    [samples, ..., width].  Gradients: x, branch and the parameters, in their types."""
+    _refuse_others("gate_add_norm", x, branch, gate, branch_weight, weight, bias, scale, shift)
+    if kind not in NORM_KINDS:
+        raise ValueError('kind is "layer", "rms" or None')
+    return _operator().gate_add_norm(x, branch, gate, branch_weight, weight, bias, scale, shift, NORM_KINDS[kind], float(eps), dtype)

@@ -9,12 +9,14 @@
 // interpreter lock twice.  Here a pass allocates one buffer for the pattern (six tensors before) and one scratch buffer for
 // mask and forward, and the backward pass runs in the engine's thread without the interpreter: 90 us (82 with the
 // kernels as they are now).  24 heads of 1,281 tokens 223 -> 133 us (116); sampling on 1,000 tokens, two heads 46 -> 28 us (17).
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
 
+#include <algorithm>
 #include <unordered_set>
 
 #include "spa2.h"
@@ -617,6 +619,262 @@ Tensor dropout_add(const Tensor& x, const OptTensor& residual, double p, int64_t
   return DropoutAdd::apply(x, residual, p, seed, offset, seed_offset);
 }
 
+// ---- a branch, normed and gated, added to the residual stream, and the norm of the sum
+struct GateInputs {
+  Tensor x, branch, gate, branch_weight, weight, bias, scale, shift;      // (packed; parameters of one type)
+  int64_t kind = 0;
+  double eps = 0.0;
+  at::ScalarType out = at::kFloat;
+  std::array<const Tensor*, 6> params() const { return {&gate, &branch_weight, &weight, &bias, &scale, &shift}; }
+  bool normed() const { return kind != SPA2_NORM_NONE; }
+  spa2_gate_shape shape() const {
+    spa2_gate_shape s = {};
+    s.width = (int32_t)x.size(-1);
+    bool own = false;
+    for (const Tensor* t : {&gate, &scale, &shift}) own = own || (t->defined() && t->dim() == 2);
+    s.samples = own ? x.size(0) : 1;
+    s.tokens = x.numel() / (s.width * s.samples);
+    auto stride = [&](const Tensor& t) { return t.defined() && t.dim() == 2 ? (int64_t)s.width : 0; };
+    s.gate_sb = stride(gate); s.scale_sb = stride(scale); s.shift_sb = stride(shift);
+    s.kind = (int32_t)kind;
+    s.post = branch_weight.defined();
+    s.x_dtype = dtype_of(x);
+    s.branch_dtype = branch.defined() ? dtype_of(branch) : s.x_dtype;
+    s.out_dtype = out == at::kBFloat16 ? SPA2_DTYPE_BF16 : SPA2_DTYPE_F32;
+    s.param_dtype = SPA2_DTYPE_F32;
+    for (const Tensor* t : params()) if (t->defined()) s.param_dtype = dtype_of(*t);
+    return s;
+  }
+  spa2_gate_params pointers() const { return {ptr(gate), ptr(branch_weight), ptr(weight), ptr(bias), ptr(scale), ptr(shift)}; }
+  variable_list saved() const { return {branch, gate, branch_weight, weight, bias, scale, shift}; }
+};
+
+// (types of the parameters apart: see gate_add_norm)
+void gate_check(const GateInputs& g) {
+  TORCH_CHECK_VALUE(g.x.is_cuda(), "x must live on the GPU: the operator has no CPU path");
+  TORCH_CHECK_VALUE(float_kind(g.x) && g.x.dim() >= 1 && g.x.numel() > 0, "x is a bf16 or fp32 tensor [..., width] with elements");
+  const bool bf16 = g.x.scalar_type() == at::kBFloat16;
+  if (g.branch.defined())
+    TORCH_CHECK_VALUE(g.branch.sizes() == g.x.sizes() && g.branch.device() == g.x.device() &&
+                      (g.branch.scalar_type() == g.x.scalar_type() || g.branch.scalar_type() == at::kBFloat16),
+                      "the branch has the shape and device of x and its type, or bf16");
+  TORCH_CHECK_VALUE(g.branch.defined() || (!g.gate.defined() && !g.branch_weight.defined()), "a gate or a norm of the branch without a branch");
+  TORCH_CHECK_VALUE(g.branch.defined() || g.normed(), "neither a branch nor a norm");
+  TORCH_CHECK_VALUE(g.normed() || (!g.weight.defined() && !g.bias.defined() && !g.scale.defined() && !g.shift.defined()),
+                    "weight, bias, scale and shift belong to a norm");
+  TORCH_CHECK_VALUE(g.out == at::kBFloat16 || (g.out == at::kFloat && !bf16), "the norm is returned in the type of x, or bf16");
+  const int64_t width = g.x.size(-1);
+  for (const Tensor* t : g.params()) {
+    if (!t->defined()) continue;
+    const bool may_differ = t == &g.gate || t == &g.scale || t == &g.shift;
+    TORCH_CHECK_VALUE(float_kind(*t) && t->device() == g.x.device(), "parameters are bf16 or fp32, on the device of x");
+    TORCH_CHECK_VALUE((t->dim() == 1 && t->size(0) == width) ||
+                      (may_differ && t->dim() == 2 && g.x.dim() >= 2 && t->size(0) == g.x.size(0) && t->size(1) == width),
+                      "parameters are vectors [width]; gate, scale and shift also [samples, width]");
+  }
+}
+
+struct GateResult { Tensor y, n, stats; };
+GateResult gate_call(const GateInputs& g, bool training) {
+  const c10::DeviceGuard device(g.x.device());
+  const spa2_gate_shape s = g.shape();
+  const spa2_gate_params p = g.pointers();
+  GateResult r;
+  if (g.branch.defined()) r.y = at::empty_like(g.x);
+  if (g.normed()) r.n = at::empty(g.x.sizes(), g.x.options().dtype(g.out));
+  if (training) r.stats = at::empty({3, s.samples * s.tokens}, g.x.options().dtype(at::kFloat));
+  check(spa2_gate_norm(g.x.data_ptr(), ptr(g.branch), &p, &s, (float)g.eps, (void*)ptr(r.y), (void*)ptr(r.n), (float*)ptr(r.stats),
+                       stream_of(g.x)), "spa2_gate_norm");
+  return r;
+}
+
+struct GateAddNorm : torch::autograd::Function<GateAddNorm> {
+  // wants: bits of x, branch and the six parameters, in their order
+  static variable_list forward(AutogradContext* ctx, const Tensor& x, const OptTensor& branch, const OptTensor& gate,
+                               const OptTensor& branch_weight, const OptTensor& weight, const OptTensor& bias, const OptTensor& scale,
+                               const OptTensor& shift, int64_t kind, double eps, bool out32, int64_t wants) {
+    GateInputs g = {packed(x), or_none(branch), or_none(gate), or_none(branch_weight), or_none(weight), or_none(bias), or_none(scale),
+                    or_none(shift), kind, eps, out32 ? at::kFloat : at::kBFloat16};
+    if (g.branch.defined()) g.branch = packed(g.branch);
+    const GateResult r = gate_call(g, true);
+    variable_list saved = g.saved();
+    saved.push_back(r.y.defined() ? r.y : x.is_same(g.x) ? x : g.x);
+    saved.push_back(r.stats);
+    ctx->save_for_backward(std::move(saved));
+    ctx->saved_data["kind"] = kind;
+    ctx->saved_data["eps"] = eps;
+    ctx->saved_data["out32"] = out32;
+    ctx->saved_data["wants"] = wants;
+    ctx->set_materialize_grads(false);
+    variable_list out;
+    if (r.y.defined()) out.push_back(r.y);
+    if (r.n.defined()) out.push_back(r.n);
+    return out;
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool graph = at::GradMode::is_enabled();
+    const at::NoGradGuard no_graph;
+    const variable_list s = ctx->get_saved_variables();
+    // (the shape of x is that of y; what is not wanted of the norm, as nobody uses it, is left out)
+    GateInputs g = {s[7], s[0], s[1], s[2], s[3], s[4], s[5], s[6], ctx->saved_data["kind"].toInt(), ctx->saved_data["eps"].toDouble(),
+                    ctx->saved_data["out32"].toBool() ? at::kFloat : at::kBFloat16};
+    gate_check(g);
+    const Tensor &y = s[7], &stats = s[8];
+    const bool added = g.branch.defined();
+    Tensor dy = added ? grads[0] : Tensor(), dn = g.normed() ? grads[added ? 1 : 0] : Tensor();
+    const c10::DeviceGuard device(y.device());
+    for (const Tensor* t : {&dy, &dn})
+      TORCH_CHECK_VALUE(!t->defined() || (t->sizes() == y.sizes() && t->device() == y.device()), "saved tensors come back in their shapes on their GPU");
+    TORCH_CHECK_VALUE(y.is_contiguous() && (!added || g.branch.is_contiguous()) && stats.device() == y.device() && stats.is_contiguous() &&
+                      stats.scalar_type() == at::kFloat, "saved tensors come back contiguous on their GPU");
+    const bool normed = dn.defined();
+    if (dy.defined()) dy = dy.to(y.scalar_type()).contiguous();
+    if (normed) dn = dn.to(g.out).contiguous();
+    spa2_gate_shape shape = g.shape();
+    TORCH_CHECK_VALUE(stats.numel() == 3 * shape.samples * shape.tokens, "the statistics come back whole");
+    for (const Tensor* t : g.params())
+      TORCH_CHECK_VALUE(!t->defined() || (t->is_contiguous() && dtype_of(*t) == shape.param_dtype), "saved parameters come back contiguous, of one type");
+    if (!normed) shape.kind = SPA2_NORM_NONE;
+    const int64_t wants = ctx->saved_data["wants"].toInt();
+    auto made = [&](int bit, const Tensor& t) { return (wants >> bit & 1) && t.defined() ? at::empty_like(t) : Tensor(); };
+    Tensor dx = made(0, y), db = made(1, g.branch), dp[6];
+    bool any = false;
+    for (int i = 0; i < 6; ++i) {
+      if (i >= 2 && !normed) continue;
+      dp[i] = made(2 + i, *g.params()[i]);
+      any = any || dp[i].defined();
+    }
+    if (dy.defined() || normed) {
+      const spa2_gate_params p = g.pointers();
+      const spa2_gate_grads d = {(void*)ptr(dp[0]), (void*)ptr(dp[1]), (void*)ptr(dp[2]), (void*)ptr(dp[3]), (void*)ptr(dp[4]), (void*)ptr(dp[5])};
+      const Tensor ws = any ? bytes((int64_t)spa2_gate_norm_bwd_workspace_bytes(&shape), y) : Tensor();
+      check(spa2_gate_norm_bwd(ptr(g.branch), &p, &shape, (float)g.eps, y.data_ptr(), ptr(dy), ptr(dn), (const float*)stats.data_ptr(),
+                               (void*)ptr(dx), (void*)ptr(db), &d, (void*)ptr(ws), any ? (size_t)ws.numel() : 0, stream_of(y)),
+            "spa2_gate_norm_bwd");
+    } else {
+      dx = db = Tensor();
+      for (Tensor& t : dp) t = Tensor();
+    }
+    return once({dx, db, dp[0], dp[1], dp[2], dp[3], dp[4], dp[5], Variable(), Variable(), Variable(), Variable()}, graph, "gate_add_norm");
+  }
+};
+
+std::tuple<Tensor, OptTensor> gate_add_norm(const Tensor& x, const OptTensor& branch, const OptTensor& gate, const OptTensor& branch_weight,
+                                            const OptTensor& weight, const OptTensor& bias, const OptTensor& scale, const OptTensor& shift,
+                                            int64_t kind, double eps, const std::optional<at::ScalarType>& dtype) {
+  GateInputs g = {x, or_none(branch), or_none(gate), or_none(branch_weight), or_none(weight), or_none(bias), or_none(scale), or_none(shift),
+                  kind, eps, dtype.value_or(x.scalar_type())};
+  gate_check(g);
+  // parameters of one type: that of all of them, else fp32 (PyTorch differentiates the change)
+  bool bf16 = true, all32 = true;
+  for (const Tensor* t : g.params())
+    if (t->defined()) (t->scalar_type() == at::kBFloat16 ? all32 : bf16) = false;
+  for (Tensor* t : {&g.gate, &g.branch_weight, &g.weight, &g.bias, &g.scale, &g.shift})
+    if (t->defined()) *t = (bf16 || all32 ? *t : t->to(at::kFloat)).contiguous();
+  const Tensor* inputs[] = {&g.x, &g.branch, &g.gate, &g.branch_weight, &g.weight, &g.bias, &g.scale, &g.shift};
+  bool seen = false;
+  int64_t wants = 0;
+  for (int i = 0; i < 8; ++i) {
+    seen = seen || differentiated({inputs[i]});
+    if (inputs[i]->defined() && inputs[i]->requires_grad()) wants |= 1 << i;
+  }
+  if (!seen) {
+    g.x = packed(g.x);
+    if (g.branch.defined()) g.branch = packed(g.branch);
+    const GateResult r = gate_call(g, false);
+    return {r.y.defined() ? r.y : x, r.n.defined() ? OptTensor(r.n) : std::nullopt};
+  }
+  capture_check(x, {x, or_none(branch), or_none(gate), or_none(branch_weight), or_none(weight), or_none(bias), or_none(scale), or_none(shift)});
+  auto some = [](const Tensor& t) { return t.defined() ? OptTensor(t) : std::nullopt; };
+  const variable_list out = GateAddNorm::apply(x, branch, some(g.gate), some(g.branch_weight), some(g.weight), some(g.bias), some(g.scale),
+                                               some(g.shift), kind, eps, g.out == at::kFloat, wants);
+  if (!branch) return {x, out[0]};
+  return {out[0], out.size() > 1 ? OptTensor(out[1]) : std::nullopt};
+}
+
+// ---- the norm over all gradients, and the gradients scaled to a largest norm
+// Nothing that is written may overlap anything else of the call: two workgroups would work on it at a time.
+// (strided: results with gaps, which are written as a whole afterwards: they may lie between each other)
+void overlap_check(const std::vector<spa2_gradient>& gradients, const std::vector<Tensor>& strided) {
+  struct Range { uintptr_t begin, end; bool written; };
+  constexpr const char* SHARED = "a gradient that is written shares memory with another one of the call";
+  std::vector<Range> ranges;
+  auto add = [&](const void* p, int64_t n, int32_t dtype, bool written) {
+    if (n) ranges.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)n * (dtype == SPA2_DTYPE_BF16 ? 2 : 4), written});
+  };
+  for (const spa2_gradient& g : gradients) {
+    if (g.out != g.x || g.out_dtype != g.dtype) add(g.x, g.n, g.dtype, false);
+    if (g.out) add(g.out, g.n, g.out_dtype, true);
+  }
+  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t read = 0, written = 0;
+  for (const Range& r : ranges) {
+    TORCH_CHECK_VALUE(r.begin >= written && (!r.written || r.begin >= read), SHARED);
+    uintptr_t& end = r.written ? written : read;
+    end = std::max(end, r.end);
+  }
+  for (size_t i = 0; i < strided.size(); ++i) {
+    const Tensor& t = strided[i];
+    const uintptr_t begin = (uintptr_t)t.data_ptr();
+    uintptr_t end = begin + t.element_size();
+    for (int64_t d = 0; d < t.dim(); ++d) end += (uintptr_t)((t.size(d) - 1) * t.stride(d)) * t.element_size();
+    for (const Range& r : ranges) TORCH_CHECK_VALUE(r.end <= begin || r.begin >= end, SHARED);
+    for (size_t j = 0; j < i; ++j) TORCH_CHECK_VALUE(strided[j].data_ptr() != t.data_ptr(), SHARED);
+  }
+}
+
+Tensor clip_gradients(const std::vector<Tensor>& tensors, double max_norm, const std::optional<std::vector<Tensor>>& out, double eps,
+                      bool scaled) {
+  TORCH_CHECK_VALUE(!tensors.empty(), "at least one gradient");
+  TORCH_CHECK_VALUE(!out || out->size() == tensors.size(), "as many results as gradients");
+  const Tensor& first = tensors[0];
+  for (size_t i = 0; i < tensors.size(); ++i) {
+    const Tensor& t = tensors[i];
+    TORCH_CHECK_VALUE(t.is_cuda(), "gradients must live on the GPU: the operator has no CPU path");
+    TORCH_CHECK_VALUE(float_kind(t) && t.device() == first.device(), "gradients are bf16 or fp32, on one GPU");
+    TORCH_CHECK_VALUE(!differentiated({&t}), "clip_gradients gets no gradient: detach them, or call it without gradients");
+    if (!out) continue;
+    const Tensor& o = (*out)[i];
+    TORCH_CHECK_VALUE(float_kind(o) && o.sizes() == t.sizes() && o.device() == first.device(), "results have the shapes of the gradients and are bf16 or fp32, on their GPU");
+    TORCH_CHECK_VALUE(!differentiated({&o}), "clip_gradients gets no gradient: its results require none");
+  }
+  const at::NoGradGuard no_graph;
+  const c10::DeviceGuard device(first.device());
+  const int64_t ws_bytes = (int64_t)spa2_clip_workspace_bytes();
+  const Tensor ws = bytes(ws_bytes, first), norm = at::empty({}, first.options().dtype(at::kFloat));
+  std::vector<spa2_gradient> gradients(tensors.size());
+  std::vector<Tensor> held, strided;                   // copies of what has gaps, and where their results go
+  std::vector<std::pair<Tensor, Tensor>> back;
+  for (size_t i = 0; i < tensors.size(); ++i) {
+    const Tensor& t = tensors[i];
+    const Tensor target = !scaled ? Tensor() : out ? (*out)[i] : t;
+    Tensor x = t, o = target;
+    const bool in_place = o.defined() && o.is_same(t);
+    if (!t.is_non_overlapping_and_dense() || (o.defined() && !in_place && o.strides() != t.strides())) {
+      x = t.is_contiguous() ? t : t.contiguous();
+      if (!x.is_same(t)) held.push_back(x);
+      if (in_place) o = x;
+    }
+    if (o.defined() && !in_place && o.strides() != x.strides()) {
+      o = at::empty(x.sizes(), o.options());
+    }
+    if (target.defined()) at::assert_no_internal_overlap(target);
+    if (o.defined() && !o.is_same(target)) {
+      back.emplace_back(target, o);
+      if (target.numel()) strided.push_back(target);
+    }
+    gradients[i] = {x.data_ptr(), o.defined() ? o.data_ptr() : nullptr, x.numel(), dtype_of(x), dtype_of(o.defined() ? o : x)};
+  }
+  overlap_check(gradients, strided);
+  if (scaled)                                          // (what autograd has saved of them is no longer what it was)
+    for (size_t i = 0; i < tensors.size(); ++i) (out ? (*out)[i] : tensors[i]).unsafeGetTensorImpl()->bump_version();
+  check(spa2_clip_gradients(gradients.data(), (int32_t)gradients.size(), max_norm, eps, (float*)norm.data_ptr(), ws.data_ptr(),
+                            (size_t)ws_bytes, stream_of(first)), "spa2_clip_gradients");
+  for (const auto& [to, from] : back) to.copy_(from);
+  return norm;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -624,5 +882,7 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("norm_rotate", &norm_rotate, py::call_guard<py::gil_scoped_release>());
   m.def("cross_attention", &cross_attention, py::call_guard<py::gil_scoped_release>());
   m.def("dropout_add", &dropout_add, py::call_guard<py::gil_scoped_release>());
+  m.def("gate_add_norm", &gate_add_norm, py::call_guard<py::gil_scoped_release>());
+  m.def("clip_gradients", &clip_gradients, py::call_guard<py::gil_scoped_release>());
   m.def("velocity_loss", &velocity_loss, py::call_guard<py::gil_scoped_release>());
 }

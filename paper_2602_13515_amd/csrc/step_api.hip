@@ -1,0 +1,115 @@
+// Entry points of the operators of a training step around the attention: argument checks, then the launches.
+#include "spa2_check.h"
+#include "step_ops.h"
+
+using namespace spa2;
+
+namespace {
+
+bool dtype_ok(int32_t t) { return t == SPA2_DTYPE_BF16 || t == SPA2_DTYPE_F32; }
+uintptr_t element_size(int32_t t) { return t == SPA2_DTYPE_BF16 ? 2 : 4; }
+
+
+constexpr int64_t GATE_MAX_SAMPLES = 1 << 22, GATE_MAX_ROWS = (int64_t)1 << 40;
+
+int check_gate_shape(const spa2_gate_shape* s) {
+  if (!s) return SPA2_ERR_NULL;
+  if (s->samples <= 0 || s->samples > GATE_MAX_SAMPLES || s->tokens <= 0 || s->tokens > GATE_MAX_ROWS / s->samples ||
+      s->width <= 0 || s->width > SPA2_GATE_MAX_WIDTH)
+    return SPA2_ERR_SHAPE;
+  for (const int64_t sb : {s->gate_sb, s->scale_sb, s->shift_sb})
+    if (sb && (sb < s->width || sb > GATE_MAX_ROWS)) return SPA2_ERR_SHAPE;
+  if (s->kind != SPA2_NORM_NONE && s->kind != SPA2_NORM_LAYER && s->kind != SPA2_NORM_RMS) return SPA2_ERR_UNSUPPORTED;
+  if (!dtype_ok(s->x_dtype) || !dtype_ok(s->branch_dtype) || !dtype_ok(s->out_dtype) || !dtype_ok(s->param_dtype))
+    return SPA2_ERR_UNSUPPORTED;
+  for (const int32_t t : {s->branch_dtype, s->out_dtype})
+    if (t != s->x_dtype && t != SPA2_DTYPE_BF16) return SPA2_ERR_UNSUPPORTED;
+  return SPA2_OK;
+}
+
+bool off_element(const void* p, int32_t dtype) { return (uintptr_t)p % element_size(dtype); }
+
+int check_gate(const void* branch, const spa2_gate_params* p, const spa2_gate_shape* s, float eps) {
+  const int rc = check_gate_shape(s);
+  if (rc != SPA2_OK) return rc;
+  if (!p) return SPA2_ERR_NULL;
+  if (off_element(branch, s->branch_dtype)) return SPA2_ERR_ALIGN;
+  for (const void* x : {p->gate, p->branch_weight, p->weight, p->bias, p->scale, p->shift})
+    if (off_element(x, s->param_dtype)) return SPA2_ERR_ALIGN;
+  if (!(eps > 0.f) || !isfinite(eps)) return SPA2_ERR_RANGE;
+  return SPA2_OK;
+}
+
+// what a call without a branch, or without its norm, does not look at
+spa2_gate_params used_params(const spa2_gate_params& p, const spa2_gate_shape& s) { return {p.gate, s.post ? p.branch_weight : nullptr, p.weight, p.bias, p.scale, p.shift}; }
+
+}  // namespace
+
+extern "C" {
+
+size_t spa2_gate_norm_bwd_workspace_bytes(const spa2_gate_shape* shape) {
+  if (check_gate_shape(shape) != SPA2_OK) return 0;
+  return round256(gate_partials_bytes(*shape));
+}
+
+int spa2_gate_norm(const void* x, const void* branch, const spa2_gate_params* params, const spa2_gate_shape* shape, float eps,
+                   void* y, void* n, float* stats, void* stream) {
+  const int rc = check_gate(branch, params, shape, eps);
+  if (rc != SPA2_OK) return rc;
+  if (!x || (branch && !y) || (shape->kind != SPA2_NORM_NONE && !n)) return SPA2_ERR_NULL;
+  if (off_element(x, shape->x_dtype) || off_element(y, shape->x_dtype) || off_element(n, shape->out_dtype) || (uintptr_t)stats % 4)
+    return SPA2_ERR_ALIGN;
+  return launch_gate_norm(x, branch, used_params(*params, *shape), *shape, eps, y, n, stats, (hipStream_t)stream) == hipSuccess
+             ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
+
+int spa2_gate_norm_bwd(const void* branch, const spa2_gate_params* params, const spa2_gate_shape* shape, float eps, const void* y,
+                       const void* dy, const void* dn, const float* stats, void* dx, void* dbranch, const spa2_gate_grads* grads,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_gate(branch, params, shape, eps);
+  if (rc != SPA2_OK) return rc;
+  const bool normed = shape->kind != SPA2_NORM_NONE;
+  if ((normed && (!y || !dn)) || ((normed || (branch && shape->post)) && !stats) || (!normed && !dy)) return SPA2_ERR_NULL;
+  if (off_element(y, shape->x_dtype) || off_element(dy, shape->x_dtype) || off_element(dn, shape->out_dtype) ||
+      (uintptr_t)stats % 4 || off_element(dx, shape->x_dtype) || off_element(dbranch, shape->branch_dtype))
+    return SPA2_ERR_ALIGN;
+  spa2_gate_grads g = {};
+  if (grads) g = *grads;
+  if (!branch) { dbranch = nullptr; g.gate = g.branch_weight = nullptr; }
+  if (!shape->post) g.branch_weight = nullptr;
+  if (!normed) g.weight = g.bias = g.scale = g.shift = nullptr;
+  bool any = false;
+  for (const void* x : {g.gate, g.branch_weight, g.weight, g.bias, g.scale, g.shift}) {
+    if (off_element(x, shape->param_dtype)) return SPA2_ERR_ALIGN;
+    any = any || x;
+  }
+  if (any && (!workspace || workspace_bytes < gate_partials_bytes(*shape))) return SPA2_ERR_WORKSPACE;
+  if (any && !aligned16(workspace)) return SPA2_ERR_ALIGN;
+  return launch_gate_norm_bwd(branch, used_params(*params, *shape), *shape, eps, y, dy, dn, stats, dx, dbranch, g, workspace,
+                              (hipStream_t)stream) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
+
+size_t spa2_clip_workspace_bytes(void) { return round256(clip_partials_bytes()); }
+
+int spa2_clip_gradients(const spa2_gradient* gradients, int32_t count, double max_norm, double eps, float* norm,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (!gradients || !norm) return SPA2_ERR_NULL;
+  if (count < 1) return SPA2_ERR_SHAPE;
+  int64_t left = (int64_t)1 << 42;       // (chunks are numbered in 32 bits)
+  for (int32_t g = 0; g < count; ++g) {
+    const spa2_gradient& x = gradients[g];
+    if (x.n < 0 || x.n > left) return SPA2_ERR_SHAPE;
+    left -= x.n;
+    if (!dtype_ok(x.dtype) || (x.out && !dtype_ok(x.out_dtype))) return SPA2_ERR_UNSUPPORTED;
+    if (x.n && !x.x) return SPA2_ERR_NULL;
+    if ((uintptr_t)x.x % element_size(x.dtype) || (x.out && (uintptr_t)x.out % element_size(x.out_dtype))) return SPA2_ERR_ALIGN;
+    if (x.out && x.out == x.x && x.out_dtype != x.dtype) return SPA2_ERR_UNSUPPORTED;
+  }
+  if ((uintptr_t)norm % 4) return SPA2_ERR_ALIGN;
+  if (!(max_norm >= 0.0) || !(eps >= 0.0) || !isfinite(eps)) return SPA2_ERR_RANGE;
+  if (!workspace || workspace_bytes < clip_partials_bytes()) return SPA2_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return SPA2_ERR_ALIGN;
+  return launch_clip(gradients, count, max_norm, eps, norm, workspace, (hipStream_t)stream) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,41 @@
+"""The gradients of a training step as a whole: their norm, and clipping to a largest norm, in two passes over all of them.
+
+They take plain CUDA tensors, in eager mode and under HIP graph capture (a captured call works on the memory that the tensors had
+then)."""
+from __future__ import annotations
+
+import math
+from typing import Iterable, Optional, Union
+
+import torch
+
+from .autograd import _operator
+from .block import _refuse_others
+
+Gradients = Union[torch.Tensor, Iterable[torch.Tensor]]
+
+
+def _list(name: str, tensors: Gradients) -> list:
+    tensors = [tensors] if isinstance(tensors, torch.Tensor) else list(tensors)
+    if not tensors:
+        raise ValueError(f"{name} takes at least one tensor")
+    _refuse_others(name, *tensors)
+    return tensors
+
+
+def clip_gradients(tensors: Gradients, max_norm: float, out: Optional[Gradients] = None, eps: float = 1e-6) -> torch.Tensor:
+    """Scales all tensors by min(1, max_norm / (norm + eps)), norm being the 2-norm over all their elements, and returns it: fp32,
+    on the GPU, without waiting for it.
+
+    tensors: bf16 and fp32, on one GPU, of any sizes.  out: None (in place; nothing is touched where the factor is 1), or a tensor of
+    the same shape for each, bf16 or fp32 whatever its gradient is (an fp32 optimizer's, say).  No memory that is written may be
+    shared between two of them: a tensor that is listed twice is refused.  (Tensors with gaps are copied, and back.)
+    max_norm: at least 0; infinity scales nothing.  Sums are taken in fp64.  An infinity or NaN makes the norm one, and the
+    formula is applied as it stands.  There is no gradient: tensors that require one are refused outside torch.no_grad()."""
+    tensors = _list("clip_gradients", tensors)
+    return _operator().clip_gradients(tensors, float(max_norm), None if out is None else _list("clip_gradients", out), float(eps), True)
+
+
+def gradient_norm(tensors: Gradients) -> torch.Tensor:
+    """The 2-norm over all elements of all tensors, as `clip_gradients` takes it."""
+    return _operator().clip_gradients(_list("gradient_norm", tensors), math.inf, None, 0.0, False)

@@ -1,0 +1,342 @@
+"""The gated sum with its norms, forward and backward, against the fp64 formulas (bounds: step_ref)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_13515_amd as spa2
+import step_ref as ref
+from gpu_util import Guarded, dev
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+NAMES = ("gate", "branch_weight", "weight", "bias", "scale", "shift")
+EPS = 1e-5
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def half(t):
+    return ref.HALF[str(t.dtype).split(".")[1]]
+
+
+def _params(g, shapes, C, dtype):
+    """Parameters of the names in `shapes`: "C" one for all samples, a number: one for each of so many."""
+    out = {}
+    for name, of in shapes.items():
+        base = 1.0 if name in ("weight", "branch_weight") else 0.0
+        size = (C,) if of == "C" else (of, C)
+        out[name] = (base + 0.4 * torch.randn(size, generator=g)).to(dtype).to(dev())
+    return out
+
+
+def _wide(params, name, otherwise):
+    p = params.get(name)
+    if p is None:
+        return otherwise
+    p = f64(p)
+    return p if p.ndim == 1 else p[:, None]
+
+
+def _compare(got, want, bound, where):
+    x = f64(got)
+    assert np.isfinite(x).all(), where
+    limit = bound * (1 + half(got)) + half(got) * np.abs(want) + 1e-37
+    err = np.abs(x - want)
+    assert (err <= limit).all(), (where, err.max(), (err / limit).max())
+
+
+def _check(x, branch, params, kind, dtype, dy, dn, eps=EPS):
+    """Values and gradients of one call; x [B, N, C]."""
+    B, N, C = x.shape
+    with torch.no_grad():
+        plain = spa2.gate_add_norm(x, branch, **params, kind=kind, eps=eps, dtype=dtype)
+    leaves = {"x": x.detach().requires_grad_(True)}
+    if branch is not None:
+        leaves["branch"] = branch.detach().requires_grad_(True)
+    leaves.update({n: p.detach().requires_grad_(True) for n, p in params.items()})
+    y, n = spa2.gate_add_norm(leaves["x"], leaves.get("branch"), **{k: v for k, v in leaves.items() if k in NAMES}, kind=kind, eps=eps,
+                              dtype=dtype)
+    assert torch.equal(y, plain[0]) and (n is None) == (kind is None) and (n is None or torch.equal(n, plain[1]))
+    gate, post = _wide(params, "gate", 1.0), _wide(params, "branch_weight", None)
+    affine = [_wide(params, name, o) for name, o in (("weight", 1.0), ("bias", 0.0), ("scale", 0.0), ("shift", 0.0))]
+    if branch is None:
+        assert y is leaves["x"] or torch.equal(y, x)
+    else:
+        want, _, _, off = ref.gate_sum(f64(x), f64(branch), gate, post, eps)
+        assert y.dtype == x.dtype and y.shape == x.shape
+        _compare(y, want, off, "y")
+    if kind is not None:
+        want, _, _, _, off = ref.gate_norm(f64(y), kind, *affine, eps)
+        assert n.dtype == (dtype or x.dtype)
+        _compare(n, want, off, "n")
+    outs, ups = [], []
+    for o, up in ((y, dy), (n, dn)):
+        if o is not None and up is not None and o is not leaves["x"]:
+            outs.append(o)
+            ups.append(up)
+    grads = torch.autograd.grad(outs, list(leaves.values()), ups, allow_unused=True)
+    again = torch.autograd.grad(spa2.gate_add_norm(leaves["x"], leaves.get("branch"), **{k: v for k, v in leaves.items() if k in NAMES},
+                                                   kind=kind, eps=eps, dtype=dtype)[0 if kind is None else 1],
+                                list(leaves.values()), dy if kind is None else dn, allow_unused=True) if len(outs) == 1 and kind is not None \
+        and dn is not None else None
+    if again is not None:
+        for a, b in zip(grads, again):
+            assert a is b or torch.equal(a, b)
+    up_y = None if dy is None or branch is None else f64(dy)
+    want = ref.gate_bwd(f64(y), None if branch is None else f64(branch), gate, post, kind, *affine, eps, up_y,
+                        None if kind is None or dn is None else f64(dn))
+    for name, t in zip(leaves, grads):
+        if name not in want:
+            assert t is None, name
+            continue
+        value, off = want[name]
+        if name in NAMES and leaves[name].dim() == 1:
+            value, off = value.sum(0), off.sum(0)
+        assert t.dtype == leaves[name].dtype and t.shape == leaves[name].shape, name
+        _compare(t, value, off + ref.SMALL * np.abs(value), name)
+    return y, n, grads
+
+
+TYPES = [(BF, BF, BF), (F32, F32, F32), (F32, F32, BF), (F32, BF, F32), (F32, BF, BF)]
+ALL = {"gate": "C", "branch_weight": "C", "weight": "C", "bias": "C", "scale": "C", "shift": "C"}
+
+
+def _data(B, N, C, types, seed, offset=0.5):
+    g = torch.Generator().manual_seed(seed + 1000 * C + 10 * N + B)
+    x = (2 * torch.randn((B, N, C), generator=g) + offset).to(types[0]).to(dev())
+    branch = torch.randn((B, N, C), generator=g).to(types[1]).to(dev())
+    dy, dn = torch.randn((B, N, C), generator=g).to(types[0]).to(dev()), torch.randn((B, N, C), generator=g).to(types[2]).to(dev())
+    return g, x, branch, dy, dn
+
+
+@pytest.mark.parametrize("types", TYPES, ids=lambda t: "-".join(str(x).split(".")[1] for x in t))
+@pytest.mark.parametrize("C", [1, 2, 7, 8, 9, 64, 511, 512, 513, 1024, 1281, 1536, 5120, 8191, 8192, 8193, 16384])
+def test_widths_and_types(C, types):
+    g, x, branch, dy, dn = _data(2, 3, C, types, 0)
+    post = C % 3 != 0
+    shapes = {"gate": 2, "weight": "C", "bias": "C", "scale": 2, "shift": 2, **({"branch_weight": "C"} if post else {})}
+    kind = "rms" if C % 2 and C > 1 else "layer"
+    _check(x, branch, _params(g, shapes, C, types[0]), kind, types[2], dy, dn)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms", None])
+@pytest.mark.parametrize("given", ["", "gate", "gate branch_weight", "weight", "weight bias", "scale shift", "gate branch_weight weight bias scale shift"])
+@pytest.mark.parametrize("own", [False, True])
+def test_any_of_the_parameters(kind, given, own):
+    names = [n for n in given.split() if kind is not None or n in ("gate", "branch_weight")]
+    g, x, branch, dy, dn = _data(3, 5, 264, (F32, BF, BF), 1)
+    shapes = {n: 3 if own and n in ("gate", "scale", "shift") else "C" for n in names}
+    _check(x, branch, _params(g, shapes, 264, F32), kind, BF, dy, dn)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("C", [96, 1283])
+def test_without_a_branch(kind, own, C):
+    g, x, _, dy, dn = _data(3, 5, C, (BF, BF, BF), 2)
+    shapes = {"weight": "C", "bias": "C", "scale": 3 if own else "C", "shift": 3 if own else "C"}
+    _check(x, None, _params(g, shapes, C, BF), kind, None, dy, dn)
+
+
+@pytest.mark.parametrize("B,N,C", [(1, 1, 256), (1, 4097, 128), (1, 3000, 1537), (700, 1, 72), (64, 77, 96), (5, 1281, 40), (2, 900, 8200)])
+@pytest.mark.parametrize("own", [False, True])
+def test_samples_and_tokens(B, N, C, own):
+    g, x, branch, dy, dn = _data(B, N, C, (F32, F32, F32), 3)
+    shapes = {**ALL, **({"gate": B, "scale": B, "shift": B} if own else {})}
+    _check(x, branch, _params(g, shapes, C, F32), "layer", None, dy, dn)
+
+
+def test_parameters_of_unlike_kinds():
+    """One vector of a sample's own among shared ones; types that differ."""
+    g, x, branch, dy, dn = _data(4, 6, 200, (F32, F32, F32), 4)
+    for own in ("gate", "scale", "shift"):
+        p = _params(g, {**ALL, own: 4}, 200, F32)
+        _check(x, branch, p, "layer", None, dy, dn)
+    p["weight"], p["gate"] = p["weight"].bfloat16(), p["gate"].bfloat16()
+    _check(x, branch, p, "layer", None, dy, dn)
+
+
+@pytest.mark.parametrize("use", ["y", "n"])
+@pytest.mark.parametrize("post", [False, True])
+def test_one_result_unused(use, post):
+    g, x, branch, dy, dn = _data(2, 9, 320, (BF, BF, BF), 5)
+    shapes = {"gate": "C", "weight": "C", **({"branch_weight": "C"} if post else {})}
+    _check(x, branch, _params(g, shapes, 320, BF), "rms", None, dy if use == "y" else None, dn if use == "n" else None)
+
+
+def test_frozen_inputs_get_no_gradient_and_change_no_other():
+    g, x, branch, dy, dn = _data(2, 9, 320, (F32, F32, F32), 6)
+    p = _params(g, {**ALL, "scale": 2}, 320, F32)
+    leaves = {"x": x, "branch": branch, **p}
+
+    def grads(wanted):
+        t = {n: v.detach().requires_grad_(n in wanted) for n, v in leaves.items()}
+        y, n = spa2.gate_add_norm(t["x"], t["branch"], **{k: t[k] for k in p}, eps=EPS)
+        torch.autograd.backward([y, n], [dy, dn])
+        return {k: v.grad for k, v in t.items()}
+    every = grads(set(leaves))
+    for wanted in ({"x"}, {"branch"}, {"gate", "shift"}, {"weight"}, {"scale", "branch_weight", "x"}):
+        some = grads(wanted)
+        for name in leaves:
+            assert (some[name] is not None) == (name in wanted)
+            if name in wanted:
+                assert torch.equal(some[name], every[name]), name
+
+
+def test_layouts_and_addresses():
+    """Tensors with gaps, transposed, from any element on; upstream gradients broadcast and misaligned."""
+    g, x, branch, dy, dn = _data(2, 6, 137, (F32, BF, BF), 7)
+    p = _params(g, ALL, 137, F32)
+    base = [t.clone() for t in spa2.gate_add_norm(x, branch, **p, eps=EPS, dtype=BF)]
+    odd = lambda t: torch.cat((torch.zeros(1, dtype=t.dtype, device=t.device), t.reshape(-1)))[1:].view(t.shape)
+    gaps = lambda t: torch.stack((t, torch.full_like(t, float("nan"))), 2)[:, :, 0]
+    turned = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)
+    for f in (odd, gaps, turned):
+        q = {n: odd(v) for n, v in p.items()}
+        got = spa2.gate_add_norm(f(x), f(branch), **q, eps=EPS, dtype=BF)
+        assert all(torch.equal(a, b) for a, b in zip(got, base)), f
+        _check(f(x), f(branch), q, "layer", BF, f(dy), f(dn))
+    one = torch.randn(137, device=dev())
+    _check(x, branch, p, "layer", BF, one.expand(2, 6, 137), one.to(BF).expand(2, 6, 137))
+    two = [t.reshape(12, 137) for t in (x, branch)]                   # a token a row
+    got = spa2.gate_add_norm(*two, **p, eps=EPS, dtype=BF)
+    assert all(torch.equal(a, b.reshape(12, 137)) for a, b in zip(got, base))
+    got = spa2.gate_add_norm(x[0, 0], branch[0, 0], **p, eps=EPS, dtype=BF)
+    assert all(torch.equal(a, b[0, 0]) for a, b in zip(got, base))
+
+
+@pytest.mark.parametrize("C", [1281, 5120])
+def test_rows_far_from_zero_keep_their_deviation(C):
+    """Means of a thousand deviations: the deviation is no difference of large sums."""
+    g, x, branch, dy, dn = _data(1, 6, C, (F32, F32, F32), 8, offset=2000.0)
+    _check(x, branch, _params(g, {"gate": "C"}, C, F32), "layer", None, dy, dn)
+
+
+def test_a_lost_row_stays_alone():
+    g, x, branch, dy, dn = _data(2, 40, 264, (F32, F32, F32), 9)
+    p = _params(g, ALL, 264, F32)
+    base = spa2.gate_add_norm(x, branch, **p, eps=EPS)
+    for bad in (float("nan"), float("inf"), 1e30):
+        x2, b2 = x.clone(), branch.clone()
+        x2[1, 7, 3] = bad
+        b2[0, 5, 200] = bad
+        got = spa2.gate_add_norm(x2, b2, **p, eps=EPS)
+        keep = torch.ones(2, 40, dtype=torch.bool, device=dev())
+        keep[1, 7] = keep[0, 5] = False
+        assert all(torch.equal(a[keep], b[keep]) for a, b in zip(got, base))
+        if not np.isfinite(bad):
+            assert not torch.isfinite(got[1][1, 7]).all()
+
+
+def test_nothing_is_written_outside():
+    from paper_2602_13515_amd import binding
+    for C, N in ((137, 5), (5120, 3), (8195, 2)):
+        gd = Guarded()
+        g, x, branch, dy, dn = _data(1, N, C, (BF, BF, BF), 10)
+        p = _params(g, ALL, C, BF)
+        params = [p[n] for n in NAMES]
+        y, n, dx, db = (gd.alloc((1, N, C), BF, dev(), float("nan")) for _ in range(4))
+        stats = gd.alloc((3, N), F32, dev(), float("nan"))
+        grads = [gd.alloc((C,), BF, dev(), float("nan")) for _ in NAMES]
+        ws = gd.alloc((binding.spa2_gate_norm_bwd_workspace_bytes(x, branch, params, "layer"),), torch.uint8, dev(), 255)
+        binding.spa2_gate_norm(x, branch, params, "layer", EPS, y, n, stats)
+        binding.spa2_gate_norm_bwd(branch, params, "layer", EPS, y, dy, dn, stats, dx, db, grads, ws)
+        torch.cuda.synchronize()
+        gd.check(f"width {C}")
+        assert all(torch.isfinite(t).all() for t in (y, n, dx, db, stats, *grads))
+
+
+def test_long_tensors():
+    """Elements behind 2^31: offsets of 64 bits."""
+    C, N = 5120, 2 ** 31 // 5120 + 40
+    x = torch.zeros((1, N, C), dtype=BF, device=dev())
+    x[0, -33:] = torch.randn((33, C), device=dev()).to(BF)
+    w = torch.randn(C, device=dev()).to(BF)
+    y, n = spa2.gate_add_norm(x, x, gate=w, weight=w, kind="rms")
+    want = spa2.gate_add_norm(x[:, -33:], x[:, -33:], gate=w, weight=w, kind="rms")
+    assert torch.equal(y[:, -33:], want[0]) and torch.equal(n[:, -33:], want[1]) and not n[0, :-33:997].any()
+
+
+def test_second_derivatives_and_tangents_are_refused():
+    x = torch.randn(2, 3, 64, device=dev(), requires_grad=True)
+    y, n = spa2.gate_add_norm(x, x * 2)
+    (d,) = torch.autograd.grad(n.sum() + y.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        d.sum().backward()
+    import torch.autograd.forward_ad as fa
+    with fa.dual_level(), pytest.raises(RuntimeError):
+        spa2.gate_add_norm(fa.make_dual(x.detach(), torch.ones_like(x)))
+
+
+def test_captured_steps_and_another_stream():
+    g, x, branch, dy, dn = _data(2, 33, 1281, (F32, BF, BF), 11)
+    p = {n: v.requires_grad_(True) for n, v in _params(g, {**ALL, "gate": 2}, 1281, F32).items()}
+    x, branch = x.requires_grad_(True), branch.requires_grad_(True)
+    leaves = [x, branch, *p.values()]
+
+    def step():
+        y, n = spa2.gate_add_norm(x, branch, **p, eps=EPS, dtype=BF)
+        return [y.detach(), n.detach(), *torch.autograd.grad([y, n], leaves, [dy, dn])]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, step()))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for replay in range(3):
+        with torch.no_grad():
+            for t in leaves:
+                t.mul_(1.1)
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)), replay
+
+
+def test_gradients_against_differences():
+    """Along random directions, in fp32: central differences with a step of 2^-6 are off by its square times third derivatives of
+    order one, and by the sums' rounding, 2^-24 of a few thousand over the step: 1 % of the terms' magnitude holds both."""
+    g, x, branch, dy, dn = _data(2, 4, 96, (F32, F32, F32), 12)
+    p = _params(g, {**ALL, "gate": 2, "scale": 2}, 96, F32)
+    leaves = {"x": x, "branch": branch, **p}
+    t = {k: v.detach().requires_grad_(True) for k, v in leaves.items()}
+    f = lambda t: sum((o.double() * u.double()).sum() for o, u in zip(
+        spa2.gate_add_norm(t["x"], t["branch"], **{k: t[k] for k in p}, eps=1e-2), (dy, dn)))
+    grads = torch.autograd.grad(f(t), list(t.values()))
+    h = 2.0 ** -6
+    for name, d in zip(leaves, grads):
+        v = torch.randn_like(leaves[name])
+        with torch.no_grad():
+            up, down = (f({**leaves, name: leaves[name] + s * h * v}) for s in (1, -1))
+        terms = (d * v).double()
+        assert abs((up - down) / (2 * h) - terms.sum()) <= 0.01 * terms.abs().sum(), name
+
+
+def test_refusals():
+    x = torch.zeros(2, 3, 64, device=dev())
+    w = torch.ones(64, device=dev())
+    bad = [dict(branch=x[..., :32]), dict(branch=x.double()), dict(branch=x.half()), dict(gate=w), dict(branch_weight=w), dict(kind=None),
+           dict(branch=x, kind=None, weight=w), dict(branch=x, kind=None, shift=w), dict(weight=w[:32]), dict(weight=torch.ones(2, 64, device=dev())),
+           dict(scale=torch.ones(3, 64, device=dev())), dict(branch=x, gate=torch.ones(2, 1, 64, device=dev())), dict(weight=w.double()),
+           dict(dtype=torch.float16), dict(kind="batch"), dict(branch=x.cpu()), dict(weight=w.cpu())]
+    for change in bad:
+        with pytest.raises(ValueError):
+            spa2.gate_add_norm(x, **change)
+    for call in (lambda: spa2.gate_add_norm(x.bfloat16(), dtype=F32), lambda: spa2.gate_add_norm(x.bfloat16(), x),
+                 lambda: spa2.gate_add_norm(x.half()), lambda: spa2.gate_add_norm(x[:0])):
+        with pytest.raises(ValueError):
+            call()
+    for change in (dict(eps=0.0), dict(eps=float("nan"))):
+        with pytest.raises(spa2.Spa2Error):
+            spa2.gate_add_norm(x, **change)
+    with pytest.raises(spa2.Spa2Error):
+        spa2.gate_add_norm(torch.zeros(1, 16385, device=dev()))
+    with pytest.raises(RuntimeError):
+        torch.func.grad(lambda t: spa2.gate_add_norm(t)[1].sum())(x)
