@@ -355,6 +355,29 @@ int spa2_dropout_add(const void* x, const void* residual /* or NULL */, int64_t 
 int spa2_dropout_bwd(const void* d_y, int64_t n, int32_t y_dtype, int32_t x_dtype, double p, uint64_t seed, uint64_t offset,
                      const int64_t* seed_offset /* or NULL */, void* dx, void* stream);
 
+/* ---- attention over a window: to the keys near a query's own place and to the first few of the sequence ----
+ *   O_i = softmax_j(scale Q_i . K_j) V_j     over the keys j < lengths[b] with  j <= p + right  and  (j >= p - left  or  j < sinks)
+ * where query i of sample b stands at place p = starts[b] + i.  Arguments as for spa2_cross_fwd and spa2_cross_bwd; besides
+ *   window   left, right: keys before and behind a query's own that it sees; negative: no limit; at most 2^28.  sinks: the first
+ *            keys, which stay visible (up to p + right).
+ *   starts   device, int32 [B]; NULL: Nk - Nq (the queries are the last of the tokens).  Any numbers: a query that sees no key (its
+ *            place is before all of them, or behind them by more than `left`) gets O = 0, LSE = -infinity and a zero gradient.
+ * Keys that none of a workgroup's 128 queries sees are not read, and gradients of keys that no query sees are zero.  (A key that is
+ * not finite reaches all queries of a block one of which sees it.)  Nq and Nk are at most 2^28.
+ * o_res may be NULL if no backward pass follows, or with Nk <= 64. */
+typedef struct spa2_window {
+  int32_t left, right, sinks;
+} spa2_window;
+size_t spa2_window_fwd_workspace_bytes(const spa2_cross_shape* shape, const spa2_window* window);
+size_t spa2_window_bwd_workspace_bytes(const spa2_cross_shape* shape, const spa2_window* window);
+int spa2_window_fwd(const void* q, const void* k, const void* v, const int32_t* lengths /* or NULL */,
+                    const int32_t* starts /* or NULL */, const spa2_cross_shape* shape, const spa2_window* window, float scale,
+                    void* o, void* o_res /* or NULL */, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+int spa2_window_bwd(const void* q, const void* k, const void* v, const int32_t* lengths /* or NULL */,
+                    const int32_t* starts /* or NULL */, const void* o, const void* o_res /* or NULL */, const void* d_o,
+                    const float* lse, const spa2_cross_shape* shape, const spa2_window* window, float scale, void* dq, void* dk,
+                    void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- a branch, normed and gated, added to the residual stream, and the norm of the sum, modulated ----
  * What stands between two branches of a transformer block, for every token's row of `width` channels:
  *   u = b * (mean b^2 + eps)^(-1/2) * w_b  (post; else u = b)       y = x + gate * u, rounded to x's type

@@ -13,9 +13,10 @@ from .binding import (  # noqa: F401
     spa2_topk_blocks, spa2_version, spa2_vd_loss, spa2_vd_loss_grad, spa2_vd_loss_workspace_bytes,
     spa2_norm_rotate, spa2_norm_rotate_bwd, spa2_norm_rotate_bwd_workspace_bytes, spa2_dropout_add, spa2_dropout_bwd,
     spa2_cross_fwd, spa2_cross_bwd, spa2_cross_fwd_workspace_bytes, spa2_cross_bwd_workspace_bytes,
+    spa2_window_fwd, spa2_window_bwd, spa2_window_fwd_workspace_bytes, spa2_window_bwd_workspace_bytes,
     spa2_gate_norm, spa2_gate_norm_bwd, spa2_gate_norm_bwd_workspace_bytes, spa2_clip_gradients, spa2_clip_workspace_bytes,
 )
 from .autograd import SpargeAttn2, build_pattern, sparge_attn2  # noqa: F401,E402
-from .block import cross_attention, dropout_add, gate_add_norm, qk_norm_rotate, rotary_table  # noqa: F401,E402
+from .block import cross_attention, dropout_add, gate_add_norm, qk_norm_rotate, rotary_table, window_attention  # noqa: F401,E402
 from .gradients import clip_gradients, gradient_norm  # noqa: F401,E402
 from .diagnostics import block_sparsity, calibrate, masking_error  # noqa: F401,E402

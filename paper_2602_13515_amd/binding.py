@@ -53,6 +53,10 @@ class _CrossShape(ctypes.Structure):
         + [(n, ctypes.c_int64) for n in ("q_sb", "q_sh", "q_sn", "k_sb", "k_sh", "k_sn", "d_sb", "d_sh", "d_sn")]
 
 
+class _Window(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("left", "right", "sinks")]
+
+
 class _GateShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("samples", "tokens", "gate_sb", "scale_sb", "shift_sb")] \
         + [(n, ctypes.c_int32) for n in ("width", "kind", "post", "x_dtype", "branch_dtype", "out_dtype", "param_dtype")]
@@ -159,6 +163,15 @@ def _load():
     lib.spa2_dropout_add.argtypes = [vp, vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
     lib.spa2_dropout_bwd.restype = ctypes.c_int
     lib.spa2_dropout_bwd.argtypes = [vp, i64, i32, i32, f64, u64, u64, vp, vp, vp]
+    win = ctypes.POINTER(_Window)
+    lib.spa2_window_fwd_workspace_bytes.restype = sz
+    lib.spa2_window_fwd_workspace_bytes.argtypes = [crs, win]
+    lib.spa2_window_bwd_workspace_bytes.restype = sz
+    lib.spa2_window_bwd_workspace_bytes.argtypes = [crs, win]
+    lib.spa2_window_fwd.restype = ctypes.c_int
+    lib.spa2_window_fwd.argtypes = [vp] * 5 + [crs, win, f32, vp, vp, vp, vp, sz, vp]
+    lib.spa2_window_bwd.restype = ctypes.c_int
+    lib.spa2_window_bwd.argtypes = [vp] * 9 + [crs, win, f32, vp, vp, vp, vp, sz, vp]
     gsh, gpr = ctypes.POINTER(_GateShape), ctypes.POINTER(_GateParams)
     lib.spa2_gate_norm_bwd_workspace_bytes.restype = sz
     lib.spa2_gate_norm_bwd_workspace_bytes.argtypes = [gsh]
@@ -183,6 +196,7 @@ EXPORTED_SYMBOLS = ("spa2_version", "spa2_strerror", "spa2_topk_blocks", "spa2_m
                     "spa2_vd_rescale", "spa2_norm_rotate", "spa2_norm_rotate_bwd", "spa2_norm_rotate_bwd_workspace_bytes",
                     "spa2_dropout_add", "spa2_dropout_bwd", "spa2_cross_fwd", "spa2_cross_bwd",
                     "spa2_cross_fwd_workspace_bytes", "spa2_cross_bwd_workspace_bytes",
+                    "spa2_window_fwd", "spa2_window_bwd", "spa2_window_fwd_workspace_bytes", "spa2_window_bwd_workspace_bytes",
                     "spa2_gate_norm", "spa2_gate_norm_bwd", "spa2_gate_norm_bwd_workspace_bytes",
                     "spa2_clip_gradients", "spa2_clip_workspace_bytes")
 
@@ -675,6 +689,54 @@ def spa2_dropout_bwd(d_y, p: float, seed: int, offset: int, dx, seed_offset=None
 
 
 # ------------------------------------------------------------------ a training step around the attention
+def _window_of(left: Optional[int], right: Optional[int], sinks: int) -> _Window:
+    for n in (left, right, sinks):
+        if n is not None and not 0 <= n < 2 ** 31:
+            raise ValueError("left, right and sinks are numbers of keys (left, right: None for no limit)")
+    return _Window(-1 if left is None else left, -1 if right is None else right, sinks)
+
+
+def _window_starts(q, starts) -> None:
+    if starts is not None and (starts.dtype != torch.int32 or starts.shape != q.shape[:1] or not starts.is_contiguous()):
+        raise ValueError("starts are int32 [B]")
+
+
+def spa2_window_fwd_workspace_bytes(q, k, left: Optional[int], right: Optional[int], sinks: int) -> int:
+    return int(_load().spa2_window_fwd_workspace_bytes(ctypes.byref(_cross_args(q, k, k, None)), ctypes.byref(_window_of(left, right, sinks))))
+
+
+def spa2_window_bwd_workspace_bytes(q, k, left: Optional[int], right: Optional[int], sinks: int) -> int:
+    return int(_load().spa2_window_bwd_workspace_bytes(ctypes.byref(_cross_args(q, k, k, None)), ctypes.byref(_window_of(left, right, sinks))))
+
+
+def spa2_window_fwd(q, k, v, lengths, starts, left: Optional[int], right: Optional[int], sinks: int, scale: float, o, lse, o_res=None,
+                    workspace=None) -> None:
+    s, w = _cross_args(q, k, v, lengths), _window_of(left, right, sinks)
+    _one_gpu(q, k, v, lengths, starts, o, o_res, lse, workspace)
+    _window_starts(q, starts)
+    _check_lse(q, lse)
+    _same_layout(q, o, *([o_res] if o_res is not None else []))
+    _check(_load().spa2_window_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), _ptr(starts), ctypes.byref(s),
+                                   ctypes.byref(w), float(scale), o.data_ptr(), _ptr(o_res), lse.data_ptr(), _ptr(workspace),
+                                   0 if workspace is None else _nbytes(workspace), _stream(q)), "spa2_window_fwd")
+
+
+def spa2_window_bwd(q, k, v, lengths, starts, left: Optional[int], right: Optional[int], sinks: int, o, d_o, lse, scale: float, dq, dk,
+                    dv, workspace, o_res=None) -> None:
+    s, w = _cross_args(q, k, v, lengths, dk), _window_of(left, right, sinks)
+    _one_gpu(q, k, v, lengths, starts, o, o_res, d_o, lse, dq, dk, dv, workspace)
+    _window_starts(q, starts)
+    _check_lse(q, lse)
+    _same_layout(q, o, d_o, dq, *([o_res] if o_res is not None else []))
+    if dk.shape != k.shape or dv.shape != k.shape or dk.stride() != dv.stride() or dk.dtype != k.dtype or dv.dtype != k.dtype \
+            or dk.stride(3) != 1:
+        raise ValueError("dk and dv have the shape and type of k and share strides, d contiguous")
+    _check(_load().spa2_window_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), _ptr(starts), o.data_ptr(), _ptr(o_res),
+                                   d_o.data_ptr(), lse.data_ptr(), ctypes.byref(s), ctypes.byref(w), float(scale), dq.data_ptr(),
+                                   dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream(q)),
+           "spa2_window_bwd")
+
+
 NORM_KINDS = {None: 0, "layer": 1, "rms": 2}
 _GATE_PARAMS = tuple(n for n, _ in _GateParams._fields_)
 

@@ -4,6 +4,7 @@
                      (`rotary_table` makes the tables of cosines and sines);
 * `cross_attention`  beside it: dense attention to another sequence, a prompt or a cache, whose samples have lengths of
                      their own;
+* `window_attention` in its place: attention to the keys near a query's own place and to the first few of the sequence;
 * `dropout_add`      behind it: dropout of a branch and the sum with the residual stream, the mask drawn from a counter-based
                      generator and never stored;
 * `gate_add_norm`    between two branches: a branch, normed and gated, added to the residual stream, and the norm of the sum,
@@ -91,6 +92,26 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: 
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[-1]) if q.dim() and q.shape[-1] else 1.0      # (those are refused there)
     return _operator().cross_attention(q, k, v, lengths, float(scale))
+
+
+def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, left: Optional[int], right: Optional[int] = 0, sinks: int = 0,
+                     lengths: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None,
+                     scale: Optional[float] = None) -> torch.Tensor:
+    """softmax(scale q k^T) v over the keys near each query's own place and the first few of the sequence: query i of sample b
+    stands at place p = starts[b] + i and sees the keys j < lengths[b] with j <= p + right and (j >= p - left or j < sinks).
+
+    q [B, Hq, Nq, d], k, v [B, Hk, Nk, d], lengths, scale: as in `cross_attention`.  left, right: None for no limit (None, 0: all keys
+    up to the query's own), at most 2^28.  starts: contiguous int32 [B] on the GPU; None: Nk - Nq, the queries are the last of Nk
+    tokens (all of them, if there are as many).  With a cache of which lengths[b] places are filled, the queries its last ones:
+    starts = lengths - Nq.  A query that sees no key gives zeros and a zero gradient; keys that no query sees get zero gradients.
+    Returns bf16 with q's shape (and memory order).  Gradients: q, k, v, as in `cross_attention`."""
+    _refuse_others("window_attention", q, k, v, lengths, starts)
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[-1]) if q.dim() and q.shape[-1] else 1.0
+    limits = [-1 if left is None else int(left), -1 if right is None else int(right), int(sinks)]
+    if min(limits[2], 0 if left is None else limits[0], 0 if right is None else limits[1]) < 0:
+        raise ValueError("left, right and sinks are numbers of keys (left, right: None for no limit)")
+    return _operator().window_attention(q, k, v, limits, lengths, starts, float(scale))
 
 
 def _signed(x: int) -> int:

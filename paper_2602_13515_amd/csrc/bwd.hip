@@ -18,6 +18,7 @@
 #include "spa2_device.h"
 #include "spa2_internal.h"
 #include "split_plan.h"
+#include "window.h"
 
 namespace spa2 {
 
@@ -36,7 +37,7 @@ hipError_t launch_bwd_delta(const void* o, const void* o_res, const void* d_o, c
 
 // ------------------------------------------------------------------ dQ
 struct DqArgs {
-  static constexpr bool CROSS = false, FINE = false;
+  static constexpr bool CROSS = false, FINE = false, WINDOW = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v; const uint16_t* d_o;
   const float* lse; const float* delta; uint16_t* dq;
   const int32_t* row_cnt; const int32_t* row_idx; const int32_t* row_order;
@@ -63,6 +64,14 @@ struct CrossDqArgs : DqArgs {
 };
 // The same with dS in two bf16 parts (cross_few).  (Many rows take one: the price of two is at CrossFwdArgs in fwd.hip.)
 struct CrossDqFineArgs : CrossDqArgs {
+  static constexpr bool FINE = true;
+};
+// Attention over a window (window.h)
+struct WindowDqArgs : CrossDqArgs {
+  static constexpr bool WINDOW = true;
+  Window win;
+};
+struct WindowDqFineArgs : WindowDqArgs {
   static constexpr bool FINE = true;
 };
 
@@ -101,7 +110,7 @@ __device__ __forceinline__ void dq_store_rows(const DqArgs& a, int64_t base, int
 // 24 heads, half the rows long 6466 / 5435; 20,010 tokens, 6 heads, d = 64 89 / 78.
 template <int D, class Args>
 __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
-  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE;
+  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE, WINDOW = Args::WINDOW;
   constexpr int NK = D / 16, NMB = D / 32;           // contraction steps of S and dP, output blocks of dQ
   // K and V tiles, XOR-swizzled and unpadded (the layout a direct global -> LDS copy can write): K is read along rows
   // (S^T) and transposed (dQ^T), V along rows (dP^T).  (Aligned: compile-time parts are XORed into addresses.)
@@ -115,6 +124,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   bool whole = false;
   int slot = (int)blockIdx.x - (CROSS ? 0 : a.front);
   int keys = a.N;             // keys that the row sees at most
+  int start = 0;              // (WINDOW) place of query 0, and what the workgroup's queries see
+  WindowSpan span;
+  bool one = false;           // (WINDOW) all keys in one tile
   if constexpr (CROSS) {
     for (int x = (int)(blockIdx.x * 256 + threadIdx.x); x < a.zeros; x += (int)(gridDim.x * 256)) a.zero[x] = 0;
     const int rows = stretch_wgs(a.BH * a.Tm);
@@ -122,9 +134,19 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     if (!hb.valid) return;
     bh = hb.bh; i = hb.blk;
     keys = cross_length(a.kv, bh / a.H);
-    const int all = (keys + BKV - 1) / BKV;
+    int all = (keys + BKV - 1) / BKV;
     part = blockIdx.x / rows;
-    parts = cross_parts_of(a, bh);
+    if constexpr (WINDOW) {
+      start = window_start(a.win, bh / a.H);
+      int p0, p1;
+      window_places(a.win, start, a.N, i * BQ, min(i * BQ + BQ, a.N) - 1, p0, p1);
+      span = window_span(a.win, keys, p0, p1);
+      all = span.count();
+      one = all <= 1;
+      parts = window_parts(a, all);
+    } else {
+      parts = cross_parts_of(a, bh);
+    }
     if (part >= max(parts, 1)) return;
     if (parts) part_len = (all + parts - 1) / parts;
     slot = (bh * a.Tm + i) * a.sp.fixed_parts + part;
@@ -163,7 +185,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   int cnt, split_at = 0, first;              // entries [first, first + part_len) of the list of a split row
   const int32_t* idx = nullptr;
   if constexpr (CROSS) {
-    cnt = (keys + BKV - 1) / BKV;
+    if constexpr (WINDOW) cnt = span.count();
+    else                  cnt = (keys + BKV - 1) / BKV;
     first = part * part_len;
   } else {
     cnt = min(max(a.row_cnt[unit], 0), a.Tn);   // clamped: see fwd.hip
@@ -189,7 +212,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   }
   float lse2 = a.lse[(int64_t)bh * N + qrow_ld] * LOG2E;
   float dlt = CROSS ? 0.f : a.delta[(int64_t)bh * N + qrow_ld];
-  if constexpr (CROSS) if (keys > BKV) {
+  if constexpr (CROSS) if (WINDOW ? !one : keys > BKV) {
     const int64_t off = base + (int64_t)qrow_ld * a.sn + 8 * hf;
     u32x4 of[D / 16], rf[D / 16];
 #pragma unroll
@@ -244,7 +267,21 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   };
   uint32_t voff[CH];
   int rows_set = -1;
-  auto set_rows = [&](int last) {            // last: last valid row of the tile (uniform)
+  auto set_rows = [&](int j) {               // for the tile of key block j (uniform)
+    if constexpr (WINDOW) {                  // (see fwd.hip)
+      const bool whole_block = span.whole(j);
+      const int code = whole_block ? 0 : j + 1;
+      if (code == rows_set) return;
+      rows_set = code;
+      const int t = fresh_tid(), ld_row = t / CPR, ld_c8 = ((t % CPR) ^ swz<D>(ld_row)) * 8;
+#pragma unroll
+      for (int r = 0; r < CH; ++r) {
+        const int row = ld_row + RSTEP * r, from = whole_block ? row : span.stand_in(j, j * BKV + row) - j * BKV;
+        voff[r] = (uint32_t)((from * key_sn + ld_c8) * 2);
+      }
+      return;
+    }
+    const int last = min(BKV - 1, keys - 1 - j * BKV);         // last valid row of the tile
     if (last == rows_set) return;
     rows_set = last;
     const int t = fresh_tid(), ld_row = t / CPR, ld_c8 = ((t % CPR) ^ swz<D>(ld_row)) * 8;
@@ -280,22 +317,33 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   const uint32_t kt_off1 = sm + 2 * swz_idx<D>(8 + 4 * hf + (s16 >> 2), 16 * hb16 + 4 * (s16 & 3));
 
   auto list_entry = [&](int t) -> int {      // t uniform, inside the chunk that idx_v holds
+    if constexpr (WINDOW) return span.block(first + t);
     if constexpr (CROSS) return first + t;
     return min(max(__builtin_amdgcn_readlane(idx_v, t & 63), 0), a.Tn - 1);
   };
   int j_cur = list_entry(0);
-  set_rows(min(BKV - 1, keys - 1 - j_cur * BKV));
+  set_rows(j_cur);
   static_for<0, NPIECE>([&](auto P) { copy_piece(P, k_head + j_cur * tile_bytes, v_head + j_cur * tile_bytes, sm); });
   raw_copies_done();
   __syncthreads();
 
+  // (WINDOW) this lane's query: what it sees of the keys from key `at` on is [first ones, early), [near, last]
+  struct Sight { int last, near, early; };
+  auto sight = [&](int at) -> Sight {
+    if constexpr (WINDOW) {
+      const int p = window_place(a.win, start, a.N, i * BQ + 32 * w + (fresh_tid() & 31));
+      return {min(p + a.win.right, keys - 1) - at, p - a.win.left - at, a.win.sinks - at};
+    }
+    return {};
+  };
   if constexpr (CROSS) {
     // All keys in one tile: LSE and D are taken again, D = sum P dP, from the very values that dS is made of.  The forward
     // pass's LSE and O are of P rounded to bf16, which few keys do not average out: with 3 keys the error of dQ and dK was
     // 1.5 times that of their own rounding to bf16, so 1.4, which is that and the rounding of dS.  (It is faster, too: 32,760
     // queries, 12 heads, 60 keys, the backward pass 204 -> 157 us, as O and what its rounding dropped are not read.)
-    if (keys <= BKV) {
+    if (WINDOW ? one : keys <= BKV) {
       float sum = 0.f, total = 0.f;
+      const Sight see = sight(j_cur * BKV + 4 * hf);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         f32x16 s = {}, dp = {};
@@ -306,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (32 * kb + 8 * (v >> 2) + (v & 3) + 4 * hf < keys) {
+          if (const int c = 32 * kb + 8 * (v >> 2) + (v & 3); WINDOW ? c <= see.last && (c >= see.near || c < see.early) : c + 4 * hf < keys) {
             const float p = fast_exp2(fmaf(s[v], a.scale_log2, -lse2));
             total += p;
             sum = fmaf(p, dp[v], sum);
@@ -314,6 +362,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       }
       total = sum_halves(total);
       dlt = sum_halves(sum) / total;
+      if (WINDOW && total == 0.f) dlt = 0.f;           // (a query that sees no key)
       lse2 += __builtin_amdgcn_logf(total);        // (log2)
 #pragma unroll
       for (int v = 0; v < 16; ++v) neg_d[v] = -dlt;
@@ -331,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     // back to back they keep the wave at the issue stage until the texture unit has taken the last one.  They are
     // unconditional (past the end of the list the last tile is requested again, into the buffer nobody reads).
     j_cur = list_entry(min(t + 1, cnt - 1));
-    set_rows(min(BKV - 1, keys - 1 - j_cur * BKV));
+    set_rows(j_cur);
     const char* kpn = k_head + j_cur * tile_bytes;
     const char* vpn = v_head + j_cur * tile_bytes;
     const uint32_t nx_stage = sm + ((t + 1) & 1) * STAGE_B;
@@ -356,7 +405,12 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       return join_tr(lds_tr4_at((kt0 ^ (mb << 6)) + o), lds_tr4_at((kt1 ^ (mb << 6)) + o));
     };
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const bool tail = (j + 1) * BKV > keys;
+    bool tail = (j + 1) * BKV > keys;
+    if constexpr (WINDOW) {
+      int p0, p1;                            // (of the wave's rows, those past the end included)
+      window_places(a.win, start, a.N, i * BQ + 32 * w, i * BQ + 32 * w + 31, p0, p1);
+      tail = !window_full(a.win, keys, p0, p1, j * BKV, j * BKV + BKV - 1);
+    }
     f32x16 s[2], dp[2];
     uint32_t dsk[2][8], ds_rest[2][8];       // (ds_rest: FINE)
     auto exp_unit = [&](auto KB, auto U) {   // P^T of two keys
@@ -366,6 +420,17 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     };
     auto mask_tail = [&](auto KB) {          // keys past N (short last block): P = 0
       constexpr int kb = decltype(KB)::v;
+      if constexpr (WINDOW) {
+        if (tail) {
+          const Sight see = sight(j * BKV + kb * 32 + 4 * ((fresh_tid() & 63) >> 5));
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int c = 8 * (v >> 2) + (v & 3);
+            if (c > see.last || (c < see.near && c >= see.early)) s[kb][v] = 0.f;
+          }
+        }
+        return;
+      }
       if (tail) {                            // (a branch: as selects it cost four instructions an element and tile)
         const int valid = keys - j * BKV - kb * 32 - 4 * ((fresh_tid() & 63) >> 5);
 #pragma unroll
@@ -436,6 +501,14 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       }
     }
   }
+  if constexpr (WINDOW) {                    // (a query that sees no key has no gradient, whatever its upstream one is)
+    if (window_blind(a.win, keys, window_place(a.win, start, a.N, i * BQ + 32 * w + (lane & 31)))) {
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[mb][v] = 0.f;
+    }
+  }
   dq_store_rows<D>(a, base, i * BQ + 32 * w, lane, sm + w * (32 * D * 2), acc);
 }
 
@@ -490,12 +563,15 @@ hipError_t launch_bwd_dq_columns(const void* q, const void* k, const void* v, co
 
 // ------------------------------------------------------------------ attention to another sequence
 // The sums of a row's parts, added in part order (see cross_fwd_join_kernel).
-template <int D>
-__global__ __launch_bounds__(256) void cross_dq_join_kernel(CrossDqArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256) void cross_dq_join_kernel(Args a) {
   constexpr int NMB = D / 32;
   __shared__ float sums[4][16][64];
   const int mb = blockIdx.x % NMB, w = blockIdx.x / NMB % 4, unit = blockIdx.x / (4 * NMB), bh = unit / a.Tm, i = unit % a.Tm;
-  const int parts = cross_parts_of(a, bh), lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  int parts;
+  if constexpr (Args::WINDOW) parts = window_parts(a, window_count(a, bh, i));
+  else                        parts = cross_parts_of(a, bh);
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
   const int row = i * BQ + 32 * w + (lane & 31), hf = lane >> 5;
   if (parts == 0 || i * BQ + 32 * w >= a.N) return;
   const float* p0 = a.sp.pool + (int64_t)unit * a.sp.fixed_parts * a.sp.slot_floats + (mb * 8 * 256 + 64 * w + lane) * 2;
@@ -521,16 +597,22 @@ __global__ __launch_bounds__(256) void cross_dq_join_kernel(CrossDqArgs a) {
   if (g || row >= a.N) return;
 #pragma unroll
   for (int v = 0; v < 16; ++v) x[v] = ((sums[0][v][lane] + sums[1][v][lane]) + (sums[2][v][lane] + sums[3][v][lane])) * a.scale;
+  if constexpr (Args::WINDOW) {
+    const int b = bh / a.H;
+    if (window_blind(a.win, cross_length(a.kv, b), window_place(a.win, window_start(a.win, b), a.N, row)))
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = 0.f;
+  }
   uint16_t* out = a.dq + (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh + (int64_t)row * a.sn + 32 * mb + 4 * hf;
 #pragma unroll
   for (int q = 0; q < 4; ++q)                            // channels 32 mb + 8 q + 4 hf ..
     *(u32x2*)(out + 8 * q) = u32x2{pack_bf16(x[4 * q], x[4 * q + 1]), pack_bf16(x[4 * q + 2], x[4 * q + 3])};
 }
 
-hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
-                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, float* lse_out,
-                           void* dq, int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
-  CrossDqFineArgs a = {};
+template <class Args>
+static void fill_cross_dq(Args& a, const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
+                          const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, float* lse_out,
+                          void* dq, int32_t* zero, int zeros, const SplitPlan& plan) {
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
   a.lse = lse; a.delta_out = delta; a.lse_out = lse_out; a.dq = (uint16_t*)dq;
   a.o = (const uint16_t*)o; a.o_res = (const uint16_t*)o_res;
@@ -540,6 +622,13 @@ hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const vo
   a.scale = scale; a.scale_log2 = scale * LOG2E;
   a.kv = cross_keys(m, lengths);
   a.sp = plan;
+}
+
+hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
+                           const float* lse, const CrossDims& m, const int32_t* lengths, float scale, float* delta, float* lse_out,
+                           void* dq, int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
+  CrossDqFineArgs a = {};
+  fill_cross_dq(a, q, k, v, o, o_res, d_o, lse, m, lengths, scale, delta, lse_out, dq, zero, zeros, plan);
   const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tm))), block(256);
   const bool fine = cross_few(m);
   if (m.q.d == 128 && fine) hipLaunchKernelGGL((dq_kernel<128, CrossDqFineArgs>), grid, block, 0, stream, a);
@@ -549,8 +638,28 @@ hipError_t launch_cross_dq(const void* q, const void* k, const void* v, const vo
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !plan.pool_slots) return e;
   const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));
-  if (m.q.d == 128) hipLaunchKernelGGL(cross_dq_join_kernel<128>, joins, block, 0, stream, a);
-  else              hipLaunchKernelGGL(cross_dq_join_kernel<64>, joins, block, 0, stream, a);
+  if (m.q.d == 128) hipLaunchKernelGGL((cross_dq_join_kernel<128, CrossDqArgs>), joins, block, 0, stream, a);
+  else              hipLaunchKernelGGL((cross_dq_join_kernel<64, CrossDqArgs>), joins, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_window_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
+                            const float* lse, const CrossDims& m, const int32_t* lengths, const Window& win, float scale, float* delta,
+                            float* lse_out, void* dq, int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream) {
+  WindowDqFineArgs a = {};
+  fill_cross_dq(a, q, k, v, o, o_res, d_o, lse, m, lengths, scale, delta, lse_out, dq, zero, zeros, plan);
+  a.win = win;
+  const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tm))), block(256);
+  const bool fine = cross_few(m);
+  if (m.q.d == 128 && fine) hipLaunchKernelGGL((dq_kernel<128, WindowDqFineArgs>), grid, block, 0, stream, a);
+  else if (m.q.d == 128)    hipLaunchKernelGGL((dq_kernel<128, WindowDqArgs>), grid, block, 0, stream, a);
+  else if (fine)            hipLaunchKernelGGL((dq_kernel<64, WindowDqFineArgs>), grid, block, 0, stream, a);
+  else                      hipLaunchKernelGGL((dq_kernel<64, WindowDqArgs>), grid, block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !plan.pool_slots) return e;
+  const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));
+  if (m.q.d == 128) hipLaunchKernelGGL((cross_dq_join_kernel<128, WindowDqArgs>), joins, block, 0, stream, a);
+  else              hipLaunchKernelGGL((cross_dq_join_kernel<64, WindowDqArgs>), joins, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -6,6 +6,7 @@
 #include "row_map.h"
 #include "spa2_device.h"
 #include "spa2_internal.h"
+#include "window.h"
 #include "work_queue.h"
 
 namespace spa2 {
@@ -22,7 +23,7 @@ __device__ __forceinline__ void mfma32_acc(bf16x8 a, bf16x8 b, f32x16& c) {
 
 // ------------------------------------------------------------------ dK, dV
 struct DkvArgs {
-  static constexpr bool CROSS = false, FINE = false;
+  static constexpr bool CROSS = false, FINE = false, WINDOW = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v; const uint16_t* d_o;
   const float* lse; const float* delta; uint16_t* dk; uint16_t* dv;
   const int32_t* col_cnt; const int32_t* col_idx; const int32_t* col_order;
@@ -44,6 +45,41 @@ struct CrossDkvArgs : DkvArgs {
 struct CrossDkvFineArgs : CrossDkvArgs {
   static constexpr bool FINE = true;
 };
+// Attention over a window (window.h): a column's list is, for every query head, the halves of query blocks from the first to the
+// last query that sees one of its keys.  Columns of first keys are cut as `sp` says, the others as `rest` does.
+struct WindowDkvArgs : CrossDkvArgs {
+  static constexpr bool WINDOW = true;
+  Window win;
+  SplitPlan rest;
+  int first_blocks;
+};
+struct WindowDkvFineArgs : WindowDkvArgs {
+  static constexpr bool FINE = true;
+};
+// The queries that a column's list is of, and its halves in a head.
+struct ColumnRows { WindowRows rows; int h0, halves, start; };
+template <class Args>
+__device__ __forceinline__ ColumnRows column_rows(const Args& a, int bh, int j) {
+  ColumnRows c = {};
+  if constexpr (Args::WINDOW) {
+    const int b = bh / a.H, keys = a.kv.lengths ? min(max(scalar_ld(a.kv.lengths + b), 0), a.kv.Nk) : a.kv.Nk;
+    c.start = window_start(a.win, b);
+    c.rows = window_rows(a.win, c.start, a.N, j * BKV, min(j * BKV + BKV, keys) - 1);
+    c.h0 = c.rows.r0 / 64;
+    c.halves = c.rows.r1 < c.rows.r0 ? 0 : c.rows.r1 / 64 - c.h0 + 1;
+  }
+  return c;
+}
+// What a lane's key (of a column's) sees of queries: its first and last one.
+template <class Args>
+__device__ __forceinline__ WindowRows key_rows(const Args& a, const ColumnRows& c, int key) {
+  WindowRows r = {0, 0};
+  if constexpr (Args::WINDOW) {
+    r.r0 = key - a.win.right - c.start;
+    r.r1 = key < a.win.sinks ? WINDOW_NO_LIMIT : key + a.win.left - c.start;
+  }
+  return r;
+}
 // the walk of a workgroup that has one item
 struct OneItem {
   int wave;
@@ -151,7 +187,7 @@ __device__ __forceinline__ void dkdv_merge(const Args& a, const WorkItem& item, 
 template <int D, class Args, class Way>
 __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, Way& walk, unsigned char* smem,
                                           unsigned char* stat_s) {
-  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE;
+  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE, WINDOW = Args::WINDOW;
   constexpr int QW = 32;                             // query rows per wave and step
   constexpr int HQ = 64;                             // query rows per workgroup and step
   constexpr int NK = D / 16;                         // 16-wide contraction steps over the head dimension
@@ -170,7 +206,10 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
   const ColumnPlace at = column_place(a, bh, base);
   int cnt;
   const int32_t* idx = nullptr;
-  if constexpr (CROSS) {
+  const ColumnRows seen = column_rows(a, bh, j);
+  if constexpr (WINDOW) {
+    cnt = a.kv.group * seen.halves;
+  } else if constexpr (CROSS) {
     cnt = j * BKV < at.keys ? a.kv.group * a.Tm : 0;
   } else {
     cnt = min(max(a.col_cnt[(int64_t)bh * a.Tn + j], 0), a.Tm);   // clamped: see fwd.hip
@@ -208,6 +247,12 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
       kf[kh][kk] = *(const bf16x8*)(a.k + off + 16 * kk);
       vf[kh][kk] = *(const bf16x8*)(a.v + off + 16 * kk);
     }
+    if constexpr (WINDOW) {                  // (a key that no query sees: whatever it holds, its gradients are zero)
+      const WindowRows r = key_rows(a, seen, key0 + 32 * kh);
+      if (r.r0 > N - 1 || r.r1 < 0)
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) kf[kh][kk] = vf[kh][kk] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+    }
   }
 
   f32x16 dk_acc[2][NMB], dv_acc[2][NMB];
@@ -226,16 +271,21 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
   // when the number of valid rows changes.
   uint32_t voff[NCP], soff = 0;
   int rows_set = -1;
-  auto set_rows = [&](int last) {            // last: last valid row of the 32 (uniform)
-    if (last == rows_set) return;
-    rows_set = last;
+  // (WINDOW: rows that see none of the column's keys repeat the next one that does; row_b is the first row that is read)
+  auto base_row = [&](int row) -> int { return WINDOW ? min(max(row, seen.rows.r0), seen.rows.r1) : min(row, N - 1); };
+  auto set_rows = [&](int row, int row_b) {  // row: first of the 32 (uniform)
+    const int last = WINDOW ? seen.rows.r1 - row_b : min(31, N - 1 - row_b), ahead = row_b - row;        // (ahead: 0 but for WINDOW)
+    const int code = !WINDOW ? last : row >= seen.rows.r0 && row + 31 <= seen.rows.r1 ? 0 : row + 1;
+    if (code == rows_set) return;
+    rows_set = code;
     const int l = fresh_lane();
+    auto from = [&](int x) -> int { return WINDOW ? min(max(x - ahead, 0), last) : min(x, last); };
 #pragma unroll
     for (int r = 0; r < NCP; ++r) {
       const int row_l = RPI * r + l / CPR;
-      voff[r] = (uint32_t)((min(row_l, last) * a.sn + (((l % CPR) ^ swz<D>(row_l)) * 8)) * 2);
+      voff[r] = (uint32_t)((from(row_l) * a.sn + (((l % CPR) ^ swz<D>(row_l)) * 8)) * 2);
     }
-    soff = (uint32_t)(min(l & 31, last) * 4);
+    soff = (uint32_t)(from(l & 31) * 4);
   };
   const char* q_head = (const char*)(a.q + base);
   const char* o_head = (const char*)(a.d_o + base);
@@ -251,6 +301,12 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
   };
   // Query rows past N get an LSE of +infinity once their copy has landed: their P is then exactly zero.
   auto mark_rows_past_end = [&](int row0, uint32_t stat_addr) {
+    if constexpr (WINDOW) {
+      if (row0 >= seen.rows.r0 && row0 + QW - 1 <= seen.rows.r1) return;
+      const int row = row0 + (fresh_lane() & 31);
+      if (row < seen.rows.r0 || row > seen.rows.r1) lds_stf(stat_addr + 4 * (row - row0), INFINITY);
+      return;
+    }
     if (row0 + QW <= N) return;
     const int row_l = fresh_lane() & 31;
     if (row0 + row_l >= N) lds_stf(stat_addr + 4 * row_l, INFINITY);
@@ -262,8 +318,13 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
   if constexpr (!CROSS) idx_v = idx[min(lane, cnt - 1)];
   // (attention to another sequence with no more queries than a half has: one half an entry.  32 rows of 8 heads, 8 samples of
   // 8192 keys, the backward pass, d = 128: 297 -> 270 us; d = 64 112 -> 97)
-  const int halves = CROSS && N <= HQ ? 0 : 1;
+  const int halves = WINDOW || (CROSS && N <= HQ) ? 0 : 1;
   auto step_row = [&](int u) -> int {        // first row of step u (uniform, inside the chunk that idx_v holds)
+    if constexpr (WINDOW) {
+      const int e = first + u;
+      g_at = a.kv.group == 1 ? 0 : e / seen.halves;
+      return (seen.h0 + e - g_at * seen.halves) * HQ + 32 * w;
+    }
     if constexpr (CROSS) {
       const CrossEntry e = cross_entry(a, first + (u >> halves));
       g_at = e.g;
@@ -286,8 +347,8 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
 
   const int steps = CROSS ? cnt << halves : 2 * cnt;    // step u: half u & 1 of list entry u >> 1
   {
-    const int row0 = step_row(0), row_b = min(row0, N - 1);
-    set_rows(min(QW - 1, N - 1 - row_b));
+    const int row0 = step_row(0), row_b = base_row(row0);
+    set_rows(row0, row_b);
     copy_stats(head_rows() + row_b, wstat);
     static_for<0, NCP>([&](auto R) {
       constexpr int r = decltype(R)::v;
@@ -315,8 +376,8 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
     const int st = u & 1;
     const int un = min(u + 1, steps - 1);    // past the end the last step is requested again (nobody reads it)
     if (!CROSS && ((u + 1) & 127) == 0 && u + 1 < steps) idx_v = list_load(idx, min(((u + 1) >> 1) + fresh_lane(), cnt - 1));   // next 64 entries
-    const int row_nx = step_row(un), row_b = min(row_nx, N - 1);
-    set_rows(min(QW - 1, N - 1 - row_b));
+    const int row_nx = step_row(un), row_b = base_row(row_nx);
+    set_rows(row_nx, row_b);
     const uint32_t nx_stage = wsm + (st ^ 1) * STAGE_B, nx_stat = wstat + (st ^ 1) * STAT_B;
     const char* qn = q_head + head_bytes() + (uint64_t)row_b * row_bytes;
     const char* on = o_head + head_bytes() + (uint64_t)row_b * row_bytes;
@@ -382,6 +443,25 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
       if constexpr (y == NK - 1) l_raw = lds_ldf4(lb);
       __builtin_amdgcn_sched_barrier(0);
     });
+    // (WINDOW) pairs that do not see each other have no weight
+    if constexpr (WINDOW) {
+      const int g = g_at, row0 = step_row(u), k0 = j * BKV, k1 = k0 + BKV - 1;
+      g_at = g;                              // (that of the step asked for last)
+      const bool full = row0 >= k1 - a.win.right - seen.start && (k1 < a.win.sinks || row0 + QW - 1 <= k0 + a.win.left - seen.start);
+      if (!full) {
+        const int l = fresh_lane(), from = row0 + 4 * (l >> 5);
+#pragma unroll
+        for (int kh = 0; kh < 2; ++kh) {
+          WindowRows r = key_rows(a, seen, k0 + 32 * kh + (l & 31));
+          r.r0 -= from; r.r1 -= from;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int c = 8 * (v >> 2) + (v & 3);
+            if (c < r.r0 || c > r.r1) s[kh][v] = -INFINITY;
+          }
+        }
+      }
+    }
     // ---- D - dP = D + dO (-V)^T, with exp(S - LSE) between the products; the next step's dO rows are requested
     bf16x8 ft[PDT];
     static_for<0, NK>([&](auto Y) {
@@ -523,7 +603,7 @@ __device__ __forceinline__ void dkdv_item(const Args& a, const WorkItem& item, W
 template <class Args, class Way>
 __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item, Way& walk, unsigned char* smem,
                                             unsigned char* stat_s) {
-  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE;
+  constexpr bool CROSS = Args::CROSS, FINE = Args::FINE, WINDOW = Args::WINDOW;
   constexpr int D = 64, NK = D / 16, NMB = D / 32;
   constexpr int HQ = 64;                             // query rows per step
   constexpr int CPR = D / 8, RPI = 64 / CPR, NCP = 32 / RPI;         // (see dkdv_item)
@@ -537,7 +617,10 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
   const ColumnPlace at = column_place(a, bh, base);
   int cnt;
   const int32_t* idx = nullptr;
-  if constexpr (CROSS) {
+  const ColumnRows seen = column_rows(a, bh, j);
+  if constexpr (WINDOW) {
+    cnt = a.kv.group * seen.halves;
+  } else if constexpr (CROSS) {
     cnt = j * BKV < at.keys ? a.kv.group * a.Tm : 0;
   } else {
     cnt = min(max(a.col_cnt[(int64_t)bh * a.Tn + j], 0), a.Tm);   // clamped: see fwd.hip
@@ -570,6 +653,12 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
       kf[kk] = *(const bf16x8*)(a.k + off + 16 * kk);
       vf[kk] = *(const bf16x8*)(a.v + off + 16 * kk);
     }
+    if constexpr (WINDOW) {                  // (see dkdv_item)
+      const WindowRows r = key_rows(a, seen, key);
+      if (r.r0 > N - 1 || r.r1 < 0)
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) kf[kk] = vf[kk] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+    }
   }
   f32x16 dk_acc[NMB], dv_acc[NMB];
 #pragma unroll
@@ -580,16 +669,21 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
   // copies of rows 32w .. 32w + 31 of a step (swizzled and clamped as in dkdv_item)
   uint32_t voff[NCP], soff = 0;
   int rows_set = -1;
-  auto set_rows = [&](int last) {            // last: last valid row of the 32 (uniform)
-    if (last == rows_set) return;
-    rows_set = last;
+  // (WINDOW: rows that see none of the column's keys repeat the next one that does; row_b is the first row that is read)
+  auto base_row = [&](int row) -> int { return WINDOW ? min(max(row, seen.rows.r0), seen.rows.r1) : min(row, N - 1); };
+  auto set_rows = [&](int row, int row_b) {  // row: first of the 32 (uniform)
+    const int last = WINDOW ? seen.rows.r1 - row_b : min(31, N - 1 - row_b), ahead = row_b - row;        // (ahead: 0 but for WINDOW)
+    const int code = !WINDOW ? last : row >= seen.rows.r0 && row + 31 <= seen.rows.r1 ? 0 : row + 1;
+    if (code == rows_set) return;
+    rows_set = code;
     const int l = fresh_lane();
+    auto from = [&](int x) -> int { return WINDOW ? min(max(x - ahead, 0), last) : min(x, last); };
 #pragma unroll
     for (int r = 0; r < NCP; ++r) {
       const int row_l = RPI * r + l / CPR;
-      voff[r] = (uint32_t)((min(row_l, last) * a.sn + (((l % CPR) ^ swz<D>(row_l)) * 8)) * 2);
+      voff[r] = (uint32_t)((from(row_l) * a.sn + (((l % CPR) ^ swz<D>(row_l)) * 8)) * 2);
     }
-    soff = (uint32_t)(min(l & 31, last) * 4);
+    soff = (uint32_t)(from(l & 31) * 4);
   };
   const char* q_head = (const char*)(a.q + base);
   const char* o_head = (const char*)(a.d_o + base);
@@ -605,6 +699,12 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
   };
   // Query rows past N get an LSE of +infinity once their copy has landed: their P is then exactly zero.
   auto mark_rows_past_end = [&](int row0, uint32_t stat_addr) {
+    if constexpr (WINDOW) {
+      if (row0 >= seen.rows.r0 && row0 + 32 - 1 <= seen.rows.r1) return;
+      const int row = row0 + (fresh_lane() & 31);
+      if (row < seen.rows.r0 || row > seen.rows.r1) lds_stf(stat_addr + 4 * (row - row0), INFINITY);
+      return;
+    }
     if (row0 + 32 <= N) return;
     const int row_l = fresh_lane() & 31;
     if (row0 + row_l >= N) lds_stf(stat_addr + 4 * row_l, INFINITY);
@@ -612,8 +712,13 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
 
   int idx_v = 0, g_at = 0;                   // the index list, 64 entries at a time (see dkdv_item)
   if constexpr (!CROSS) idx_v = idx[min(lane, cnt - 1)];
-  const int halves = CROSS && N <= HQ ? 0 : 1;         // (see dkdv_item)
+  const int halves = WINDOW || (CROSS && N <= HQ) ? 0 : 1;         // (see dkdv_item)
   auto step_row = [&](int u) -> int {        // this wave's first row of step u (uniform, inside the chunk that idx_v holds)
+    if constexpr (WINDOW) {
+      const int e = first + u;
+      g_at = a.kv.group == 1 ? 0 : e / seen.halves;
+      return (seen.h0 + e - g_at * seen.halves) * HQ + 32 * w;
+    }
     if constexpr (CROSS) {
       const CrossEntry e = cross_entry(a, first + (u >> halves));
       g_at = e.g;
@@ -632,8 +737,8 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
 
   const int steps = CROSS ? cnt << halves : 2 * cnt;    // step u: half u & 1 of list entry u >> 1
   {
-    const int row0 = step_row(0), row_b = min(row0, N - 1);
-    set_rows(min(31, N - 1 - row_b));
+    const int row0 = step_row(0), row_b = base_row(row0);
+    set_rows(row0, row_b);
     copy_stats(head_rows() + row_b, stat_w);
     static_for<0, NCP>([&](auto R) {
       constexpr int r = decltype(R)::v;
@@ -660,8 +765,8 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
     const int st = u & 1;
     const int un = min(u + 1, steps - 1);    // past the end the last step is requested again (nobody reads it)
     if (!CROSS && ((u + 1) & 127) == 0 && u + 1 < steps) idx_v = list_load(idx, min(((u + 1) >> 1) + fresh_lane(), cnt - 1));   // next 64 entries
-    const int row_nx = step_row(un), row_b = min(row_nx, N - 1);
-    set_rows(min(31, N - 1 - row_b));
+    const int row_nx = step_row(un), row_b = base_row(row_nx);
+    set_rows(row_nx, row_b);
     const uint32_t nx_stage = sm_w + (st ^ 1) * STAGE_B, nx_stat = stat_w + (st ^ 1) * 2 * STAT_B;
     const char* qn = q_head + head_bytes() + (uint64_t)row_b * row_bytes;
     const char* on = o_head + head_bytes() + (uint64_t)row_b * row_bytes;
@@ -722,6 +827,23 @@ __device__ __forceinline__ void dkdv_item64(const Args& a, const WorkItem& item,
       if constexpr (y == NR - 1) l_raw = lds_ldf4(lb);
       __builtin_amdgcn_sched_barrier(0);
     });
+    if constexpr (WINDOW) {                  // (see dkdv_item; the rows of both waves)
+      const int g = g_at, row0 = step_row(u) - 32 * w, k0 = j * BKV + 32 * w, k1 = k0 + 31;
+      g_at = g;
+      const bool full = row0 >= k1 - a.win.right - seen.start && (k1 < a.win.sinks || row0 + HQ - 1 <= k0 + a.win.left - seen.start);
+      if (!full) {
+        const int l = fresh_lane(), from = row0 + 4 * (l >> 5);
+        WindowRows r = key_rows(a, seen, k0 + (l & 31));
+        r.r0 -= from; r.r1 -= from;
+#pragma unroll
+        for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int c = 32 * rh + 8 * (v >> 2) + (v & 3);
+            if (c < r.r0 || c > r.r1) s[rh][v] = -INFINITY;
+          }
+      }
+    }
     // ---- D - dP = D + dO (-V)^T, with exp(S - LSE) between the products
     bf16x8 ft[PDT];
     static_for<0, NR>([&](auto Y) {
@@ -838,6 +960,29 @@ void cross_dkdv_kernel(Args) {
   __shared__ __align__(1024) unsigned char smem[2 * 2 * 64 * D * 2];
   __shared__ __align__(1024) unsigned char stat_s[2 * 2 * 512];
   const Args& a = fresh_args<Args>();
+  if constexpr (Args::WINDOW) {
+    const int firsts = a.first_blocks ? stretch_wgs(a.BH * a.first_blocks) : 0, blocks = a.Tn - a.first_blocks;
+    const bool first = (int)blockIdx.x < firsts * a.sp.fixed_parts;
+    const int per_head = first ? a.first_blocks : blocks, columns = stretch_wgs(a.BH * per_head);
+    const int wg = (int)blockIdx.x - (first ? 0 : firsts * a.sp.fixed_parts);
+    const SplitPlan& sp = first ? a.sp : a.rest;
+    const HeadBlock hb = stretch_row(wg % columns, a.BH, per_head);
+    if (!hb.valid) return;
+    WorkItem item;
+    item.bh = hb.bh; item.blk = hb.blk + (first ? 0 : a.first_blocks);
+    item.part = wg / columns; item.parts = 0; item.part_len = 0; item.slot = 0;
+    const int all = a.kv.group * column_rows(a, item.bh, item.blk).halves;
+    if (all > sp.fixed_len) {
+      item.parts = (all + sp.fixed_len - 1) / sp.fixed_len;
+      item.part_len = (all + item.parts - 1) / item.parts;
+      item.slot = (hb.bh * per_head + hb.blk) * sp.fixed_parts + item.part + (first ? 0 : a.sp.pool_slots);
+    }
+    if (item.part >= max(item.parts, 1)) return;
+    OneItem walk{__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)};
+    if constexpr (D == 128) dkdv_item<D>(a, item, walk, smem, stat_s);
+    else                    dkdv_item64(a, item, walk, smem, stat_s);
+    return;
+  }
   const int columns = stretch_wgs(a.BH * a.Tn);
   const HeadBlock hb = stretch_row(blockIdx.x % columns, a.BH, a.Tn);
   if (!hb.valid) return;
@@ -857,10 +1002,9 @@ void cross_dkdv_kernel(Args) {
   else                    dkdv_item64(a, item, walk, smem, stat_s);
 }
 
-hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
-                             const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
-                             hipStream_t stream) {
-  CrossDkvFineArgs a = {};
+template <class Args>
+static void fill_cross_dkdv(Args& a, const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
+                            const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv) {
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.d_o = (const uint16_t*)d_o;
   a.lse = lse; a.delta = delta; a.dk = (uint16_t*)dk; a.dv = (uint16_t*)dv;
   a.BH = m.q.B * m.Hk; a.H = m.Hk; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
@@ -868,6 +1012,13 @@ hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const 
   a.scale = scale; a.scale_log2 = scale * LOG2E;
   a.kv = cross_keys(m, lengths);
   a.dsb = m.dsb; a.dsh = m.dsh; a.dsn = m.dsn;
+}
+
+hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
+                             const CrossDims& m, const int32_t* lengths, float scale, void* dk, void* dv, const SplitPlan& plan,
+                             hipStream_t stream) {
+  CrossDkvFineArgs a = {};
+  fill_cross_dkdv(a, q, k, v, d_o, lse, delta, m, lengths, scale, dk, dv);
   a.sp = plan;
   const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tn))), block(128);
   const bool fine = cross_few(m);
@@ -875,6 +1026,29 @@ hipError_t launch_cross_dkdv(const void* q, const void* k, const void* v, const 
   else if (m.q.d == 128)    hipLaunchKernelGGL((cross_dkdv_kernel<128, CrossDkvArgs>), grid, block, 0, stream, a);
   else if (fine)            hipLaunchKernelGGL((cross_dkdv_kernel<64, CrossDkvFineArgs>), grid, block, 0, stream, a);
   else                      hipLaunchKernelGGL((cross_dkdv_kernel<64, CrossDkvArgs>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_window_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
+                              const CrossDims& m, const int32_t* lengths, const Window& win, float scale, void* dk, void* dv,
+                              const WindowColumns& cuts, void* counters, void* pool, hipStream_t stream) {
+  WindowDkvFineArgs a = {};
+  fill_cross_dkdv(a, q, k, v, d_o, lse, delta, m, lengths, scale, dk, dv);
+  a.win = win;
+  a.first_blocks = cuts.blocks;
+  a.sp = cross_plan(cuts.first, counters, pool, dkdv_slot_bytes(m.q));
+  a.rest = cross_plan(cuts.rest, counters, pool, dkdv_slot_bytes(m.q));
+  // (slots are numbered through: the others' behind those of the first keys)
+  a.sp.arrive = (int32_t*)counters; a.sp.pool = (float*)pool; a.sp.slot_floats = (int)(dkdv_slot_bytes(m.q) / 4);
+  const int blocks = a.Tn - a.first_blocks;
+  const int64_t wgs = (a.first_blocks ? (int64_t)a.sp.fixed_parts * stretch_wgs(a.BH * a.first_blocks) : 0) +
+                      (blocks ? (int64_t)a.rest.fixed_parts * stretch_wgs(a.BH * blocks) : 0);
+  const dim3 grid((unsigned)wgs), block(128);
+  const bool fine = cross_few(m);
+  if (m.q.d == 128 && fine) hipLaunchKernelGGL((cross_dkdv_kernel<128, WindowDkvFineArgs>), grid, block, 0, stream, a);
+  else if (m.q.d == 128)    hipLaunchKernelGGL((cross_dkdv_kernel<128, WindowDkvArgs>), grid, block, 0, stream, a);
+  else if (fine)            hipLaunchKernelGGL((cross_dkdv_kernel<64, WindowDkvFineArgs>), grid, block, 0, stream, a);
+  else                      hipLaunchKernelGGL((cross_dkdv_kernel<64, WindowDkvArgs>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

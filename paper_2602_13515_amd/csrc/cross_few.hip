@@ -22,10 +22,12 @@
 #include "cross.h"
 #include "row_map.h"
 #include "spa2_device.h"
+#include "window.h"
 
 namespace spa2 {
 
 struct FewArgs {
+  static constexpr bool WINDOW = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v;
   uint16_t* o; uint16_t* o_res; float* lse;
   CrossKeys kv;
@@ -35,21 +37,36 @@ struct FewArgs {
   float scale_log2;
   float* pool; int slot_floats;  // partial results (few_slot)
 };
+// Attention over a window (window.h): a sample's keys are those blocks that its queries see, first ones and window in one line.
+struct WindowFewArgs : FewArgs {
+  static constexpr bool WINDOW = true;
+  Window win;
+};
+template <class Args>
+__device__ __forceinline__ WindowSpan few_span(const Args& a, int b, int keys) {
+  const int start = a.win.starts ? window_clamp(a.win.starts[b]) : a.win.start;
+  return window_span(a.win, keys, start, start + a.win.nq - 1);
+}
 
 constexpr int FEW_WAVES = 2;     // (two workgroups of 64 KB share a compute unit; of four waves and 128 KB one: 127 / 140 us)
 // Blocks of a sample in the line: one at least, so that every sample is somebody's.
-__device__ __forceinline__ int few_blocks(int keys) { return max((keys + BKV - 1) / BKV, 1); }
+template <class Args>
+__device__ __forceinline__ int few_blocks(const Args& a, int b, int keys) {
+  if constexpr (Args::WINDOW) return max(few_span(a, b, keys).count(), 1);
+  else                        return max((keys + BKV - 1) / BKV, 1);
+}
 
 // The line: blocks of the samples lane, 64 + lane, ..., and how many a stretch has.
 constexpr int FEW_CHUNKS = FEW_SAMPLES / 64;
 struct FewLine { int n[FEW_CHUNKS], total, per; };
-__device__ __forceinline__ FewLine few_line(const FewArgs& a, int lane) {
+template <class Args>
+__device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
   FewLine r;
   r.total = 0;
 #pragma unroll
   for (int c = 0; c < FEW_CHUNKS; ++c) {
     const int b = 64 * c + lane;
-    r.n[c] = b < a.B ? few_blocks(a.kv.lengths ? min(max(a.kv.lengths[b], 0), a.kv.Nk) : a.kv.Nk) : 0;
+    r.n[c] = b < a.B ? few_blocks(a, b, a.kv.lengths ? min(max(a.kv.lengths[b], 0), a.kv.Nk) : a.kv.Nk) : 0;
   }
 #pragma unroll
   for (int c = 0; c < FEW_CHUNKS; ++c) r.total += r.n[c];
@@ -109,8 +126,12 @@ __device__ __forceinline__ int few_slot(const FewArgs& a, const FewParts& s, int
 __device__ __forceinline__ int64_t few_row(const FewArgs& a, int b, int hk, int r) {
   return b * a.sb + ((int64_t)hk * a.kv.group + r / a.Nq) * a.sh + (r % a.Nq) * a.sn;
 }
-__device__ __forceinline__ void few_finish(const FewArgs& a, int b, int hk, int row, int c, f32x4 x, float m, float l) {
-  const float inv = 1.f / l;
+template <class Args>
+__device__ __forceinline__ void few_finish(const Args& a, int b, int hk, int row, int c, f32x4 x, float m, float l) {
+  float inv = 1.f / l;
+  if constexpr (Args::WINDOW) {
+    if (window_blind(a.win, cross_length(a.kv, b), window_start(a.win, b) + row % a.win.nq)) inv = 0.f;
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] *= inv;
   const u32x2 out = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -135,9 +156,11 @@ struct FewLds {
 };
 
 // Keys [key0, key1) of sample b and key head hk; its result goes to a slot where others share the sample (slot >= 0).
+// (WINDOW: keys of the line of the sample's blocks, so many from its start)
 struct FewPiece { int b, hk, key0, key1, slot; };
-template <int D>
-__device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, FewLds<D>& lds) {
+template <int D, class Args>
+__device__ __forceinline__ void few_piece(const Args& a, const FewPiece& pc, FewLds<D>& lds) {
+  constexpr bool WINDOW = Args::WINDOW;
   constexpr int TK = 32, NK = D / 16, NMB = D / 32, CPR = D / 8, RPI = 64 / CPR, NCP = TK / RPI, WAVES = FEW_WAVES, NT = 64 * WAVES;
   constexpr int TILE_B = FewLds<D>::TILE_B, STAGE_B = FewLds<D>::STAGE_B, WAVE_B = FewLds<D>::WAVE_B;
   constexpr int PITCH = D + 4;                                                        // floats a row in the exchange
@@ -166,18 +189,37 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
   const int tiles_all = (key1 - key0 + TK - 1) / TK, tiles = (tiles_all - w + WAVES - 1) / WAVES;   // this wave's: w, w + WAVES, ...
   uint32_t voff[NCP];
   int rows_set = -1;
+  // (WINDOW) what the sample's queries see, and this lane's: first keys and from `near` to `last`
+  WindowSpan span;
+  int keys = 0, start = 0, last_seen = 0, near = 0;
+  if constexpr (WINDOW) {
+    keys = cross_length(a.kv, b);
+    start = window_start(a.win, b);
+    span = window_span(a.win, keys, start, start + a.win.nq - 1);
+    const int p = start + min(r32, a.rows - 1) % a.win.nq;
+    last_seen = min(p + a.win.right, keys - 1);
+    near = p - a.win.left;
+  }
+  auto place = [&](int t) -> int {                       // first key of this wave's tile t
+    const int at = key0 + (w + WAVES * t) * TK;
+    if constexpr (WINDOW) return span.block(at / BKV) * BKV + at % BKV;
+    else                  return at;
+  };
   auto copy_tile = [&](int t, uint32_t stage) {
-    const int at = key0 + (w + WAVES * t) * TK, last = min(TK, key1 - at) - 1;
+    // (WINDOW: keys that none of the queries sees are not read; offsets are then those from the block's start)
+    const int at = place(t);
+    const bool part_seen = WINDOW && !span.whole(at / BKV);
+    const int last = WINDOW ? (part_seen ? TK + at : TK - 1) : min(TK, key1 - at) - 1, origin = part_seen ? at / BKV * BKV : at;
     if (last != rows_set) {
       rows_set = last;
 #pragma unroll
       for (int r = 0; r < NCP; ++r) {
-        const int row = RPI * r + lane / CPR;
-        voff[r] = (uint32_t)((min(row, last) * a.kv.sn + (((lane % CPR) ^ swz<D>(row)) * 8)) * 2);
+        const int row = RPI * r + lane / CPR, from = part_seen ? span.stand_in(at / BKV, at + row) - origin : min(row, last);
+        voff[r] = (uint32_t)((from * a.kv.sn + (((lane % CPR) ^ swz<D>(row)) * 8)) * 2);
       }
     }
-    const char* kp = k_head + (uint64_t)at * row_bytes;
-    const char* vp = v_head + (uint64_t)at * row_bytes;
+    const char* kp = k_head + (uint64_t)origin * row_bytes;
+    const char* vp = v_head + (uint64_t)origin * row_bytes;
     static_for<0, NCP>([&](auto R) { raw_copy16_to_lds_at<decltype(R)::v * 1024>(kp, voff[decltype(R)::v], stage); });
     static_for<0, NCP>([&](auto R) { raw_copy16_to_lds_at<TILE_B + decltype(R)::v * 1024>(vp, voff[decltype(R)::v], stage); });
   };
@@ -212,8 +254,16 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
     f32x16 s = zero;
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) s = mfma32(lds_ld16(ka ^ (kk << 5)), qf[kk], s);
-    const int valid = key1 - (key0 + (w + WAVES * t) * TK) - 4 * hf;
-    if (valid + 4 * hf < TK) {
+    const int at = place(t), valid = key1 - at - 4 * hf;
+    if constexpr (WINDOW) {
+      if (!window_full(a.win, keys, start, start + a.win.nq - 1, at, at + TK - 1)) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int key = at + 8 * (v >> 2) + (v & 3) + 4 * hf;
+          if (key > last_seen || (key < near && key >= a.win.sinks)) s[v] = -INFINITY;
+        }
+      }
+    } else if (valid + 4 * hf < TK) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         if (8 * (v >> 2) + (v & 3) >= valid) s[v] = -INFINITY;
@@ -294,11 +344,21 @@ __device__ __forceinline__ void few_piece(const FewArgs& a, const FewPiece& pc, 
   }
 }
 
-template <int D>
-__global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(FewArgs a) {
+// keys of a sample's line
+template <class Args>
+__device__ __forceinline__ int few_keys(const Args& a, int b) {
+  const int keys = cross_length(a.kv, b);
+  if constexpr (Args::WINDOW) {
+    const WindowSpan s = few_span(a, b, keys);
+    return s.count() ? (s.count() - 1) * BKV + min(BKV, s.hi - s.block(s.count() - 1) * BKV) : 0;
+  }
+  return keys;
+}
+template <int D, class Args>
+__global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(Args a) {
   __shared__ __align__(1024) FewLds<D> lds;
   if (a.workers == 0) {
-    const int b = blockIdx.x / a.Hk, keys = cross_length(a.kv, b);
+    const int b = blockIdx.x / a.Hk, keys = few_keys(a, b);
     few_piece<D>(a, FewPiece{b, (int)blockIdx.x % a.Hk, 0, keys, -1}, lds);
     return;
   }
@@ -309,7 +369,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(FewArgs a) {
   const FewSample start = few_sample(a, line, begin, lane);
   int first = start.first;                               // of sample b
   for (int b = start.b, at = begin; at < stop; ++b) {
-    const int keys = cross_length(a.kv, b), n = few_blocks(keys), end = min(first + n, stop);
+    const int keys = few_keys(a, b), n = few_blocks(a, b, cross_length(a.kv, b)), end = min(first + n, stop);
     const FewParts s = few_parts(first, n, line.per);
     const FewPiece pc = {b, hk, (at - first) * BKV, min(keys, (end - first) * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, i - s.i0)};
     few_piece<D>(a, pc, lds);
@@ -321,15 +381,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(FewArgs a) {
 
 // Row `row` of a (sample, key head) whose keys several workgroups shared: their results, joined.  A thread takes four channels and
 // every G-th part, in order; then the G are added in order.
-template <int D>
-__global__ __launch_bounds__(256) void cross_few_join_kernel(FewArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256) void cross_few_join_kernel(Args a) {
   constexpr int QUADS = D / 4, G = 256 / QUADS;
   __shared__ __align__(16) float sums[G][D];
   __shared__ float stat[G][2];
   const int row = blockIdx.x % a.rows, unit = blockIdx.x / a.rows, b = unit / a.Hk, hk = unit % a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % QUADS, g = tid / QUADS;
   const FewLine line = few_line(a, lane);
-  const FewParts s = few_parts(few_first(line, b, lane), few_blocks(cross_length(a.kv, b)), line.per);
+  const FewParts s = few_parts(few_first(line, b, lane), few_blocks(a, b, cross_length(a.kv, b)), line.per);
   if (s.parts == 1) return;
   float m = -INFINITY, l = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -371,27 +431,39 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(FewArgs a) {
   few_finish(a, b, hk, row, c, sum, m, l);
 }
 
-hipError_t launch_cross_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
-                            void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
-  FewArgs a = {};
+template <class Args>
+static hipError_t launch_few(Args& a, const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
+                             void* o, void* o_res, float* lse, int workers, void* ws, hipStream_t stream) {
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
   a.o = (uint16_t*)o; a.o_res = (uint16_t*)o_res; a.lse = lse;
   a.kv = cross_keys(m, lengths);
   a.B = m.q.B; a.Hk = m.Hk; a.Nq = m.q.N; a.rows = m.group * m.q.N;
   a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
   a.scale_log2 = scale * LOG2E;
-  a.workers = cross_few_ws(m).workers;
+  a.workers = workers;
   a.pool = (float*)ws;
   a.slot_floats = (int)(few_slot_bytes(a.rows, m.q.d) / 4);
   const dim3 grid((unsigned)((a.workers ? a.workers : m.q.B) * m.Hk)), block(64 * FEW_WAVES);
-  if (m.q.d == 128) hipLaunchKernelGGL(cross_few_kernel<128>, grid, block, 0, stream, a);
-  else              hipLaunchKernelGGL(cross_few_kernel<64>, grid, block, 0, stream, a);
+  if (m.q.d == 128) hipLaunchKernelGGL((cross_few_kernel<128, Args>), grid, block, 0, stream, a);
+  else              hipLaunchKernelGGL((cross_few_kernel<64, Args>), grid, block, 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.workers <= 1) return e;
   const dim3 rows((unsigned)(m.q.B * m.Hk * a.rows));
-  if (m.q.d == 128) hipLaunchKernelGGL(cross_few_join_kernel<128>, rows, dim3(256), 0, stream, a);
-  else              hipLaunchKernelGGL(cross_few_join_kernel<64>, rows, dim3(256), 0, stream, a);
+  if (m.q.d == 128) hipLaunchKernelGGL((cross_few_join_kernel<128, Args>), rows, dim3(256), 0, stream, a);
+  else              hipLaunchKernelGGL((cross_few_join_kernel<64, Args>), rows, dim3(256), 0, stream, a);
   return hipGetLastError();
+}
+
+hipError_t launch_cross_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
+                            void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
+  FewArgs a = {};
+  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, cross_few_ws(m).workers, ws, stream);
+}
+hipError_t launch_window_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,
+                             float scale, void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
+  WindowFewArgs a = {};
+  a.win = win;
+  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, window_few_ws(m, win).workers, ws, stream);
 }
 
 }  // namespace spa2

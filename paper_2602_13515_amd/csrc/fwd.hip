@@ -18,11 +18,12 @@
 #include "row_map.h"
 #include "spa2_device.h"
 #include "spa2_internal.h"
+#include "window.h"
 
 namespace spa2 {
 
 struct FwdArgs {
-  static constexpr bool CROSS = false;
+  static constexpr bool CROSS = false, WINDOW = false;
   const uint16_t* q; const uint16_t* k; const uint16_t* v;
   uint16_t* o; uint16_t* o_res; float* lse;
   const int32_t* row_cnt; const int32_t* row_idx; const int32_t* row_order;
@@ -43,6 +44,12 @@ struct CrossFwdArgs : FwdArgs {
   CrossKeys kv;
 };
 
+// Attention over a window (window.h): a row's list is its blocks of first keys, then those of its window.
+struct WindowFwdArgs : CrossFwdArgs {
+  static constexpr bool WINDOW = true;
+  Window win;
+};
+
 // Partial result of one part of a split row: the unnormalised accumulator as [pair of accumulator registers][thread],
 // so that the 64 lanes of a wave write and read consecutive 8-byte pieces, then per thread the running maximum (log2
 // units) and the row sum, both already combined over the two halves of the wave.
@@ -53,8 +60,8 @@ size_t fwd_slot_bytes(const Dims& m) { return (size_t)(m.d == 128 ? fwd_slot_flo
 // area: LDS of the wave's own for both outputs, which the other waves may still be reading.
 template <int D>
 __device__ __forceinline__ void fwd_store_rows(const FwdArgs& a, int bh, int64_t base, int q0, int lane, uint32_t area,
-                                               const f32x16 (&oacc)[D / 32], float m_run, float l_tot) {
-  const float inv = 1.f / l_tot;
+                                               const f32x16 (&oacc)[D / 32], float m_run, float l_tot, bool blind = false) {
+  const float inv = blind ? 0.f : 1.f / l_tot;         // (blind: a row that sees no key)
   const int r32 = lane & 31, hf = lane >> 5, valid = min(32, a.N - q0);
   constexpr int RES = 32 * D * 2;
   __syncthreads();
@@ -84,7 +91,7 @@ __device__ __forceinline__ void fwd_store_rows(const FwdArgs& a, int bh, int64_t
 
 template <int D, class Args>
 __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
-  constexpr bool CROSS = Args::CROSS;
+  constexpr bool CROSS = Args::CROSS, WINDOW = Args::WINDOW;
   constexpr int NK = D / 16, NMB = D / 32;           // contraction steps of S, output blocks of O
   // Three K and two V tiles, XOR-swizzled and unpadded (the layout a direct global -> LDS copy can write); two
   // workgroups of 80 KB share a compute unit.  (Aligned: compile-time parts are XORed into addresses.)
@@ -97,15 +104,26 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   bool whole = false;         // a row of the plan that may be split: its parts are the first workgroups
   int slot = blockIdx.x;
   int keys = a.N;             // keys that the row sees at most
+  int start = 0;              // (WINDOW) place of query 0, and what the workgroup's queries see
+  WindowSpan span;
   if constexpr (CROSS) {
     const int rows = stretch_wgs(a.BH * a.Tm);
     const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
     if (!hb.valid) return;
     bh = hb.bh; i = hb.blk;
     keys = cross_length(a.kv, bh / a.H);
-    const int all = (keys + BKV - 1) / BKV;
+    int all = (keys + BKV - 1) / BKV;
     part = blockIdx.x / rows;
-    parts = cross_parts_of(a, bh);
+    if constexpr (WINDOW) {
+      start = window_start(a.win, bh / a.H);
+      int p0, p1;
+      window_places(a.win, start, a.N, i * BQ, min(i * BQ + BQ, a.N) - 1, p0, p1);
+      span = window_span(a.win, keys, p0, p1);
+      all = span.count();
+      parts = window_parts(a, all);
+    } else {
+      parts = cross_parts_of(a, bh);
+    }
     if (part >= max(parts, 1)) return;
     if (parts) part_len = (all + parts - 1) / parts;
     slot = (bh * a.Tm + i) * a.sp.fixed_parts + part;
@@ -146,7 +164,8 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   int cnt, split_at = 0, first;              // entries [first, first + part_len) of the list of a split row (never empty)
   const int32_t* idx = nullptr;
   if constexpr (CROSS) {
-    cnt = (keys + BKV - 1) / BKV;
+    if constexpr (WINDOW) cnt = span.count();
+    else                  cnt = (keys + BKV - 1) / BKV;
     first = part * part_len;
   } else {
     cnt = min(max(a.row_cnt[unit], 0), a.Tn);
@@ -212,6 +231,19 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   uint32_t voff[CH];
   int rows_set = -1;
   auto set_rows = [&](int j) {               // for the tile of key block j (uniform)
+    if constexpr (WINDOW) {                  // (keys that none of the workgroup's queries sees are not read)
+      const bool whole_block = span.whole(j);
+      const int code = whole_block ? 0 : j + 1;
+      if (code == rows_set) return;
+      rows_set = code;
+      const int t = fresh_tid(), ld_row = t / CPR, ld_c8 = ((t % CPR) ^ swz<D>(ld_row)) * 8;
+#pragma unroll
+      for (int r = 0; r < CH; ++r) {
+        const int row = ld_row + RSTEP * r, from = whole_block ? row : span.stand_in(j, j * BKV + row) - j * BKV;
+        voff[r] = (uint32_t)((from * key_sn + ld_c8) * 2);
+      }
+      return;
+    }
     const int last = min(BKV - 1, keys - 1 - j * BKV);
     if (last == rows_set) return;
     rows_set = last;
@@ -268,7 +300,8 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   int left = cnt - 1;                        // entries behind the one at pos (past the end the last one is taken again)
   auto next_entry = [&]() -> int {
     if constexpr (CROSS) {
-      const int j = first + pos;
+      int j = first + pos;
+      if constexpr (WINDOW) j = span.block(j);
       if (left > 0) { --left; ++pos; }
       return j;
     }
@@ -295,6 +328,23 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   };
   // keys past N (short last block) do not take part in the softmax
   auto mask_tail = [&](f32x16 (&s)[2], int j) {
+    if constexpr (WINDOW) {
+      int p0, p1;                            // (of the wave's rows, those past the end included)
+      window_places(a.win, start, a.N, i * BQ + 32 * w, i * BQ + 32 * w + 31, p0, p1);
+      if (!window_full(a.win, keys, p0, p1, j * BKV, j * BKV + BKV - 1)) {
+        const int t = fresh_tid() & 63, at = j * BKV + 4 * (t >> 5);
+        const int p = window_place(a.win, start, a.N, i * BQ + 32 * w + (t & 31));
+        const int last = min(p + a.win.right, keys - 1) - at, near = p - a.win.left - at, early = a.win.sinks - at;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int c = kb * 32 + 8 * (v >> 2) + (v & 3);
+            if (c > last || (c < near && c >= early)) s[kb][v] = -INFINITY;
+          }
+      }
+      return;
+    }
     if ((j + 1) * BKV > keys) {
       const int valid = keys - j * BKV - 4 * ((fresh_tid() & 63) >> 5);
 #pragma unroll
@@ -505,7 +555,9 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
     return;
   }
   // O_i = diag(l)^-1 O (step 18) and the log-sum-exp the backward pass needs
-  fwd_store_rows<D>(a, bh, base, i * BQ + 32 * w, lane, sm + w * OUT_B, oacc, m_run, l_tot);
+  bool blind = false;
+  if constexpr (WINDOW) blind = window_blind(a.win, keys, window_place(a.win, start, a.N, i * BQ + 32 * w + (lane & 31)));
+  fwd_store_rows<D>(a, bh, base, i * BQ + 32 * w, lane, sm + w * OUT_B, oacc, m_run, l_tot, blind);
 }
 
 hipError_t launch_fwd(const void* q, const void* k, const void* v, const Dims& m, const int32_t* row_cnt,
@@ -535,13 +587,22 @@ hipError_t launch_fwd(const void* q, const void* k, const void* v, const Dims& m
 // The results of a row's parts, joined in part order: a workgroup takes 32 rows and 32 channels, each of its waves every fourth
 // part, and then adds up the four.  (Joined by the last part to arrive,
 // 128 queries, 2 heads, 65,536 keys, d = 128 took 96 us, forward and backward 263; now 62 and 192.)
-template <int D>
-__global__ __launch_bounds__(256) void cross_fwd_join_kernel(CrossFwdArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256) void cross_fwd_join_kernel(Args a) {
   constexpr int NMB = D / 32;
   __shared__ float sums[4][16][64], stat[4][2][64];
   const int mb = blockIdx.x % NMB, w = blockIdx.x / NMB % 4, unit = blockIdx.x / (4 * NMB), bh = unit / a.Tm, i = unit % a.Tm;
-  const int parts = cross_parts_of(a, bh), lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  int parts;
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
   const int row = i * BQ + 32 * w + (lane & 31), hf = lane >> 5;
+  bool blind = false;
+  if constexpr (Args::WINDOW) {
+    const int keys = cross_length(a.kv, bh / a.H), start = window_start(a.win, bh / a.H);
+    parts = window_parts(a, window_count(a, bh, i));
+    blind = window_blind(a.win, keys, window_place(a.win, start, a.N, row));
+  } else {
+    parts = cross_parts_of(a, bh);
+  }
   if (parts == 0 || i * BQ + 32 * w >= a.N) return;
   const float* p0 = a.sp.pool + (int64_t)unit * a.sp.fixed_parts * a.sp.slot_floats;
   float m = -INFINITY, l = 0.f, x[16];
@@ -583,7 +644,7 @@ __global__ __launch_bounds__(256) void cross_fwd_join_kernel(CrossFwdArgs a) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) x[v] = fmaf(sums[u][v][lane], f, x[v]);
   }
-  const float inv = 1.f / l;
+  const float inv = blind ? 0.f : 1.f / l;
   const int64_t off = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh + (int64_t)row * a.sn + 32 * mb + 4 * hf;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {                          // channels 32 mb + 8 q + 4 hf ..
@@ -618,8 +679,31 @@ hipError_t launch_cross_fwd(const void* q, const void* k, const void* v, const C
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !w.s.slots) return e;
   const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));
-  if (m.q.d == 128) hipLaunchKernelGGL(cross_fwd_join_kernel<128>, joins, block, 0, stream, a);
-  else              hipLaunchKernelGGL(cross_fwd_join_kernel<64>, joins, block, 0, stream, a);
+  if (m.q.d == 128) hipLaunchKernelGGL((cross_fwd_join_kernel<128, CrossFwdArgs>), joins, block, 0, stream, a);
+  else              hipLaunchKernelGGL((cross_fwd_join_kernel<64, CrossFwdArgs>), joins, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_window_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,
+                             float scale, void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
+  WindowFwdArgs a = {};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.o = (uint16_t*)o; a.o_res = (uint16_t*)o_res; a.lse = lse;
+  a.BH = m.q.B * m.q.H; a.H = m.q.H; a.N = m.q.N; a.Tm = m.q.Tm; a.Tn = m.q.Tn;
+  a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
+  a.scale_log2 = scale * LOG2E;
+  a.kv = cross_keys(m, lengths);
+  a.win = win;
+  const CrossSection s = window_fwd_section(m, win);
+  a.sp = cross_plan(s, nullptr, ws, fwd_slot_bytes(m.q));
+  const dim3 grid((unsigned)(s.cut.parts * stretch_wgs(a.BH * a.Tm))), block(256);
+  if (m.q.d == 128) hipLaunchKernelGGL((fwd_kernel<128, WindowFwdArgs>), grid, block, 0, stream, a);
+  else              hipLaunchKernelGGL((fwd_kernel<64, WindowFwdArgs>), grid, block, 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !s.slots) return e;
+  const dim3 joins((unsigned)(a.BH * a.Tm * (m.q.d / 32) * 4));
+  if (m.q.d == 128) hipLaunchKernelGGL((cross_fwd_join_kernel<128, WindowFwdArgs>), joins, block, 0, stream, a);
+  else              hipLaunchKernelGGL((cross_fwd_join_kernel<64, WindowFwdArgs>), joins, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -619,6 +619,94 @@ Tensor dropout_add(const Tensor& x, const OptTensor& residual, double p, int64_t
   return DropoutAdd::apply(x, residual, p, seed, offset, seed_offset);
 }
 
+// ---- attention over a window
+// (limits: left, right, negative for none, and sinks)
+void window_check(const Tensor& q, const Tensor& k, const Tensor& starts, const std::vector<int64_t>& limits) {
+  TORCH_CHECK_VALUE(!starts.defined() || (starts.scalar_type() == at::kInt && starts.dim() == 1 && starts.size(0) == q.size(0) &&
+                                          starts.is_contiguous() && starts.device() == q.device()),
+                    "starts are int32 [B] on the device of q");
+  TORCH_CHECK_VALUE(starts.defined() || q.size(2) <= k.size(2), "more queries than keys: starts say where they stand");
+  for (const int64_t n : limits) TORCH_CHECK_VALUE(n <= (1 << 28), "left, right and sinks are at most 2^28 (None: no limit)");
+}
+spa2_window window_of(const std::vector<int64_t>& limits) {
+  return {(int32_t)std::max<int64_t>(limits[0], -1), (int32_t)std::max<int64_t>(limits[1], -1), (int32_t)limits[2]};
+}
+
+CrossResult window_call(const Tensor& q_in, const Tensor& k_in, const Tensor& v_in, const Tensor& lengths, const Tensor& starts,
+                        const std::vector<int64_t>& limits, double scale, bool training) {
+  const c10::DeviceGuard device(q_in.device());
+  const bool one_layout = strides_of(k_in) == strides_of(v_in);
+  CrossResult r;
+  r.q = without_gaps(q_in);
+  r.k = one_layout ? k_in : copy_of(k_in);
+  r.v = one_layout ? v_in : in_order(v_in, r.k);
+  const CrossShape c(r.q, r.k, r.k);
+  const spa2_window w = window_of(limits);
+  r.o = like(r.q);
+  if (training && r.k.size(2) > 64) r.o_res = like(r.q);
+  const int64_t need = (int64_t)spa2_window_fwd_workspace_bytes(&c.s, &w), at = (need + 255) & ~(int64_t)255;
+  const int64_t rows = r.q.size(0) * r.q.size(1) * r.q.size(2);
+  if (training) r.lse = at::empty({r.q.size(0), r.q.size(1), r.q.size(2)}, r.q.options().dtype(at::kFloat));
+  const Tensor ws = !training || need ? bytes(training ? need : at + 4 * rows, r.q) : Tensor();
+  float* lse = training ? (float*)r.lse.data_ptr() : (float*)((char*)ws.data_ptr() + at);
+  check(spa2_window_fwd(r.q.data_ptr(), r.k.data_ptr(), r.v.data_ptr(), (const int32_t*)ptr(lengths), (const int32_t*)ptr(starts), &c.s,
+                        &w, (float)scale, r.o.data_ptr(), (void*)ptr(r.o_res), lse, (void*)ptr(ws), (size_t)need, stream_of(r.q)),
+        "spa2_window_fwd");
+  return r;
+}
+
+struct WindowAttention : torch::autograd::Function<WindowAttention> {
+  static Tensor forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const OptTensor& lengths_,
+                        const OptTensor& starts_, const std::vector<int64_t>& limits, double scale) {
+    const Tensor lengths = or_none(lengths_), starts = or_none(starts_);
+    const CrossResult r = window_call(q, k, v, lengths, starts, limits, scale, true);
+    ctx->save_for_backward({r.q, r.k, r.v, r.o, r.o_res, r.lse, lengths, starts});
+    ctx->saved_data["keys"] = r.k.sizes().vec();
+    ctx->saved_data["limits"] = limits;
+    ctx->saved_data["scale"] = scale;
+    return r.o;
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const bool graph = at::GradMode::is_enabled();
+    const at::NoGradGuard no_graph;
+    const variable_list s = ctx->get_saved_variables();
+    const Tensor &q = s[0], &k = s[1], &v = s[2], &o = s[3], &o_res = s[4], &lse = s[5], &lengths = s[6], &starts = s[7];
+    const std::vector<int64_t> limits = ctx->saved_data["limits"].toIntVector();
+    // (saved-tensor hooks may bring something else back)
+    cross_check(q, k, v, lengths);
+    window_check(q, k, starts, limits);
+    TORCH_CHECK_VALUE(k.sizes().vec() == ctx->saved_data["keys"].toIntVector() && strides_of(k) == strides_of(v),
+                      "saved k and v come back in their shape and one layout");
+    TORCH_CHECK_VALUE(grads[0].sizes() == q.sizes() && grads[0].device() == q.device(), "saved q comes back in its shape on its GPU");
+    same_layout(q, {&o});
+    if (o_res.defined()) same_layout(q, {&o_res});
+    TORCH_CHECK_VALUE(lse.device() == q.device() && lse.scalar_type() == at::kFloat && lse.is_contiguous() &&
+                      lse.numel() == q.size(0) * q.size(1) * q.size(2), "the log-sum-exp comes back as B * H * N contiguous fp32 numbers");
+    const c10::DeviceGuard device(q.device());
+    const Tensor d_o = in_order(grads[0].to(at::kBFloat16), q);
+    const Tensor dq = like(q), dk = dense_like(k, k.scalar_type()), dv = dense_like(k, k.scalar_type());
+    const CrossShape c(q, k, dk);
+    const spa2_window w = window_of(limits);
+    const int64_t need = (int64_t)spa2_window_bwd_workspace_bytes(&c.s, &w);
+    const Tensor ws = bytes(need, q);
+    check(spa2_window_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), (const int32_t*)ptr(lengths), (const int32_t*)ptr(starts), o.data_ptr(),
+                          (void*)ptr(o_res), d_o.data_ptr(), (const float*)lse.data_ptr(), &c.s, &w,
+                          (float)ctx->saved_data["scale"].toDouble(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(),
+                          (size_t)need, stream_of(q)), "spa2_window_bwd");
+    return once({dq, dk, dv, Variable(), Variable(), Variable(), Variable()}, graph, "window_attention");
+  }
+};
+
+Tensor window_attention(const Tensor& q, const Tensor& k, const Tensor& v, const std::vector<int64_t>& limits, const OptTensor& lengths,
+                        const OptTensor& starts, double scale) {
+  cross_check(q, k, v, or_none(lengths));
+  window_check(q, k, or_none(starts), limits);
+  if (!differentiated({&q, &k, &v})) return window_call(q, k, v, or_none(lengths), or_none(starts), limits, scale, false).o;
+  capture_check(q, {q, k, v});
+  return WindowAttention::apply(q, k, v, lengths, starts, limits, scale);
+}
+
 // ---- a branch, normed and gated, added to the residual stream, and the norm of the sum
 struct GateInputs {
   Tensor x, branch, gate, branch_weight, weight, bias, scale, shift;      // (packed; parameters of one type)
@@ -882,6 +970,7 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("norm_rotate", &norm_rotate, py::call_guard<py::gil_scoped_release>());
   m.def("cross_attention", &cross_attention, py::call_guard<py::gil_scoped_release>());
   m.def("dropout_add", &dropout_add, py::call_guard<py::gil_scoped_release>());
+  m.def("window_attention", &window_attention, py::call_guard<py::gil_scoped_release>());
   m.def("gate_add_norm", &gate_add_norm, py::call_guard<py::gil_scoped_release>());
   m.def("clip_gradients", &clip_gradients, py::call_guard<py::gil_scoped_release>());
   m.def("velocity_loss", &velocity_loss, py::call_guard<py::gil_scoped_release>());

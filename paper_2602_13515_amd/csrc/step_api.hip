@@ -1,6 +1,7 @@
 // Entry points of the operators of a training step around the attention: argument checks, then the launches.
-#include "spa2_check.h"
+#include "cross_check.h"
 #include "step_ops.h"
+#include "window.h"
 
 using namespace spa2;
 
@@ -43,9 +44,101 @@ int check_gate(const void* branch, const spa2_gate_params* p, const spa2_gate_sh
 // what a call without a branch, or without its norm, does not look at
 spa2_gate_params used_params(const spa2_gate_params& p, const spa2_gate_shape& s) { return {p.gate, s.post ? p.branch_weight : nullptr, p.weight, p.bias, p.scale, p.shift}; }
 
+// ---- attention over a window
+int check_window(const spa2_cross_shape* s, const spa2_window* w) {
+  const int rc = check_cross_shape(s);
+  if (rc != SPA2_OK) return rc;
+  if (!w) return SPA2_ERR_NULL;
+  if (s->Nq > WINDOW_MOST || s->Nk > WINDOW_MOST) return SPA2_ERR_SHAPE;
+  if (w->left > WINDOW_MOST || w->right > WINDOW_MOST || w->sinks < 0 || w->sinks > WINDOW_MOST) return SPA2_ERR_RANGE;
+  return SPA2_OK;
+}
+
+Window window_of(const spa2_cross_shape& s, const spa2_window& w, const int32_t* starts) {
+  Window r;
+  r.starts = starts;
+  r.start = s.Nk - s.Nq;
+  r.left = w.left < 0 ? WINDOW_NO_LIMIT : w.left;
+  r.right = w.right < 0 ? WINDOW_NO_LIMIT : w.right;
+  r.sinks = w.left < 0 ? 0 : w.sinks < s.Nk ? w.sinks : s.Nk;
+  r.nq = s.Nq;
+  return r;
+}
+
+// Query heads of a key head are taken as one head of more rows where that widens no block's places: heads of up to half a block.
+constexpr int WINDOW_JOIN = 64;
+CrossDims window_dims(const spa2_cross_shape& s) { return cross_dims(s, WINDOW_JOIN); }
+// (dK/dV goes through a column's queries by their place: head by head)
+CrossDims window_bwd_dims(const spa2_cross_shape& s) { return cross_dims(s, 0); }
+
+size_t window_fwd_bytes(const CrossDims& m, const Window& w) {
+  return cross_few(m) ? window_few_ws(m, w).total : window_fwd_section(m, w).pool;
+}
+
+int check_window_call(const void* q, const void* k, const void* v, const int32_t* lengths, const int32_t* starts, const void* o,
+                      const void* o_res, const float* lse, const spa2_cross_shape* s, const spa2_window* w, float scale) {
+  const int rc = check_window(s, w);
+  if (rc != SPA2_OK) return rc;
+  if (!q || !k || !v || !o || !lse) return SPA2_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_res) || (uintptr_t)lengths % 4 ||
+      (uintptr_t)starts % 4 || (uintptr_t)lse % 4)
+    return SPA2_ERR_ALIGN;
+  if (!(scale > 0.f) || !isfinite(scale)) return SPA2_ERR_RANGE;
+  return SPA2_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t spa2_window_fwd_workspace_bytes(const spa2_cross_shape* shape, const spa2_window* window) {
+  if (check_window(shape, window) != SPA2_OK) return 0;
+  return window_fwd_bytes(window_dims(*shape), window_of(*shape, *window, nullptr));
+}
+
+size_t spa2_window_bwd_workspace_bytes(const spa2_cross_shape* shape, const spa2_window* window) {
+  if (check_window(shape, window) != SPA2_OK) return 0;
+  return window_bwd_ws(window_bwd_dims(*shape), window_of(*shape, *window, nullptr)).total;
+}
+
+int spa2_window_fwd(const void* q, const void* k, const void* v, const int32_t* lengths, const int32_t* starts,
+                    const spa2_cross_shape* shape, const spa2_window* window, float scale, void* o, void* o_res, float* lse,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  const int rc = check_window_call(q, k, v, lengths, starts, o, o_res, lse, shape, window, scale);
+  if (rc != SPA2_OK) return rc;
+  const CrossDims m = window_dims(*shape);
+  const Window w = window_of(*shape, *window, starts);
+  const size_t need = window_fwd_bytes(m, w);
+  if (need && (!workspace || workspace_bytes < need)) return SPA2_ERR_WORKSPACE;
+  if (need && !aligned16(workspace)) return SPA2_ERR_ALIGN;
+  return (cross_few(m) ? launch_window_few : launch_window_fwd)(q, k, v, m, lengths, w, scale, o, o_res, lse, workspace,
+                                                               (hipStream_t)stream) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
+
+int spa2_window_bwd(const void* q, const void* k, const void* v, const int32_t* lengths, const int32_t* starts, const void* o,
+                    const void* o_res, const void* d_o, const float* lse, const spa2_cross_shape* shape, const spa2_window* window,
+                    float scale, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_window_call(q, k, v, lengths, starts, o, o_res, lse, shape, window, scale);
+  if (rc == SPA2_OK) rc = check_strides(shape->d_sb, shape->d_sh, shape->d_sn, 1, shape->d);
+  if (rc != SPA2_OK) return rc;
+  if (!d_o || !dq || !dk || !dv) return SPA2_ERR_NULL;
+  if (!aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv)) return SPA2_ERR_ALIGN;
+  const CrossDims m = window_bwd_dims(*shape);
+  const Window w = window_of(*shape, *window, starts);
+  const WindowBwdWs s = window_bwd_ws(m, w);
+  if (!workspace || workspace_bytes < s.total) return SPA2_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return SPA2_ERR_ALIGN;
+  char* ws = (char*)workspace;
+  float *delta = (float*)ws, *lse_again = (float*)(ws + s.lse);
+  int32_t* counters = (int32_t*)(ws + s.dkdv_at);
+  hipStream_t st = (hipStream_t)stream;
+  const SplitPlan rows = cross_plan(s.dq, nullptr, ws + s.dq_at, dq_slot_bytes(m.q));
+  if (launch_window_dq(q, k, v, o, o_res, d_o, lse, m, lengths, w, scale, delta, lse_again, dq, counters,
+                       s.dkdv.first.slots + s.dkdv.rest.slots, rows, st) != hipSuccess)
+    return SPA2_ERR_LAUNCH;
+  return launch_window_dkdv(q, k, v, d_o, lse_again, delta, m, lengths, w, scale, dk, dv, s.dkdv, counters,
+                            ws + s.dkdv_at + s.dkdv.counters, st) == hipSuccess ? SPA2_OK : SPA2_ERR_LAUNCH;
+}
 
 size_t spa2_gate_norm_bwd_workspace_bytes(const spa2_gate_shape* shape) {
   if (check_gate_shape(shape) != SPA2_OK) return 0;

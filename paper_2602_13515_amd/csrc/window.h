@@ -1,0 +1,169 @@
+// Attention over a window: which keys a query sees, and which blocks of keys (queries) a block of queries (keys) has to do with.
+//
+//   query i of sample b stands at place p = start_b + i and sees the keys j < length_b with j <= p + right and (j >= p - left or
+//   j < sinks).
+//
+// Places fit 32 bits with room for a window: |start| <= 2^29, sizes and limits <= 2^28, no limit is 2^30.
+#pragma once
+#include "cross.h"
+#include "spa2_device.h"
+
+namespace spa2 {
+
+constexpr int WINDOW_MOST = 1 << 28, WINDOW_NO_LIMIT = 1 << 30;
+
+struct Window {
+  const int32_t* starts;         // device, [B], or null: start
+  int start;
+  int left, right, sinks;        // sinks <= Nk; 0 where left has no limit
+  int nq;                        // queries of a head: row r of (several heads' rows as one head) is query r % nq
+};
+
+__host__ __device__ __forceinline__ int window_clamp(int start) { return start < -(1 << 29) ? -(1 << 29) : start > 1 << 29 ? 1 << 29 : start; }
+__device__ __forceinline__ int window_start(const Window& w, int b) { return w.starts ? window_clamp(scalar_ld(w.starts + b)) : w.start; }
+
+// What queries at places p0 .. p1 see between them: keys before `sinks` and lo .. hi - 1, in blocks 0 .. ns - 1 and w0 .. w1 - 1.
+struct WindowSpan {
+  int lo, hi, sinks, ns, w0, w1;
+  __host__ __device__ __forceinline__ int count() const { return ns + w1 - w0; }
+  __host__ __device__ __forceinline__ int block(int t) const { return t < ns ? t : t - ns + w0; }
+  // whether all of block j is seen (by some query)
+  __host__ __device__ __forceinline__ bool whole(int j) const {
+    return (j + 1) * BKV <= hi && (j * BKV >= lo || (j + 1) * BKV <= sinks);
+  }
+  // the key that stands in for key `key` of block j in a copy: itself where some query sees it, else the nearest such of the block
+  __host__ __device__ __forceinline__ int stand_in(int j, int key) const {
+    const int k = key < hi ? key : hi - 1;
+    return k >= sinks && k < lo ? (j * BKV < sinks ? sinks - 1 : lo) : k;
+  }
+};
+__host__ __device__ __forceinline__ WindowSpan window_span(const Window& w, int keys, int p0, int p1) {
+  WindowSpan s;
+  s.hi = p1 + w.right + 1 < keys ? p1 + w.right + 1 : keys;
+  s.hi = s.hi > 0 ? s.hi : 0;
+  s.lo = p0 - w.left > 0 ? p0 - w.left : 0;
+  s.sinks = w.sinks < s.hi ? w.sinks : s.hi;
+  s.ns = (s.sinks + BKV - 1) / BKV;
+  s.w0 = s.lo / BKV > s.ns ? s.lo / BKV : s.ns;
+  s.w1 = (s.hi + BKV - 1) / BKV;
+  if (s.lo >= s.hi || s.w1 < s.w0) s.w1 = s.w0;
+  return s;
+}
+// Places of rows first .. last of a head.
+__host__ __device__ __forceinline__ void window_places(const Window& w, int start, int rows, int first, int last, int& p0, int& p1) {
+  if (rows > w.nq) { p0 = start; p1 = start + w.nq - 1; }
+  else             { p0 = start + first; p1 = start + last; }
+}
+__host__ __device__ __forceinline__ int window_place(const Window& w, int start, int rows, int row) { return start + (rows > w.nq ? row % w.nq : row); }
+// Whether the query at place p sees no key at all.
+__host__ __device__ __forceinline__ bool window_blind(const Window& w, int keys, int p) {
+  const int last = p + w.right < keys - 1 ? p + w.right : keys - 1;
+  return last < 0 || (p - w.left > last && w.sinks == 0);
+}
+// Whether all queries at places p0 .. p1 see all of keys first .. last (inside the span).
+__host__ __device__ __forceinline__ bool window_full(const Window& w, int keys, int p0, int p1, int first, int last) {
+  return last < keys && last <= p0 + w.right && (first >= p1 - w.left || last < w.sinks);
+}
+
+// Queries r0 .. r1 (none: r1 < r0) that see some key of first .. last; of `rows` queries from place `start` on.
+struct WindowRows { int r0, r1; };
+__host__ __device__ __forceinline__ WindowRows window_rows(const Window& w, int start, int rows, int first, int last) {
+  WindowRows r;
+  r.r0 = first - w.right - start > 0 ? first - w.right - start : 0;
+  r.r1 = first < w.sinks || last + w.left - start > rows - 1 ? rows - 1 : last + w.left - start;
+  if (last < first) r.r1 = r.r0 - 1;
+  return r;
+}
+
+// Blocks of keys of row i of head bh; parts that a row of `count` blocks is cut into, 0: walked whole.
+template <class Args>
+__device__ __forceinline__ int window_count(const Args& a, int bh, int i) {
+  const int b = bh / a.H, start = window_start(a.win, b);
+  const int keys = a.kv.lengths ? min(max(scalar_ld(a.kv.lengths + b), 0), a.kv.Nk) : a.kv.Nk;
+  int p0, p1;
+  window_places(a.win, start, a.N, i * BQ, min(i * BQ + BQ, a.N) - 1, p0, p1);
+  return window_span(a.win, keys, p0, p1).count();
+}
+template <class Args>
+__device__ __forceinline__ int window_parts(const Args& a, int count) {
+  return count > a.sp.fixed_len ? (count + a.sp.fixed_len - 1) / a.sp.fixed_len : 0;
+}
+
+// ------------------------------------------------------------------ cuts (host)
+// The longest list of a block of queries, in key blocks, and of a block of keys, in halves of a query block (of one query head).
+inline int window_row_list(const CrossDims& m, const Window& w) {
+  const int64_t near = ((int64_t)w.left + w.right + BQ - 1 + BKV - 1) / BKV + 1 + (w.sinks + BKV - 1) / BKV;
+  return near < m.q.Tn ? (int)near : m.q.Tn;
+}
+inline int window_column_list(const CrossDims& m, const Window& w) {
+  const int64_t all = (m.q.N + 63) / 64, near = ((int64_t)w.left + w.right + BKV - 1 + 63) / 64 + 1;
+  return (int)(near < all ? near : all);
+}
+inline CrossSection window_fwd_section(const CrossDims& m, const Window& w) {
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, window_row_list(m, w), RESIDENT_WGS, CutCost{3.5, 0.03, 8, true}, fwd_slot_bytes(m.q));
+}
+inline CrossSection window_dq_section(const CrossDims& m, const Window& w) {
+  return cross_section((int64_t)m.q.B * m.q.H * m.q.Tm, window_row_list(m, w), RESIDENT_WGS, CutCost{3.5, 0.03, 8, true}, dq_slot_bytes(m.q));
+}
+// dK/dV: the columns of first keys, which many more queries see, are cut apart from the others.  Their parts are launched first and
+// are at most a quarter of what a workgroup slot of the chip has to do in all, so that they are through when the others are.
+struct WindowColumns { CrossSection first, rest; int blocks; size_t counters, total; };      // blocks: of first keys
+inline WindowColumns window_columns(const CrossDims& m, const Window& w) {
+  WindowColumns c = {};
+  const int resident = dkdv_resident(m.q), list = m.group * window_column_list(m, w), all = m.group * (int)((m.q.N + 63) / 64);
+  c.blocks = (w.sinks + BKV - 1) / BKV;
+  if (c.blocks > m.q.Tn) c.blocks = m.q.Tn;
+  const int64_t heads = (int64_t)m.q.B * m.Hk, firsts = heads * c.blocks, rest = heads * (m.q.Tn - c.blocks);
+  const CutCost cost = {2.6, 0.8, 8, false};
+  if (rest) c.rest = cross_section(rest, list, resident, cost, dkdv_slot_bytes(m.q));
+  else      c.rest.cut = {list, 1};
+  c.first.cut = {all, 1};
+  if (firsts) {
+    c.first = cross_section(firsts, all, resident, cost, dkdv_slot_bytes(m.q));
+    const int64_t share = (firsts * all + rest * (int64_t)list) / resident / 4;
+    const int len = (int)(share < 16 ? 16 : share < all ? share : all);
+    const int64_t parts = (all + len - 1) / len;
+    if (rest && parts > c.first.cut.parts && firsts * parts <= SPLIT_POOL_MAX) {
+      c.first.cut = {(int)((all + parts - 1) / parts), (int)parts};
+      c.first.cut.parts = (all + c.first.cut.len - 1) / c.first.cut.len;
+      c.first.slots = c.first.cut.parts > 1 ? (int)(firsts * c.first.cut.parts) : 0;
+    }
+  }
+  c.counters = round256((size_t)(c.first.slots + c.rest.slots) * 4);
+  c.total = c.counters + round256((size_t)(c.first.slots + c.rest.slots) * dkdv_slot_bytes(m.q));
+  return c;
+}
+// Workspace of the backward pass: D, LSE, counters and results of dK/dV, results of dQ.
+struct WindowBwdWs { WindowColumns dkdv; CrossSection dq; size_t lse, dkdv_at, dq_at, total; };
+inline WindowBwdWs window_bwd_ws(const CrossDims& m, const Window& w) {
+  WindowBwdWs s;
+  s.dkdv = window_columns(m, w);
+  s.dq = window_dq_section(m, w);
+  s.lse = round256((size_t)m.q.B * m.q.H * m.q.N * sizeof(float));
+  s.dkdv_at = 2 * s.lse;
+  s.dq_at = s.dkdv_at + s.dkdv.total;
+  s.total = s.dq_at + s.dq.pool;
+  return s;
+}
+// The kernel for few rows: as cross_few_ws, with the blocks that a sample's queries see at most.
+inline CrossFewWs window_few_ws(const CrossDims& m, const Window& w) {
+  CrossDims seen = m;
+  const int64_t near = ((int64_t)w.left + w.right + w.nq - 1 + BKV - 1) / BKV + 1 + (w.sinks + BKV - 1) / BKV;
+  if (near < seen.q.Tn) seen.q.Tn = (int)near;
+  return cross_few_ws(seen);
+}
+
+hipError_t launch_window_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,
+                             float scale, void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
+hipError_t launch_window_fwd(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,
+                             float scale, void* o, void* o_res, float* lse, void* ws, hipStream_t stream);
+// (see launch_cross_dq)
+hipError_t launch_window_dq(const void* q, const void* k, const void* v, const void* o, const void* o_res, const void* d_o,
+                            const float* lse, const CrossDims& m, const int32_t* lengths, const Window& win, float scale, float* delta,
+                            float* lse_out, void* dq, int32_t* zero, int zeros, const SplitPlan& plan, hipStream_t stream);
+// (counters, pool: of the first keys' parts, then of the others')
+hipError_t launch_window_dkdv(const void* q, const void* k, const void* v, const void* d_o, const float* lse, const float* delta,
+                              const CrossDims& m, const int32_t* lengths, const Window& win, float scale, void* dk, void* dv,
+                              const WindowColumns& cuts, void* counters, void* pool, hipStream_t stream);
+
+}  // namespace spa2

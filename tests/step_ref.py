@@ -73,3 +73,60 @@ def clip_factor(arrays, max_norm, eps):
         return norm, 1.0
     f = max_norm / (norm + eps) if norm + eps != 0 else 1.0
     return norm, 1.0 if f >= 1 else f
+
+
+# ------------------------------------------------------------------ attention over a window
+def window_mask(Nq, Nk, length, start, left, right, sinks):
+    """[Nq, Nk]: which pairs see each other (left, right: None for no limit)."""
+    p, j = start + np.arange(Nq)[:, None], np.arange(Nk)[None]
+    m = np.broadcast_to(j < length, (Nq, Nk)).copy()
+    if right is not None:
+        m &= j <= p + right
+    if left is not None:
+        m &= (j >= p - left) | (j < sinks)
+    return m
+
+
+def window(q, k, v, lengths, starts, left, right, sinks, scale, do=None):
+    """fp64 arrays [B, H, N, d]; {name: (value, bound)}, and the log-sum-exp.  The bounds count what the kernels round, as
+    block_ref.cross does: weights rounded to bf16 and divided by the sum of the rounded ones, U of each against their mean; dS
+    rounded, and off by what P's log-sum-exp and D hold of the weights' rounding; results rounded; 2^-13 for what is fp32."""
+    U, small = 2.0 ** -8, 2.0 ** -13
+    B, Hq, Nq, d = q.shape
+    Hk, Nk = k.shape[1:3]
+    out = {n: (np.zeros(s), np.zeros(s)) for n, s in (("o", q.shape), ("dq", q.shape), ("dk", k.shape), ("dv", k.shape))}
+    lse = np.full((B, Hq, Nq), -np.inf)
+    for b in range(B):
+        n = Nk if lengths is None else int(min(max(lengths[b], 0), Nk))
+        seen = window_mask(Nq, Nk, n, Nk - Nq if starts is None else int(starts[b]), left, right, sinks)
+        rows, keys = seen.any(1), seen.any(0)
+        if not rows.any():
+            continue
+        m = seen[np.ix_(rows, keys)]
+        for h in range(Hq):
+            g = h // (Hq // Hk)
+            qq, kk, vv = q[b, h][rows], k[b, g][keys], v[b, g][keys]
+            s = np.where(m, scale * qq @ kk.T, -np.inf)
+            top = s.max(-1, keepdims=True)
+            e = np.exp(s - top)
+            p = e / e.sum(-1, keepdims=True)
+            lse[b, h, rows] = top[:, 0] + np.log(e.sum(-1))
+            o, pv = p @ vv, p @ np.abs(vv)
+            weights = U * (pv + np.abs(o)) + small * pv
+            out["o"][0][b, h, rows], out["o"][1][b, h, rows] = o, weights + U * np.abs(o)
+            if do is None:
+                continue
+            up = do[b, h][rows]
+            dp = np.where(m, up @ vv.T, 0.0)
+            D = (up * o).sum(-1, keepdims=True)
+            ds = p * (dp - D)
+            ds_bound = p * (np.abs(up) * (weights + 2.0 ** -15 * np.abs(o))).sum(-1, keepdims=True) + 3 * U * np.abs(ds) \
+                + small * p * (np.abs(up) @ np.abs(vv).T + np.abs(D))
+            out["dq"][0][b, h, rows], out["dq"][1][b, h, rows] = scale * ds @ kk, scale * ds_bound @ np.abs(kk)
+            for name, value, bound in (("dk", scale * ds.T @ qq, scale * ds_bound.T @ np.abs(qq)),
+                                       ("dv", p.T @ up, (2 * U + small) * p.T @ np.abs(up))):
+                out[name][0][b, g, keys] += value
+                out[name][1][b, g, keys] += bound
+    for n in ("dq", "dk", "dv"):
+        out[n] = (out[n][0], out[n][1] + U * np.abs(out[n][0]))
+    return out, lse
