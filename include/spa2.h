@@ -391,7 +391,8 @@ int spa2_window_bwd(const void* q, const void* k, const void* v, const int32_t* 
  *   params      vectors of `width` elements of one type (param_dtype), each or NULL (gate 1, weights 1, bias, scale and shift 0);
  *               gate, scale, shift with an element stride between samples (gate_sb, ..., 0: one for all of them).
  *   stats       fp32 [3][samples * tokens] (written), what the backward pass needs besides y; or NULL.
- * All addresses are multiples of their elements' size; rows may start anywhere (width is any number up to SPA2_GATE_MAX_WIDTH).
+ * All addresses are multiples of their elements' size; rows may start anywhere (width is any number from
+ * SPA2_GATE_MIN_WIDTH to SPA2_GATE_MAX_WIDTH).
  * spa2_gate_norm_bwd: dy (x_dtype) and dn (out_dtype) are the upstream gradients of y and n (dy may be NULL: zero; dn is only
  * read with a norm), y and stats those of the forward call (without a branch y is x).  dx and dbranch have x's and the branch's type
  * and may be NULL (not wanted); so may the members of grads, which have the parameters' shapes and type.  Sums over tokens are
@@ -402,7 +403,8 @@ int spa2_window_bwd(const void* q, const void* k, const void* v, const int32_t* 
 #define SPA2_NORM_NONE  0
 #define SPA2_NORM_LAYER 1
 #define SPA2_NORM_RMS   2
-#define SPA2_GATE_MAX_WIDTH 16384
+#define SPA2_GATE_MIN_WIDTH 8
+#define SPA2_GATE_MAX_WIDTH 8192
 typedef struct spa2_gate_shape {
   int64_t samples, tokens;
   int64_t gate_sb, scale_sb, shift_sb;

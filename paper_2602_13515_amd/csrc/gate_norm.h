@@ -1,12 +1,23 @@
 // Device parts that the forward and the backward pass of the gated sum with its norms share.
 #pragma once
+#include "block_ops.h"
 #include "spa2_device.h"
 #include "step_ops.h"
 
 namespace spa2 {
 
-// A row's channels: thread t of a workgroup of `threads` owns chunks of eight, t, t + threads, ... (GATE_CHUNKS of them).
-constexpr int GATE_WAVES = 8;                          // of a workgroup, at most
+// A row is a workgroup's: thread t has the eight channels from 8 t on.  Where the width is no multiple of eight (ODD) the last thread has
+// the row's last eight, some of which are its neighbour's as well: both work them out, bit for bit the same, and the neighbour's
+// count in the sums.  So all loads and stores are whole vectors.
+constexpr int GATE_WAVES = SPA2_GATE_MAX_WIDTH / 512;  // of a workgroup, at most
+struct GateLane { int at, shift; bool there; };        // first channel; how many of the eight do not count; whether it has any
+__device__ __forceinline__ GateLane gate_lane(int t, int width) {
+  GateLane l;
+  l.at = min(8 * t, width - 8);
+  l.shift = 8 * t - l.at;
+  l.there = 8 * t < width;
+  return l;
+}
 
 struct GateArgs {
   const void* x; const void* branch; const void* y_in; const void* dy; const void* dn;      // (y_in, dy, dn: backward)
@@ -20,69 +31,82 @@ struct GateArgs {
   float eps;
 };
 
+int gate_threads(int width);
+GateArgs gate_args(const spa2_gate_shape& s, const spa2_gate_params& p, float eps, bool backward);
+// Whether the call's tensors are larger than the memory-side cache, so that next to nothing of them would be there when they are read
+// next.  Measured, us, forward and backward, the same tensors every time, through the cache / past it: 5000 x 768, bf16 (8 MB a
+// tensor) 56 / 88; 20,010 x 384, fp32 (31 MB) 104 / 126; 32,760 x 1536, fp32 and bf16 (201 and 101 MB) 291 / 300; 16,000 x 5120, bf16
+// (164 MB) 317 / 289; 32,760 x 5120 (335 MB) 634 / 574; 75,600 x 5120 (774 MB) 1458 / 1347.
+inline bool gate_past(const GateArgs& a) { return a.rows * a.width * 2 > CACHE_BYTES / 2; }
+
 // 16 bytes from any element on: rows of odd width start anywhere
 typedef u32x4 __attribute__((aligned(2))) gate_u32x4;
 typedef f32x4 __attribute__((aligned(4))) gate_f32x4;
 
-// left: channels from here to the row's end (ODD: fewer than eight maybe; the others are zero)
-template <bool ODD>
-__device__ __forceinline__ void gate_load(const uint16_t* p, int left, float (&x)[8]) {
-  if (!ODD || left >= 8) {
-    const u32x4 v = *(const gate_u32x4*)p;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t u = v[c];
-      x[2 * c] = __builtin_bit_cast(float, u << 16);
-      x[2 * c + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < left ? __builtin_bit_cast(float, (uint32_t)p[e] << 16) : 0.f;
+// PAST: past the memory-side cache, loads and stores: rows of tensors that do not fit it (see gate_past).
+template <bool PAST, typename P> __device__ __forceinline__ P gate_get(const P* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load(p);
+  else                return *p;
+}
+template <bool PAST, typename P, typename V> __device__ __forceinline__ void gate_put(P* p, V x) {
+  if constexpr (PAST) __builtin_nontemporal_store((P)x, p);
+  else                *p = x;
+}
+// Eight channels as they are loaded (zero where a thread has none).
+template <typename T> struct GateRaw;
+template <> struct GateRaw<uint16_t> { u32x4 v; };
+template <> struct GateRaw<float> { f32x4 lo, hi; };
+template <bool PAST = false>
+__device__ __forceinline__ void gate_fetch(const uint16_t* p, bool there, GateRaw<uint16_t>& r) {
+  r.v = u32x4{0, 0, 0, 0};
+  if (there) r.v = gate_get<PAST>((const gate_u32x4*)p);
+}
+template <bool PAST = false>
+__device__ __forceinline__ void gate_fetch(const float* p, bool there, GateRaw<float>& r) {
+  r.lo = r.hi = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (there) {
+    r.lo = gate_get<PAST>((const gate_f32x4*)p);
+    r.hi = gate_get<PAST>((const gate_f32x4*)(p + 4));
   }
 }
-template <bool ODD>
-__device__ __forceinline__ void gate_load(const float* p, int left, float (&x)[8]) {
-  if (!ODD || left >= 8) {
-    const f32x4 a = *(const gate_f32x4*)p, b = *(const gate_f32x4*)(p + 4);
+__device__ __forceinline__ void gate_unpack(const GateRaw<uint16_t>& r, float (&x)[8]) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) { x[c] = a[c]; x[4 + c] = b[c]; }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < left ? p[e] : 0.f;
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t u = r.v[c];
+    x[2 * c] = __builtin_bit_cast(float, u << 16);
+    x[2 * c + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
   }
 }
-template <bool ODD>
-__device__ __forceinline__ void gate_store(uint16_t* p, int left, const float (&x)[8]) {
-  const u32x4 v = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
-  if (!ODD || left >= 8) {
-    *(gate_u32x4*)p = v;
-  } else {
+__device__ __forceinline__ void gate_unpack(const GateRaw<float>& r, float (&x)[8]) {
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < left) p[e] = (uint16_t)(e & 1 ? v[e / 2] >> 16 : v[e / 2]);
-  }
+  for (int c = 0; c < 4; ++c) { x[c] = r.lo[c]; x[4 + c] = r.hi[c]; }
 }
-template <bool ODD>
-__device__ __forceinline__ void gate_store(float* p, int left, const float (&x)[8]) {
-  if (!ODD || left >= 8) {
-    *(gate_f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
-    *(gate_f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < left) p[e] = x[e];
-  }
+template <bool PAST = false>
+__device__ __forceinline__ void gate_store(uint16_t* p, const float (&x)[8]) {
+  gate_put<PAST>((gate_u32x4*)p, u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])});
 }
-// eight parameters, or `otherwise`
-template <bool ODD>
-__device__ __forceinline__ void gate_param(const void* p, bool fp32, int64_t at, int left, float otherwise, float (&x)[8]) {
+template <bool PAST = false>
+__device__ __forceinline__ void gate_store(float* p, const float (&x)[8]) {
+  gate_put<PAST>((gate_f32x4*)p, f32x4{x[0], x[1], x[2], x[3]});
+  gate_put<PAST>((gate_f32x4*)(p + 4), f32x4{x[4], x[5], x[6], x[7]});
+}
+// Eight parameters: requested (all vectors of a call before the first is looked at), and as numbers, `otherwise` without a vector.
+struct GateParam { u32x4 lo, hi; };
+__device__ __forceinline__ void gate_param_fetch(const void* p, bool fp32, int64_t at, bool there, GateParam& r) {
+  r.lo = r.hi = u32x4{0, 0, 0, 0};
+  if (!p || !there) return;
+  const char* q = (const char*)p + at * (fp32 ? 4 : 2);
+  r.lo = *(const gate_u32x4*)q;
+  if (fp32) r.hi = *(const gate_u32x4*)(q + 16);
+}
+__device__ __forceinline__ void gate_param(const void* p, bool fp32, const GateParam& r, float otherwise, float (&x)[8]) {
   if (!p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = otherwise;
   } else if (fp32) {
-    gate_load<ODD>((const float*)p + at, left, x);
+    gate_unpack(GateRaw<float>{__builtin_bit_cast(f32x4, r.lo), __builtin_bit_cast(f32x4, r.hi)}, x);
   } else {
-    gate_load<ODD>((const uint16_t*)p + at, left, x);
+    gate_unpack(GateRaw<uint16_t>{r.lo}, x);
   }
 }
 __device__ __forceinline__ float gate_one(const void* p, bool fp32, int64_t at, float otherwise) {
@@ -90,21 +114,36 @@ __device__ __forceinline__ float gate_one(const void* p, bool fp32, int64_t at, 
   return fp32 ? ((const float*)p)[at] : __builtin_bit_cast(float, (uint32_t)((const uint16_t*)p)[at] << 16);
 }
 
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s, 64);
-  return x;
+// Sums on the vector ALU, without a trip through LDS: over rows of 16 lanes (exchanges inside a row), over the wave.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true);
+  return x + __builtin_bit_cast(float, y);
 }
-// Sums over the workgroup of two numbers that every lane of a wave has, in every thread.  lds: one of two arrays in turn (a wave may
-// still read the one before, none the one before that), so that one barrier is enough.
+__device__ __forceinline__ float row16_sum(float x) {
+  x = dpp_add<0xB1>(x);                  // quad_perm: lane ^ 1
+  x = dpp_add<0x4E>(x);                  // quad_perm: lane ^ 2
+  x = dpp_add<0x141>(x);                 // row_half_mirror: the other four of eight
+  return dpp_add<0x140>(x);              // row_mirror: the other eight
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x = row16_sum(x);
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return sum_halves(__builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float first_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+// Sums over the workgroup of two numbers that every lane of a wave has, in every thread (uniform).  lds: one of two arrays in turn (a
+// wave may still read the one before, none the one before that), so that one barrier is enough.
 struct GatePair { float a, b; };
-__device__ __forceinline__ GatePair block_sum(GatePair x, float (&lds)[GATE_WAVES][2], int waves, int w, int lane) {
-  if (waves == 1) return x;
-  if (lane == 0) { lds[w][0] = x.a; lds[w][1] = x.b; }
+__device__ __forceinline__ GatePair block_sum(GatePair x, f32x2* lds, int waves, int w, int lane) {
+  if (waves == 1) return {first_lane(x.a), first_lane(x.b)};
+  if (lane == 0) lds[w] = f32x2{x.a, x.b};
   __syncthreads();
-  GatePair r = {lds[0][0], lds[0][1]};
-  for (int i = 1; i < waves; ++i) { r.a += lds[i][0]; r.b += lds[i][1]; }
-  return r;
+  const f32x2 y = lane < waves ? lds[lane] : f32x2{0.f, 0.f};
+  return {first_lane(row16_sum(y[0])), first_lane(row16_sum(y[1]))};
 }
 
 }  // namespace spa2

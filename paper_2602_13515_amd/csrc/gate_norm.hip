@@ -12,82 +12,78 @@
 
 namespace spa2 {
 
-template <typename X, typename B, typename N, int CHUNKS, bool ODD>
+template <typename X, typename B, typename N, bool ODD, bool PAST>
 __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_kernel(GateArgs a) {
-  __shared__ float lds[2][GATE_WAVES][2];
-  const int threads = blockDim.x, waves = threads / 64, t = threadIdx.x, lane = t & 63;
+  __shared__ f32x2 lds[2][GATE_WAVES];
+  const int waves = blockDim.x / 64, t = threadIdx.x, lane = t & 63;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int64_t b = blockIdx.x / a.per_sample, first = blockIdx.x % a.per_sample;
-  float gate[CHUNKS][8], mul[CHUNKS][8], add[CHUNKS][8];
-  float own = 0.f;                                     // channels of this wave
-#pragma unroll
-  for (int k = 0; k < CHUNKS; ++k) {
-    const int at = 8 * (t + threads * k), left = a.width - at;
-    own += (float)min(max(a.width - 8 * (64 * w + threads * k), 0), 512);
-    if (left <= 0) continue;
+  const GateLane l = gate_lane(t, a.width);
+  const int64_t b = blockIdx.x / a.per_sample;
+  int64_t token = blockIdx.x % a.per_sample;
+  GateRaw<X> xr;
+  GateRaw<B> br;
+  auto fetch = [&](int64_t token) {                    // rows are requested one ahead
+    const int64_t base = (b * a.tokens + token) * a.width + l.at;
+    gate_fetch<PAST>((const X*)a.x + base, l.there, xr);
+    if (a.branch) gate_fetch<PAST>((const B*)a.branch + base, l.there, br);
+  };
+  fetch(token);
+  float gate[8], mul[8], add[8];
+  {
+    const bool f = a.params32;
+    GateParam raw[6];
+    gate_param_fetch(a.p.gate, f, b * a.gate_sb + l.at, l.there, raw[0]);
+    gate_param_fetch(a.p.branch_weight, f, l.at, l.there, raw[1]);
+    gate_param_fetch(a.p.weight, f, l.at, l.there, raw[2]);
+    gate_param_fetch(a.p.bias, f, l.at, l.there, raw[3]);
+    gate_param_fetch(a.p.scale, f, b * a.scale_sb + l.at, l.there, raw[4]);
+    gate_param_fetch(a.p.shift, f, b * a.shift_sb + l.at, l.there, raw[5]);
     float s[8], c[8];
-    gate_param<ODD>(a.p.gate, a.params32, b * a.gate_sb + at, left, 1.f, gate[k]);
-    gate_param<ODD>(a.p.branch_weight, a.params32, at, left, 1.f, s);
+    gate_param(a.p.gate, f, raw[0], 1.f, gate);
+    gate_param(a.p.branch_weight, f, raw[1], 1.f, s);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) gate[k][e] *= s[e];
-    gate_param<ODD>(a.p.weight, a.params32, at, left, 1.f, mul[k]);
-    gate_param<ODD>(a.p.bias, a.params32, at, left, 0.f, c);
-    gate_param<ODD>(a.p.scale, a.params32, b * a.scale_sb + at, left, 0.f, s);
-    gate_param<ODD>(a.p.shift, a.params32, b * a.shift_sb + at, left, 0.f, add[k]);
+    for (int e = 0; e < 8; ++e) gate[e] *= s[e];
+    gate_param(a.p.weight, f, raw[2], 1.f, mul);
+    gate_param(a.p.bias, f, raw[3], 0.f, c);
+    gate_param(a.p.scale, f, raw[4], 0.f, s);
+    gate_param(a.p.shift, f, raw[5], 0.f, add);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      mul[k][e] *= 1.f + s[e];
-      add[k][e] = fmaf(c[e], 1.f + s[e], add[k][e]);
+      mul[e] *= 1.f + s[e];
+      add[e] = fmaf(c[e], 1.f + s[e], add[e]);
     }
   }
-  const float per = 1.f / (float)a.width;
-  int turn = 0;
-  auto buffer = [&]() -> float (&)[GATE_WAVES][2] {
-    turn ^= 1;
-    return lds[turn];
+  auto counts = [&](int e) -> bool { return ODD ? e >= l.shift : true; };
+  auto squares = [&](const float (&x)[8]) -> float {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = counts(e) ? fmaf(x[e], x[e], s) : s;
+    return s;
   };
-  for (int64_t token = first; token < a.tokens; token += a.per_sample) {
-    const int64_t row = b * a.tokens + token, base = row * a.width;
-    float y[CHUNKS][8], u[CHUNKS][8];
-#pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-      const int at = 8 * (t + threads * k), left = a.width - at;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[k][e] = u[k][e] = 0.f;
-      if (left <= 0) continue;
-      gate_load<ODD>((const X*)a.x + base + at, left, y[k]);
-      if (a.branch) gate_load<ODD>((const B*)a.branch + base + at, left, u[k]);
-    }
+  const float per = 1.f / (float)a.width;
+  const float own = (float)min(a.width - 512 * w, 512), lanes_own = (float)min(max(a.width - 512 * lane, 1), 512);     // channels of a wave
+  int turn = 0;
+  for (; token < a.tokens; token += a.per_sample) {
+    const int64_t row = b * a.tokens + token, base = row * a.width + l.at;
+    float y[8], u[8];
+    gate_unpack(xr, y);
+    if (a.branch) gate_unpack(br, u);
+    if (token + a.per_sample < a.tokens) fetch(token + a.per_sample);
     if (a.branch) {
       float rb = 1.f;
       if (a.post) {
-        float sq = 0.f;
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sq = fmaf(u[k][e], u[k][e], sq);
-        sq = block_sum({wave_sum(sq), 0.f}, buffer(), waves, w, lane).a;
-        rb = rsqrtf(fmaf(sq, per, a.eps));
+        rb = rsqrtf(fmaf(block_sum({wave_sum(squares(u)), 0.f}, lds[turn ^= 1], waves, w, lane).a, per, a.eps));
         if (a.stats && t == 0) a.stats[2 * a.rows + row] = rb;
       }
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k) {
-        const int at = 8 * (t + threads * k), left = a.width - at;
-        if (left <= 0) continue;
+      for (int e = 0; e < 8; ++e) y[e] = fmaf(u[e] * rb, gate[e], y[e]);
+      if (l.there) gate_store<PAST>((X*)a.y + base, y);
+      if constexpr (sizeof(X) == 2) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[k][e] = fmaf(u[k][e] * rb, gate[k][e], y[k][e]);
-        gate_store<ODD>((X*)a.y + base + at, left, y[k]);
-        if constexpr (sizeof(X) == 2) {
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const uint32_t p = pack_bf16(y[k][e], y[k][e + 1]);
-            y[k][e] = __builtin_bit_cast(float, p << 16);
-            y[k][e + 1] = __builtin_bit_cast(float, p & 0xffff0000u);
-          }
-        }
-        if constexpr (ODD) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[k][e] = e < left ? y[k][e] : 0.f;
+        for (int e = 0; e < 8; e += 2) {
+          const uint32_t p = pack_bf16(y[e], y[e + 1]);
+          y[e] = __builtin_bit_cast(float, p << 16);
+          y[e + 1] = __builtin_bit_cast(float, p & 0xffff0000u);
         }
       }
     }
@@ -96,68 +92,52 @@ __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_kernel(GateArgs a) 
     if (a.kind == SPA2_NORM_LAYER) {
       float s = 0.f, dev = 0.f;
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += y[k][e];
+      for (int e = 0; e < 8; ++e) s += counts(e) ? y[e] : 0.f;
       s = wave_sum(s);
       const float here = s / own;
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k) {
-        const int left = a.width - 8 * (t + threads * k);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float d = y[k][e] - here;
-          dev = left > (ODD ? e : 0) ? fmaf(d, d, dev) : dev;
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float d = y[e] - here;
+        dev = counts(e) ? fmaf(d, d, dev) : dev;
       }
-      dev = wave_sum(dev);
+      dev = wave_sum(l.there ? dev : 0.f);
       if (waves == 1) {
-        mean = here;
-      } else {
-        float (&x)[GATE_WAVES][2] = buffer();
-        if (lane == 0) { x[w][0] = s; x[w][1] = dev; }
+        mean = first_lane(here);
+        dev = first_lane(dev);
+      } else {                                         // lane i joins wave i's
+        f32x2* z = lds[turn ^= 1];
+        if (lane == 0) z[w] = f32x2{s, dev};
         __syncthreads();
-        for (int i = 0; i < waves; ++i) mean += x[i][0];
-        mean *= per;
-        dev = 0.f;
-        for (int i = 0; i < waves; ++i) {
-          float n = 0.f;                               // channels of wave i
-#pragma unroll
-          for (int k = 0; k < CHUNKS; ++k) n += (float)min(max(a.width - 8 * (64 * i + threads * k), 0), 512);
-          const float off = x[i][0] / n - mean;
-          dev += fmaf(n * off, off, x[i][1]);
-        }
+        const f32x2 x = lane < waves ? z[lane] : f32x2{0.f, 0.f};
+        mean = first_lane(row16_sum(x[0])) * per;
+        const float off = x[0] / lanes_own - mean;
+        dev = first_lane(row16_sum(lane < waves ? fmaf(lanes_own * off, off, x[1]) : 0.f));
       }
       r = rsqrtf(fmaf(dev, per, a.eps));
     } else {
-      float sq = 0.f;
-#pragma unroll
-      for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq = fmaf(y[k][e], y[k][e], sq);
-      sq = block_sum({wave_sum(sq), 0.f}, buffer(), waves, w, lane).a;
-      r = rsqrtf(fmaf(sq, per, a.eps));
+      r = rsqrtf(fmaf(block_sum({wave_sum(squares(y)), 0.f}, lds[turn ^= 1], waves, w, lane).a, per, a.eps));
     }
     if (a.stats && t == 0) { a.stats[row] = mean; a.stats[a.rows + row] = r; }
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-      const int at = 8 * (t + threads * k), left = a.width - at;
-      if (left <= 0) continue;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[k][e] = fmaf((y[k][e] - mean) * r, mul[k][e], add[k][e]);
-      gate_store<ODD>((N*)a.n + base + at, left, y[k]);
-    }
+    for (int e = 0; e < 8; ++e) y[e] = fmaf((y[e] - mean) * r, mul[e], add[e]);
+    if (l.there) gate_store<PAST>((N*)a.n + base, y);
   }
 }
 
-// Workgroups: as many as run at a time (16 waves a compute unit), each with the rows p, p + per_sample, ... of a sample, so that
-// those that run at a time work on one stretch of memory.
-constexpr int GATE_FWD_WAVES = 16, GATE_BWD_WAVES = 12, CUS = 256;
-static int gate_chunks(int width) { return width <= 512 * 2 * GATE_WAVES ? 2 : 4; }
-int gate_threads(int width) { const int each = 512 * gate_chunks(width); return 64 * ((width + each - 1) / each); }
+// Workgroups: so many a compute unit that about GATE_AHEAD bytes of rows are on their way to it, three times as many where the branch
+// is normed, too (two reductions a row, one waiting for the other), each with the rows p, p + per_sample, ... of a sample.  Those
+// that run at a time work on one stretch of memory, which the fewer they are is the shorter, and leave fewer sums.  Measured, us,
+// forward and backward, workgroups a compute unit: 32,760 x 1536, fp32 and bf16 (9 and 18 KB of a row) 6 and 5 314, 3 and 2 291, 2 and
+// 1 281, 1 and 1 311; with the branch normed, all fp32 (12 and 25 KB) 2 and 1 584, 3 and 2 447, 5 and 3 404; 75,600 x 5120, bf16 (20
+// and 40 KB) 2 and 1 1488, 1 and 1 1458.
+constexpr int GATE_AHEAD = 20 << 10, GATE_WAVES_CU = 16, CUS = 256;
+int gate_threads(int width) { return 64 * ((width + 511) / 512); }
 int gate_per_sample(const spa2_gate_shape& s, bool backward) {
-  const int64_t wgs = CUS * (backward ? GATE_BWD_WAVES : GATE_FWD_WAVES) / (gate_threads(s.width) / 64);
-  int64_t per = (wgs + s.samples - 1) / s.samples;
+  auto size = [](int32_t t) { return t == SPA2_DTYPE_F32 ? 4 : 2; };
+  const int bytes = s.width * (backward ? 2 * size(s.x_dtype) + size(s.branch_dtype) + size(s.out_dtype) : size(s.x_dtype) + size(s.branch_dtype));
+  const int most = GATE_WAVES_CU / (gate_threads(s.width) / 64), wanted = ((s.post ? 3 : 1) * GATE_AHEAD + bytes / 2) / bytes;
+  const int64_t wgs = CUS * (int64_t)(wanted < 1 ? 1 : wanted < most ? wanted : most);
+  const int64_t per = (wgs + s.samples - 1) / s.samples;
   return (int)(per < s.tokens ? per : s.tokens);
 }
 
@@ -174,11 +154,11 @@ GateArgs gate_args(const spa2_gate_shape& s, const spa2_gate_params& p, float ep
 
 template <typename X, typename B, typename N>
 static void launch_types(const GateArgs& a, const dim3& grid, const dim3& block, hipStream_t stream) {
-  const bool odd = a.width % 8, wide = gate_chunks(a.width) == 4;
-  if (wide && odd)      hipLaunchKernelGGL((gate_norm_kernel<X, B, N, 4, true>), grid, block, 0, stream, a);
-  else if (wide)        hipLaunchKernelGGL((gate_norm_kernel<X, B, N, 4, false>), grid, block, 0, stream, a);
-  else if (odd)         hipLaunchKernelGGL((gate_norm_kernel<X, B, N, 2, true>), grid, block, 0, stream, a);
-  else                  hipLaunchKernelGGL((gate_norm_kernel<X, B, N, 2, false>), grid, block, 0, stream, a);
+  const bool odd = a.width % 8, past = gate_past(a);
+  if (odd && past) hipLaunchKernelGGL((gate_norm_kernel<X, B, N, true, true>), grid, block, 0, stream, a);
+  else if (odd)    hipLaunchKernelGGL((gate_norm_kernel<X, B, N, true, false>), grid, block, 0, stream, a);
+  else if (past)   hipLaunchKernelGGL((gate_norm_kernel<X, B, N, false, true>), grid, block, 0, stream, a);
+  else             hipLaunchKernelGGL((gate_norm_kernel<X, B, N, false, false>), grid, block, 0, stream, a);
 }
 
 hipError_t launch_gate_norm(const void* x, const void* branch, const spa2_gate_params& p, const spa2_gate_shape& s, float eps,

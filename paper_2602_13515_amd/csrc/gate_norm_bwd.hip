@@ -14,126 +14,106 @@
 
 namespace spa2 {
 
-int gate_threads(int width);
-GateArgs gate_args(const spa2_gate_shape& s, const spa2_gate_params& p, float eps, bool backward);
-
-template <typename X, typename B, typename N, int CHUNKS, bool ODD>
+template <typename X, typename B, typename N, bool ODD, bool PAST>
 __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_bwd_kernel(GateArgs a) {
-  __shared__ float lds[2][GATE_WAVES][2];
-  const int threads = blockDim.x, waves = threads / 64, t = threadIdx.x, lane = t & 63;
+  __shared__ f32x2 lds[2][GATE_WAVES];
+  const int waves = blockDim.x / 64, t = threadIdx.x, lane = t & 63;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int64_t b = blockIdx.x / a.per_sample, first = blockIdx.x % a.per_sample;
+  const GateLane l = gate_lane(t, a.width);
+  const int64_t b = blockIdx.x / a.per_sample;
+  int64_t token = blockIdx.x % a.per_sample;
   const bool normed = a.kind != SPA2_NORM_NONE, layer = a.kind == SPA2_NORM_LAYER;
-  float gate[CHUNKS][8], mul[CHUNKS][8], s1[CHUNKS][8], s2[CHUNKS][8], sg[CHUNKS][8];
-#pragma unroll
-  for (int k = 0; k < CHUNKS; ++k) {
-    const int at = 8 * (t + threads * k), left = a.width - at;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s1[k][e] = s2[k][e] = sg[k][e] = 0.f;
-    if (left <= 0) continue;
+  GateRaw<X> yr, dr;
+  GateRaw<N> nr;
+  GateRaw<B> br;
+  float stat[3];
+  auto fetch = [&](int64_t token) {                    // rows are requested one ahead
+    const int64_t row = b * a.tokens + token, base = row * a.width + l.at;
+    gate_fetch<PAST>((const N*)a.dn + base, l.there && normed, nr);
+    gate_fetch<PAST>((const X*)a.y_in + base, l.there && normed, yr);
+    gate_fetch<PAST>((const X*)a.dy + base, l.there && a.dy, dr);
+    gate_fetch<PAST>((const B*)a.branch + base, l.there && a.branch, br);
+    if (normed) { stat[0] = a.stats[row]; stat[1] = a.stats[a.rows + row]; }
+    if (a.post) stat[2] = a.stats[2 * a.rows + row];
+  };
+  fetch(token);
+  float gate[8], mul[8], s1[8], s2[8], sg[8];
+  {
+    const bool f = a.params32;
+    GateParam raw[4];
+    gate_param_fetch(a.p.gate, f, b * a.gate_sb + l.at, l.there, raw[0]);
+    gate_param_fetch(a.p.branch_weight, f, l.at, l.there, raw[1]);
+    gate_param_fetch(a.p.weight, f, l.at, l.there, raw[2]);
+    gate_param_fetch(a.p.scale, f, b * a.scale_sb + l.at, l.there, raw[3]);
     float s[8];
-    gate_param<ODD>(a.p.gate, a.params32, b * a.gate_sb + at, left, 1.f, gate[k]);
-    gate_param<ODD>(a.p.branch_weight, a.params32, at, left, 1.f, s);
+    gate_param(a.p.gate, f, raw[0], 1.f, gate);
+    gate_param(a.p.branch_weight, f, raw[1], 1.f, s);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) gate[k][e] *= s[e];
-    gate_param<ODD>(a.p.weight, a.params32, at, left, 1.f, mul[k]);
-    gate_param<ODD>(a.p.scale, a.params32, b * a.scale_sb + at, left, 0.f, s);
+    for (int e = 0; e < 8; ++e) { gate[e] *= s[e]; s1[e] = s2[e] = sg[e] = 0.f; }
+    gate_param(a.p.weight, f, raw[2], 1.f, mul);
+    gate_param(a.p.scale, f, raw[3], 0.f, s);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mul[k][e] *= 1.f + s[e];
+    for (int e = 0; e < 8; ++e) mul[e] *= 1.f + s[e];
   }
+  auto counts = [&](int e) -> bool { return ODD ? e >= l.shift : true; };
   const float per = 1.f / (float)a.width;
   int turn = 0;
-  auto buffer = [&]() -> float (&)[GATE_WAVES][2] {
-    turn ^= 1;
-    return lds[turn];
-  };
-  for (int64_t token = first; token < a.tokens; token += a.per_sample) {
-    const int64_t row = b * a.tokens + token, base = row * a.width;
-    // d: dy, then D;  h: y, then the normed sum;  g: dn, then dn a;  u: the branch, normed
-    float d[CHUNKS][8], h[CHUNKS][8], g[CHUNKS][8], u[CHUNKS][8];
-#pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-      const int at = 8 * (t + threads * k), left = a.width - at;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d[k][e] = h[k][e] = g[k][e] = u[k][e] = 0.f;
-      if (left <= 0) continue;
-      if (normed) {
-        gate_load<ODD>((const N*)a.dn + base + at, left, g[k]);
-        gate_load<ODD>((const X*)a.y_in + base + at, left, h[k]);
-      }
-      if (a.dy) gate_load<ODD>((const X*)a.dy + base + at, left, d[k]);
-      if (a.branch) gate_load<ODD>((const B*)a.branch + base + at, left, u[k]);
-    }
+  for (; token < a.tokens; token += a.per_sample) {
+    const int64_t base = (b * a.tokens + token) * a.width + l.at;
+    // (a thread without channels has zeros, but for h, which meets a g of zero)
+    const GateRaw<X> up = dr;
+    const GateRaw<B> bu = br;
+    float h[8], g[8], d[8];
+    gate_unpack(nr, g);
+    gate_unpack(yr, h);
+    const float mean = first_lane(stat[0]), r = first_lane(stat[1]), rb = a.post ? first_lane(stat[2]) : 1.f;
+    if (token + a.per_sample < a.tokens) fetch(token + a.per_sample);
     if (normed) {
-      const float mean = a.stats[row], r = a.stats[a.rows + row];
       float sum = 0.f, along = 0.f;
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k) {
-        if (a.width - 8 * (t + threads * k) <= 0) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          h[k][e] = (h[k][e] - mean) * r;              // (behind the row's end: times a g of zero)
-          s1[k][e] = fmaf(g[k][e], h[k][e], s1[k][e]);
-          s2[k][e] += g[k][e];
-          g[k][e] *= mul[k][e];
-          sum += g[k][e];
-          along = fmaf(g[k][e], h[k][e], along);
-        }
+      for (int e = 0; e < 8; ++e) {
+        h[e] = (h[e] - mean) * r;
+        s1[e] = fmaf(g[e], h[e], s1[e]);
+        s2[e] += g[e];
+        g[e] *= mul[e];
+        sum += counts(e) ? g[e] : 0.f;
+        along = counts(e) ? fmaf(g[e], h[e], along) : along;
       }
-      const GatePair all = block_sum({layer ? wave_sum(sum) : 0.f, wave_sum(along)}, buffer(), waves, w, lane);
+      const GatePair all = block_sum({layer ? wave_sum(sum) : 0.f, wave_sum(along)}, lds[turn ^= 1], waves, w, lane);
       const float m = all.a * per, c = all.b * per;
+      gate_unpack(up, d);
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[k][e] = fmaf(r, fmaf(-h[k][e], c, g[k][e] - m), d[k][e]);
+      for (int e = 0; e < 8; ++e) d[e] = fmaf(r, fmaf(-h[e], c, g[e] - m), d[e]);
+    } else {
+      gate_unpack(up, d);
     }
-    if (a.dx) {
-#pragma unroll
-      for (int k = 0; k < CHUNKS; ++k) {
-        const int at = 8 * (t + threads * k), left = a.width - at;
-        if (left > 0) gate_store<ODD>((X*)a.dx + base + at, left, d[k]);
-      }
-    }
+    if (a.dx && l.there) gate_store<PAST>((X*)a.dx + base, d);
     if (!a.branch) continue;
-    float rb = 1.f, c = 0.f;
+    float u[8], c = 0.f;                               // the branch, normed
+    gate_unpack(bu, u);
     if (a.post) {
-      rb = a.stats[2 * a.rows + row];
       float along = 0.f;
 #pragma unroll
-      for (int k = 0; k < CHUNKS; ++k) {
-        if (a.width - 8 * (t + threads * k) <= 0) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          u[k][e] *= rb;
-          along = fmaf(d[k][e] * gate[k][e], u[k][e], along);
-        }
-      }
-      c = block_sum({wave_sum(along), 0.f}, buffer(), waves, w, lane).a * per;
-    }
-#pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-      const int at = 8 * (t + threads * k), left = a.width - at;
-      if (left <= 0) continue;
-#pragma unroll
       for (int e = 0; e < 8; ++e) {
-        sg[k][e] = fmaf(d[k][e], u[k][e], sg[k][e]);
-        d[k][e] = a.post ? rb * fmaf(-u[k][e], c, d[k][e] * gate[k][e]) : d[k][e] * gate[k][e];
+        u[e] *= rb;
+        along = counts(e) ? fmaf(d[e] * gate[e], u[e], along) : along;
       }
-      if (a.dbranch) gate_store<ODD>((B*)a.dbranch + base + at, left, d[k]);
+      c = block_sum({wave_sum(l.there ? along : 0.f), 0.f}, lds[turn ^= 1], waves, w, lane).a * per;
     }
-  }
-  if (!a.part) return;
-  float* part = a.part + (int64_t)blockIdx.x * 3 * a.width;
 #pragma unroll
-  for (int k = 0; k < CHUNKS; ++k) {
-    const int at = 8 * (t + threads * k), left = a.width - at;
-    if (left <= 0) continue;
-    if (normed) {
-      gate_store<ODD>(part + at, left, s1[k]);
-      gate_store<ODD>(part + a.width + at, left, s2[k]);
+    for (int e = 0; e < 8; ++e) {
+      sg[e] = fmaf(d[e], u[e], sg[e]);
+      d[e] = rb * fmaf(-u[e], c, d[e] * gate[e]);
     }
-    if (a.branch) gate_store<ODD>(part + 2 * (int64_t)a.width + at, left, sg[k]);
+    if (a.dbranch && l.there) gate_store<PAST>((B*)a.dbranch + base, d);
   }
+  if (!a.part || !l.there) return;
+  float* part = a.part + (int64_t)blockIdx.x * 3 * a.width + l.at;
+  if (normed) {
+    gate_store(part, s1);
+    gate_store(part + a.width, s2);
+  }
+  if (a.branch) gate_store(part + 2 * (int64_t)a.width, sg);
 }
 
 // ------------------------------------------------------------------ gradients of the parameters
@@ -145,7 +125,8 @@ struct GateSums {
   int samples, per_sample, width, columns;               // columns: workgroups that share a sample's channels
   bool params32, normed, branch;
 };
-constexpr int SUM_GROUPS = 16;           // a workgroup: 64 channels, the summands in 16 groups
+constexpr int SUM_CHANNELS = 32, SUM_GROUPS = 32;      // of a workgroup: channels, groups of the summands
+constexpr int SUM_WAVES = 16, SUM_LANES = SUM_CHANNELS / 4;        // (gate_sums_kernel: a thread has four channels)
 
 __device__ __forceinline__ void grad_put(const GateSums& a, void* p, int64_t at, double x) {
   if (!p) return;
@@ -154,59 +135,76 @@ __device__ __forceinline__ void grad_put(const GateSums& a, void* p, int64_t at,
 }
 
 // Sums of a sample's workgroups; parameters of its own.  With one sample all gradients are written here, with several the sums
-// take the place of the first workgroup's.
-__global__ __launch_bounds__(64 * SUM_GROUPS) void gate_sums_kernel(GateSums a) {
-  __shared__ double lds[3][SUM_GROUPS][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, b = blockIdx.x / a.columns, c = blockIdx.x % a.columns * 64 + lane;
-  double s[3] = {0.0, 0.0, 0.0};
-  float* part = a.part + (int64_t)b * a.per_sample * 3 * a.width + c;
-  if (c < a.width) {
-    for (int p = g; p < a.per_sample; p += 4 * SUM_GROUPS) {         // four in flight
-      float x[4][3];
+// take the place of the first workgroup's.  A thread adds up four channels of every 128th workgroup, requested four at a time: the
+// kernel is as long as its loads' round trips.  (One channel a thread, 1280 workgroups of 1536 channels: 49 us.)
+__global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
+  __shared__ double lds[SUM_WAVES][3][SUM_CHANNELS];
+  const int t = threadIdx.x, b = blockIdx.x / a.columns, c0 = blockIdx.x % a.columns * SUM_CHANNELS;
+  // (the last channels are taken by whole vectors, too: those in front of c0 are another workgroup's and not written)
+  auto first = [&](int lane) -> int { return min(c0 + 4 * lane, a.width - 4); };
+  const float* part = a.part + (int64_t)b * a.per_sample * 3 * a.width;
+  double s[3][4] = {};
+  for (int p = t / SUM_LANES; p < a.per_sample; p += 4 * 64 * SUM_WAVES / SUM_LANES) {
+    f32x4 x[4][3];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float* q = part + (int64_t)min(p + u * SUM_GROUPS, a.per_sample - 1) * 3 * a.width;
-        x[u][0] = a.normed ? q[0] : 0.f;
-        x[u][1] = a.normed ? q[a.width] : 0.f;
-        x[u][2] = a.branch ? q[2 * (int64_t)a.width] : 0.f;
+    for (int u = 0; u < 4; ++u) {
+      const float* q = part + (int64_t)min(p + u * (64 * SUM_WAVES / SUM_LANES), a.per_sample - 1) * 3 * a.width + first(t % SUM_LANES);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        x[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (i < 2 ? a.normed : a.branch) x[u][i] = *(const gate_f32x4*)(q + i * (int64_t)a.width);
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int i = 0; i < 3; ++i) s[i] += p + u * SUM_GROUPS < a.per_sample ? (double)x[u][i] : 0.0;
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (p + u * (64 * SUM_WAVES / SUM_LANES) < a.per_sample)
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][e] += (double)x[u][i][e];
   }
 #pragma unroll
-  for (int i = 0; i < 3; ++i) lds[i][g][lane] = s[i];
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int k = SUM_LANES; k < 64; k <<= 1) s[i][e] += __shfl_xor(s[i][e], k, 64);
+  if ((t & 63) < SUM_LANES)
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[t >> 6][i][4 * (t & 63) + e] = s[i][e];
   __syncthreads();
-  if (g || c >= a.width) return;
+  const int c = first(t / 4) + t % 4;
+  if (t >= SUM_CHANNELS || c < c0 + t / 4 * 4) return;
+  double sum[3] = {0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (int k = 0; k < SUM_WAVES; ++k)
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    s[i] = 0.0;
-    for (int k = 0; k < SUM_GROUPS; ++k) s[i] += lds[i][k][lane];
-  }
+    for (int i = 0; i < 3; ++i) sum[i] += lds[k][i][t];
   const double weight = gate_one(a.p.weight, a.params32, c, 1.f), bias = gate_one(a.p.bias, a.params32, c, 0.f);
   const double post = gate_one(a.p.branch_weight, a.params32, c, 1.f), gate = gate_one(a.p.gate, a.params32, b * a.gate_sb + c, 1.f);
   const double scale = 1.0 + gate_one(a.p.scale, a.params32, b * a.scale_sb + c, 0.f);
   const bool one = a.samples == 1;
-  if (one || a.gate_sb) grad_put(a, a.d.gate, b * a.gate_sb + c, post * s[2]);
-  if (one || a.scale_sb) grad_put(a, a.d.scale, b * a.scale_sb + c, weight * s[0] + bias * s[1]);
-  if (one || a.shift_sb) grad_put(a, a.d.shift, b * a.shift_sb + c, s[1]);
+  if (one || a.gate_sb) grad_put(a, a.d.gate, b * a.gate_sb + c, post * sum[2]);
+  if (one || a.scale_sb) grad_put(a, a.d.scale, b * a.scale_sb + c, weight * sum[0] + bias * sum[1]);
+  if (one || a.shift_sb) grad_put(a, a.d.shift, b * a.shift_sb + c, sum[1]);
   if (one) {
-    grad_put(a, a.d.weight, c, scale * s[0]);
-    grad_put(a, a.d.bias, c, scale * s[1]);
-    grad_put(a, a.d.branch_weight, c, gate * s[2]);
+    grad_put(a, a.d.weight, c, scale * sum[0]);
+    grad_put(a, a.d.bias, c, scale * sum[1]);
+    grad_put(a, a.d.branch_weight, c, gate * sum[2]);
     return;
   }
-  part[0] = (float)s[0];
-  part[a.width] = (float)s[1];
-  part[2 * (int64_t)a.width] = (float)s[2];
+  float* joined = a.part + (int64_t)b * a.per_sample * 3 * a.width + c;
+  joined[0] = (float)sum[0];
+  joined[a.width] = (float)sum[1];
+  joined[2 * (int64_t)a.width] = (float)sum[2];
 }
 
 // Gradients of what all samples share: sums over the samples.
-__global__ __launch_bounds__(64 * SUM_GROUPS) void gate_shared_kernel(GateSums a) {
-  __shared__ double lds[6][SUM_GROUPS][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+__global__ __launch_bounds__(SUM_CHANNELS * SUM_GROUPS) void gate_shared_kernel(GateSums a) {
+  __shared__ double lds[6][SUM_GROUPS][SUM_CHANNELS];
+  const int lane = threadIdx.x % SUM_CHANNELS, g = threadIdx.x / SUM_CHANNELS, c = blockIdx.x * SUM_CHANNELS + lane;
   double s[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
   if (c < a.width) {
     const double weight = gate_one(a.p.weight, a.params32, c, 1.f), bias = gate_one(a.p.bias, a.params32, c, 0.f);
@@ -232,6 +230,7 @@ __global__ __launch_bounds__(64 * SUM_GROUPS) void gate_shared_kernel(GateSums a
 #pragma unroll
   for (int i = 0; i < 6; ++i) {
     s[i] = 0.0;
+#pragma unroll 4
     for (int k = 0; k < SUM_GROUPS; ++k) s[i] += lds[i][k][lane];
   }
   grad_put(a, a.d.weight, c, s[0]);
@@ -244,11 +243,11 @@ __global__ __launch_bounds__(64 * SUM_GROUPS) void gate_shared_kernel(GateSums a
 
 template <typename X, typename B, typename N>
 static void launch_types(const GateArgs& a, const dim3& grid, const dim3& block, hipStream_t stream) {
-  const bool odd = a.width % 8, wide = a.width > 512 * 2 * GATE_WAVES;
-  if (wide && odd)      hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, 4, true>), grid, block, 0, stream, a);
-  else if (wide)        hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, 4, false>), grid, block, 0, stream, a);
-  else if (odd)         hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, 2, true>), grid, block, 0, stream, a);
-  else                  hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, 2, false>), grid, block, 0, stream, a);
+  const bool odd = a.width % 8, past = gate_past(a);
+  if (odd && past) hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, true, true>), grid, block, 0, stream, a);
+  else if (odd)    hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, true, false>), grid, block, 0, stream, a);
+  else if (past)   hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, false, true>), grid, block, 0, stream, a);
+  else             hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, false, false>), grid, block, 0, stream, a);
 }
 
 size_t gate_partials_bytes(const spa2_gate_shape& s) {
@@ -271,15 +270,15 @@ hipError_t launch_gate_norm_bwd(const void* branch, const spa2_gate_params& p, c
   else                  launch_types<float, uint16_t, uint16_t>(a, grid, block, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !any) return e;
-  const int columns = (s.width + 63) / 64;
+  const int columns = (s.width + SUM_CHANNELS - 1) / SUM_CHANNELS;
   GateSums q = {a.part, p, grads, s.gate_sb, s.scale_sb, s.shift_sb, (int)s.samples, a.per_sample, s.width, columns, a.params32,
                 s.kind != SPA2_NORM_NONE, branch != nullptr};
-  hipLaunchKernelGGL(gate_sums_kernel, dim3((unsigned)(columns * s.samples)), dim3(64 * SUM_GROUPS), 0, stream, q);
+  hipLaunchKernelGGL(gate_sums_kernel, dim3((unsigned)(columns * s.samples)), dim3(64 * SUM_WAVES), 0, stream, q);
   e = hipGetLastError();
   const bool shared = grads.weight || grads.bias || grads.branch_weight || (grads.gate && !s.gate_sb) || (grads.scale && !s.scale_sb) ||
                       (grads.shift && !s.shift_sb);
   if (e != hipSuccess || s.samples == 1 || !shared) return e;
-  hipLaunchKernelGGL(gate_shared_kernel, dim3((unsigned)columns), dim3(64 * SUM_GROUPS), 0, stream, q);
+  hipLaunchKernelGGL(gate_shared_kernel, dim3((unsigned)columns), dim3(SUM_CHANNELS * SUM_GROUPS), 0, stream, q);
   return hipGetLastError();
 }
 

@@ -16,7 +16,7 @@ constexpr int64_t GATE_MAX_SAMPLES = 1 << 22, GATE_MAX_ROWS = (int64_t)1 << 40;
 int check_gate_shape(const spa2_gate_shape* s) {
   if (!s) return SPA2_ERR_NULL;
   if (s->samples <= 0 || s->samples > GATE_MAX_SAMPLES || s->tokens <= 0 || s->tokens > GATE_MAX_ROWS / s->samples ||
-      s->width <= 0 || s->width > SPA2_GATE_MAX_WIDTH)
+      s->width < SPA2_GATE_MIN_WIDTH || s->width > SPA2_GATE_MAX_WIDTH)
     return SPA2_ERR_SHAPE;
   for (const int64_t sb : {s->gate_sb, s->scale_sb, s->shift_sb})
     if (sb && (sb < s->width || sb > GATE_MAX_ROWS)) return SPA2_ERR_SHAPE;
