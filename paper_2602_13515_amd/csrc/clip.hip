@@ -13,8 +13,10 @@
 namespace spa2 {
 
 constexpr int CLIP_TABLE = 120;          // tensors of a launch: their table fills most of the 4 KB that its arguments may have
-constexpr int CLIP_CHUNK = 4096;         // elements that a workgroup takes at a time, 16 a thread
-constexpr int CLIP_WGS = 2048;           // workgroups at most: all that run at a time
+constexpr int CLIP_VECTORS = 4;          // of 16 bytes, that a thread takes at a time
+constexpr int CLIP_NORM_WGS = 768, CLIP_SCALE_WGS = 256;           // workgroups at most (see launch_clip)
+constexpr int clip_elements(bool fp32) { return fp32 ? 4 : 8; }    // of a vector
+constexpr int clip_chunk(bool fp32) { return 256 * CLIP_VECTORS * clip_elements(fp32); }     // of what a workgroup takes at a time
 
 struct ClipItem { const void* x; void* out; int64_t n; };
 struct ClipArgs {
@@ -27,48 +29,103 @@ struct ClipArgs {
   float* norm;                           // written by the launch that has it
   double max_norm, eps;
   bool again;                            // not the first launch of its pass: sums are added to those that are there
+  bool in_place;                         // every result of the launch lies where its gradient does
 };
 static_assert(sizeof(ClipArgs) <= 4096, "arguments of a launch");
 
-// 16 bytes from any element on
+// 16 or 8 bytes from any element on: results (gradients are read from 16-byte boundaries)
 typedef u32x4 __attribute__((aligned(2))) clip_u32x4;
-typedef f32x4 __attribute__((aligned(4))) clip_f32x4;
+typedef u32x2 __attribute__((aligned(2))) clip_u32x2;
 
+struct ClipPiece { u32x4 v[CLIP_VECTORS]; };
+// Elements of a tensor in front of which its first vector starts, on a 16-byte boundary.
+__host__ __device__ __forceinline__ int clip_skew(const void* x, bool fp32) { return (int)(((uintptr_t)x & 15) / (fp32 ? 4 : 2)); }
+// Whether the chunk from element `base` on lies inside the tensor (uniform).
 template <bool F32>
-__device__ __forceinline__ void clip_load8(const void* p, int64_t at, float (&x)[8]) {
-  if constexpr (F32) {
-    const f32x4 a = *(const clip_f32x4*)((const float*)p + at), b = *(const clip_f32x4*)((const float*)p + at + 4);
+__device__ __forceinline__ bool clip_whole(const ClipItem& t, int64_t base) { return base >= 0 && base + clip_chunk(F32) <= t.n; }
+// This thread's vectors of a chunk from element `base` on (-skew for the first): vector v of the workgroup's 256 CLIP_VECTORS goes to
+// thread v % 256.  Elements outside the tensor are zero.
+template <bool F32>
+__device__ __forceinline__ void clip_fetch(const ClipItem& t, int64_t base, ClipPiece& p) {
+  constexpr int V = clip_elements(F32);
+  if (clip_whole<F32>(t, base)) {
+    const char* x = (const char*)t.x + base * (F32 ? 4 : 2) + 16 * threadIdx.x;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) { x[c] = a[c]; x[4 + c] = b[c]; }
-  } else {
-    const u32x4 v = *(const clip_u32x4*)((const uint16_t*)p + at);
+    for (int r = 0; r < CLIP_VECTORS; ++r) p.v[r] = *(const u32x4*)(x + 4096 * r);
+    return;
+  }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t u = v[c];
+  for (int r = 0; r < CLIP_VECTORS; ++r) {
+    const int64_t at = base + V * (int)(threadIdx.x + 256 * r);
+    p.v[r] = u32x4{0, 0, 0, 0};
+    if (at >= 0 && at + V <= t.n) {
+      p.v[r] = *(const u32x4*)((const char*)t.x + at * (F32 ? 4 : 2));
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if (at + e < 0 || at + e >= t.n) continue;
+        if (F32) p.v[r][e] = ((const uint32_t*)t.x)[at + e];
+        else     p.v[r][e / 2] |= (uint32_t)((const uint16_t*)t.x)[at + e] << (16 * (e & 1));
+      }
+    }
+  }
+}
+// its numbers
+template <bool F32>
+__device__ __forceinline__ void clip_unpack(u32x4 v, float (&x)[clip_elements(F32)]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t u = v[c];
+    if constexpr (F32) {
+      x[c] = __builtin_bit_cast(float, u);
+    } else {
       x[2 * c] = __builtin_bit_cast(float, u << 16);
       x[2 * c + 1] = __builtin_bit_cast(float, u & 0xffff0000u);
     }
   }
 }
-template <bool F32>
-__device__ __forceinline__ void clip_store8(void* p, int64_t at, const float (&x)[8]) {
-  if constexpr (F32) {
-    *(clip_f32x4*)((float*)p + at) = f32x4{x[0], x[1], x[2], x[3]};
-    *(clip_f32x4*)((float*)p + at + 4) = f32x4{x[4], x[5], x[6], x[7]};
-  } else {
-    *(clip_u32x4*)((uint16_t*)p + at) = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+template <int V>
+__device__ __forceinline__ void clip_store(uint16_t* p, const float (&x)[V]) {
+  if constexpr (V == 8) *(clip_u32x4*)p = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+  else                  *(clip_u32x2*)p = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+}
+template <int V>
+__device__ __forceinline__ void clip_store(float* p, const float (&x)[V]) {
+#pragma unroll
+  for (int q = 0; q < V; q += 4)
+    *(clip_u32x4*)(p + q) = u32x4{__builtin_bit_cast(uint32_t, x[q]), __builtin_bit_cast(uint32_t, x[q + 1]),
+                                  __builtin_bit_cast(uint32_t, x[q + 2]), __builtin_bit_cast(uint32_t, x[q + 3])};
+}
+__device__ __forceinline__ void clip_one(uint16_t* p, float x) { *p = (uint16_t)pack_bf16(x, x); }
+__device__ __forceinline__ void clip_one(float* p, float x) { *p = x; }
+
+// The chunk that a workgroup has in hand, and the next one (UP: onwards, else backwards) on its way.
+template <bool UP>
+struct ClipWalk {
+  int c, t;
+  ClipPiece piece;
+  __device__ __forceinline__ bool inside(const ClipArgs& a) const { return UP ? c < a.first[a.count] : c >= 0; }
+  __device__ __forceinline__ int64_t base(const ClipArgs& a) const {
+    const bool fp32 = a.types[t] & 1;
+    return (int64_t)(c - a.first[t]) * clip_chunk(fp32) - clip_skew(a.item[t].x, fp32);
   }
-}
-template <bool F32>
-__device__ __forceinline__ float clip_one(const void* p, int64_t at) {
-  if constexpr (F32) return ((const float*)p)[at];
-  else               return __builtin_bit_cast(float, (uint32_t)((const uint16_t*)p)[at] << 16);
-}
-template <bool F32>
-__device__ __forceinline__ void clip_put(void* p, int64_t at, float x) {
-  if constexpr (F32) ((float*)p)[at] = x;
-  else               ((uint16_t*)p)[at] = (uint16_t)pack_bf16(x, x);
-}
+  __device__ __forceinline__ void fetch(const ClipArgs& a) {
+    if (!inside(a)) return;
+    if (UP) while (c >= a.first[t + 1]) ++t;
+    else    while (c < a.first[t]) --t;
+    if (a.types[t] & 1) clip_fetch<true>(a.item[t], base(a), piece);
+    else                clip_fetch<false>(a.item[t], base(a), piece);
+  }
+  __device__ __forceinline__ void start(const ClipArgs& a) {
+    c = UP ? (int)blockIdx.x : a.first[a.count] - 1 - (int)blockIdx.x;
+    t = UP ? 0 : a.count - 1;
+    fetch(a);
+  }
+  __device__ __forceinline__ void next(const ClipArgs& a) {
+    c += UP ? (int)gridDim.x : -(int)gridDim.x;
+    fetch(a);
+  }
+};
 
 // sum over the workgroup, in every thread (lds: four numbers)
 __device__ __forceinline__ double clip_block_sum(double x, double* lds) {
@@ -80,60 +137,59 @@ __device__ __forceinline__ double clip_block_sum(double x, double* lds) {
 }
 
 template <bool F32>
-__device__ __forceinline__ double clip_squares(const ClipItem& t, int64_t base, double sum) {
-  const int tid = threadIdx.x;
-  float x[2][8];
+__device__ __forceinline__ double clip_squares(const ClipPiece& p, double sum) {
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int64_t at = base + r * (CLIP_CHUNK / 2) + 8 * tid;
-    if (at + 8 <= t.n) {
-      clip_load8<F32>(t.x, at, x[r]);
-    } else {
+  for (int r = 0; r < CLIP_VECTORS; ++r) {
+    float x[clip_elements(F32)];
+    clip_unpack<F32>(p.v[r], x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[r][e] = at + e < t.n ? clip_one<F32>(t.x, at + e) : 0.f;
-    }
+    for (int e = 0; e < clip_elements(F32); ++e) sum = fma((double)x[e], (double)x[e], sum);
   }
-#pragma unroll
-  for (int r = 0; r < 2; ++r)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fma((double)x[r][e], (double)x[r][e], sum);
   return sum;
 }
 
 __global__ __launch_bounds__(256) void clip_norm_kernel(ClipArgs a) {
   __shared__ double lds[4];
   double sum = 0.0;
-  int t = 0;
-  for (int c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
-    while (c >= a.first[t + 1]) ++t;
-    const ClipItem item = a.item[t];
-    const int64_t base = (int64_t)(c - a.first[t]) * CLIP_CHUNK;
-    sum = a.types[t] & 1 ? clip_squares<true>(item, base, sum) : clip_squares<false>(item, base, sum);
+  ClipWalk<true> walk;
+  walk.start(a);
+  while (walk.inside(a)) {
+    const ClipPiece p = walk.piece;
+    const bool fp32 = a.types[walk.t] & 1;
+    walk.next(a);
+    sum = fp32 ? clip_squares<true>(p, sum) : clip_squares<false>(p, sum);
   }
   sum = clip_block_sum(sum, lds);
   if (threadIdx.x == 0) a.part[blockIdx.x] = a.again ? a.part[blockIdx.x] + sum : sum;
 }
 
-template <bool F32, bool OUT32>
-__device__ __forceinline__ void clip_chunk(const ClipItem& t, int64_t base, double factor) {
+template <bool F32, typename O>
+__device__ __forceinline__ void clip_scaled(const ClipPiece& p, const ClipItem& t, int64_t base, double factor) {
+  constexpr int V = clip_elements(F32);
+  const bool whole = clip_whole<F32>(t, base);
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    const int64_t at = base + r * (CLIP_CHUNK / 2) + 8 * threadIdx.x;
-    if (at + 8 <= t.n) {
-      float x[8];
-      clip_load8<F32>(t.x, at, x);
+  for (int r = 0; r < CLIP_VECTORS; ++r) {
+    float x[V];
+    clip_unpack<F32>(p.v[r], x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (float)((double)x[e] * factor);
-      clip_store8<OUT32>(t.out, at, x);
+    for (int e = 0; e < V; ++e) x[e] = (float)((double)x[e] * factor);
+    const int64_t at = base + V * (int)(threadIdx.x + 256 * r);
+    O* out = (O*)t.out + at;
+    if (whole) {
+      clip_store<V>(out, x);
     } else {
-      for (int e = 0; e < 8 && at + e < t.n; ++e)
-        clip_put<OUT32>(t.out, at + e, (float)((double)clip_one<F32>(t.x, at + e) * factor));
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (at + e >= 0 && at + e < t.n) clip_one(out + e, x[e]);
     }
   }
 }
 
+// (from the end to the start: begins with what the first pass has read last)
 __global__ __launch_bounds__(256) void clip_scale_kernel(ClipArgs a) {
   __shared__ double lds[4];
+  ClipWalk<false> walk;
+  if (!a.in_place) walk.start(a);                      // (in place nothing may have to be read)
   double sum = 0.0;
   for (int p = threadIdx.x; p < a.parts; p += 256) sum += a.part[p];
   const double norm = sqrt(clip_block_sum(sum, lds)), size = norm + a.eps;
@@ -142,39 +198,54 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipArgs a) {
   double factor = 1.0;
   if (a.max_norm < (double)INFINITY && size != 0.0) factor = a.max_norm / size;
   if (factor >= 1.0) factor = 1.0;
-  int t = 0;
-  for (int c = blockIdx.x; c < a.first[a.count]; c += gridDim.x) {
-    while (c >= a.first[t + 1]) ++t;
-    const ClipItem item = a.item[t];
+  if (a.in_place) {
+    if (factor == 1.0) return;
+    walk.start(a);
+  }
+  while (walk.inside(a)) {
+    const ClipPiece p = walk.piece;
+    const int types = a.types[walk.t];
+    const ClipItem item = a.item[walk.t];
+    const int64_t base = walk.base(a);
+    walk.next(a);
     if (factor == 1.0 && item.out == item.x) continue;
-    const int64_t base = (int64_t)(c - a.first[t]) * CLIP_CHUNK;
-    switch (a.types[t]) {
-      case 0: clip_chunk<false, false>(item, base, factor); break;
-      case 1: clip_chunk<true, false>(item, base, factor); break;
-      case 2: clip_chunk<false, true>(item, base, factor); break;
-      default: clip_chunk<true, true>(item, base, factor); break;
+    switch (types) {
+      case 0: clip_scaled<false, uint16_t>(p, item, base, factor); break;
+      case 1: clip_scaled<true, uint16_t>(p, item, base, factor); break;
+      case 2: clip_scaled<false, float>(p, item, base, factor); break;
+      default: clip_scaled<true, float>(p, item, base, factor); break;
     }
   }
 }
 
-size_t clip_partials_bytes() { return CLIP_WGS * sizeof(double); }
+size_t clip_partials_bytes() { return CLIP_NORM_WGS * sizeof(double); }
 
+// Workgroups: the fewer, the shorter is the stretch of memory that they work on at a time, as long as enough is on its way (16 KB each,
+// and 16 KB in hand).  Measured, us, first and second pass' workgroups: 1.13 G elements of fp32 into another tensor 1024 and 512 2521,
+// 768 and 768 2482, 768 and 512 2512, 768 and 384 2525, 768 and 256 2343 (5.8 TB/s; without the next chunk on its way 2048 and 2048
+// 2565); the norm of 2.5 GB of bf16 2048 417, 1024 414, 768 411 (6.1 TB/s), 512 527.  Loads from 16-byte boundaries: 1.6 GB of bf16
+// from an odd element on 325 -> 261, as much as from a boundary.
 hipError_t launch_clip(const spa2_gradient* gradients, int count, double max_norm, double eps, float* norm, void* ws,
                        hipStream_t stream) {
   ClipArgs a;
   a.part = (double*)ws;
   a.max_norm = max_norm; a.eps = eps;
-  auto chunks_of = [](int64_t n) { return (int)((n + CLIP_CHUNK - 1) / CLIP_CHUNK); };
+  auto chunks_of = [](const spa2_gradient& x) {
+    const int64_t each = clip_chunk(x.dtype == SPA2_DTYPE_F32);
+    return (int)((x.n + clip_skew(x.x, x.dtype == SPA2_DTYPE_F32) + each - 1) / each);
+  };
   // the next table from gradient g on; whether it is for the second pass (only what has a result)
   auto fill = [&](int& g, bool scale) {
     a.count = 0;
     a.first[0] = 0;
+    a.in_place = true;
     for (; g < count && a.count < CLIP_TABLE; ++g) {
       const spa2_gradient& x = gradients[g];
       if (x.n == 0 || (scale && !x.out)) continue;
       a.item[a.count] = {x.x, x.out, x.n};
       a.types[a.count] = (uint8_t)((x.dtype == SPA2_DTYPE_F32) | (x.out_dtype == SPA2_DTYPE_F32) << 1);
-      a.first[a.count + 1] = a.first[a.count] + chunks_of(x.n);
+      a.first[a.count + 1] = a.first[a.count] + chunks_of(x);
+      a.in_place = a.in_place && x.out == x.x;
       ++a.count;
     }
   };
@@ -182,7 +253,7 @@ hipError_t launch_clip(const spa2_gradient* gradients, int count, double max_nor
   for (int g = 0; g < count;) {
     fill(g, false);
     const int chunks = a.first[a.count];
-    a.parts = a.parts > chunks ? a.parts : chunks < CLIP_WGS ? chunks : CLIP_WGS;
+    a.parts = a.parts > chunks ? a.parts : chunks < CLIP_NORM_WGS ? chunks : CLIP_NORM_WGS;
   }
   a.norm = nullptr;
   a.again = false;
@@ -198,7 +269,7 @@ hipError_t launch_clip(const spa2_gradient* gradients, int count, double max_nor
     fill(g, true);
     const int chunks = a.first[a.count];
     if (!chunks && !a.norm) continue;
-    hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)(chunks < 1 ? 1 : chunks < CLIP_WGS ? chunks : CLIP_WGS)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(clip_scale_kernel, dim3((unsigned)(chunks < 1 ? 1 : chunks < CLIP_SCALE_WGS ? chunks : CLIP_SCALE_WGS)), dim3(256), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.norm = nullptr;
