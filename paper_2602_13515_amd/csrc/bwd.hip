@@ -70,6 +70,7 @@ struct CrossDqFineArgs : CrossDqArgs {
 struct WindowDqArgs : CrossDqArgs {
   static constexpr bool WINDOW = true;
   Window win;
+  WindowDeal deal;
 };
 struct WindowDqFineArgs : WindowDqArgs {
   static constexpr bool FINE = true;
@@ -129,8 +130,14 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   bool one = false;           // (WINDOW) all keys in one tile
   if constexpr (CROSS) {
     for (int x = (int)(blockIdx.x * 256 + threadIdx.x); x < a.zeros; x += (int)(gridDim.x * 256)) a.zero[x] = 0;
-    const int rows = stretch_wgs(a.BH * a.Tm);
-    const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
+    int rows = stretch_wgs(a.BH * a.Tm);
+    HeadBlock hb;
+    if constexpr (WINDOW) {
+      rows = a.deal.wgs;
+      hb = window_dealt(a.deal, blockIdx.x % rows);
+    } else {
+      hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
+    }
     if (!hb.valid) return;
     bh = hb.bh; i = hb.blk;
     keys = cross_length(a.kv, bh / a.H);
@@ -649,7 +656,8 @@ hipError_t launch_window_dq(const void* q, const void* k, const void* v, const v
   WindowDqFineArgs a = {};
   fill_cross_dq(a, q, k, v, o, o_res, d_o, lse, m, lengths, scale, delta, lse_out, dq, zero, zeros, plan);
   a.win = win;
-  const dim3 grid((unsigned)(plan.fixed_parts * stretch_wgs(a.BH * a.Tm))), block(256);
+  a.deal = window_deal(win, m, a.BH, a.Tm, true);
+  const dim3 grid((unsigned)(plan.fixed_parts * a.deal.wgs)), block(256);
   const bool fine = cross_few(m);
   if (m.q.d == 128 && fine) hipLaunchKernelGGL((dq_kernel<128, WindowDqFineArgs>), grid, block, 0, stream, a);
   else if (m.q.d == 128)    hipLaunchKernelGGL((dq_kernel<128, WindowDqArgs>), grid, block, 0, stream, a);

@@ -52,6 +52,7 @@ struct WindowDkvArgs : CrossDkvArgs {
   Window win;
   SplitPlan rest;
   int first_blocks;
+  WindowDeal first_deal, rest_deal;
 };
 struct WindowDkvFineArgs : WindowDkvArgs {
   static constexpr bool FINE = true;
@@ -961,12 +962,11 @@ void cross_dkdv_kernel(Args) {
   __shared__ __align__(1024) unsigned char stat_s[2 * 2 * 512];
   const Args& a = fresh_args<Args>();
   if constexpr (Args::WINDOW) {
-    const int firsts = a.first_blocks ? stretch_wgs(a.BH * a.first_blocks) : 0, blocks = a.Tn - a.first_blocks;
-    const bool first = (int)blockIdx.x < firsts * a.sp.fixed_parts;
-    const int per_head = first ? a.first_blocks : blocks, columns = stretch_wgs(a.BH * per_head);
-    const int wg = (int)blockIdx.x - (first ? 0 : firsts * a.sp.fixed_parts);
+    const bool first = (int)blockIdx.x < a.first_deal.wgs * a.sp.fixed_parts;
+    const WindowDeal& deal = first ? a.first_deal : a.rest_deal;
+    const int wg = (int)blockIdx.x - (first ? 0 : a.first_deal.wgs * a.sp.fixed_parts), columns = deal.wgs, per_head = deal.blocks;
     const SplitPlan& sp = first ? a.sp : a.rest;
-    const HeadBlock hb = stretch_row(wg % columns, a.BH, per_head);
+    const HeadBlock hb = window_dealt(deal, wg % columns);
     if (!hb.valid) return;
     WorkItem item;
     item.bh = hb.bh; item.blk = hb.blk + (first ? 0 : a.first_blocks);
@@ -1040,9 +1040,9 @@ hipError_t launch_window_dkdv(const void* q, const void* k, const void* v, const
   a.rest = cross_plan(cuts.rest, counters, pool, dkdv_slot_bytes(m.q));
   // (slots are numbered through: the others' behind those of the first keys)
   a.sp.arrive = (int32_t*)counters; a.sp.pool = (float*)pool; a.sp.slot_floats = (int)(dkdv_slot_bytes(m.q) / 4);
-  const int blocks = a.Tn - a.first_blocks;
-  const int64_t wgs = (a.first_blocks ? (int64_t)a.sp.fixed_parts * stretch_wgs(a.BH * a.first_blocks) : 0) +
-                      (blocks ? (int64_t)a.rest.fixed_parts * stretch_wgs(a.BH * blocks) : 0);
+  a.first_deal = window_deal(win, m, a.BH, a.first_blocks, false);
+  a.rest_deal = window_deal(win, m, a.BH, a.Tn - a.first_blocks, false);
+  const int64_t wgs = (int64_t)a.sp.fixed_parts * a.first_deal.wgs + (int64_t)a.rest.fixed_parts * a.rest_deal.wgs;
   const dim3 grid((unsigned)wgs), block(128);
   const bool fine = cross_few(m);
   if (m.q.d == 128 && fine) hipLaunchKernelGGL((cross_dkdv_kernel<128, WindowDkvFineArgs>), grid, block, 0, stream, a);

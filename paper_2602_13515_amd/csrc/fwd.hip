@@ -48,6 +48,7 @@ struct CrossFwdArgs : FwdArgs {
 struct WindowFwdArgs : CrossFwdArgs {
   static constexpr bool WINDOW = true;
   Window win;
+  WindowDeal deal;
 };
 
 // Partial result of one part of a split row: the unnormalised accumulator as [pair of accumulator registers][thread],
@@ -107,8 +108,14 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   int start = 0;              // (WINDOW) place of query 0, and what the workgroup's queries see
   WindowSpan span;
   if constexpr (CROSS) {
-    const int rows = stretch_wgs(a.BH * a.Tm);
-    const HeadBlock hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
+    int rows = stretch_wgs(a.BH * a.Tm);
+    HeadBlock hb;
+    if constexpr (WINDOW) {
+      rows = a.deal.wgs;
+      hb = window_dealt(a.deal, blockIdx.x % rows);
+    } else {
+      hb = stretch_row(blockIdx.x % rows, a.BH, a.Tm);
+    }
     if (!hb.valid) return;
     bh = hb.bh; i = hb.blk;
     keys = cross_length(a.kv, bh / a.H);
@@ -694,9 +701,10 @@ hipError_t launch_window_fwd(const void* q, const void* k, const void* v, const 
   a.scale_log2 = scale * LOG2E;
   a.kv = cross_keys(m, lengths);
   a.win = win;
+  a.deal = window_deal(win, m, a.BH, a.Tm, true);
   const CrossSection s = window_fwd_section(m, win);
   a.sp = cross_plan(s, nullptr, ws, fwd_slot_bytes(m.q));
-  const dim3 grid((unsigned)(s.cut.parts * stretch_wgs(a.BH * a.Tm))), block(256);
+  const dim3 grid((unsigned)(s.cut.parts * a.deal.wgs)), block(256);
   if (m.q.d == 128) hipLaunchKernelGGL((fwd_kernel<128, WindowFwdArgs>), grid, block, 0, stream, a);
   else              hipLaunchKernelGGL((fwd_kernel<64, WindowFwdArgs>), grid, block, 0, stream, a);
   const hipError_t e = hipGetLastError();

@@ -106,6 +106,23 @@ int main() {
     }
     CHECK(cols.total >= cols.counters + (size_t)(cols.first.slots + cols.rest.slots) * dkdv_slot_bytes(m.q));
   }
+  for (int heads : {1, 2, 3, 8, 12, 40, 300})
+    for (int blocks : {0, 1, 7, 15, 16, 17, 33, 100, 256, 487, 512, 591})
+      for (int turn = 0; turn < 6; ++turn) {
+        const Window w = {nullptr, 0, turn % 3 == 1 ? WINDOW_NO_LIMIT : 5, turn % 3 == 2 ? WINDOW_NO_LIMIT : 7, 0, 100};
+        CrossDims m = {};
+        m.Nk = 1000; m.q.d = 128;
+        const WindowDeal d = window_deal(w, m, heads, blocks, turn < 3);
+        std::vector<int> seen((size_t)heads * blocks, 0);
+        for (int wg = 0; wg < d.wgs; ++wg) {
+          const HeadBlock hb = window_dealt(d, wg);
+          if (!hb.valid) continue;
+          if (hb.bh < 0 || hb.bh >= heads || hb.blk < 0 || hb.blk >= blocks) { std::printf("dealt outside\n"); return 1; }
+          ++seen[(size_t)hb.bh * blocks + hb.blk];
+        }
+        for (int n : seen)
+          if (n != 1) { std::printf("%d heads of %d blocks: one is dealt %d times\n", heads, blocks, n); return 1; }
+      }
   std::printf("windows hold\n");
   return 0;
 }
