@@ -5,7 +5,8 @@ without them is the training step itself: a frozen teacher with full attention, 
 initialisation and differs only in the attention operator, identical noisy inputs x_t = t x_1 + (1 - t) x_0
 for both, and the loss ||u_sparse - u_full||^2 back-propagated through the block-sparse backward kernels.
 `ToyBlock` is one pre-norm attention block that stands in for the velocity network; on request with what such a network has
-around its attention: the norm of q and k with the rotation by position, attention to a prompt, dropout of its branches.
+around its attention: the norm of q and k with the rotation by position, attention to a prompt, dropout of its branches, gates and
+modulated norms; the student's attention may be one over a window instead, and the loop clips the gradients, on request.
 """
 from __future__ import annotations
 
@@ -16,7 +17,10 @@ import torch
 
 from . import binding as _b
 from .autograd import _operator, _plain, sparge_attn2
-from .block import cross_attention, dropout_add, qk_norm_rotate, rotary_table
+from .block import cross_attention, dropout_add, gate_add_norm, qk_norm_rotate, rotary_table, window_attention
+from .gradients import clip_gradients
+
+Window = Tuple[Optional[int], Optional[int], int]
 
 
 class ToyBlock(torch.nn.Module):
@@ -26,11 +30,18 @@ class ToyBlock(torch.nn.Module):
     grid: extents of the tokens' grid (frames, height, width): the heads of q and k are normed and rotated by position.
     context_dim: a second branch attends to `context` [B, M, context_dim], of which sample b has `lengths[b]` rows (a batch of
     prompts, padded).  dropout: of both branches, in training mode; the masks' seed comes from PyTorch's default generator, in
-    a captured step from the GPU's, so that every replay draws other masks."""
+    a captured step from the GPU's, so that every replay draws other masks.
+
+    window: (left, right, sinks) of `window_attention`, which then takes the place of the block-sparse attention.  gated: each
+    branch is added through a gate, a vector that is learnt, in the pass that norms the sum for the next branch
+    (`gate_add_norm`).  condition_dim: with `gated`, each sample's gates, and a scale and a shift of its norms, come from a
+    projection of `condition` [B, condition_dim] instead."""
 
     def __init__(self, dim: int, heads: int, k_frac: Optional[float] = None, top_p: Optional[float] = None,
-                 grid: Optional[Sequence[int]] = None, context_dim: Optional[int] = None, dropout: float = 0.0):
+                 grid: Optional[Sequence[int]] = None, context_dim: Optional[int] = None, dropout: float = 0.0,
+                 window: Optional[Window] = None, gated: bool = False, condition_dim: Optional[int] = None):
         super().__init__()
+        assert condition_dim is None or gated
         assert dim % heads == 0 and dim // heads in (64, 128)
         self.heads, self.k_frac, self.top_p, self.dropout = heads, k_frac, top_p, float(dropout)
         self.norm = torch.nn.LayerNorm(dim)
@@ -46,9 +57,17 @@ class ToyBlock(torch.nn.Module):
             self.context_q = torch.nn.Linear(dim, dim)
             self.context_kv = torch.nn.Linear(context_dim, 2 * dim)
             self.context_proj = torch.nn.Linear(dim, dim)
+        self.window, self.gated, self.condition_dim = window, gated, condition_dim
+        branches = 1 if context_dim is None else 2
+        if condition_dim is not None:         # (gate, scale and shift of each branch)
+            self.modulation = torch.nn.Linear(condition_dim, 3 * branches * dim)
+        elif gated:
+            self.gates = torch.nn.Parameter(torch.ones(branches, dim))
         self._full = None                     # the all-ones pattern, built once per input shape
 
     def _attention(self, q, k, v):
+        if self.window is not None:
+            return window_attention(q, k, v, *self.window)
         if self.k_frac is not None:
             return sparge_attn2(q, k, v, self.k_frac, self.top_p)
         B, H, N, _ = q.shape
@@ -72,12 +91,17 @@ class ToyBlock(torch.nn.Module):
             return x + branch
         return dropout_add(branch, x, self.dropout, *((seed, number) if isinstance(seed, int) else (seed[number],)))
 
-    def forward(self, x: torch.Tensor, context: Optional[torch.Tensor] = None,
-                lengths: Optional[torch.Tensor] = None) -> torch.Tensor:
-        B, N, C = x.shape
+    def _modulated(self, condition: Optional[torch.Tensor]) -> Sequence[Tuple[Optional[torch.Tensor], ...]]:
+        """(gate, scale, shift) of each branch."""
+        if self.condition_dim is None:
+            return [(gate, None, None) for gate in self.gates]
+        return list(zip(*[iter(self.modulation(condition).chunk(3 * (1 if self.context_dim is None else 2), dim=-1))] * 3))
+
+    def _self_branch(self, h: torch.Tensor) -> torch.Tensor:
+        """Of the normed tokens h: attention among them, projected."""
+        B, N, C = h.shape
         d = C // self.heads
-        seed = self._seed(x)
-        qkv = self.qkv(self.norm(x))
+        qkv = self.qkv(h)
         if self.grid is None:
             qkv = qkv.to(torch.bfloat16).view(B, N, 3, self.heads, d)
             q, k, v = (qkv[:, :, i].permute(0, 2, 1, 3) for i in range(3))         # [B, H, N, d] views
@@ -86,21 +110,54 @@ class ToyBlock(torch.nn.Module):
             q, k = qk_norm_rotate(q, k, self.q_weight, self.k_weight, self.cos, self.sin, interleaved=True)
             v = v.to(torch.bfloat16)
         o = self._attention(q, k, v)                                            # strides of q
-        x = self._add(x, self.proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float()), seed, 0)
-        if self.context_dim is None:
-            return x
-        q = self.context_q(self.context_norm(x)).to(torch.bfloat16).view(B, N, self.heads, d).permute(0, 2, 1, 3)
+        return self.proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float())
+
+    def _context_branch(self, h: torch.Tensor, context: torch.Tensor, lengths: Optional[torch.Tensor]) -> torch.Tensor:
+        B, N, C = h.shape
+        d = C // self.heads
+        q = self.context_q(h).to(torch.bfloat16).view(B, N, self.heads, d).permute(0, 2, 1, 3)
         k, v = (t.permute(0, 2, 1, 3) for t in
                 self.context_kv(context).to(torch.bfloat16).view(B, -1, 2, self.heads, d).unbind(2))
         o = cross_attention(q, k, v, lengths)
-        return self._add(x, self.context_proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float()), seed, 1)
+        return self.context_proj(o.permute(0, 2, 1, 3).reshape(B, N, C).float())
+
+    def _dropped(self, branch: torch.Tensor, seed: Union[None, int, torch.Tensor], number: int) -> torch.Tensor:
+        if seed is None:
+            return branch
+        return dropout_add(branch, None, self.dropout, *((seed, number) if isinstance(seed, int) else (seed[number],)))
+
+    def _gated_forward(self, x, context, lengths, condition) -> torch.Tensor:
+        seed = self._seed(x)
+        mods, norm = self._modulated(condition), self.norm
+        gate, scale, shift = mods[0]
+        _, h = gate_add_norm(x, weight=norm.weight, bias=norm.bias, scale=scale, shift=shift, eps=norm.eps)
+        branch = self._dropped(self._self_branch(h), seed, 0)
+        if self.context_dim is None:
+            return gate_add_norm(x, branch, gate, kind=None)[0]
+        norm, (next_gate, scale, shift) = self.context_norm, mods[1]
+        x, h = gate_add_norm(x, branch, gate, weight=norm.weight, bias=norm.bias, scale=scale, shift=shift, eps=norm.eps)
+        branch = self._dropped(self._context_branch(h, context, lengths), seed, 1)
+        return gate_add_norm(x, branch, next_gate, kind=None)[0]
+
+    def forward(self, x: torch.Tensor, context: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                condition: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if self.gated:
+            return self._gated_forward(x, context, lengths, condition)
+        seed = self._seed(x)
+        x = self._add(x, self._self_branch(self.norm(x)), seed, 0)
+        if self.context_dim is None:
+            return x
+        return self._add(x, self._context_branch(self.context_norm(x), context, lengths), seed, 1)
 
 
-def make_student(teacher: ToyBlock, k_frac: float, top_p: float, dropout: float = 0.0) -> ToyBlock:
-    """Alg. 2 steps 3-4: same weights, attention replaced by SpargeAttn2(., ., ., k%, p%); the teacher is frozen.  `dropout` is
-    the student's (the teacher keeps its own)."""
+def make_student(teacher: ToyBlock, k_frac: Optional[float], top_p: Optional[float], dropout: float = 0.0,
+                 window: Optional[Window] = None) -> ToyBlock:
+    """Alg. 2 steps 3-4: same weights, attention replaced by SpargeAttn2(., ., ., k%, p%), or by attention over a window (k_frac and
+    top_p are then not looked at); the teacher is frozen.  `dropout` is the student's (the teacher keeps its own)."""
     student = copy.deepcopy(teacher)
-    student.k_frac, student.top_p, student._full, student.dropout = float(k_frac), float(top_p), None, float(dropout)
+    student._full, student.dropout, student.window = None, float(dropout), window
+    if window is None:
+        student.k_frac, student.top_p = float(k_frac), float(top_p)
     for p in teacher.parameters():
         p.requires_grad_(False)
     return student
@@ -152,11 +209,13 @@ def velocity_distillation_loss(u_sparse: torch.Tensor, u_full: torch.Tensor, red
 
 
 def distill(student: torch.nn.Module, teacher: torch.nn.Module, batches: Iterable[Tuple[torch.Tensor, ...]],
-            lr: float = 1e-3, on_step: Optional[Callable[[int, float], None]] = None) -> Dict[str, list]:
+            lr: float = 1e-3, on_step: Optional[Callable[[int, float], None]] = None,
+            max_norm: Optional[float] = None) -> Dict[str, list]:
     """The loop of Alg. 2 over `batches` of (x_1, x_0, t): teacher and student see the same x_t, only the student
-    is updated.  What a batch holds behind these three (a context and its lengths) both get too.  Returns the loss per step."""
+    is updated.  What a batch holds behind these three (a context, its lengths, a condition) both get too.  max_norm: the gradients are
+    clipped to it before every update.  Returns the loss per step, and with max_norm the gradients' norm ("norm")."""
     opt = torch.optim.Adam([p for p in student.parameters() if p.requires_grad], lr=lr)
-    losses = []
+    losses, norms = [], []
     for step, (x1, x0, t, *more) in enumerate(batches):
         xt = noisy_latent(x1, x0, t)
         with torch.no_grad():
@@ -164,8 +223,10 @@ def distill(student: torch.nn.Module, teacher: torch.nn.Module, batches: Iterabl
         loss = velocity_distillation_loss(student(xt, *more), u_full)
         opt.zero_grad(set_to_none=True)
         loss.backward()
+        if max_norm is not None:
+            norms.append(clip_gradients([p.grad for p in student.parameters() if p.grad is not None], max_norm))
         opt.step()
         losses.append(float(loss.item()))
         if on_step is not None:
             on_step(step, losses[-1])
-    return {"loss": losses}
+    return {"loss": losses} if max_norm is None else {"loss": losses, "norm": [float(n) for n in norms]}
