@@ -42,31 +42,46 @@ struct WindowFewArgs : FewArgs {
   static constexpr bool WINDOW = true;
   Window win;
 };
+// A sample's keys, and the place of its first query.
+struct FewSeen { int keys, start; };
 template <class Args>
-__device__ __forceinline__ WindowSpan few_span(const Args& a, int b, int keys) {
-  const int start = a.win.starts ? window_clamp(a.win.starts[b]) : a.win.start;
-  return window_span(a.win, keys, start, start + a.win.nq - 1);
+__device__ __forceinline__ FewSeen few_seen(const Args& a, int b) {
+  FewSeen s = {cross_length(a.kv, b), 0};
+  if constexpr (Args::WINDOW) s.start = window_start(a.win, b);
+  return s;
 }
+template <class Args>
+__device__ __forceinline__ WindowSpan few_span(const Args& a, FewSeen s) { return window_span(a.win, s.keys, s.start, s.start + a.win.nq - 1); }
 
 constexpr int FEW_WAVES = 2;     // (two workgroups of 64 KB share a compute unit; of four waves and 128 KB one: 127 / 140 us)
 // Blocks of a sample in the line: one at least, so that every sample is somebody's.
 template <class Args>
-__device__ __forceinline__ int few_blocks(const Args& a, int b, int keys) {
-  if constexpr (Args::WINDOW) return max(few_span(a, b, keys).count(), 1);
-  else                        return max((keys + BKV - 1) / BKV, 1);
+__device__ __forceinline__ int few_blocks(const Args& a, FewSeen s) {
+  if constexpr (Args::WINDOW) return max(few_span(a, s).count(), 1);
+  else                        return max((s.keys + BKV - 1) / BKV, 1);
 }
 
 // The line: blocks of the samples lane, 64 + lane, ..., and how many a stretch has.
 constexpr int FEW_CHUNKS = FEW_SAMPLES / 64;
-struct FewLine { int n[FEW_CHUNKS], total, per; };
+struct FewLine {
+  int n[FEW_CHUNKS], keys[FEW_CHUNKS], start[FEW_CHUNKS], total, per;
+};
 template <class Args>
 __device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
   FewLine r;
   r.total = 0;
 #pragma unroll
   for (int c = 0; c < FEW_CHUNKS; ++c) {
-    const int b = 64 * c + lane;
-    r.n[c] = b < a.B ? few_blocks(a, b, a.kv.lengths ? min(max(a.kv.lengths[b], 0), a.kv.Nk) : a.kv.Nk) : 0;
+    r.n[c] = r.keys[c] = r.start[c] = 0;
+    if (64 * c < a.B) {
+      const int b = min(64 * c + lane, a.B - 1);         // (lengths and starts are requested together)
+      int keys = a.kv.Nk, start = 0;
+      if constexpr (Args::WINDOW) start = a.win.starts ? a.win.starts[b] : a.win.start;
+      if (a.kv.lengths) keys = a.kv.lengths[b];
+      r.keys[c] = min(max(keys, 0), a.kv.Nk);
+      if constexpr (Args::WINDOW) r.start[c] = window_clamp(start);
+      r.n[c] = 64 * c + lane < a.B ? few_blocks(a, FewSeen{r.keys[c], r.start[c]}) : 0;
+    }
   }
 #pragma unroll
   for (int c = 0; c < FEW_CHUNKS; ++c) r.total += r.n[c];
@@ -75,6 +90,16 @@ __device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
   r.total = __builtin_amdgcn_readfirstlane(r.total);
   r.per = max((r.total + a.workers - 1) / a.workers, FEW_LEAST);
   return r;
+}
+// What the line holds of sample b.
+__device__ __forceinline__ FewSeen few_seen(const FewLine& line, int b) {
+  int keys = line.keys[0], start = line.start[0];
+#pragma unroll
+  for (int c = 1; c < FEW_CHUNKS; ++c) {
+    keys = b >= 64 * c ? line.keys[c] : keys;
+    start = b >= 64 * c ? line.start[c] : start;
+  }
+  return FewSeen{__builtin_amdgcn_readlane(keys, b & 63), __builtin_amdgcn_readlane(start, b & 63)};
 }
 // First place of sample b.
 __device__ __forceinline__ int few_first(const FewLine& line, int b, int lane) {
@@ -127,10 +152,10 @@ __device__ __forceinline__ int64_t few_row(const FewArgs& a, int b, int hk, int 
   return b * a.sb + ((int64_t)hk * a.kv.group + r / a.Nq) * a.sh + (r % a.Nq) * a.sn;
 }
 template <class Args>
-__device__ __forceinline__ void few_finish(const Args& a, int b, int hk, int row, int c, f32x4 x, float m, float l) {
+__device__ __forceinline__ void few_finish(const Args& a, int b, FewSeen seen, int hk, int row, int c, f32x4 x, float m, float l) {
   float inv = 1.f / l;
   if constexpr (Args::WINDOW) {
-    if (window_blind(a.win, cross_length(a.kv, b), window_start(a.win, b) + row % a.win.nq)) inv = 0.f;
+    if (window_blind(a.win, seen.keys, seen.start + row % a.win.nq)) inv = 0.f;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] *= inv;
@@ -157,7 +182,7 @@ struct FewLds {
 
 // Keys [key0, key1) of sample b and key head hk; its result goes to a slot where others share the sample (slot >= 0).
 // (WINDOW: keys of the line of the sample's blocks, so many from its start)
-struct FewPiece { int b, hk, key0, key1, slot; };
+struct FewPiece { int b, hk, key0, key1, slot; FewSeen seen; };
 template <int D, class Args>
 __device__ __forceinline__ void few_piece(const Args& a, const FewPiece& pc, FewLds<D>& lds) {
   constexpr bool WINDOW = Args::WINDOW;
@@ -193,9 +218,9 @@ __device__ __forceinline__ void few_piece(const Args& a, const FewPiece& pc, Few
   WindowSpan span;
   int keys = 0, start = 0, last_seen = 0, near = 0;
   if constexpr (WINDOW) {
-    keys = cross_length(a.kv, b);
-    start = window_start(a.win, b);
-    span = window_span(a.win, keys, start, start + a.win.nq - 1);
+    keys = pc.seen.keys;
+    start = pc.seen.start;
+    span = few_span(a, pc.seen);
     const int p = start + min(r32, a.rows - 1) % a.win.nq;
     last_seen = min(p + a.win.right, keys - 1);
     near = p - a.win.left;
@@ -336,7 +361,7 @@ __device__ __forceinline__ void few_piece(const Args& a, const FewPiece& pc, Few
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(y[e], f, sum[e]);
     }
     if (pc.slot < 0) {
-      few_finish(a, b, hk, row, c, sum, m, l);
+      few_finish(a, b, pc.seen, hk, row, c, sum, m, l);
     } else {
       *(f32x4*)(slot + row * D + 4 * c) = sum;
       if (c == 0) *(f32x2*)(slot + a.rows * D + 2 * row) = f32x2{m, l};
@@ -346,20 +371,20 @@ __device__ __forceinline__ void few_piece(const Args& a, const FewPiece& pc, Few
 
 // keys of a sample's line
 template <class Args>
-__device__ __forceinline__ int few_keys(const Args& a, int b) {
-  const int keys = cross_length(a.kv, b);
+__device__ __forceinline__ int few_keys(const Args& a, FewSeen seen) {
   if constexpr (Args::WINDOW) {
-    const WindowSpan s = few_span(a, b, keys);
+    const WindowSpan s = few_span(a, seen);
     return s.count() ? (s.count() - 1) * BKV + min(BKV, s.hi - s.block(s.count() - 1) * BKV) : 0;
   }
-  return keys;
+  return seen.keys;
 }
 template <int D, class Args>
 __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(Args a) {
   __shared__ __align__(1024) FewLds<D> lds;
   if (a.workers == 0) {
-    const int b = blockIdx.x / a.Hk, keys = few_keys(a, b);
-    few_piece<D>(a, FewPiece{b, (int)blockIdx.x % a.Hk, 0, keys, -1}, lds);
+    const int b = blockIdx.x / a.Hk;
+    const FewSeen seen = few_seen(a, b);
+    few_piece<D>(a, FewPiece{b, (int)blockIdx.x % a.Hk, 0, few_keys(a, seen), -1, seen}, lds);
     return;
   }
   const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk, lane = threadIdx.x & 63;
@@ -369,9 +394,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(Args a) {
   const FewSample start = few_sample(a, line, begin, lane);
   int first = start.first;                               // of sample b
   for (int b = start.b, at = begin; at < stop; ++b) {
-    const int keys = few_keys(a, b), n = few_blocks(a, b, cross_length(a.kv, b)), end = min(first + n, stop);
+    const FewSeen seen = few_seen(line, b);
+    const int keys = few_keys(a, seen), n = few_blocks(a, seen), end = min(first + n, stop);
     const FewParts s = few_parts(first, n, line.per);
-    const FewPiece pc = {b, hk, (at - first) * BKV, min(keys, (end - first) * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, i - s.i0)};
+    const FewPiece pc = {b, hk, (at - first) * BKV, min(keys, (end - first) * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, i - s.i0), seen};
     few_piece<D>(a, pc, lds);
     __syncthreads();                                     // (the next piece's tiles land where this one's results were)
     first += n;
@@ -389,7 +415,8 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(Args a) {
   const int row = blockIdx.x % a.rows, unit = blockIdx.x / a.rows, b = unit / a.Hk, hk = unit % a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % QUADS, g = tid / QUADS;
   const FewLine line = few_line(a, lane);
-  const FewParts s = few_parts(few_first(line, b, lane), few_blocks(a, b, cross_length(a.kv, b)), line.per);
+  const FewSeen seen = few_seen(line, b);
+  const FewParts s = few_parts(few_first(line, b, lane), few_blocks(a, seen), line.per);
   if (s.parts == 1) return;
   float m = -INFINITY, l = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -428,7 +455,7 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(Args a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] = fmaf(x[e], f, sum[e]);
   }
-  few_finish(a, b, hk, row, c, sum, m, l);
+  few_finish(a, b, seen, hk, row, c, sum, m, l);
 }
 
 template <class Args>
