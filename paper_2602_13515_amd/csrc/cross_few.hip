@@ -61,80 +61,77 @@ __device__ __forceinline__ int few_blocks(const Args& a, FewSeen s) {
   else                        return max((s.keys + BKV - 1) / BKV, 1);
 }
 
-// The line: blocks of the samples lane, 64 + lane, ..., and how many a stretch has.
-constexpr int FEW_CHUNKS = FEW_SAMPLES / 64;
-struct FewLine {
-  int n[FEW_CHUNKS], keys[FEW_CHUNKS], start[FEW_CHUNKS], total, per;
-};
+// Sum over the lanes of a wave.
+__device__ __forceinline__ int few_sum(int x) {
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) x += __shfl_xor(x, s, 64);
+  return __builtin_amdgcn_readfirstlane(x);
+}
+// The line, 64 samples at a time: a lane holds sample 64 c + lane's blocks (0 past the last), keys and place.  Blocks in all, blocks
+// of a stretch.
+struct FewLine { int c, n, keys, start, total, per; };
+template <class Args>
+__device__ __forceinline__ void few_chunk(const Args& a, FewLine& line, int c, int lane) {
+  const int b = min(64 * c + lane, a.B - 1);             // (lengths and starts are requested together)
+  int keys = a.kv.Nk, start = 0;
+  if constexpr (Args::WINDOW) start = a.win.starts ? a.win.starts[b] : a.win.start;
+  if (a.kv.lengths) keys = a.kv.lengths[b];
+  line.c = c;
+  line.keys = min(max(keys, 0), a.kv.Nk);
+  line.start = 0;
+  if constexpr (Args::WINDOW) line.start = window_clamp(start);
+  line.n = 64 * c + lane < a.B ? few_blocks(a, FewSeen{line.keys, line.start}) : 0;
+}
 template <class Args>
 __device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
   FewLine r;
-  r.total = 0;
-#pragma unroll
-  for (int c = 0; c < FEW_CHUNKS; ++c) {
-    r.n[c] = r.keys[c] = r.start[c] = 0;
-    if (64 * c < a.B) {
-      const int b = min(64 * c + lane, a.B - 1);         // (lengths and starts are requested together)
-      int keys = a.kv.Nk, start = 0;
-      if constexpr (Args::WINDOW) start = a.win.starts ? a.win.starts[b] : a.win.start;
-      if (a.kv.lengths) keys = a.kv.lengths[b];
-      r.keys[c] = min(max(keys, 0), a.kv.Nk);
-      if constexpr (Args::WINDOW) r.start[c] = window_clamp(start);
-      r.n[c] = 64 * c + lane < a.B ? few_blocks(a, FewSeen{r.keys[c], r.start[c]}) : 0;
-    }
+  int n = 0;
+  for (int c = (a.B - 1) / 64; c >= 0; --c) {
+    few_chunk(a, r, c, lane);
+    n += r.n;
   }
-#pragma unroll
-  for (int c = 0; c < FEW_CHUNKS; ++c) r.total += r.n[c];
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) r.total += __shfl_xor(r.total, s, 64);
-  r.total = __builtin_amdgcn_readfirstlane(r.total);
+  r.total = few_sum(n);
   r.per = max((r.total + a.workers - 1) / a.workers, FEW_LEAST);
   return r;
 }
 // What the line holds of sample b.
-__device__ __forceinline__ FewSeen few_seen(const FewLine& line, int b) {
-  int keys = line.keys[0], start = line.start[0];
-#pragma unroll
-  for (int c = 1; c < FEW_CHUNKS; ++c) {
-    keys = b >= 64 * c ? line.keys[c] : keys;
-    start = b >= 64 * c ? line.start[c] : start;
-  }
-  return FewSeen{__builtin_amdgcn_readlane(keys, b & 63), __builtin_amdgcn_readlane(start, b & 63)};
+template <class Args>
+__device__ __forceinline__ FewSeen few_seen(const Args& a, FewLine& line, int b, int lane) {
+  if (b / 64 != line.c) few_chunk(a, line, b / 64, lane);
+  return FewSeen{__builtin_amdgcn_readlane(line.keys, b & 63), __builtin_amdgcn_readlane(line.start, b & 63)};
 }
 // First place of sample b.
-__device__ __forceinline__ int few_first(const FewLine& line, int b, int lane) {
+template <class Args>
+__device__ __forceinline__ int few_first(const Args& a, FewLine& line, int b, int lane) {
   int before = 0;
-#pragma unroll
-  for (int c = 0; c < FEW_CHUNKS; ++c) before += 64 * c + lane < b ? line.n[c] : 0;
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) before += __shfl_xor(before, s, 64);
-  return __builtin_amdgcn_readfirstlane(before);
+  for (int c = 0; 64 * c < b; ++c) {
+    if (c != line.c) few_chunk(a, line, c, lane);
+    before += 64 * c + lane < b ? line.n : 0;
+  }
+  return few_sum(before);
 }
-// The sample that place `at` (inside the line) belongs to, and that sample's first place.
+// The sample that place `place` (inside the line) belongs to, and that sample's first place.
 struct FewSample { int b, first; };
-__device__ __forceinline__ FewSample few_sample(const FewArgs& a, const FewLine& line, int place, int lane) {
-  FewSample r = {0, 0};
+template <class Args>
+__device__ __forceinline__ FewSample few_sample(const Args& a, FewLine& line, int place, int lane) {
   int run = 0;
-#pragma unroll
-  for (int c = 0; c < FEW_CHUNKS; ++c) {
-    if (64 * c >= a.B) break;
-    int sum = line.n[c];                                 // of this sample and those before it
+  for (int c = 0; 64 * c < a.B; ++c) {
+    if (c != line.c) few_chunk(a, line, c, lane);
+    int sum = line.n;                                    // of this sample and those before it
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
       const int x = __shfl_up(sum, s, 64);
       sum += lane >= s ? x : 0;
     }
-    const int at = run + sum - line.n[c];
-    const uint64_t here = __builtin_amdgcn_ballot_w64(line.n[c] > 0 && at <= place && place < at + line.n[c]);
+    const int at = run + sum - line.n;
+    const uint64_t here = __builtin_amdgcn_ballot_w64(line.n > 0 && at <= place && place < at + line.n);
     if (here) {
       const int l = __builtin_ctzll(here);
-      r.b = 64 * c + l;
-      r.first = __shfl(at, l, 64);
+      return FewSample{64 * c + l, __builtin_amdgcn_readlane(at, l)};
     }
-    run += __shfl(sum, 63, 64);
+    run += __builtin_amdgcn_readlane(sum, 63);
   }
-  r.b = __builtin_amdgcn_readfirstlane(r.b); r.first = __builtin_amdgcn_readfirstlane(r.first);
-  return r;
+  return FewSample{0, 0};
 }
 // Stretches that a sample lies in, and where part p of its result lies: a stretch has two slots, for the sample that it begins
 // inside of or with and for the one that it ends inside of.
@@ -388,13 +385,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(Args a) {
     return;
   }
   const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk, lane = threadIdx.x & 63;
-  const FewLine line = few_line(a, lane);
+  FewLine line = few_line(a, lane);
   const int begin = i * line.per, stop = min(begin + line.per, line.total);
   if (begin >= stop) return;
   const FewSample start = few_sample(a, line, begin, lane);
   int first = start.first;                               // of sample b
   for (int b = start.b, at = begin; at < stop; ++b) {
-    const FewSeen seen = few_seen(line, b);
+    const FewSeen seen = few_seen(a, line, b, lane);
     const int keys = few_keys(a, seen), n = few_blocks(a, seen), end = min(first + n, stop);
     const FewParts s = few_parts(first, n, line.per);
     const FewPiece pc = {b, hk, (at - first) * BKV, min(keys, (end - first) * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, i - s.i0), seen};
@@ -414,9 +411,10 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(Args a) {
   __shared__ float stat[G][2];
   const int row = blockIdx.x % a.rows, unit = blockIdx.x / a.rows, b = unit / a.Hk, hk = unit % a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % QUADS, g = tid / QUADS;
-  const FewLine line = few_line(a, lane);
-  const FewSeen seen = few_seen(line, b);
-  const FewParts s = few_parts(few_first(line, b, lane), few_blocks(a, seen), line.per);
+  FewLine line = few_line(a, lane);
+  const int first = few_first(a, line, b, lane);
+  const FewSeen seen = few_seen(a, line, b, lane);
+  const FewParts s = few_parts(first, few_blocks(a, seen), line.per);
   if (s.parts == 1) return;
   float m = -INFINITY, l = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
