@@ -92,15 +92,15 @@ constexpr int FEW_ROWS = 32;
 inline bool cross_few(const CrossDims& m) { return (int64_t)m.group * m.q.N <= FEW_ROWS; }
 // The kernel for few rows: workgroups of a key head that share the line of its key blocks (cross_few.hip), or 0; a part's result:
 // [row][D] unnormalised sums, then (maximum in log2 units, sum) of each row.
-constexpr int FEW_LEAST = 8;            // key blocks that a stretch of the line has at least
+constexpr int FEW_LEAST = 8;            // key blocks that a stretch of the line has at least (without a window)
 constexpr int FEW_SAMPLES = 1024;       // samples that a line may have
 inline size_t few_slot_bytes(int rows, int d) { return ((size_t)rows * (d + 2) * 4 + 15) & ~(size_t)15; }
-struct CrossFewWs { int workers; size_t total; };
-inline CrossFewWs cross_few_ws(const CrossDims& m) {
-  CrossFewWs w = {0, 0};
+struct CrossFewWs { int workers, least; size_t total; };
+inline CrossFewWs cross_few_ws(const CrossDims& m, int least = FEW_LEAST) {
+  CrossFewWs w = {0, least, 0};
   const int64_t units = (int64_t)m.q.B * m.Hk, resident = 512 * 128 / m.q.d;        // (workgroups that run at a time)
-  if (m.q.B > FEW_SAMPLES || units >= 2 * resident || m.q.Tn < 2 * FEW_LEAST) return w;
-  const int64_t most = ((int64_t)m.q.B * m.q.Tn + FEW_LEAST - 1) / FEW_LEAST, want = (resident + m.Hk - 1) / m.Hk;
+  if (m.q.B > FEW_SAMPLES || units >= 2 * resident || m.q.Tn < 2 * least) return w;
+  const int64_t most = ((int64_t)m.q.B * m.q.Tn + least - 1) / least, want = (resident + m.Hk - 1) / m.Hk;
   w.workers = (int)(want < most ? want : most);
   // (one stretch a head: nothing is shared)
   if (w.workers > 1) w.total = round256((size_t)2 * w.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d));

@@ -32,7 +32,7 @@ struct FewArgs {
   uint16_t* o; uint16_t* o_res; float* lse;
   CrossKeys kv;
   int B, Hk, Nq, rows;           // rows = group * Nq
-  int workers;                   // workgroups of a key head that share the line of key blocks; 0: one a (sample, key head)
+  int workers, least;            // workgroups of a key head that share the line of key blocks, 0: one a (sample, key head); blocks of a stretch
   int64_t sb, sh, sn;
   float scale_log2;
   float* pool; int slot_floats;  // partial results (few_slot)
@@ -91,7 +91,7 @@ __device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
     n += r.n;
   }
   r.total = few_sum(n);
-  r.per = max((r.total + a.workers - 1) / a.workers, FEW_LEAST);
+  r.per = max((r.total + a.workers - 1) / a.workers, a.least);
   return r;
 }
 // What the line holds of sample b.
@@ -458,14 +458,14 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(Args a) {
 
 template <class Args>
 static hipError_t launch_few(Args& a, const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
-                             void* o, void* o_res, float* lse, int workers, void* ws, hipStream_t stream) {
+                             void* o, void* o_res, float* lse, const CrossFewWs& share, void* ws, hipStream_t stream) {
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
   a.o = (uint16_t*)o; a.o_res = (uint16_t*)o_res; a.lse = lse;
   a.kv = cross_keys(m, lengths);
   a.B = m.q.B; a.Hk = m.Hk; a.Nq = m.q.N; a.rows = m.group * m.q.N;
   a.sb = m.q.sb; a.sh = m.q.sh; a.sn = m.q.sn;
   a.scale_log2 = scale * LOG2E;
-  a.workers = workers;
+  a.workers = share.workers; a.least = share.least;
   a.pool = (float*)ws;
   a.slot_floats = (int)(few_slot_bytes(a.rows, m.q.d) / 4);
   const dim3 grid((unsigned)((a.workers ? a.workers : m.q.B) * m.Hk)), block(64 * FEW_WAVES);
@@ -482,13 +482,13 @@ static hipError_t launch_few(Args& a, const void* q, const void* k, const void* 
 hipError_t launch_cross_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, float scale,
                             void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
   FewArgs a = {};
-  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, cross_few_ws(m).workers, ws, stream);
+  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, cross_few_ws(m), ws, stream);
 }
 hipError_t launch_window_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,
                              float scale, void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
   WindowFewArgs a = {};
   a.win = win;
-  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, window_few_ws(m, win).workers, ws, stream);
+  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, window_few_ws(m, win), ws, stream);
 }
 
 }  // namespace spa2

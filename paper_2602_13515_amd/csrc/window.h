@@ -177,12 +177,22 @@ inline WindowBwdWs window_bwd_ws(const CrossDims& m, const Window& w) {
   s.total = s.dq_at + s.dq.pool;
   return s;
 }
-// The kernel for few rows: as cross_few_ws, with the blocks that a sample's queries see at most.
+// The kernel for few rows: as cross_few_ws, with the blocks that a sample's queries see at most.  Windows of up to 256 blocks differ less
+// in length than whole caches do and seldom fill the card: stretches are shorter, and a workgroup takes a (sample, key head) by itself
+// where there are more than 256 of those, or few blocks.  us, one query:
+//   a stretch of 8 / 4 / 2 blocks at least: 4096 keys, one sample, 8 heads 25.3 / 19.9 / 18.6, d = 64 19.3 / 16.5 / 15.1; 1024 keys, 8
+//   samples, 8 heads 29.9 / 23.4 / 19.4; 512 keys, one head 20.5 / 18.7 / 15.7; of more blocks the join takes longer than that saves: 32,768
+//   keys, 2 heads 28.5 / 26.6 / 27.1, d = 64 21.0 / 19.5 / 21.4;
+//   shared / by themselves: 2000 keys, 128 pairs 35.4 / 49.6, 256 52.6 / 55.7, 512 103 / 96, 1000 216 / 181, d = 64 26.4 / 38.2, 36.8 / 39.0,
+//   57.9 / 50.9, 135 / 93; 512 keys 21.9 / 22.6, 24.8 / 24.0, 36 / 29, 94 / 55, d = 64 15.9 / 16.6, 20.7 / 18.2, 25.2 / 21.9, 67 / 27.
 inline CrossFewWs window_few_ws(const CrossDims& m, const Window& w) {
   CrossDims seen = m;
   const int64_t near = ((int64_t)w.left + w.right + w.nq - 1 + BKV - 1) / BKV + 1 + (w.sinks + BKV - 1) / BKV;
   if (near < seen.q.Tn) seen.q.Tn = (int)near;
-  return cross_few_ws(seen);
+  if (seen.q.Tn > 256) return cross_few_ws(seen, 4);
+  const int64_t units = (int64_t)m.q.B * m.Hk;
+  if (units > 256 || seen.q.Tn < 8 || 16 * (int64_t)seen.q.Tn < units) return CrossFewWs{0, 0, 0};
+  return cross_few_ws(seen, 2);
 }
 
 hipError_t launch_window_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,

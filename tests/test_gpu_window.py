@@ -128,6 +128,24 @@ def test_long_caches_are_shared_out(Nq, B, left, sinks):
     _check(q, k, v, do, left, 0, sinks)
 
 
+@pytest.mark.parametrize("B,Nk", [(63, 1100), (64, 1100), (65, 1100), (130, 1100), (256, 1100), (500, 1100), (1024, 1100), (70, 17000)])
+def test_many_samples_share_a_line(B, Nk):
+    """One query of many samples of unlike length and place, empty ones among them: stretches that begin and end inside samples."""
+    g = torch.Generator().manual_seed(B)
+    lengths = torch.randint(0, 1100, (B,), generator=g)
+    lengths[::7] = 0
+    lengths[B // 2] = Nk
+    starts = (lengths - 1 - torch.randint(0, 90, (B,), generator=g)).tolist()
+    q, k, v, do = _inputs(B, 3, 1, 1, Nk, 64)
+    for left, right, sinks in ((300, 0, 5), (None, 100, 0), (40, 40, 0)):
+        _check(q, k, v, do, left, right, sinks, lengths=lengths.tolist(), starts=starts, whole=False)
+    want, _ = ref.window(f64(q), f64(k), f64(v), lengths.tolist(), None, None, None, 0, 64 ** -0.5, f64(do))
+    value, bound = want["o"]
+    with torch.no_grad():
+        o = spa2.cross_attention(q, k, v, _i32(lengths.tolist()))
+    assert (np.abs(f64(o) - value) <= bound + 1e-30).all()
+
+
 def test_columns_of_first_keys_are_shared_out():
     """Long columns of first keys among short ones, one head: parts, joined by the last to arrive; and columns that are all long."""
     for d in (64, 128):
