@@ -392,7 +392,7 @@ int spa2_window_bwd(const void* q, const void* k, const void* v, const int32_t* 
  *               gate, scale, shift with an element stride between samples (gate_sb, ..., 0: one for all of them).
  *   stats       fp32 [3][samples * tokens] (written), what the backward pass needs besides y; or NULL.
  * All addresses are multiples of their elements' size; rows may start anywhere (width is any number from
- * SPA2_GATE_MIN_WIDTH to SPA2_GATE_MAX_WIDTH).
+ * SPA2_GATE_MIN_WIDTH to SPA2_GATE_MAX_WIDTH).  Up to 2^22 samples, and of more than 7680 channels less than that.
  * spa2_gate_norm_bwd: dy (x_dtype) and dn (out_dtype) are the upstream gradients of y and n (dy may be NULL: zero; dn is only
  * read with a norm), y and stats those of the forward call (without a branch y is x).  dx and dbranch have x's and the branch's type
  * and may be NULL (not wanted); so may the members of grads, which have the parameters' shapes and type.  Sums over tokens are

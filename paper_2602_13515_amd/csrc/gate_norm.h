@@ -24,6 +24,7 @@ struct GateArgs {
   void* y; void* n; float* stats;                      // stats: [3][rows] mean and 1 / deviation of y, 1 / size of the branch
   void* dx; void* dbranch; float* part;                // part: [workgroup][3][width] sums over its rows
   spa2_gate_params p;
+  spa2_gate_grads own;                                 // (backward: gradients of the parameters of each sample's own, by its only workgroup)
   int64_t gate_sb, scale_sb, shift_sb;
   int64_t tokens, rows;                                // of a sample, of all
   int width, per_sample, kind;                         // workgroups of a sample
@@ -31,8 +32,7 @@ struct GateArgs {
   float eps;
 };
 
-int gate_threads(int width);
-GateArgs gate_args(const spa2_gate_shape& s, const spa2_gate_params& p, float eps, bool backward);
+GateArgs gate_args(const void* branch, const spa2_gate_shape& s, const spa2_gate_params& p, float eps, bool backward);
 // Whether the call's tensors are larger than the memory-side cache, so that next to nothing of them would be there when they are read
 // next.  Measured, us, forward and backward, the same tensors every time, through the cache / past it: 5000 x 768, bf16 (8 MB a
 // tensor) 56 / 88; 20,010 x 384, fp32 (31 MB) 104 / 126; 32,760 x 1536, fp32 and bf16 (201 and 101 MB) 291 / 300; 16,000 x 5120, bf16

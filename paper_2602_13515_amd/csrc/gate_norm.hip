@@ -131,7 +131,6 @@ __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_kernel(GateArgs a) 
 // 1 281, 1 and 1 311; with the branch normed, all fp32 (12 and 25 KB) 2 and 1 584, 3 and 2 447, 5 and 3 404; 75,600 x 5120, bf16 (20
 // and 40 KB) 2 and 1 1488, 1 and 1 1458.
 constexpr int GATE_AHEAD = 20 << 10, GATE_WAVES_CU = 16, CUS = 256;
-int gate_threads(int width) { return 64 * ((width + 511) / 512); }
 int gate_per_sample(const spa2_gate_shape& s, bool backward) {
   auto size = [](int32_t t) { return t == SPA2_DTYPE_F32 ? 4 : 2; };
   const int bytes = s.width * (backward ? 2 * size(s.x_dtype) + size(s.branch_dtype) + size(s.out_dtype) : size(s.x_dtype) + size(s.branch_dtype));
@@ -141,12 +140,13 @@ int gate_per_sample(const spa2_gate_shape& s, bool backward) {
   return (int)(per < s.tokens ? per : s.tokens);
 }
 
-GateArgs gate_args(const spa2_gate_shape& s, const spa2_gate_params& p, float eps, bool backward) {
+GateArgs gate_args(const void* branch, const spa2_gate_shape& s, const spa2_gate_params& p, float eps, bool backward) {
   GateArgs a = {};
+  a.branch = branch;
   a.p = p;
   a.gate_sb = s.gate_sb; a.scale_sb = s.scale_sb; a.shift_sb = s.shift_sb;
   a.tokens = s.tokens; a.rows = s.samples * s.tokens;
-  a.width = s.width; a.kind = s.kind; a.params32 = s.param_dtype == SPA2_DTYPE_F32; a.post = s.post != 0;
+  a.width = s.width; a.kind = s.kind; a.params32 = s.param_dtype == SPA2_DTYPE_F32; a.post = branch && s.post;
   a.eps = eps;
   a.per_sample = gate_per_sample(s, backward);
   return a;
@@ -163,8 +163,8 @@ static void launch_types(const GateArgs& a, const dim3& grid, const dim3& block,
 
 hipError_t launch_gate_norm(const void* x, const void* branch, const spa2_gate_params& p, const spa2_gate_shape& s, float eps,
                             void* y, void* n, float* stats, hipStream_t stream) {
-  GateArgs a = gate_args(s, p, eps, false);
-  a.x = x; a.branch = branch; a.y = y; a.n = n; a.stats = stats;
+  GateArgs a = gate_args(branch, s, p, eps, false);
+  a.x = x; a.y = y; a.n = n; a.stats = stats;
   const dim3 grid((unsigned)(a.per_sample * s.samples)), block((unsigned)gate_threads(s.width));
   const bool x32 = s.x_dtype == SPA2_DTYPE_F32, b32 = s.branch_dtype == SPA2_DTYPE_F32, n32 = s.out_dtype == SPA2_DTYPE_F32;
   if (!x32)             launch_types<uint16_t, uint16_t, uint16_t>(a, grid, block, stream);

@@ -8,11 +8,24 @@
 //
 // h and u are made again from y and the branch and the statistics that the forward pass leaves.  A workgroup takes rows of one
 // sample and keeps the three sums of its channels in registers; they are joined by a launch behind, in fp64 and a fixed order, and
-// those of all samples by another one where a parameter is shared and there are several.
+// those of all samples by another one where a parameter is shared and there are several.  Where a sample has one workgroup alone (a
+// modulation for every token, say) that one writes the gradients of the sample's own parameters itself.
 // Bound: HBM.
 #include "gate_norm.h"
 
 namespace spa2 {
+
+// Gradients of parameters from element `at` on, if they are wanted.
+__device__ __forceinline__ void grad_put(void* p, bool fp32, int64_t at, double x) {
+  if (!p) return;
+  if (fp32) ((float*)p)[at] = (float)x;
+  else      ((uint16_t*)p)[at] = (uint16_t)pack_bf16((float)x, 0.f);
+}
+__device__ __forceinline__ void grad_put(void* p, bool fp32, int64_t at, const float (&x)[8]) {
+  if (!p) return;
+  if (fp32) gate_store((float*)p + at, x);
+  else      gate_store((uint16_t*)p + at, x);
+}
 
 template <typename X, typename B, typename N, bool ODD, bool PAST>
 __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_bwd_kernel(GateArgs a) {
@@ -107,7 +120,26 @@ __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_bwd_kernel(GateArgs
     }
     if (a.dbranch && l.there) gate_store<PAST>((B*)a.dbranch + base, d);
   }
-  if (!a.part || !l.there) return;
+  if (!l.there) return;
+  if (a.own.gate || a.own.scale || a.own.shift) {
+    const bool f = a.params32;
+    GateParam raw[3];
+    gate_param_fetch(a.p.branch_weight, f, l.at, true, raw[0]);
+    gate_param_fetch(a.p.weight, f, l.at, true, raw[1]);
+    gate_param_fetch(a.p.bias, f, l.at, true, raw[2]);
+    float x[8], z[8];
+    gate_param(a.p.branch_weight, f, raw[0], 1.f, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= sg[e];
+    grad_put(a.own.gate, f, b * a.gate_sb + l.at, x);
+    gate_param(a.p.weight, f, raw[1], 1.f, x);
+    gate_param(a.p.bias, f, raw[2], 0.f, z);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], s1[e], z[e] * s2[e]);
+    grad_put(a.own.scale, f, b * a.scale_sb + l.at, x);
+    grad_put(a.own.shift, f, b * a.shift_sb + l.at, s2);
+  }
+  if (!a.part) return;
   float* part = a.part + (int64_t)blockIdx.x * 3 * a.width + l.at;
   if (normed) {
     gate_store(part, s1);
@@ -123,32 +155,31 @@ struct GateSums {
   spa2_gate_grads d;
   int64_t gate_sb, scale_sb, shift_sb;
   int samples, per_sample, width, columns;               // columns: workgroups that share a sample's channels
+  int stretches;                         // of the samples, in gate_shared_kernel
+  double* joined;                        // [stretch][6][width], if there are several
   bool params32, normed, branch;
 };
 constexpr int SUM_CHANNELS = 32, SUM_GROUPS = 32;      // of a workgroup: channels, groups of the summands
-constexpr int SUM_WAVES = 16, SUM_LANES = SUM_CHANNELS / 4;        // (gate_sums_kernel: a thread has four channels)
-
-__device__ __forceinline__ void grad_put(const GateSums& a, void* p, int64_t at, double x) {
-  if (!p) return;
-  if (a.params32) ((float*)p)[at] = (float)x;
-  else            ((uint16_t*)p)[at] = (uint16_t)pack_bf16((float)x, 0.f);
-}
+constexpr int SUM_WAVES = 16, SUM_LANES = SUM_CHANNELS / 4;        // (gate_sums_kernel: waves at most; a thread has four channels)
+constexpr int SUM_STRETCH = 256, SUM_STRETCHES = 64;   // of gate_shared_kernel: samples at least, stretches at most
 
 // Sums of a sample's workgroups; parameters of its own.  With one sample all gradients are written here, with several the sums
-// take the place of the first workgroup's.  A thread adds up four channels of every 128th workgroup, requested four at a time: the
-// kernel is as long as its loads' round trips.  (One channel a thread, 1280 workgroups of 1536 channels: 49 us.)
+// take the place of the first workgroup's.  A thread adds up four channels of every (8 waves)-th workgroup, requested four at a time:
+// the kernel is as long as its loads' round trips.  (One channel a thread, 1280 workgroups of 1536 channels: 49 us, this way 8.)  So
+// many waves as have a request each: of 3 workgroups of 512 samples 16 took 350 us.
 __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
   __shared__ double lds[SUM_WAVES][3][SUM_CHANNELS];
-  const int t = threadIdx.x, b = blockIdx.x / a.columns, c0 = blockIdx.x % a.columns * SUM_CHANNELS;
+  const int t = threadIdx.x, waves = blockDim.x / 64, groups = waves * (64 / SUM_LANES);
+  const int b = blockIdx.x / a.columns, c0 = blockIdx.x % a.columns * SUM_CHANNELS;
   // (the last channels are taken by whole vectors, too: those in front of c0 are another workgroup's and not written)
   auto first = [&](int lane) -> int { return min(c0 + 4 * lane, a.width - 4); };
   const float* part = a.part + (int64_t)b * a.per_sample * 3 * a.width;
   double s[3][4] = {};
-  for (int p = t / SUM_LANES; p < a.per_sample; p += 4 * 64 * SUM_WAVES / SUM_LANES) {
+  for (int p = t / SUM_LANES; p < a.per_sample; p += 4 * groups) {
     f32x4 x[4][3];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float* q = part + (int64_t)min(p + u * (64 * SUM_WAVES / SUM_LANES), a.per_sample - 1) * 3 * a.width + first(t % SUM_LANES);
+      const float* q = part + (int64_t)min(p + u * groups, a.per_sample - 1) * 3 * a.width + first(t % SUM_LANES);
 #pragma unroll
       for (int i = 0; i < 3; ++i) {
         x[u][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -157,7 +188,7 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (p + u * (64 * SUM_WAVES / SUM_LANES) < a.per_sample)
+      if (p + u * groups < a.per_sample)
 #pragma unroll
         for (int i = 0; i < 3; ++i)
 #pragma unroll
@@ -179,20 +210,20 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
   if (t >= SUM_CHANNELS || c < c0 + t / 4 * 4) return;
   double sum[3] = {0.0, 0.0, 0.0};
 #pragma unroll 4
-  for (int k = 0; k < SUM_WAVES; ++k)
+  for (int k = 0; k < waves; ++k)
 #pragma unroll
     for (int i = 0; i < 3; ++i) sum[i] += lds[k][i][t];
   const double weight = gate_one(a.p.weight, a.params32, c, 1.f), bias = gate_one(a.p.bias, a.params32, c, 0.f);
   const double post = gate_one(a.p.branch_weight, a.params32, c, 1.f), gate = gate_one(a.p.gate, a.params32, b * a.gate_sb + c, 1.f);
   const double scale = 1.0 + gate_one(a.p.scale, a.params32, b * a.scale_sb + c, 0.f);
   const bool one = a.samples == 1;
-  if (one || a.gate_sb) grad_put(a, a.d.gate, b * a.gate_sb + c, post * sum[2]);
-  if (one || a.scale_sb) grad_put(a, a.d.scale, b * a.scale_sb + c, weight * sum[0] + bias * sum[1]);
-  if (one || a.shift_sb) grad_put(a, a.d.shift, b * a.shift_sb + c, sum[1]);
+  if (one || a.gate_sb) grad_put(a.d.gate, a.params32, b * a.gate_sb + c, post * sum[2]);
+  if (one || a.scale_sb) grad_put(a.d.scale, a.params32, b * a.scale_sb + c, weight * sum[0] + bias * sum[1]);
+  if (one || a.shift_sb) grad_put(a.d.shift, a.params32, b * a.shift_sb + c, sum[1]);
   if (one) {
-    grad_put(a, a.d.weight, c, scale * sum[0]);
-    grad_put(a, a.d.bias, c, scale * sum[1]);
-    grad_put(a, a.d.branch_weight, c, gate * sum[2]);
+    grad_put(a.d.weight, a.params32, c, scale * sum[0]);
+    grad_put(a.d.bias, a.params32, c, scale * sum[1]);
+    grad_put(a.d.branch_weight, a.params32, c, gate * sum[2]);
     return;
   }
   float* joined = a.part + (int64_t)b * a.per_sample * 3 * a.width + c;
@@ -201,16 +232,27 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
   joined[2 * (int64_t)a.width] = (float)sum[2];
 }
 
-// Gradients of what all samples share: sums over the samples.
+// Gradients of what all samples share, channel c: s, sums over the samples.
+__device__ __forceinline__ void shared_put(const GateSums& a, int c, const double (&s)[6]) {
+  grad_put(a.d.weight, a.params32, c, s[0]);
+  grad_put(a.d.bias, a.params32, c, s[1]);
+  grad_put(a.d.branch_weight, a.params32, c, s[2]);
+  if (!a.gate_sb) grad_put(a.d.gate, a.params32, c, s[3]);
+  if (!a.scale_sb) grad_put(a.d.scale, a.params32, c, s[4]);
+  if (!a.shift_sb) grad_put(a.d.shift, a.params32, c, s[5]);
+}
+// These sums, over a stretch of the samples; several stretches are joined by a launch behind.
 __global__ __launch_bounds__(SUM_CHANNELS * SUM_GROUPS) void gate_shared_kernel(GateSums a) {
   __shared__ double lds[6][SUM_GROUPS][SUM_CHANNELS];
-  const int lane = threadIdx.x % SUM_CHANNELS, g = threadIdx.x / SUM_CHANNELS, c = blockIdx.x * SUM_CHANNELS + lane;
+  const int lane = threadIdx.x % SUM_CHANNELS, g = threadIdx.x / SUM_CHANNELS, c = blockIdx.x % a.columns * SUM_CHANNELS + lane;
+  const int stretch = blockIdx.x / a.columns, each = (a.samples + a.stretches - 1) / a.stretches;
+  const int64_t b1 = min((int64_t)(stretch + 1) * each, (int64_t)a.samples);
   double s[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
   if (c < a.width) {
     const double weight = gate_one(a.p.weight, a.params32, c, 1.f), bias = gate_one(a.p.bias, a.params32, c, 0.f);
     const double post = gate_one(a.p.branch_weight, a.params32, c, 1.f);
 #pragma unroll 1
-    for (int64_t b = g; b < a.samples; b += SUM_GROUPS) {
+    for (int64_t b = (int64_t)stretch * each + g; b < b1; b += SUM_GROUPS) {
       const float* q = a.part + b * a.per_sample * 3 * a.width + c;
       const double gate = gate_one(a.p.gate, a.params32, b * a.gate_sb + c, 1.f);
       const double scale = 1.0 + gate_one(a.p.scale, a.params32, b * a.scale_sb + c, 0.f);
@@ -233,12 +275,19 @@ __global__ __launch_bounds__(SUM_CHANNELS * SUM_GROUPS) void gate_shared_kernel(
 #pragma unroll 4
     for (int k = 0; k < SUM_GROUPS; ++k) s[i] += lds[i][k][lane];
   }
-  grad_put(a, a.d.weight, c, s[0]);
-  grad_put(a, a.d.bias, c, s[1]);
-  grad_put(a, a.d.branch_weight, c, s[2]);
-  if (!a.gate_sb) grad_put(a, a.d.gate, c, s[3]);
-  if (!a.scale_sb) grad_put(a, a.d.scale, c, s[4]);
-  if (!a.shift_sb) grad_put(a, a.d.shift, c, s[5]);
+  if (a.stretches == 1) { shared_put(a, c, s); return; }
+#pragma unroll
+  for (int i = 0; i < 6; ++i) a.joined[((int64_t)stretch * 6 + i) * a.width + c] = s[i];
+}
+__global__ __launch_bounds__(64) void gate_joined_kernel(GateSums a) {
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  if (c >= a.width) return;
+  double s[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (int k = 0; k < a.stretches; ++k)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) s[i] += a.joined[((int64_t)k * 6 + i) * a.width + c];
+  shared_put(a, c, s);
 }
 
 template <typename X, typename B, typename N>
@@ -250,17 +299,34 @@ static void launch_types(const GateArgs& a, const dim3& grid, const dim3& block,
   else             hipLaunchKernelGGL((gate_norm_bwd_kernel<X, B, N, false, false>), grid, block, 0, stream, a);
 }
 
+// Workspace: the workgroups' sums, then those of the stretches.
+static int gate_stretches(const spa2_gate_shape& s) {
+  const int64_t n = (s.samples + SUM_STRETCH - 1) / SUM_STRETCH;
+  return (int)(n < SUM_STRETCHES ? n : SUM_STRETCHES);
+}
+static size_t gate_joined_at(const spa2_gate_shape& s) {
+  return ((size_t)s.samples * gate_per_sample(s, true) * 3 * (size_t)s.width * sizeof(float) + 15) & ~(size_t)15;
+}
 size_t gate_partials_bytes(const spa2_gate_shape& s) {
-  return (size_t)s.samples * gate_per_sample(s, true) * 3 * (size_t)s.width * sizeof(float);
+  const int stretches = gate_stretches(s);
+  return gate_joined_at(s) + (stretches > 1 ? (size_t)stretches * 6 * (size_t)s.width * sizeof(double) : 0);
 }
 
 hipError_t launch_gate_norm_bwd(const void* branch, const spa2_gate_params& p, const spa2_gate_shape& s, float eps, const void* y,
                                 const void* dy, const void* dn, const float* stats, void* dx, void* dbranch,
                                 const spa2_gate_grads& grads, void* ws, hipStream_t stream) {
-  GateArgs a = gate_args(s, p, eps, true);
-  a.branch = branch; a.y_in = y; a.dy = dy; a.dn = dn; a.stats = (float*)stats; a.dx = dx; a.dbranch = dbranch;
-  const bool any = grads.gate || grads.branch_weight || grads.weight || grads.bias || grads.scale || grads.shift;
-  a.part = any ? (float*)ws : nullptr;
+  GateArgs a = gate_args(branch, s, p, eps, true);
+  a.y_in = y; a.dy = dy; a.dn = dn; a.stats = (float*)stats; a.dx = dx; a.dbranch = dbranch;
+  const bool alone = a.per_sample == 1 && s.samples > 1;
+  const bool shared = grads.weight || grads.bias || grads.branch_weight || (grads.gate && !s.gate_sb) || (grads.scale && !s.scale_sb) ||
+                      (grads.shift && !s.shift_sb);
+  const bool sums = shared || (!alone && (grads.gate || grads.scale || grads.shift));
+  a.part = sums ? (float*)ws : nullptr;
+  if (alone) {
+    a.own.gate = s.gate_sb ? grads.gate : nullptr;
+    a.own.scale = s.scale_sb ? grads.scale : nullptr;
+    a.own.shift = s.shift_sb ? grads.shift : nullptr;
+  }
   const dim3 grid((unsigned)(a.per_sample * s.samples)), block((unsigned)gate_threads(s.width));
   const bool x32 = s.x_dtype == SPA2_DTYPE_F32, b32 = s.branch_dtype == SPA2_DTYPE_F32, n32 = s.out_dtype == SPA2_DTYPE_F32;
   if (!x32)             launch_types<uint16_t, uint16_t, uint16_t>(a, grid, block, stream);
@@ -269,16 +335,20 @@ hipError_t launch_gate_norm_bwd(const void* branch, const spa2_gate_params& p, c
   else if (n32)         launch_types<float, uint16_t, float>(a, grid, block, stream);
   else                  launch_types<float, uint16_t, uint16_t>(a, grid, block, stream);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !any) return e;
+  if (e != hipSuccess || !sums) return e;
   const int columns = (s.width + SUM_CHANNELS - 1) / SUM_CHANNELS;
-  GateSums q = {a.part, p, grads, s.gate_sb, s.scale_sb, s.shift_sb, (int)s.samples, a.per_sample, s.width, columns, a.params32,
-                s.kind != SPA2_NORM_NONE, branch != nullptr};
-  hipLaunchKernelGGL(gate_sums_kernel, dim3((unsigned)(columns * s.samples)), dim3(64 * SUM_WAVES), 0, stream, q);
-  e = hipGetLastError();
-  const bool shared = grads.weight || grads.bias || grads.branch_weight || (grads.gate && !s.gate_sb) || (grads.scale && !s.scale_sb) ||
-                      (grads.shift && !s.shift_sb);
+  GateSums q = {a.part, p, grads, s.gate_sb, s.scale_sb, s.shift_sb, (int)s.samples, a.per_sample, s.width, columns, gate_stretches(s),
+                (double*)((char*)ws + gate_joined_at(s)), a.params32, s.kind != SPA2_NORM_NONE, branch != nullptr};
+  if (!alone) {                            // (alone: the sums are those of whole samples)
+    const int waves = (a.per_sample + 64 / SUM_LANES - 1) / (64 / SUM_LANES);
+    hipLaunchKernelGGL(gate_sums_kernel, dim3((unsigned)(columns * s.samples)), dim3(64 * (waves < SUM_WAVES ? waves : SUM_WAVES)), 0, stream, q);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || s.samples == 1 || !shared) return e;
-  hipLaunchKernelGGL(gate_shared_kernel, dim3((unsigned)columns), dim3(SUM_CHANNELS * SUM_GROUPS), 0, stream, q);
+  hipLaunchKernelGGL(gate_shared_kernel, dim3((unsigned)(columns * q.stretches)), dim3(SUM_CHANNELS * SUM_GROUPS), 0, stream, q);
+  e = hipGetLastError();
+  if (e != hipSuccess || q.stretches == 1) return e;
+  hipLaunchKernelGGL(gate_joined_kernel, dim3((unsigned)((s.width + 63) / 64)), dim3(64), 0, stream, q);
   return hipGetLastError();
 }
 

@@ -854,6 +854,7 @@ std::tuple<Tensor, OptTensor> gate_add_norm(const Tensor& x, const OptTensor& br
   GateInputs g = {x, or_none(branch), or_none(gate), or_none(branch_weight), or_none(weight), or_none(bias), or_none(scale), or_none(shift),
                   kind, eps, dtype.value_or(x.scalar_type())};
   gate_check(g);
+  capture_check(x, {x, g.branch, g.gate, g.branch_weight, g.weight, g.bias, g.scale, g.shift});
   // parameters of one type: that of all of them, else fp32 (PyTorch differentiates the change)
   bool bf16 = true, all32 = true;
   for (const Tensor* t : g.params())
@@ -873,7 +874,6 @@ std::tuple<Tensor, OptTensor> gate_add_norm(const Tensor& x, const OptTensor& br
     const GateResult r = gate_call(g, false);
     return {r.y.defined() ? r.y : x, r.n.defined() ? OptTensor(r.n) : std::nullopt};
   }
-  capture_check(x, {x, or_none(branch), or_none(gate), or_none(branch_weight), or_none(weight), or_none(bias), or_none(scale), or_none(shift)});
   auto some = [](const Tensor& t) { return t.defined() ? OptTensor(t) : std::nullopt; };
   const variable_list out = GateAddNorm::apply(x, branch, some(g.gate), some(g.branch_weight), some(g.weight), some(g.bias), some(g.scale),
                                                some(g.shift), kind, eps, g.out == at::kFloat, wants);

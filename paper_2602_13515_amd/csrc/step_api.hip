@@ -10,7 +10,6 @@ namespace {
 bool dtype_ok(int32_t t) { return t == SPA2_DTYPE_BF16 || t == SPA2_DTYPE_F32; }
 uintptr_t element_size(int32_t t) { return t == SPA2_DTYPE_BF16 ? 2 : 4; }
 
-
 constexpr int64_t GATE_MAX_SAMPLES = 1 << 22, GATE_MAX_ROWS = (int64_t)1 << 40;
 
 int check_gate_shape(const spa2_gate_shape* s) {
@@ -18,6 +17,8 @@ int check_gate_shape(const spa2_gate_shape* s) {
   if (s->samples <= 0 || s->samples > GATE_MAX_SAMPLES || s->tokens <= 0 || s->tokens > GATE_MAX_ROWS / s->samples ||
       s->width < SPA2_GATE_MIN_WIDTH || s->width > SPA2_GATE_MAX_WIDTH)
     return SPA2_ERR_SHAPE;
+  // (a launch has less than 2^32 threads)
+  if (s->samples * gate_threads(s->width) >= (int64_t)1 << 32) return SPA2_ERR_SHAPE;
   for (const int64_t sb : {s->gate_sb, s->scale_sb, s->shift_sb})
     if (sb && (sb < s->width || sb > GATE_MAX_ROWS)) return SPA2_ERR_SHAPE;
   if (s->kind != SPA2_NORM_NONE && s->kind != SPA2_NORM_LAYER && s->kind != SPA2_NORM_RMS) return SPA2_ERR_UNSUPPORTED;

@@ -9,6 +9,7 @@
 
 namespace spa2 {
 
+inline int gate_threads(int width) { return 64 * ((width + 511) / 512); }      // of a workgroup
 int gate_per_sample(const spa2_gate_shape& s, bool backward);
 size_t gate_partials_bytes(const spa2_gate_shape& s);
 hipError_t launch_gate_norm(const void* x, const void* branch, const spa2_gate_params& p, const spa2_gate_shape& s, float eps,

@@ -70,7 +70,8 @@ int main(void) {
   h = g; h.x_dtype = 0; EXPECT(GATE(h), SPA2_ERR_UNSUPPORTED);             /* (fp32 branch into a bf16 stream) */
   h = g; h.param_dtype = 2; EXPECT(GATE_BWD(h, fake, big), SPA2_ERR_UNSUPPORTED);
   EXPECT(GATE_BWD(g, 0, big), SPA2_ERR_WORKSPACE); EXPECT(GATE_BWD(g, fake, 64), SPA2_ERR_WORKSPACE); EXPECT(GATE_BWD(g, odd, big), SPA2_ERR_ALIGN);
-  h = g; h.samples = 1 << 22; h.tokens = 1 << 18; h.width = 8192; h.gate_sb = h.scale_sb = h.shift_sb = 8192;
+  h = g; h.samples = 1 << 22; h.width = 8192; EXPECT(GATE(h), SPA2_ERR_SHAPE);      /* (2^32 threads) */
+  h = g; h.samples = 1 << 21; h.tokens = 1 << 18; h.width = 8192; h.gate_sb = h.scale_sb = h.shift_sb = 8192;
   EXPECT(GATE_BWD(h, fake, ((size_t)1 << 38)), SPA2_ERR_WORKSPACE);
   q = p; q.weight = odd; EXPECT(spa2_gate_norm(fake, fake, &q, &g, 1e-6f, fake, fake, f, 0), SPA2_ERR_ALIGN);
   e = d; e.bias = odd; EXPECT(spa2_gate_norm_bwd(fake, &p, &g, 1e-6f, fake, fake, fake, f, fake, fake, &e, fake, big, 0), SPA2_ERR_ALIGN);

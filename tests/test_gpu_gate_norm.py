@@ -148,6 +148,19 @@ def test_samples_and_tokens(B, N, C, own):
     _check(x, branch, _params(g, shapes, C, F32), "layer", None, dy, dn)
 
 
+@pytest.mark.parametrize("B,N,C", [(300, 2, 1536), (257, 1, 1283), (600, 3, 5120), (5000, 1, 72), (5000, 2, 41), (20_000, 1, 8)])
+@pytest.mark.parametrize("own", ["gate scale shift", "scale", "gate shift", ""])
+def test_many_samples(B, N, C, own):
+    """Modulations of their own for (nearly) every token: a workgroup a sample; sums of what they share, over stretches of them."""
+    g, x, branch, dy, dn = _data(B, N, C, (F32, BF, BF), 13)
+    shapes = {**ALL, "scale": B, **{n: B for n in own.split()}}
+    if own == "gate shift":
+        shapes = {"gate": B, "scale": "C", "shift": B, "bias": "C"}
+    if own == "":
+        shapes = {"gate": B, "shift": B, "scale": B}
+    _check(x, branch, _params(g, shapes, C, BF if C % 2 else F32), "layer" if N > 1 else "rms", BF, dy, dn)
+
+
 def test_parameters_of_unlike_kinds():
     """One vector of a sample's own among shared ones; types that differ."""
     g, x, branch, dy, dn = _data(4, 6, 200, (F32, F32, F32), 4)
@@ -233,19 +246,49 @@ def test_a_lost_row_stays_alone():
 def test_nothing_is_written_outside():
     from paper_2602_13515_amd import binding
     for C, N in ((137, 5), (5120, 3), (8189, 2)):
-        gd = Guarded()
-        g, x, branch, dy, dn = _data(1, N, C, (BF, BF, BF), 10)
-        p = _params(g, ALL, C, BF)
-        params = [p[n] for n in NAMES]
-        y, n, dx, db = (gd.alloc((1, N, C), BF, dev(), float("nan")) for _ in range(4))
-        stats = gd.alloc((3, N), F32, dev(), float("nan"))
-        grads = [gd.alloc((C,), BF, dev(), float("nan")) for _ in NAMES]
-        ws = gd.alloc((binding.spa2_gate_norm_bwd_workspace_bytes(x, branch, params, "layer"),), torch.uint8, dev(), 255)
-        binding.spa2_gate_norm(x, branch, params, "layer", EPS, y, n, stats)
-        binding.spa2_gate_norm_bwd(branch, params, "layer", EPS, y, dy, dn, stats, dx, db, grads, ws)
-        torch.cuda.synchronize()
-        gd.check(f"width {C}")
-        assert all(torch.isfinite(t).all() for t in (y, n, dx, db, stats, *grads))
+        _guarded(binding, 1, N, C, ALL)
+    for C, B in ((137, 700), (5120, 300), (8189, 2)):
+        _guarded(binding, B, 2, C, {**ALL, "gate": B, "scale": B, "shift": B})
+
+
+def _guarded(binding, B, N, C, shapes):
+    gd = Guarded()
+    g, x, branch, dy, dn = _data(B, N, C, (BF, BF, BF), 10)
+    p = _params(g, shapes, C, BF)
+    params = [p[n] for n in NAMES]
+    y, n, dx, db = (gd.alloc((B, N, C), BF, dev(), float("nan")) for _ in range(4))
+    stats = gd.alloc((3, B * N), F32, dev(), float("nan"))
+    grads = [gd.alloc(tuple(t.shape), BF, dev(), float("nan")) for t in params]
+    ws = gd.alloc((binding.spa2_gate_norm_bwd_workspace_bytes(x, branch, params, "layer"),), torch.uint8, dev(), 255)
+    binding.spa2_gate_norm(x, branch, params, "layer", EPS, y, n, stats)
+    binding.spa2_gate_norm_bwd(branch, params, "layer", EPS, y, dy, dn, stats, dx, db, grads, ws)
+    torch.cuda.synchronize()
+    gd.check(f"width {C}")
+    assert all(torch.isfinite(t).all() for t in (y, n, dx, db, stats, *grads))
+
+
+def test_many_samples_of_wide_rows():
+    """More samples than workgroups of all threads a launch may have: each is worked out as it is among few."""
+    B, C = 100_000, 1536
+    g = torch.Generator(device=dev()).manual_seed(11)
+    x, branch, dy, dn = (torch.randn((B, 1, C), generator=g, device=dev()).to(BF) for _ in range(4))
+    own = [torch.randn((B, C), generator=g, device=dev()).to(BF) for _ in range(3)]
+
+    def run(last):
+        leaves = [t[-last:].detach().requires_grad_(True) for t in (x, branch, *own)]
+        y, n = spa2.gate_add_norm(leaves[0], leaves[1], gate=leaves[2], scale=leaves[3], shift=leaves[4])
+        return [y, n, *torch.autograd.grad((y, n), leaves, (dy[-last:], dn[-last:]))]
+    for a, b in zip(run(B), run(33)):
+        assert torch.equal(a[-33:], b)
+
+
+def test_a_norm_of_a_branch_that_is_not_there_is_not_looked_at():
+    from paper_2602_13515_amd import binding
+    g, x, _, dy, dn = _data(2, 3, 64, (F32, F32, F32), 12)
+    params = [None, torch.ones(64, device=dev()), None, None, None, None]
+    dx = torch.empty_like(x)
+    binding.spa2_gate_norm_bwd(None, params, None, EPS, x, dy, None, None, dx)
+    assert torch.equal(dx, dy)
 
 
 def test_long_tensors():
