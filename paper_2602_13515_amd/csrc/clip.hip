@@ -7,6 +7,9 @@
 // workgroups; every workgroup of the second adds up all of these, in the same order, and has the factor without a launch between.
 // Squares are taken and summed in fp64, where those of fp32 numbers are exact and do not overflow, in a fixed order.  The second
 // pass multiplies in fp64 and rounds once; where the factor is 1 and a result lies where its gradient does, nothing is touched.
+// Bound: HBM, read once for the norm and once more to be scaled.  Measured, us: 1.13 G elements of fp32 in 440 tensors, into others,
+// 2343 (13.6 GB, 5.8 TB/s; 4.5 GB fit no cache, so the second read is paid); 2.5 GB of bf16 whose factor is 1 411 (6.1 TB/s) and 5 for
+// the second pass; 11 tensors of 3 MB in all 4 + 6.
 #include "spa2_device.h"
 #include "step_ops.h"
 

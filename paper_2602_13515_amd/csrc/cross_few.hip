@@ -38,6 +38,9 @@ struct FewArgs {
   float* pool; int slot_floats;  // partial results (few_slot)
 };
 // Attention over a window (window.h): a sample's keys are those blocks that its queries see, first ones and window in one line.
+// Measured: one query, the last 4096 of up to 32,760 keys and four first ones, 8 samples, 40 heads sharing 8, d = 128 34 to 38 us
+// (134 MB, 3.6 to 4.0 TB/s), the join 4.8: a workgroup has nine blocks of the line, four tiles of a wave's nine on their way before the
+// first is worked on.  Lengths and places are read once, together (one after another, and again for every piece: 3 us more).
 struct WindowFewArgs : FewArgs {
   static constexpr bool WINDOW = true;
   Window win;

@@ -7,7 +7,9 @@
 // The norm is that of y as it is stored, which is also what the backward pass reads.  A workgroup takes rows of one sample, whose
 // parameters it holds in registers, combined to three factors a channel: gate w_b, w (1 + scale), c (1 + scale) + shift.  The
 // deviation is taken about each wave's own mean and the waves' are joined (no difference of large sums), with one barrier a row.
-// Bound: HBM.
+// Bound: HBM.  Measured, us: 75,600 x 5120, bf16 3.1 GB 553 (5.6 TB/s); 32,760 x 1536, fp32 with a bf16 branch and norm 0.6 GB 101
+// (6.0 TB/s, some of it from the memory-side cache); 3 x 1281 x 1281, fp32 79 MB 17 (4.6 TB/s); 16 rows of 5120 4.4, a
+// launch and its loads' round trip.
 #include "gate_norm.h"
 
 namespace spa2 {
