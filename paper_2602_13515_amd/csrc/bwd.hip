@@ -432,6 +432,13 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
       if constexpr (WINDOW) {
         if (tail) {
           const Sight see = sight(j * BKV + kb * 32 + 4 * ((fresh_tid() & 63) >> 5));
+          if (j * BKV >= a.win.sinks) {      // (none of the first keys)
+            const WindowRange seen = window_range(see.near, see.last);
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (8 * (v >> 2) + (v & 3) - seen.lo > seen.extent) s[kb][v] = 0.f;
+            return;
+          }
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
             const int c = 8 * (v >> 2) + (v & 3);

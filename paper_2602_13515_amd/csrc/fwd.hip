@@ -348,6 +348,15 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
         const int t = fresh_tid() & 63, at = j * BKV + 4 * (t >> 5);
         const int p = window_place(a.win, start, a.N, i * BQ + 32 * w + (t & 31));
         const int last = min(p + a.win.right, keys - 1) - at, near = p - a.win.left - at, early = a.win.sinks - at;
+        if (j * BKV >= a.win.sinks) {        // (none of the first keys)
+          const WindowRange seen = window_range(near, last);
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (kb * 32 + 8 * (v >> 2) + (v & 3) - seen.lo > seen.extent) s[kb][v] = -INFINITY;
+          return;
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll

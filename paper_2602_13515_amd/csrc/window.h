@@ -65,6 +65,15 @@ __host__ __device__ __forceinline__ bool window_full(const Window& w, int keys, 
   return last < keys && last <= p0 + w.right && (first >= p1 - w.left || last < w.sinks);
 }
 
+// Places first .. last (none: last < first) as one comparison: x - lo <= extent, in 32 bits without a sign.  Measured against two comparisons
+// and their join, us: 32,760 queries, 12 heads, d = 128, 6240 to the left and 1560 first ones, forward 1438 / 1415, dQ 1991 / 1739 (which had
+// spilled); 4 samples of 1281, 6 heads, 255 to the left 21.3 / 18.9, 26.3 / 22.4, d = 64 16.5 / 13.4, 17.6 / 14.9.  (dK/dV compares twice: 2457
+// and with this 2550.)
+struct WindowRange { uint32_t lo, extent; };
+__device__ __forceinline__ WindowRange window_range(int first, int last) {
+  return first <= last ? WindowRange{(uint32_t)first, (uint32_t)(last - first)} : WindowRange{1u << 30, 0};
+}
+
 // Queries r0 .. r1 (none: r1 < r0) that see some key of first .. last; of `rows` queries from place `start` on.
 struct WindowRows { int r0, r1; };
 __host__ __device__ __forceinline__ WindowRows window_rows(const Window& w, int start, int rows, int first, int last) {
