@@ -148,6 +148,8 @@ inline CrossSection window_dq_section(const CrossDims& m, const Window& w) {
 }
 // dK/dV: the columns of first keys, which many more queries see, are cut apart from the others.  Their parts are launched first and
 // are at most a quarter of what a workgroup slot of the chip has to do in all, so that they are through when the others are.
+// (Eight halves at least: 4 samples of 1281, 6 heads of 2 key heads, 255 to the left and 5 first ones, dK/dV of 16 / 8 / 6 / 4 at least 41.9 / 41.4 /
+// 46.6 / 47.3 us, d = 64 28.2 / 27.5 / 29.0 / 29.8; 32 heads of 8, 4096 queries 89 / 84 / 98 / 99: the last to arrive adds up all parts.)
 struct WindowColumns { CrossSection first, rest; int blocks; size_t counters, total; };      // blocks: of first keys
 inline WindowColumns window_columns(const CrossDims& m, const Window& w) {
   WindowColumns c = {};
@@ -162,7 +164,7 @@ inline WindowColumns window_columns(const CrossDims& m, const Window& w) {
   if (firsts) {
     c.first = cross_section(firsts, all, resident, cost, dkdv_slot_bytes(m.q));
     const int64_t share = (firsts * all + rest * (int64_t)list) / resident / 4;
-    const int len = (int)(share < 16 ? 16 : share < all ? share : all);
+    const int len = (int)(share < 8 ? 8 : share < all ? share : all);
     const int64_t parts = (all + len - 1) / len;
     if (rest && parts > c.first.cut.parts && firsts * parts <= SPLIT_POOL_MAX) {
       c.first.cut = {(int)((all + parts - 1) / parts), (int)parts};
