@@ -63,10 +63,24 @@ struct WindowFwdArgs : CrossFwdArgs {
 template <int D> constexpr int fwd_slot_floats() { return 256 * (D / 2) + 512; }
 size_t fwd_slot_bytes(const Dims& m) { return (size_t)(m.d == 128 ? fwd_slot_floats<128>() : fwd_slot_floats<64>()) * 4; }
 
+// Where a row's channels lie, from its head's first row on; rows of several heads as those of one (attention over a window).
+template <class Args>
+__device__ __forceinline__ bool joined_rows(const Args& a) {
+  if constexpr (Args::WINDOW) return a.N > a.win.nq;
+  return false;
+}
+template <class Args>
+__device__ __forceinline__ int64_t row_offset(const Args& a, int row) {
+  if constexpr (Args::WINDOW) {
+    if (joined_rows(a)) return row / a.win.nq * a.win.head_step + row % a.win.nq * a.win.query_step;
+  }
+  return (int64_t)row * a.sn;
+}
+
 // O_i = diag(l)^-1 O (Alg. 1 step 18) -> bf16 (+ optional residual), LSE = m ln 2 + log l.  q0: first row of the wave;
 // area: LDS of the wave's own for both outputs, which the other waves may still be reading.
-template <int D>
-__device__ __forceinline__ void fwd_store_rows(const FwdArgs& a, int bh, int64_t base, int q0, int lane, uint32_t area,
+template <int D, class Args>
+__device__ __forceinline__ void fwd_store_rows(const Args& a, int bh, int64_t base, int q0, int lane, uint32_t area,
                                                const f32x16 (&oacc)[D / 32], float m_run, float l_tot, bool blind = false) {
   const float inv = blind ? 0.f : 1.f / l_tot;         // (blind: a row that sees no key)
   const int r32 = lane & 31, hf = lane >> 5, valid = min(32, a.N - q0);
@@ -90,9 +104,25 @@ __device__ __forceinline__ void fwd_store_rows(const FwdArgs& a, int bh, int64_t
         row_piece_put<D>(area + RES, r32, 4 * mb + g, hf, pr);
       }
     }
-  const int64_t off = base + (int64_t)q0 * a.sn;
-  rows_store<D>(area, a.o + off, a.sn, valid, lane);
-  if (a.o_res) rows_store<D>(area + RES, a.o_res + off, a.sn, valid, lane);
+  if (Args::WINDOW && joined_rows(a)) {      // (as rows_store, rows of several heads)
+    constexpr int CPR = D / 8, RPI = 64 / CPR;
+    const int c = lane % CPR;
+#pragma unroll
+    for (int r = 0; r < 32; r += RPI) {
+      const int row = r + lane / CPR;
+      const uint32_t from = area + row * (D * 2) + ((c ^ (row & (CPR - 1))) << 4);
+      const int64_t to = base + row_offset(a, q0 + row) + 8 * c;
+      const u32x4 x = lds_ldu4(from), y = a.o_res ? lds_ldu4(from + RES) : x;
+      if (row < valid) {
+        *(u32x4*)(a.o + to) = x;
+        if (a.o_res) *(u32x4*)(a.o_res + to) = y;
+      }
+    }
+  } else {
+    const int64_t off = base + (int64_t)q0 * a.sn;
+    rows_store<D>(area, a.o + off, a.sn, valid, lane);
+    if (a.o_res) rows_store<D>(area + RES, a.o_res + off, a.sn, valid, lane);
+  }
   if (hf == 0 && r32 < valid) a.lse[(int64_t)bh * a.N + q0 + r32] = m_run * LN2 + __logf(l_tot);
 }
 
@@ -197,7 +227,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   const int qrow_ld = qrow < N ? qrow : N - 1;
   bf16x8 qf[D / 16];
   {
-    const uint16_t* qp = a.q + base + (int64_t)qrow_ld * a.sn + 8 * hf;
+    const uint16_t* qp = a.q + base + row_offset(a, qrow_ld) + 8 * hf;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *(const bf16x8*)(qp + 16 * kk);
   }
@@ -207,7 +237,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
 
   if (cnt == 0) {   // a row without any selected block (never produced by the masker): O = 0, LSE = -inf
     if (qrow < N) {
-      uint16_t* op = a.o + base + (int64_t)qrow * a.sn + (D / 2) * hf;
+      uint16_t* op = a.o + base + row_offset(a, qrow) + (D / 2) * hf;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) *(u32x4*)(op + 8 * c) = u32x4{0, 0, 0, 0};
       if (a.o_res) {
@@ -667,7 +697,7 @@ __global__ __launch_bounds__(256) void cross_fwd_join_kernel(Args a) {
     for (int v = 0; v < 16; ++v) x[v] = fmaf(sums[u][v][lane], f, x[v]);
   }
   const float inv = blind ? 0.f : 1.f / l;
-  const int64_t off = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh + (int64_t)row * a.sn + 32 * mb + 4 * hf;
+  const int64_t off = (int64_t)(bh / a.H) * a.sb + (int64_t)(bh % a.H) * a.sh + row_offset(a, row) + 32 * mb + 4 * hf;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {                          // channels 32 mb + 8 q + 4 hf ..
     float y[4];

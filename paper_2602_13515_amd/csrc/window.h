@@ -17,6 +17,7 @@ struct Window {
   int start;
   int left, right, sinks;        // sinks <= Nk; 0 where left has no limit
   int nq;                        // queries of a head: row r of (several heads' rows as one head) is query r % nq
+  int64_t head_step, query_step; // elements between the heads, and the queries, of which such rows are
 };
 
 __host__ __device__ __forceinline__ int window_clamp(int start) { return start < -(1 << 29) ? -(1 << 29) : start > 1 << 29 ? 1 << 29 : start; }

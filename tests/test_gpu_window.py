@@ -128,6 +128,17 @@ def test_long_caches_are_shared_out(Nq, B, left, sinks):
     _check(q, k, v, do, left, 0, sinks)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq,Hq,Hk", [(8, 10, 2), (20, 10, 2), (64, 6, 3), (33, 2, 1), (2, 40, 2), (63, 9, 3)])
+@pytest.mark.parametrize("layout", ["bnhd", "bhnd", "gaps"])
+def test_some_tokens_of_heads_that_share_keys(Nq, Hq, Hk, d, layout):
+    """Rows of several heads as those of one, wherever they lie, in blocks that heads begin and end inside of; long lists in parts."""
+    for B, Nk, lengths in ((2, 9000, [9000, 4321]), (3, 300, [300, 0, 17])):
+        q, k, v, do = _inputs(B, Hq, Hk, Nq, Nk, d, (layout, "bnhd", "bnhd"))
+        for left, right, sinks in ((200, 0, 4), (None, 0, 0)):
+            _check(q, k, v, do, left, right, sinks, lengths=lengths, starts=[n - Nq for n in lengths], whole=False)
+
+
 @pytest.mark.parametrize("B,Nk", [(63, 1100), (64, 1100), (65, 1100), (130, 1100), (256, 1100), (500, 1100), (1024, 1100), (70, 17000)])
 def test_many_samples_share_a_line(B, Nk):
     """One query of many samples of unlike length and place, empty ones among them: stretches that begin and end inside samples."""
