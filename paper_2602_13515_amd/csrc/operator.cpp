@@ -708,8 +708,13 @@ Tensor window_attention(const Tensor& q, const Tensor& k, const Tensor& v, const
 }
 
 // ---- a branch, normed and gated, added to the residual stream, and the norm of the sum
+// Samples' vectors as the kernels take them: one after another, or with gaps, as pieces of one projection lie.  (Gradients get the same
+// gaps: up to 15 widths.)
+bool samples_apart(const Tensor& t) {
+  return t.dim() == 2 && t.size(0) > 1 && t.stride(1) == 1 && t.stride(0) >= t.size(1) && t.stride(0) <= 16 * t.size(1);
+}
 struct GateInputs {
-  Tensor x, branch, gate, branch_weight, weight, bias, scale, shift;      // (packed; parameters of one type)
+  Tensor x, branch, gate, branch_weight, weight, bias, scale, shift;      // (packed but for samples_apart; parameters of one type)
   int64_t kind = 0;
   double eps = 0.0;
   at::ScalarType out = at::kFloat;
@@ -722,7 +727,9 @@ struct GateInputs {
     for (const Tensor* t : {&gate, &scale, &shift}) own = own || (t->defined() && t->dim() == 2);
     s.samples = own ? x.size(0) : 1;
     s.tokens = x.numel() / (s.width * s.samples);
-    auto stride = [&](const Tensor& t) { return t.defined() && t.dim() == 2 ? (int64_t)s.width : 0; };
+    auto stride = [&](const Tensor& t) -> int64_t {
+      return !t.defined() || t.dim() != 2 ? 0 : samples_apart(t) ? t.stride(0) : s.width;
+    };
     s.gate_sb = stride(gate); s.scale_sb = stride(scale); s.shift_sb = stride(shift);
     s.kind = (int32_t)kind;
     s.post = branch_weight.defined();
@@ -822,10 +829,14 @@ struct GateAddNorm : torch::autograd::Function<GateAddNorm> {
     spa2_gate_shape shape = g.shape();
     TORCH_CHECK_VALUE(stats.numel() == 3 * shape.samples * shape.tokens, "the statistics come back whole");
     for (const Tensor* t : g.params())
-      TORCH_CHECK_VALUE(!t->defined() || (t->is_contiguous() && dtype_of(*t) == shape.param_dtype), "saved parameters come back contiguous, of one type");
+      TORCH_CHECK_VALUE(!t->defined() || ((t->is_contiguous() || samples_apart(*t)) && dtype_of(*t) == shape.param_dtype),
+                        "saved parameters come back without gaps, of one type");
     if (!normed) shape.kind = SPA2_NORM_NONE;
     const int64_t wants = ctx->saved_data["wants"].toInt();
-    auto made = [&](int bit, const Tensor& t) { return (wants >> bit & 1) && t.defined() ? at::empty_like(t) : Tensor(); };
+    auto made = [&](int bit, const Tensor& t) {
+      if (!(wants >> bit & 1) || !t.defined()) return Tensor();
+      return t.is_contiguous() ? at::empty_like(t) : at::empty_strided(t.sizes(), t.strides(), t.options());
+    };
     Tensor dx = made(0, y), db = made(1, g.branch), dp[6];
     bool any = false;
     for (int i = 0; i < 6; ++i) {
@@ -860,7 +871,10 @@ std::tuple<Tensor, OptTensor> gate_add_norm(const Tensor& x, const OptTensor& br
   for (const Tensor* t : g.params())
     if (t->defined()) (t->scalar_type() == at::kBFloat16 ? all32 : bf16) = false;
   for (Tensor* t : {&g.gate, &g.branch_weight, &g.weight, &g.bias, &g.scale, &g.shift})
-    if (t->defined()) *t = (bf16 || all32 ? *t : t->to(at::kFloat)).contiguous();
+    if (t->defined()) {
+      if (!bf16 && !all32) *t = t->to(at::kFloat);
+      if (!samples_apart(*t)) *t = t->contiguous();
+    }
   const Tensor* inputs[] = {&g.x, &g.branch, &g.gate, &g.branch_weight, &g.weight, &g.bias, &g.scale, &g.shift};
   bool seen = false;
   int64_t wants = 0;

@@ -220,6 +220,26 @@ def test_layouts_and_addresses():
     assert all(torch.equal(a, b[0, 0]) for a, b in zip(got, base))
 
 
+@pytest.mark.parametrize("C", [8, 131, 1536])
+@pytest.mark.parametrize("B", [1, 2, 300])
+@pytest.mark.parametrize("pieces", [3, 6, 20])
+def test_modulations_that_are_pieces_of_one_projection(C, B, pieces):
+    """Samples' vectors with gaps between each other: as copies without."""
+    g, x, branch, dy, dn = _data(B, 5, C, (F32, BF, BF), 14)
+    whole = torch.randn((B, pieces * C), generator=g).to(dev()).requires_grad_(True)
+    weight = torch.randn(C, generator=g).to(dev()).requires_grad_(True)
+    leaves = [x.requires_grad_(True), branch.requires_grad_(True), whole, weight]
+
+    def run(copy):
+        gate, scale, shift = (t.contiguous() if copy else t for t in whole.chunk(pieces, dim=-1)[:3])
+        y, n = spa2.gate_add_norm(x, branch, gate=gate, scale=scale, shift=shift, weight=weight, eps=EPS, dtype=BF)
+        with torch.no_grad():
+            plain = spa2.gate_add_norm(x, branch, gate=gate, scale=scale, shift=shift, weight=weight, eps=EPS, dtype=BF)
+        return [y, n, *plain, *torch.autograd.grad((y, n), leaves, (dy, dn))]
+    for a, b in zip(run(False), run(True)):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("C", [1281, 5120])
 def test_rows_far_from_zero_keep_their_deviation(C):
     """Means of a thousand deviations: the deviation is no difference of large sums."""
