@@ -126,17 +126,20 @@ __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_kernel(GateArgs a) 
   }
 }
 
-// Workgroups: so many a compute unit that about GATE_AHEAD bytes of rows are on their way to it, three times as many where the branch
-// is normed, too (two reductions a row, one waiting for the other), each with the rows p, p + per_sample, ... of a sample.  Those
-// that run at a time work on one stretch of memory, which the fewer they are is the shorter, and leave fewer sums.  Measured, us,
-// forward and backward, workgroups a compute unit: 32,760 x 1536, fp32 and bf16 (9 and 18 KB of a row) 6 and 5 314, 3 and 2 291, 2 and
-// 1 281, 1 and 1 311; with the branch normed, all fp32 (12 and 25 KB) 2 and 1 584, 3 and 2 447, 5 and 3 404; 75,600 x 5120, bf16 (20
-// and 40 KB) 2 and 1 1488, 1 and 1 1458.
+// Workgroups: so many a compute unit that about GATE_AHEAD bytes of rows are on their way to it, twice as many where the tensors are a
+// fraction of the memory-side cache and rows few, three times as many where the branch is normed, too (two reductions a row, one
+// waiting for the other), each with the rows p, p + per_sample, ... of a sample.  Those that run at a time work on one stretch of
+// memory, which the fewer they are is the shorter, and leave fewer sums.  Measured, us, forward and backward, workgroups a compute
+// unit: 32,760 x 1536, fp32 and bf16 (9 and 18 KB of a row) 6 and 5 314, 3 and 2 291, 2 and 1 281, 1 and 1 311; with the branch normed,
+// all fp32 (12 and 25 KB) 2 and 1 584, 3 and 2 447, 5 and 3 404; 75,600 x 5120, bf16 (20 and 40 KB) 2 and 1 1488, 1 and 1 1458.
+// GATE_AHEAD 20 / 40 / 60 KB: 3 x 1281 x 1281, fp32 61 / 51 / 51; 4000 x 1536, fp32 and bf16 44.7 / 42.4 / 44.0; 10,000 x 1536 91.6 / 87.3 /
+// 88.7; 16,384 x 4096, bf16 253 / 259 / 269; 32,760 x 1536 280 / 289 / 299.
 constexpr int GATE_AHEAD = 20 << 10, GATE_WAVES_CU = 16, CUS = 256;
 int gate_per_sample(const spa2_gate_shape& s, bool backward) {
   auto size = [](int32_t t) { return t == SPA2_DTYPE_F32 ? 4 : 2; };
   const int bytes = s.width * (backward ? 2 * size(s.x_dtype) + size(s.branch_dtype) + size(s.out_dtype) : size(s.x_dtype) + size(s.branch_dtype));
-  const int most = GATE_WAVES_CU / (gate_threads(s.width) / 64), wanted = ((s.post ? 3 : 1) * GATE_AHEAD + bytes / 2) / bytes;
+  const int ahead = s.samples * s.tokens * s.width * 2 > CACHE_BYTES / 4 ? GATE_AHEAD : 2 * GATE_AHEAD;
+  const int most = GATE_WAVES_CU / (gate_threads(s.width) / 64), wanted = ((s.post ? 3 : 1) * ahead + bytes / 2) / bytes;
   const int64_t wgs = CUS * (int64_t)(wanted < 1 ? 1 : wanted < most ? wanted : most);
   const int64_t per = (wgs + s.samples - 1) / s.samples;
   return (int)(per < s.tokens ? per : s.tokens);
