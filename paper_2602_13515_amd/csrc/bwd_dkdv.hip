@@ -47,8 +47,8 @@ struct CrossDkvFineArgs : CrossDkvArgs {
 };
 // Attention over a window (window.h): a column's list is, for every query head, the halves of query blocks from the first to the
 // last query that sees one of its keys.  Columns of first keys are cut as `sp` says, the others as `rest` does.  Bound by the matrix
-// cores.  Measured: 32,760 queries, 12 heads, d = 128, 6240 keys to the left and 1560 first ones 2.49 to 2.59 ms (4 products of 0.69 T
-// operations: 1.07 to 1.11 PFLOP/s); 4 samples of 1281, 6 heads of 2 key heads, d = 64, 255 to the left 28 us, one round of lists of up
+// cores.  Measured: 32,760 queries, 12 heads, d = 128, 6240 keys to the left and 1560 first ones 2.43 to 2.73 ms by card (4 products of
+// 0.69 T operations: 1.0 to 1.1 PFLOP/s); 4 samples of 1281, 6 heads of 2 key heads, d = 64, 255 to the left 25 us, one round of lists of up
 // to 18 halves, which wait for their copies.
 struct WindowDkvArgs : CrossDkvArgs {
   static constexpr bool WINDOW = true;

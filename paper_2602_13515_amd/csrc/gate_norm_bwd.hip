@@ -11,8 +11,8 @@
 // those of all samples by another one where a parameter is shared and there are several.  Where a sample has one workgroup alone (a
 // modulation for every token, say) that one writes the gradients of the sample's own parameters itself.
 // Bound: HBM; y and the branch are read again.  Measured, us, this kernel and the sums: 75,600 x 5120, bf16 4.6 GB 808 + 9 (5.7 TB/s);
-// 32,760 x 1536, fp32 with a bf16 branch and norm 0.9 GB 183 + 9 (5.0 TB/s); 3 x 1281 x 1281, fp32, modulations of each sample 118 MB 39 +
-// 7 + 5; 32,760 tokens of 1536 with modulations of their own 400 all in all, 756 with a weight that they share.
+// 32,760 x 1536, fp32 with a bf16 branch and norm 0.9 GB 183 + 9 (5.0 TB/s); 3 x 1281 x 1281, fp32, modulations of each sample 118 MB 28 to
+// 32 + 8 + 5; 32,760 tokens of 1536 with modulations of their own 400 all in all, 756 with a weight that they share.
 #include "gate_norm.h"
 
 namespace spa2 {
