@@ -129,6 +129,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   int keys = a.N;             // keys that the row sees at most
   int start = 0;              // (WINDOW) place of query 0, and what the workgroup's queries see
   WindowSpan span;
+  WindowBlocks copied = {}, full = {};       // (see fwd.hip)
   bool one = false;           // (WINDOW) all keys in one tile
   if constexpr (CROSS) {
     for (int x = (int)(blockIdx.x * 256 + threadIdx.x); x < a.zeros; x += (int)(gridDim.x * 256)) a.zero[x] = 0;
@@ -190,6 +191,12 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);     // wave-uniform, in a scalar register
   const int r32 = lane & 31, hf = lane >> 5;
   const int N = a.N;
+  if constexpr (WINDOW) {
+    int p0, p1;                              // (of the wave's rows, those past the end included)
+    window_places(a.win, start, a.N, i * BQ + 32 * w, i * BQ + 32 * w + 31, p0, p1);
+    copied = window_blocks(span.sinks, span.lo, span.hi);
+    full = window_full_blocks(a.win, keys, p0, p1);
+  }
   const int64_t unit = (int64_t)bh * a.Tm + i;
   int cnt, split_at = 0, first;              // entries [first, first + part_len) of the list of a split row
   const int32_t* idx = nullptr;
@@ -278,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
   int rows_set = -1;
   auto set_rows = [&](int j) {               // for the tile of key block j (uniform)
     if constexpr (WINDOW) {                  // (see fwd.hip)
-      const bool whole_block = span.whole(j);
+      const bool whole_block = copied.has(j);
       const int code = whole_block ? 0 : j + 1;
       if (code == rows_set) return;
       rows_set = code;
@@ -415,11 +422,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(Args a) {
     };
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool tail = (j + 1) * BKV > keys;
-    if constexpr (WINDOW) {
-      int p0, p1;                            // (of the wave's rows, those past the end included)
-      window_places(a.win, start, a.N, i * BQ + 32 * w, i * BQ + 32 * w + 31, p0, p1);
-      tail = !window_full(a.win, keys, p0, p1, j * BKV, j * BKV + BKV - 1);
-    }
+    if constexpr (WINDOW) tail = !full.has(j);
     f32x16 s[2], dp[2];
     uint32_t dsk[2][8], ds_rest[2][8];       // (ds_rest: FINE)
     auto exp_unit = [&](auto KB, auto U) {   // P^T of two keys

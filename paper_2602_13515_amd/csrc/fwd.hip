@@ -144,6 +144,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   int keys = a.N;             // keys that the row sees at most
   int start = 0;              // (WINDOW) place of query 0, and what the workgroup's queries see
   WindowSpan span;
+  WindowBlocks copied = {}, full = {};       // (WINDOW) blocks all of whose keys some query sees, that all queries of the wave see
   if constexpr (CROSS) {
     int rows = stretch_wgs(a.BH * a.Tm);
     HeadBlock hb;
@@ -204,6 +205,12 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   const int N = a.N;
   // counts and indices come from the caller's pattern: clamp them so that a corrupt list cannot
   // address memory outside the tensors
+  if constexpr (WINDOW) {
+    int p0, p1;                              // (of the wave's rows, those past the end included)
+    window_places(a.win, start, a.N, i * BQ + 32 * w, i * BQ + 32 * w + 31, p0, p1);
+    copied = window_blocks(span.sinks, span.lo, span.hi);
+    full = window_full_blocks(a.win, keys, p0, p1);
+  }
   const int64_t unit = (int64_t)bh * a.Tm + i;
   int cnt, split_at = 0, first;              // entries [first, first + part_len) of the list of a split row (never empty)
   const int32_t* idx = nullptr;
@@ -276,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   int rows_set = -1;
   auto set_rows = [&](int j) {               // for the tile of key block j (uniform)
     if constexpr (WINDOW) {                  // (keys that none of the workgroup's queries sees are not read)
-      const bool whole_block = span.whole(j);
+      const bool whole_block = copied.has(j);
       const int code = whole_block ? 0 : j + 1;
       if (code == rows_set) return;
       rows_set = code;
@@ -373,9 +380,7 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(Args a) {
   // keys past N (short last block) do not take part in the softmax
   auto mask_tail = [&](f32x16 (&s)[2], int j) {
     if constexpr (WINDOW) {
-      int p0, p1;                            // (of the wave's rows, those past the end included)
-      window_places(a.win, start, a.N, i * BQ + 32 * w, i * BQ + 32 * w + 31, p0, p1);
-      if (!window_full(a.win, keys, p0, p1, j * BKV, j * BKV + BKV - 1)) {
+      if (!full.has(j)) {
         const int t = fresh_tid() & 63, at = j * BKV + 4 * (t >> 5);
         const int p = window_place(a.win, start, a.N, i * BQ + 32 * w + (t & 31));
         const int last = min(p + a.win.right, keys - 1) - at, near = p - a.win.left - at, early = a.win.sinks - at;

@@ -78,10 +78,13 @@ int main() {
           CHECK(!seen || from == key);
         }
         CHECK(!s.whole(j) || whole);
+        CHECK(window_blocks(s.sinks, s.lo, s.hi).has(j) == s.whole(j));
         for (int wave = 0; wave < 4; ++wave) {
           int q0, q1;
           window_places(w, start, rows, i * BQ + 32 * wave, i * BQ + 32 * wave + 31, q0, q1);
-          if (!window_full(w, keys, q0, q1, j * BKV, j * BKV + BKV - 1)) continue;
+          const bool full = window_full(w, keys, q0, q1, j * BKV, j * BKV + BKV - 1);
+          CHECK(window_full_blocks(w, keys, q0, q1).has(j) == full);
+          if (!full) continue;
           for (int r = i * BQ + 32 * wave; r < i * BQ + 32 * wave + 32 && r < rows; ++r)
             for (int x = 0; x < BKV; ++x) CHECK(sees(window_place(w, start, rows, r), j * BKV + x));
         }
