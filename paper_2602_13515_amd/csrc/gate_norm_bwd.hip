@@ -8,11 +8,11 @@
 //
 // h and u are made again from y and the branch and the statistics that the forward pass leaves.  A workgroup takes rows of one
 // sample and keeps the three sums of its channels in registers; they are joined by a launch behind, in fp64 and a fixed order, and
-// those of all samples by another one where a parameter is shared and there are several.  Where a sample has one workgroup alone (a
+// those of more than eight samples by another one where a parameter is shared.  Where a sample has one workgroup alone (a
 // modulation for every token, say) that one writes the gradients of the sample's own parameters itself.
 // Bound: HBM; y and the branch are read again.  Measured, us, this kernel and the sums: 75,600 x 5120, bf16 4.6 GB 808 + 9 (5.7 TB/s);
 // 32,760 x 1536, fp32 with a bf16 branch and norm 0.9 GB 183 + 9 (5.0 TB/s); 3 x 1281 x 1281, fp32, modulations of each sample 118 MB 28 to
-// 32 + 8 + 5; 32,760 tokens of 1536 with modulations of their own 400 all in all, 756 with a weight that they share.
+// 32 + 10; 32,760 tokens of 1536 with modulations of their own 400 all in all, 756 with a weight that they share.
 #include "gate_norm.h"
 
 namespace spa2 {
@@ -157,27 +157,39 @@ struct GateSums {
   spa2_gate_grads d;
   int64_t gate_sb, scale_sb, shift_sb;
   int samples, per_sample, width, columns;               // columns: workgroups that share a sample's channels
-  int stretches;                         // of the samples, in gate_shared_kernel
+  int together, stretches;               // samples of a workgroup of gate_sums_kernel; stretches of them in gate_shared_kernel
   double* joined;                        // [stretch][6][width], if there are several
   bool params32, normed, branch;
 };
 constexpr int SUM_CHANNELS = 32, SUM_GROUPS = 32;      // of a workgroup: channels, groups of the summands
 constexpr int SUM_WAVES = 16, SUM_LANES = SUM_CHANNELS / 4;        // (gate_sums_kernel: waves at most; a thread has four channels)
+constexpr int SUM_SAMPLES = 8;           // that a workgroup takes together
 constexpr int SUM_STRETCH = 256, SUM_STRETCHES = 64;   // of gate_shared_kernel: samples at least, stretches at most
 
-// Sums of a sample's workgroups; parameters of its own.  With one sample all gradients are written here, with several the sums
-// take the place of the first workgroup's.  A thread adds up four channels of every (8 waves)-th workgroup, requested four at a time:
-// the kernel is as long as its loads' round trips.  (One channel a thread, 1280 workgroups of 1536 channels: 49 us, this way 8.)  So
-// many waves as have a request each: of 3 workgroups of 512 samples 16 took 350 us.
+// Gradients of what all samples share, channel c: s, sums over the samples.
+__device__ __forceinline__ void shared_put(const GateSums& a, int c, const double (&s)[6]) {
+  grad_put(a.d.weight, a.params32, c, s[0]);
+  grad_put(a.d.bias, a.params32, c, s[1]);
+  grad_put(a.d.branch_weight, a.params32, c, s[2]);
+  if (!a.gate_sb) grad_put(a.d.gate, a.params32, c, s[3]);
+  if (!a.scale_sb) grad_put(a.d.scale, a.params32, c, s[4]);
+  if (!a.shift_sb) grad_put(a.d.shift, a.params32, c, s[5]);
+}
+// Sums of a sample's workgroups, and gradients of the parameters of its own.  A workgroup takes one sample, whose sums, unless it is the
+// only one, take the place of its first workgroup's; or all of up to SUM_SAMPLES that share parameters, a wave one of them, and then the
+// gradients of what they share, too.  A thread adds up four channels of every (8 waves)-th workgroup, requested four at a time: the kernel is as long as its
+// loads' round trips.  (One channel a thread, 1280 workgroups of 1536 channels: 49 us, this way 8.)  So many waves as have a request
+// each: of 3 workgroups of 512 samples 16 took 350 us.  3 samples of 1281 channels, a launch
+// for what they share behind / together 8.2 + 4.8 / 9.7, 113 / 109 for forward and backward pass.
 __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
-  __shared__ double lds[SUM_WAVES][3][SUM_CHANNELS];
-  const int t = threadIdx.x, waves = blockDim.x / 64, groups = waves * (64 / SUM_LANES);
-  const int b = blockIdx.x / a.columns, c0 = blockIdx.x % a.columns * SUM_CHANNELS;
+  __shared__ double lds[SUM_WAVES][3][SUM_CHANNELS], shares[SUM_SAMPLES][6][SUM_CHANNELS];
+  const int t = threadIdx.x, n = a.together, each = blockDim.x / 64 / n, groups = each * (64 / SUM_LANES);      // waves of a sample, groups of its summands
+  const int w = __builtin_amdgcn_readfirstlane(t / 64), b0 = blockIdx.x / a.columns * n, c0 = blockIdx.x % a.columns * SUM_CHANNELS;
   // (the last channels are taken by whole vectors, too: those in front of c0 are another workgroup's and not written)
   auto first = [&](int lane) -> int { return min(c0 + 4 * lane, a.width - 4); };
-  const float* part = a.part + (int64_t)b * a.per_sample * 3 * a.width;
+  const float* part = a.part + (int64_t)(b0 + w % n) * a.per_sample * 3 * a.width;
   double s[3][4] = {};
-  for (int p = t / SUM_LANES; p < a.per_sample; p += 4 * groups) {
+  for (int p = w / n * (64 / SUM_LANES) + t % 64 / SUM_LANES; p < a.per_sample; p += 4 * groups) {
     f32x4 x[4][3];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -206,44 +218,49 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
 #pragma unroll
     for (int i = 0; i < 3; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) lds[t >> 6][i][4 * (t & 63) + e] = s[i][e];
+      for (int e = 0; e < 4; ++e) lds[w][i][4 * (t & 63) + e] = s[i][e];
   __syncthreads();
-  const int c = first(t / 4) + t % 4;
-  if (t >= SUM_CHANNELS || c < c0 + t / 4 * 4) return;
-  double sum[3] = {0.0, 0.0, 0.0};
+  auto channel = [&](int x) -> int { return first(x / 4) + x % 4; };
+  auto counts = [&](int x) -> bool { return channel(x) >= c0 + x / 4 * 4; };
+  for (int x = t; x < SUM_CHANNELS * n; x += blockDim.x) {
+    const int at = x % SUM_CHANNELS, m = x / SUM_CHANNELS, b = b0 + m, c = channel(at);
+    if (!counts(at)) continue;
+    double sum[3] = {0.0, 0.0, 0.0};
 #pragma unroll 4
-  for (int k = 0; k < waves; ++k)
+    for (int k = 0; k < each; ++k)
 #pragma unroll
-    for (int i = 0; i < 3; ++i) sum[i] += lds[k][i][t];
-  const double weight = gate_one(a.p.weight, a.params32, c, 1.f), bias = gate_one(a.p.bias, a.params32, c, 0.f);
-  const double post = gate_one(a.p.branch_weight, a.params32, c, 1.f), gate = gate_one(a.p.gate, a.params32, b * a.gate_sb + c, 1.f);
-  const double scale = 1.0 + gate_one(a.p.scale, a.params32, b * a.scale_sb + c, 0.f);
-  const bool one = a.samples == 1;
-  if (one || a.gate_sb) grad_put(a.d.gate, a.params32, b * a.gate_sb + c, post * sum[2]);
-  if (one || a.scale_sb) grad_put(a.d.scale, a.params32, b * a.scale_sb + c, weight * sum[0] + bias * sum[1]);
-  if (one || a.shift_sb) grad_put(a.d.shift, a.params32, b * a.shift_sb + c, sum[1]);
-  if (one) {
-    grad_put(a.d.weight, a.params32, c, scale * sum[0]);
-    grad_put(a.d.bias, a.params32, c, scale * sum[1]);
-    grad_put(a.d.branch_weight, a.params32, c, gate * sum[2]);
-    return;
+      for (int i = 0; i < 3; ++i) sum[i] += lds[k * n + m][i][at];
+    const double weight = gate_one(a.p.weight, a.params32, c, 1.f), bias = gate_one(a.p.bias, a.params32, c, 0.f);
+    const double post = gate_one(a.p.branch_weight, a.params32, c, 1.f), gate = gate_one(a.p.gate, a.params32, b * a.gate_sb + c, 1.f);
+    const double scale = 1.0 + gate_one(a.p.scale, a.params32, b * a.scale_sb + c, 0.f);
+    const double of_gate = post * sum[2], of_scale = weight * sum[0] + bias * sum[1];
+    if (a.gate_sb) grad_put(a.d.gate, a.params32, b * a.gate_sb + c, of_gate);
+    if (a.scale_sb) grad_put(a.d.scale, a.params32, b * a.scale_sb + c, of_scale);
+    if (a.shift_sb) grad_put(a.d.shift, a.params32, b * a.shift_sb + c, sum[1]);
+    const double shared[6] = {scale * sum[0], scale * sum[1], gate * sum[2], of_gate, of_scale, sum[1]};
+    if (n > 1) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) shares[m][i][at] = shared[i];
+    } else if (a.samples == 1) {
+      shared_put(a, c, shared);
+    } else {
+      float* joined = a.part + (int64_t)b * a.per_sample * 3 * a.width + c;
+      joined[0] = (float)sum[0];
+      joined[a.width] = (float)sum[1];
+      joined[2 * (int64_t)a.width] = (float)sum[2];
+    }
   }
-  float* joined = a.part + (int64_t)b * a.per_sample * 3 * a.width + c;
-  joined[0] = (float)sum[0];
-  joined[a.width] = (float)sum[1];
-  joined[2 * (int64_t)a.width] = (float)sum[2];
+  if (n == 1) return;
+  __syncthreads();
+  if (t >= SUM_CHANNELS || !counts(t)) return;
+  double sum[6] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
+  for (int m = 0; m < n; ++m)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) sum[i] += shares[m][i][t];
+  shared_put(a, channel(t), sum);
 }
 
-// Gradients of what all samples share, channel c: s, sums over the samples.
-__device__ __forceinline__ void shared_put(const GateSums& a, int c, const double (&s)[6]) {
-  grad_put(a.d.weight, a.params32, c, s[0]);
-  grad_put(a.d.bias, a.params32, c, s[1]);
-  grad_put(a.d.branch_weight, a.params32, c, s[2]);
-  if (!a.gate_sb) grad_put(a.d.gate, a.params32, c, s[3]);
-  if (!a.scale_sb) grad_put(a.d.scale, a.params32, c, s[4]);
-  if (!a.shift_sb) grad_put(a.d.shift, a.params32, c, s[5]);
-}
-// These sums, over a stretch of the samples; several stretches are joined by a launch behind.
+// Sums over a stretch of many samples, of what they share; several stretches are joined by a launch behind.
 __global__ __launch_bounds__(SUM_CHANNELS * SUM_GROUPS) void gate_shared_kernel(GateSums a) {
   __shared__ double lds[6][SUM_GROUPS][SUM_CHANNELS];
   const int lane = threadIdx.x % SUM_CHANNELS, g = threadIdx.x / SUM_CHANNELS, c = blockIdx.x % a.columns * SUM_CHANNELS + lane;
@@ -339,14 +356,17 @@ hipError_t launch_gate_norm_bwd(const void* branch, const spa2_gate_params& p, c
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !sums) return e;
   const int columns = (s.width + SUM_CHANNELS - 1) / SUM_CHANNELS;
-  GateSums q = {a.part, p, grads, s.gate_sb, s.scale_sb, s.shift_sb, (int)s.samples, a.per_sample, s.width, columns, gate_stretches(s),
-                (double*)((char*)ws + gate_joined_at(s)), a.params32, s.kind != SPA2_NORM_NONE, branch != nullptr};
+  GateSums q = {a.part, p, grads, s.gate_sb, s.scale_sb, s.shift_sb, (int)s.samples, a.per_sample, s.width, columns,
+                shared && s.samples <= SUM_SAMPLES ? (int)s.samples : 1, gate_stretches(s), (double*)((char*)ws + gate_joined_at(s)),
+                a.params32, s.kind != SPA2_NORM_NONE, branch != nullptr};
   if (!alone) {                            // (alone: the sums are those of whole samples)
-    const int waves = (a.per_sample + 64 / SUM_LANES - 1) / (64 / SUM_LANES);
-    hipLaunchKernelGGL(gate_sums_kernel, dim3((unsigned)(columns * s.samples)), dim3(64 * (waves < SUM_WAVES ? waves : SUM_WAVES)), 0, stream, q);
+    const int wanted = (a.per_sample + 64 / SUM_LANES - 1) / (64 / SUM_LANES), most = SUM_WAVES / q.together;
+    hipLaunchKernelGGL(gate_sums_kernel, dim3((unsigned)(columns * (s.samples / q.together))), dim3(64 * q.together * (wanted < most ? wanted : most)),
+                       0, stream, q);
     e = hipGetLastError();
+    if (e != hipSuccess || q.together == s.samples) return e;
   }
-  if (e != hipSuccess || s.samples == 1 || !shared) return e;
+  if (!shared) return e;
   hipLaunchKernelGGL(gate_shared_kernel, dim3((unsigned)(columns * q.stretches)), dim3(SUM_CHANNELS * SUM_GROUPS), 0, stream, q);
   e = hipGetLastError();
   if (e != hipSuccess || q.stretches == 1) return e;
