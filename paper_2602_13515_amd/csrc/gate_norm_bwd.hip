@@ -133,13 +133,13 @@ __global__ __launch_bounds__(64 * GATE_WAVES) void gate_norm_bwd_kernel(GateArgs
     gate_param(a.p.branch_weight, f, raw[0], 1.f, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= sg[e];
-    grad_put(a.own.gate, f, b * a.gate_sb + l.at, x);
+    grad_put(a.own.gate, f, b * a.width + l.at, x);
     gate_param(a.p.weight, f, raw[1], 1.f, x);
     gate_param(a.p.bias, f, raw[2], 0.f, z);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], s1[e], z[e] * s2[e]);
-    grad_put(a.own.scale, f, b * a.scale_sb + l.at, x);
-    grad_put(a.own.shift, f, b * a.shift_sb + l.at, s2);
+    grad_put(a.own.scale, f, b * a.width + l.at, x);
+    grad_put(a.own.shift, f, b * a.width + l.at, s2);
   }
   if (!a.part) return;
   float* part = a.part + (int64_t)blockIdx.x * 3 * a.width + l.at;
@@ -234,9 +234,10 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void gate_sums_kernel(GateSums a) {
     const double post = gate_one(a.p.branch_weight, a.params32, c, 1.f), gate = gate_one(a.p.gate, a.params32, b * a.gate_sb + c, 1.f);
     const double scale = 1.0 + gate_one(a.p.scale, a.params32, b * a.scale_sb + c, 0.f);
     const double of_gate = post * sum[2], of_scale = weight * sum[0] + bias * sum[1];
-    if (a.gate_sb) grad_put(a.d.gate, a.params32, b * a.gate_sb + c, of_gate);
-    if (a.scale_sb) grad_put(a.d.scale, a.params32, b * a.scale_sb + c, of_scale);
-    if (a.shift_sb) grad_put(a.d.shift, a.params32, b * a.shift_sb + c, sum[1]);
+    const int64_t own = (int64_t)b * a.width + c;
+    if (a.gate_sb) grad_put(a.d.gate, a.params32, own, of_gate);
+    if (a.scale_sb) grad_put(a.d.scale, a.params32, own, of_scale);
+    if (a.shift_sb) grad_put(a.d.shift, a.params32, own, sum[1]);
     const double shared[6] = {scale * sum[0], scale * sum[1], gate * sum[2], of_gate, of_scale, sum[1]};
     if (n > 1) {
 #pragma unroll

@@ -708,11 +708,8 @@ Tensor window_attention(const Tensor& q, const Tensor& k, const Tensor& v, const
 }
 
 // ---- a branch, normed and gated, added to the residual stream, and the norm of the sum
-// Samples' vectors as the kernels take them: one after another, or with gaps, as pieces of one projection lie.  (Gradients get the same
-// gaps: up to 15 widths.)
-bool samples_apart(const Tensor& t) {
-  return t.dim() == 2 && t.size(0) > 1 && t.stride(1) == 1 && t.stride(0) >= t.size(1) && t.stride(0) <= 16 * t.size(1);
-}
+// Samples' vectors with gaps between each other, as pieces of one projection lie.
+bool samples_apart(const Tensor& t) { return t.dim() == 2 && t.size(0) > 1 && t.stride(1) == 1 && t.stride(0) >= t.size(1); }
 struct GateInputs {
   Tensor x, branch, gate, branch_weight, weight, bias, scale, shift;      // (packed but for samples_apart; parameters of one type)
   int64_t kind = 0;
@@ -834,8 +831,7 @@ struct GateAddNorm : torch::autograd::Function<GateAddNorm> {
     if (!normed) shape.kind = SPA2_NORM_NONE;
     const int64_t wants = ctx->saved_data["wants"].toInt();
     auto made = [&](int bit, const Tensor& t) {
-      if (!(wants >> bit & 1) || !t.defined()) return Tensor();
-      return t.is_contiguous() ? at::empty_like(t) : at::empty_strided(t.sizes(), t.strides(), t.options());
+      return (wants >> bit & 1) && t.defined() ? at::empty(t.sizes(), t.options()) : Tensor();
     };
     Tensor dx = made(0, y), db = made(1, g.branch), dp[6];
     bool any = false;

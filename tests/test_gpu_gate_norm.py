@@ -222,7 +222,7 @@ def test_layouts_and_addresses():
 
 @pytest.mark.parametrize("C", [8, 131, 1536])
 @pytest.mark.parametrize("B", [1, 2, 300])
-@pytest.mark.parametrize("pieces", [3, 6, 20])
+@pytest.mark.parametrize("pieces", [3, 6, 40])
 def test_modulations_that_are_pieces_of_one_projection(C, B, pieces):
     """Samples' vectors with gaps between each other: as copies without."""
     g, x, branch, dy, dn = _data(B, 5, C, (F32, BF, BF), 14)
