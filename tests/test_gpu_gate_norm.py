@@ -322,6 +322,30 @@ def test_long_tensors():
     assert torch.equal(y[:, -33:], want[0]) and torch.equal(n[:, -33:], want[1]) and not n[0, :-33:997].any()
 
 
+def test_gradients_of_long_tensors():
+    """The last rows of more than 2^31 elements, a modulation for every token and one for all: as among few."""
+    C = 5120
+    N = 2 ** 31 // C + 40
+    g = torch.Generator(device=dev()).manual_seed(15)
+    x = torch.zeros((N, C), dtype=BF, device=dev())
+    up = torch.zeros((N, C), dtype=BF, device=dev())
+    x[-33:], up[-33:] = (torch.randn((33, C), generator=g, device=dev()).to(BF) for _ in range(2))
+    w = torch.randn(C, generator=g, device=dev()).to(BF)
+
+    def run(last, gate):
+        leaves = [x[-last:].detach().requires_grad_(True) for _ in range(2)] + [gate[-last:].detach().requires_grad_(True)]
+        y, n = spa2.gate_add_norm(leaves[0], leaves[1], gate=leaves[2], weight=w, kind="rms")
+        return torch.autograd.grad((y, n), leaves, (up[-last:], up[-last:]))
+    for a, b in zip(run(N, up), run(33, up)):
+        assert torch.equal(a[-33:], b) and not a[0:-33:997].any()
+    leaves = [x.detach().requires_grad_(True), w.detach().requires_grad_(True)]
+    few = [x[-33:].detach().requires_grad_(True), w.detach().requires_grad_(True)]
+    got, want = ([*torch.autograd.grad(spa2.gate_add_norm(p, weight=v, kind="layer")[1], (p, v), u)] for (p, v), u in ((leaves, up), (few, up[-33:])))
+    assert torch.equal(got[0][-33:], want[0])
+    # (the rows of zeros add nothing; 33 numbers in another order in fp32, whose roundings stay far below 2^-10, and one rounding to bf16 each)
+    assert ((got[1].float() - want[1].float()).abs() <= 2 * 2.0 ** -8 * want[1].float().abs() + 2.0 ** -10).all()
+
+
 def test_second_derivatives_and_tangents_are_refused():
     x = torch.randn(2, 3, 64, device=dev(), requires_grad=True)
     y, n = spa2.gate_add_norm(x, x * 2)
