@@ -38,12 +38,14 @@ struct FewArgs {
   float* pool; int slot_floats;  // partial results (few_slot)
 };
 // Attention over a window (window.h): a sample's keys are those blocks that its queries see, first ones and window in one line.
-// Measured: one query, the last 4096 of up to 32,760 keys and four first ones, 8 samples, 40 heads sharing 8, d = 128 34 to 38 us
-// (134 MB, 3.6 to 4.0 TB/s), the join 4.8: a workgroup has nine blocks of the line, four tiles of a wave's nine on their way before the
-// first is worked on.  Lengths and places are read once, together (one after another, and again for every piece: 3 us more).
+// Measured: one query, the last 4096 of up to 32,760 keys and four first ones, 8 samples, 40 heads sharing 8, d = 128 28 to 32 us
+// (134 MB, 4.2 to 4.7 TB/s), the join 4.4: a workgroup has eight or nine blocks, two of a wave's eight or nine tiles on their way before
+// the first is worked on.  Lengths and places are read once, together (one after another, and again for every piece: 3 us more).
 struct WindowFewArgs : FewArgs {
   static constexpr bool WINDOW = true;
   Window win;
+  int aim;                       // parts of a key head's samples in all, about (workers: at most)
+  int32_t* plan;                 // [sample][2]: its first part, its parts; for the join
 };
 // A sample's keys, and the place of its first query.
 struct FewSeen { int keys, start; };
@@ -72,6 +74,12 @@ __device__ __forceinline__ int few_sum(int x) {
 }
 // The line, 64 samples at a time: a lane holds sample 64 c + lane's blocks (0 past the last), keys and place.  Blocks in all, blocks
 // of a stretch.
+// WINDOW: windows are mostly of one length, and a workgroup that takes the end of one and the start of the next waits for its first
+// copies twice.  A sample's blocks are therefore cut into parts, as even as can be, of at most `per` blocks, the least that makes no more
+// parts than there are workgroups, and the parts stand in the line (total: parts); where they stand goes to the join by memory.  Measured, us,
+// kernel and join, one query, stretches of one line / this: 4096 keys, 8 samples, 8 key heads 33.7 + 4.5 / 28.3 + 4.3, of unlike length 31.0 + 4.6 /
+// 26.8 + 4.2; one long sample among short ones, no limit to the left 35.6 + 6.6 / 27.0 + 6.0; 2048 keys, 100 samples, one head 25.6 + 5.7 / 23.2 +
+// 4.2; 600 samples of 20,000 keys, one head, d = 64 515 + 24 / 566 + 8.
 struct FewLine { int c, n, keys, start, total, per; };
 template <class Args>
 __device__ __forceinline__ void few_chunk(const Args& a, FewLine& line, int c, int lane) {
@@ -85,6 +93,9 @@ __device__ __forceinline__ void few_chunk(const Args& a, FewLine& line, int c, i
   if constexpr (Args::WINDOW) line.start = window_clamp(start);
   line.n = 64 * c + lane < a.B ? few_blocks(a, FewSeen{line.keys, line.start}) : 0;
 }
+// What the lane's sample takes of the line: blocks; parts.
+template <class Args>
+__device__ __forceinline__ int few_units(const FewLine& line) { return Args::WINDOW ? (line.n + line.per - 1) / line.per : line.n; }
 template <class Args>
 __device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
   FewLine r;
@@ -94,7 +105,20 @@ __device__ __forceinline__ FewLine few_line(const Args& a, int lane) {
     n += r.n;
   }
   r.total = few_sum(n);
-  r.per = max((r.total + a.workers - 1) / a.workers, a.least);
+  if constexpr (Args::WINDOW) {
+    for (r.per = max((r.total + a.aim - 1) / a.aim, a.least);; r.per += max(r.per / 16, 1)) {
+      n = 0;
+      for (int c = (a.B - 1) / 64; c >= 0; --c) {
+        if (c != r.c) few_chunk(a, r, c, lane);
+        n += few_units<Args>(r);
+      }
+      n = few_sum(n);
+      if (n <= a.workers) break;             // (at the latest with the longest sample's blocks: there are no less workgroups than samples)
+    }
+    r.total = n;
+  } else {
+    r.per = max((r.total + a.workers - 1) / a.workers, a.least);
+  }
   return r;
 }
 // What the line holds of sample b.
@@ -109,7 +133,7 @@ __device__ __forceinline__ int few_first(const Args& a, FewLine& line, int b, in
   int before = 0;
   for (int c = 0; 64 * c < b; ++c) {
     if (c != line.c) few_chunk(a, line, c, lane);
-    before += 64 * c + lane < b ? line.n : 0;
+    before += 64 * c + lane < b ? few_units<Args>(line) : 0;
   }
   return few_sum(before);
 }
@@ -120,14 +144,15 @@ __device__ __forceinline__ FewSample few_sample(const Args& a, FewLine& line, in
   int run = 0;
   for (int c = 0; 64 * c < a.B; ++c) {
     if (c != line.c) few_chunk(a, line, c, lane);
-    int sum = line.n;                                    // of this sample and those before it
+    const int n = few_units<Args>(line);
+    int sum = n;                                         // of this sample and those before it
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
       const int x = __shfl_up(sum, s, 64);
       sum += lane >= s ? x : 0;
     }
-    const int at = run + sum - line.n;
-    const uint64_t here = __builtin_amdgcn_ballot_w64(line.n > 0 && at <= place && place < at + line.n);
+    const int at = run + sum - n;
+    const uint64_t here = __builtin_amdgcn_ballot_w64(n > 0 && at <= place && place < at + n);
     if (here) {
       const int l = __builtin_ctzll(here);
       return FewSample{64 * c + l, __builtin_amdgcn_readlane(at, l)};
@@ -138,12 +163,17 @@ __device__ __forceinline__ FewSample few_sample(const Args& a, FewLine& line, in
 }
 // Stretches that a sample lies in, and where part p of its result lies: a stretch has two slots, for the sample that it begins
 // inside of or with and for the one that it ends inside of.
+// (WINDOW: parts of the sample, each of which has a slot.)
 struct FewParts { int i0, parts, starts; };
+template <class Args>
 __device__ __forceinline__ FewParts few_parts(int first, int n, int per) {
+  if constexpr (Args::WINDOW) return {first, (n + per - 1) / per, 1};
   const int i0 = first / per;
   return {i0, (first + n - 1) / per - i0 + 1, first == i0 * per};
 }
-__device__ __forceinline__ int few_slot(const FewArgs& a, const FewParts& s, int hk, int p) {
+template <class Args>
+__device__ __forceinline__ int few_slot(const Args& a, const FewParts& s, int hk, int p) {
+  if constexpr (Args::WINDOW) return hk * a.workers + s.i0 + p;
   return 2 * (hk * a.workers + s.i0 + p) + (p == 0 && !s.starts);
 }
 
@@ -389,6 +419,17 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(Args a) {
   }
   const int hk = blockIdx.x % a.Hk, i = blockIdx.x / a.Hk, lane = threadIdx.x & 63;
   FewLine line = few_line(a, lane);
+  if constexpr (Args::WINDOW) {
+    if (i >= line.total) return;
+    const FewSample at = few_sample(a, line, i, lane);
+    const FewSeen seen = few_seen(a, line, at.b, lane);
+    const int n = few_blocks(a, seen), p = i - at.first;
+    const FewParts s = few_parts<Args>(at.first, n, line.per);
+    if (p == 0 && hk == 0 && threadIdx.x == 0) { a.plan[2 * at.b] = s.i0; a.plan[2 * at.b + 1] = s.parts; }
+    const int even = n / s.parts, more = n % s.parts, k0 = p * even + min(p, more), k1 = k0 + even + (p < more);
+    few_piece<D>(a, FewPiece{at.b, hk, k0 * BKV, min(few_keys(a, seen), k1 * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, p), seen}, lds);
+    return;
+  }
   const int begin = i * line.per, stop = min(begin + line.per, line.total);
   if (begin >= stop) return;
   const FewSample start = few_sample(a, line, begin, lane);
@@ -396,7 +437,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void cross_few_kernel(Args a) {
   for (int b = start.b, at = begin; at < stop; ++b) {
     const FewSeen seen = few_seen(a, line, b, lane);
     const int keys = few_keys(a, seen), n = few_blocks(a, seen), end = min(first + n, stop);
-    const FewParts s = few_parts(first, n, line.per);
+    const FewParts s = few_parts<Args>(first, n, line.per);
     const FewPiece pc = {b, hk, (at - first) * BKV, min(keys, (end - first) * BKV), s.parts == 1 ? -1 : few_slot(a, s, hk, i - s.i0), seen};
     few_piece<D>(a, pc, lds);
     __syncthreads();                                     // (the next piece's tiles land where this one's results were)
@@ -414,10 +455,17 @@ __global__ __launch_bounds__(256) void cross_few_join_kernel(Args a) {
   __shared__ float stat[G][2];
   const int row = blockIdx.x % a.rows, unit = blockIdx.x / a.rows, b = unit / a.Hk, hk = unit % a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, c = tid % QUADS, g = tid / QUADS;
-  FewLine line = few_line(a, lane);
-  const int first = few_first(a, line, b, lane);
-  const FewSeen seen = few_seen(a, line, b, lane);
-  const FewParts s = few_parts(first, few_blocks(a, seen), line.per);
+  FewSeen seen;
+  FewParts s;
+  if constexpr (Args::WINDOW) {
+    seen = few_seen(a, b);
+    s = FewParts{scalar_ld(a.plan + 2 * b), scalar_ld(a.plan + 2 * b + 1), 1};
+  } else {
+    FewLine line = few_line(a, lane);
+    const int first = few_first(a, line, b, lane);
+    seen = few_seen(a, line, b, lane);
+    s = few_parts<Args>(first, few_blocks(a, seen), line.per);
+  }
   if (s.parts == 1) return;
   float m = -INFINITY, l = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -491,7 +539,10 @@ hipError_t launch_window_few(const void* q, const void* k, const void* v, const 
                              float scale, void* o, void* o_res, float* lse, void* ws, hipStream_t stream) {
   WindowFewArgs a = {};
   a.win = win;
-  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, window_few_ws(m, win), ws, stream);
+  const WindowFewWs share = window_few_ws(m, win);
+  a.aim = share.aim;
+  a.plan = (int32_t*)((char*)ws + share.plan);
+  return launch_few(a, q, k, v, m, lengths, scale, o, o_res, lse, share, ws, stream);
 }
 
 }  // namespace spa2

@@ -210,15 +210,27 @@ inline WindowBwdWs window_bwd_ws(const CrossDims& m, const Window& w) {
 //   samples, 8 heads 29.9 / 23.4 / 19.4; 512 keys, one head 20.5 / 18.7 / 15.7; of more blocks the join takes longer than that saves: 32,768
 //   keys, 2 heads 28.5 / 26.6 / 27.1, d = 64 21.0 / 19.5 / 21.4;
 //   shared / by themselves: 2000 keys, 128 pairs 35.4 / 49.6, 256 52.6 / 55.7, 512 103 / 96, 1000 216 / 181, d = 64 26.4 / 38.2, 36.8 / 39.0,
-//   57.9 / 50.9, 135 / 93; 512 keys 21.9 / 22.6, 24.8 / 24.0, 36 / 29, 94 / 55, d = 64 15.9 / 16.6, 20.7 / 18.2, 25.2 / 21.9, 67 / 27.
-inline CrossFewWs window_few_ws(const CrossDims& m, const Window& w) {
+//   57.9 / 50.9, 135 / 93; 512 keys 21.9 / 22.6, 24.8 / 24.0, 36 / 29, 94 / 55, d = 64 15.9 / 16.6, 20.7 / 18.2, 25.2 / 21.9, 67 / 27
+// (all of these as stretches of one line; cut into parts as cross_few.hip does now, shared ones take 5 to 15 % less).
+struct WindowFewWs : CrossFewWs { int aim; size_t plan; };         // (parts of a key head's samples, about; workers: at most)
+inline WindowFewWs window_few_ws(const CrossDims& m, const Window& w) {
   CrossDims seen = m;
   const int64_t near = ((int64_t)w.left + w.right + w.nq - 1 + BKV - 1) / BKV + 1 + (w.sinks + BKV - 1) / BKV;
   if (near < seen.q.Tn) seen.q.Tn = (int)near;
-  if (seen.q.Tn > 256) return cross_few_ws(seen, 4);
+  const bool many = seen.q.Tn > 256;
   const int64_t units = (int64_t)m.q.B * m.Hk;
-  if (units > 256 || seen.q.Tn < 8 || 16 * (int64_t)seen.q.Tn < units) return CrossFewWs{0, 0, 0};
-  return cross_few_ws(seen, 2);
+  const WindowFewWs none = {};
+  if (!many && (units > 256 || seen.q.Tn < 8 || 16 * (int64_t)seen.q.Tn < units)) return none;
+  WindowFewWs r = {cross_few_ws(seen, many ? 4 : 2), 0, 0};
+  if (r.workers <= 1) return none;
+  r.aim = r.workers;
+  if (2 * m.q.B > r.aim) {                 // (so many samples: parts small enough that the last of them do not count)
+    r.aim *= 4;
+    r.workers = r.aim + m.q.B;
+  }
+  r.plan = round256((size_t)r.workers * m.Hk * few_slot_bytes(m.group * m.q.N, m.q.d));
+  r.total = r.plan + round256((size_t)m.q.B * 8);
+  return r;
 }
 
 hipError_t launch_window_few(const void* q, const void* k, const void* v, const CrossDims& m, const int32_t* lengths, const Window& win,
